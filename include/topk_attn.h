@@ -315,6 +315,120 @@ size_t topk_attn_backward_workspace_bytes(int64_t B, int64_t H, int64_t Lq, int6
 size_t topk_ffn_backward_workspace_bytes(int64_t N, int64_t d_model, int64_t d_ff, int64_t k, int dtype);
 
 /*
+ * Rotary positions: pair p of a head's features turns by the angle
+ * positions[axis(p)] * freqs[p],
+ *     y_a = x_a cos - x_b sin,  y_b = x_a sin + x_b cos,
+ * in the first d_rot features; the others pass. A token has one position, or one on
+ * each of up to 4 axes (time, height and width of a video).
+ *
+ *   positions   device, int32 or int64 (position_bytes 4 or 8): axis a of token l of
+ *               batch entry b at a * axis_stride + b * batch_stride + l * token_stride
+ *               elements; any value (angles are formed in 64 bits)
+ *   freqs       device, d_rot / 2 doubles: radians a position
+ *   pair_axis   HOST, d_rot / 2 entries: the axis each pair turns by (NULL: axis 0);
+ *               read during the call
+ *   adjacent    0: pair p is features p and p + d_rot / 2; 1: features 2p and 2p + 1
+ *   inverse     1: turn by the opposite angles (the gradient of the rotation)
+ */
+typedef struct {
+  const void* positions;
+  const double* freqs;
+  const uint8_t* pair_axis;
+  int64_t d_rot;  /* 0 to d, even; 0 = no rotation */
+  int64_t axis_stride, batch_stride, token_stride;
+  int n_axes, position_bytes, adjacent, inverse;
+} topk_rotation;
+
+/*
+ * topk_rope -- rotary positions on heads. x [B, H, L, d] with head row (b, h, l) at
+ * b * batch_stride + h * head_stride + l * token_stride elements; out contiguous
+ * [B, H, L, d], not overlapping x unless it is x itself with the same strides. Any
+ * even d up to 512; tensors need the alignment of their elements only (16 bytes, and
+ * strides and pairs that are multiples of 16 bytes, run fastest). Its gradient is the
+ * same call with `inverse` changed.
+ */
+int topk_rope(const void* x, void* out, int64_t B, int64_t H, int64_t L, int64_t d,
+              int64_t batch_stride, int64_t head_stride, int64_t token_stride,
+              const topk_rotation* rot, int dtype, void* hip_stream);
+
+/*
+ * topk_qk_norm_rope -- the packed projection taken apart into heads: qkv holds for each
+ * token (b, l), at b * batch_stride + l * token_stride elements, H query heads, Hkv key
+ * heads and Hkv value heads of d features. Query and key heads are divided by their root
+ * mean square and scaled (norm = 1: n = w * x / sqrt(mean(x^2) + eps); norm = 0: n = x)
+ * and rotated (rot NULL: not); value heads are copied. Squares are summed in fp32.
+ *
+ *   q_weight, k_weight   [d], in dtype; NULL: ones
+ *   q [B, H, L, d], k, v [B, Hkv, L, d]   written, contiguous: what topk_attn takes
+ *
+ * d and alignment as topk_rope.
+ */
+int topk_qk_norm_rope(const void* qkv, const void* q_weight, const void* k_weight, void* q, void* k, void* v,
+                      int64_t B, int64_t L, int64_t H, int64_t Hkv, int64_t d,
+                      int64_t batch_stride, int64_t token_stride, int norm, float eps,
+                      const topk_rotation* rot, int dtype, void* hip_stream);
+
+/*
+ * The serving form: keys and values go to caches instead, those of token l of request b to
+ * row lengths[b] + l. Caches hold S rows a request and head, row (b, h, s) at
+ * b * batch + h * head + s * row strides; a token whose row is not in [0, S) is not
+ * stored, and no other row is touched. lengths (device, int32 [B]) is read, not advanced.
+ */
+int topk_qk_norm_rope_append(const void* qkv, const void* q_weight, const void* k_weight, void* q,
+                             void* k_cache, void* v_cache, const int32_t* lengths,
+                             int64_t B, int64_t L, int64_t H, int64_t Hkv, int64_t d,
+                             int64_t batch_stride, int64_t token_stride, int64_t S,
+                             int64_t k_batch_stride, int64_t k_head_stride, int64_t k_row_stride,
+                             int64_t v_batch_stride, int64_t v_head_stride, int64_t v_row_stride,
+                             int norm, float eps, const topk_rotation* rot, int dtype, void* hip_stream);
+
+/*
+ * Gradients of topk_qk_norm_rope, recomputed from its input: d_q [B, H, L, d], d_k, d_v
+ * [B, Hkv, L, d] (contiguous) to d_qkv [B, L, (H + 2 Hkv) d] (contiguous) and, where not
+ * NULL, d_q_weight and d_k_weight [d], sums over every token and head in a fixed order.
+ * rot as in the forward call. Workspace for the weights' gradients:
+ * topk_qk_norm_rope_backward_workspace_bytes (0 for invalid arguments).
+ */
+int topk_qk_norm_rope_backward(const void* qkv, const void* q_weight, const void* k_weight,
+                               const void* d_q, const void* d_k, const void* d_v,
+                               void* d_qkv, void* d_q_weight, void* d_k_weight,
+                               int64_t B, int64_t L, int64_t H, int64_t Hkv, int64_t d,
+                               int64_t batch_stride, int64_t token_stride, int norm, float eps,
+                               const topk_rotation* rot, int dtype, void* hip_stream);
+size_t topk_qk_norm_rope_backward_workspace_bytes(int64_t B, int64_t L, int64_t H, int64_t Hkv, int64_t d,
+                                                  int64_t d_rot, int dtype);
+
+/*
+ * topk_attn_prefix -- attention (every valid key, Eq. 1) of B requests that share a prefix of
+ * P keys and values and hold up to S of their own behind it; H / Hkv query heads share a
+ * key head.
+ *
+ *   Q          [B, H, Lq, d]   contiguous
+ *   prefix_K, prefix_V [Hkv, P, d]; K, V [B, Hkv, S, d]: strides in elements (NULL:
+ *              contiguous), multiples of 8; not read where P = 0 or S = 0
+ *   lengths    device, int32 [B]: request b holds lengths[b] keys (taken into [0, S]; NULL:
+ *              S); rows at and behind it are not used, whatever they hold
+ *   causal     1: the queries are the request's last Lq positions: query i sees the prefix
+ *              and own keys j <= lengths[b] - Lq + i; 0: every key
+ *   out        [B, H, Lq, d]   written; a row that sees no key is 0
+ *   lse        NULL, or fp32 [B, H, Lq]: log sum_j exp(scale * s_j), -inf where no key is seen
+ *
+ * bf16 with d = 64 or 128 (else TOPK_E_UNSUPPORTED). Softmax statistics and sums in fp32.
+ * Workspace: topk_attn_prefix_workspace_bytes, partial results of key ranges in fp32 (0
+ * where none is needed, or for invalid arguments). Stages 0 and 3 of the stage timing.
+ */
+typedef struct {
+  int64_t prefix_k_head, prefix_k_key, prefix_v_head, prefix_v_key;
+  int64_t k_batch, k_head, k_key, v_batch, v_head, v_key;
+} topk_prefix_strides;
+int topk_attn_prefix(const void* Q, const void* prefix_K, const void* prefix_V, const void* K, const void* V,
+                     const int32_t* lengths, void* out, float* lse,
+                     int64_t B, int64_t H, int64_t Hkv, int64_t Lq, int64_t P, int64_t S, int64_t d,
+                     const topk_prefix_strides* strides, int causal, float scale, int dtype, void* hip_stream);
+size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t Lq, int64_t P, int64_t S,
+                                        int64_t d, int dtype);
+
+/*
  * Test hook: the number of query rows that the last topk_attn_debug /
  * topk_ffn_debug call on the calling thread selected through a fallback path
  * (rows whose sampled threshold or candidate buffers could not prove the

@@ -2,7 +2,9 @@
 // path choice, the chunk scheduler (how many query chunks are in flight per pass
 // under the workspace budget) and the kernel sequence of each pass.
 #include "topk_attn.h"
+#include "topk_heads.h"
 #include "topk_internal.h"
+#include "topk_prefix.h"
 
 #include <math.h>
 #include <stdarg.h>
@@ -751,6 +753,185 @@ int scratch_for_current_device(void** out) {
   return TOPK_OK;
 }
 
+// ---------------------------------------------------------------- heads: norms, rotation, caches
+constexpr int64_t STRIDE_MAX = int64_t(1) << 40;
+
+int stride_ok(const char* name, std::initializer_list<int64_t> strides, int64_t most = STRIDE_MAX) {
+  for (int64_t s : strides)
+    if (s < 0 || s >= most) return fail(TOPK_E_INVAL, "a stride of %s is out of range: %lld", name, (long long)s);
+  return TOPK_OK;
+}
+
+int rotation_for(Rotation* r, const topk_rotation* in, int64_t d) {
+  *r = Rotation{};
+  if (!in || in->d_rot == 0) return TOPK_OK;
+  if (in->d_rot < 0 || in->d_rot > d || in->d_rot % 2)
+    return fail(TOPK_E_INVAL, "rotated features must be an even number from 0 to %lld (got %lld)", (long long)d, (long long)in->d_rot);
+  if (in->n_axes < 1 || in->n_axes > ROPE_MAX_AXES)
+    return fail(TOPK_E_INVAL, "need 1 to %d position axes (got %d)", ROPE_MAX_AXES, in->n_axes);
+  if (!in->positions || !in->freqs) return fail(TOPK_E_NULL, "positions or freqs is NULL");
+  if (in->position_bytes != 4 && in->position_bytes != 8) return fail(TOPK_E_INVAL, "positions must be of 4 or 8 bytes");
+  if (((uintptr_t)in->positions) % in->position_bytes || ((uintptr_t)in->freqs) % 8)
+    return fail(TOPK_E_ALIGN, "positions or freqs is not aligned to its elements");
+  if ((in->adjacent != 0 && in->adjacent != 1) || (in->inverse != 0 && in->inverse != 1))
+    return fail(TOPK_E_INVAL, "adjacent and inverse must be 0 or 1");
+  int rc = stride_ok("positions", {in->axis_stride, in->batch_stride, in->token_stride});
+  if (rc) return rc;
+  r->positions = in->positions;
+  r->freqs = in->freqs;
+  r->pos_sa = in->axis_stride;
+  r->pos_sb = in->batch_stride;
+  r->pos_sl = in->token_stride;
+  r->half = (int)(in->d_rot / 2);
+  r->pos64 = in->position_bytes == 8;
+  r->adjacent = in->adjacent;
+  r->inverse = in->inverse;
+  for (int p = 0; in->pair_axis && p < r->half; ++p) {
+    const int a = in->pair_axis[p];
+    if (a >= in->n_axes) return fail(TOPK_E_INVAL, "pair %d turns by axis %d of %d", p, a, in->n_axes);
+    r->axis[p >> 4] |= (uint32_t)a << (2 * (p & 15));
+  }
+  return TOPK_OK;
+}
+
+// Sizes common to every call on heads; H and Hkv as they stand in the packed row.
+int heads_shape(HeadsProblem* hp, int64_t B, int64_t L, int64_t H, int64_t Hkv, int64_t d, int norm, float eps, const topk_rotation* rot,
+                int dtype) {
+  *hp = HeadsProblem{};
+  if (B < 1 || L < 1 || H < 1 || Hkv < 0 || d < 1)
+    return fail(TOPK_E_INVAL, "sizes must be >= 1 (got B = %lld, L = %lld, H = %lld, d = %lld)", (long long)B, (long long)L, (long long)H, (long long)d);
+  if (dtype != TOPK_F32 && dtype != TOPK_BF16) return fail(TOPK_E_INVAL, "dtype must be TOPK_F32 or TOPK_BF16");
+  if (d % 2 || d > ROPE_MAX_D)
+    return fail(TOPK_E_UNSUPPORTED, "feature size %lld: head calls need an even number, at most %d", (long long)d, ROPE_MAX_D);
+  if (norm != 0 && norm != 1) return fail(TOPK_E_INVAL, "norm must be 0 or 1");
+  if (norm && !(isfinite(eps) && eps >= 0.f)) return fail(TOPK_E_INVAL, "eps must be finite and >= 0");
+  if (H > 16384 || Hkv > 16384) return fail(TOPK_E_UNSUPPORTED, "more than 16384 heads");
+  if (B > (int64_t(1) << 31) / L) return fail(TOPK_E_UNSUPPORTED, "more than 2^31 tokens");
+  hp->B = B;
+  hp->L = L;
+  hp->heads[0] = H;
+  hp->heads[1] = hp->heads[2] = Hkv;
+  hp->d = (int)d;
+  hp->dtype = dtype;
+  hp->norm = norm;
+  hp->eps = eps;
+  return rotation_for(&hp->rot, rot, d);
+}
+
+int elem_ptr(const void* p, const char* name, int dtype) {
+  if (!p) return fail(TOPK_E_NULL, "%s is NULL", name);
+  if (((uintptr_t)p) % (dtype == TOPK_BF16 ? 2 : 4)) return fail(TOPK_E_ALIGN, "%s is not aligned to its elements", name);
+  return TOPK_OK;
+}
+int weight_ptr(const void* p, const char* name, const HeadsProblem& hp) {
+  if (!p) return TOPK_OK;
+  if (!hp.norm) return fail(TOPK_E_INVAL, "%s scales a norm that is switched off", name);
+  return elem_ptr(p, name, hp.dtype);
+}
+HeadRows plain_heads(const void* p, int64_t H, int64_t L, int64_t d) { return {(void*)p, H * L * d, L * d, d}; }
+
+// The packed row of the qkv calls; q goes to contiguous heads.
+int qkv_problem(HeadsProblem* hp, const void* qkv, const void* q_weight, const void* k_weight, int64_t B, int64_t L, int64_t H,
+                int64_t Hkv, int64_t d, int64_t batch_stride, int64_t token_stride, int norm, float eps, const topk_rotation* rot,
+                int dtype) {
+  int rc = heads_shape(hp, B, L, H, Hkv, d, norm, eps, rot, dtype);
+  if (rc) return rc;
+  if (Hkv < 1) return fail(TOPK_E_INVAL, "need at least one key head");
+  if ((rc = elem_ptr(qkv, "qkv", dtype)) || (rc = weight_ptr(q_weight, "q_weight", *hp)) || (rc = weight_ptr(k_weight, "k_weight", *hp)) ||
+      (rc = stride_ok("qkv", {batch_stride, token_stride})))
+    return rc;
+  hp->x = {(void*)qkv, batch_stride, d, token_stride};
+  hp->w[0] = q_weight;
+  hp->w[1] = k_weight;
+  return TOPK_OK;
+}
+
+int run_heads(const HeadsProblem& hp, hipStream_t st) {
+  const hipError_t e = launch_heads(hp, st);
+  if (e != hipSuccess) return fail(TOPK_E_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return TOPK_OK;
+}
+
+// A call's workspace: the registered one, or one allocated on the stream (freed by release()).
+struct Scratch {
+  char* p = nullptr;
+  bool own = false;
+  int get(size_t need, const char* what, hipStream_t st) {
+    if (!need) return TOPK_OK;
+    if (g_ws) {
+      if (need > g_ws_bytes)
+        return fail(TOPK_E_NOMEM, "registered workspace of %zu bytes is below the %zu bytes %s needs", g_ws_bytes, need, what);
+      p = (char*)g_ws;
+      return TOPK_OK;
+    }
+    if (hipMallocAsync((void**)&p, need, st) != hipSuccess) {
+      p = nullptr;
+      return fail(TOPK_E_NOMEM, "could not allocate %zu bytes of workspace", need);
+    }
+    own = true;
+    return TOPK_OK;
+  }
+  void release(hipStream_t st) {
+    if (own) hipFreeAsync(p, st);
+  }
+};
+
+// ---------------------------------------------------------------- shared-prefix attention
+int prefix_shape(PrefixProblem* pp, int64_t B, int64_t H, int64_t Hkv, int64_t Lq, int64_t P, int64_t S, int64_t d, int causal,
+                 float scale, int dtype) {
+  *pp = PrefixProblem{};
+  if (B < 1 || H < 1 || Hkv < 1 || Lq < 1 || d < 1 || P < 0 || S < 0)
+    return fail(TOPK_E_INVAL, "sizes must be >= 1, P and S >= 0 (got B = %lld, H = %lld, Hkv = %lld, Lq = %lld, P = %lld, S = %lld, d = %lld)",
+                (long long)B, (long long)H, (long long)Hkv, (long long)Lq, (long long)P, (long long)S, (long long)d);
+  if (H % Hkv) return fail(TOPK_E_INVAL, "%lld query heads do not share %lld key heads evenly", (long long)H, (long long)Hkv);
+  if (causal != 0 && causal != 1) return fail(TOPK_E_INVAL, "causal must be 0 or 1");
+  if (!(isfinite(scale) && scale > 0.f)) return fail(TOPK_E_INVAL, "scale must be finite and > 0");
+  if (dtype != TOPK_F32 && dtype != TOPK_BF16) return fail(TOPK_E_INVAL, "dtype must be TOPK_F32 or TOPK_BF16");
+  if (dtype != TOPK_BF16 || (d != 64 && d != 128))
+    return fail(TOPK_E_UNSUPPORTED, "shared-prefix attention runs on bf16 inputs with d = 64 or 128");
+  if (P > 0x7FFFFFFFLL || S > 0x7FFFFFFFLL) return fail(TOPK_E_UNSUPPORTED, "more than 2^31 - 1 keys");
+  if (H > (int64_t(1) << 31) / B || Lq > (int64_t(1) << 31) / (B * H)) return fail(TOPK_E_UNSUPPORTED, "more than 2^31 query rows");
+  pp->B = B;
+  pp->H = H;
+  pp->Hkv = Hkv;
+  pp->Lq = Lq;
+  pp->P = P;
+  pp->S = S;
+  pp->d = (int)d;
+  pp->causal = causal;
+  pp->scale = scale;
+  return TOPK_OK;
+}
+
+int cache_ptr(const char* name, const void* p, std::initializer_list<int64_t> strides) {
+  int rc = check_ptr(p, name);
+  if (rc || (rc = stride_ok(name, strides))) return rc;
+  for (int64_t s : strides)
+    if (s % 8) return fail(TOPK_E_ALIGN, "a stride of %s is not a multiple of 8 elements: %lld", name, (long long)s);
+  const int64_t key = *(strides.end() - 1);
+  if (key >= int64_t(1) << 26) return fail(TOPK_E_UNSUPPORTED, "the keys of %s lie 2^26 elements apart or more", name);
+  return TOPK_OK;
+}
+
+int run_prefix(const PrefixProblem& pp, hipStream_t st) {
+  const PrefixPlan pl = prefix_plan(pp);
+  Scratch ws;
+  int rc = ws.get(prefix_bytes(pp, pl), "shared-prefix attention", st);
+  if (rc) return rc;
+  hipError_t e;
+  {
+    StageTimer t(st, ST_SCORE);
+    e = launch_prefix(pp, pl, ws.p, st);
+  }
+  if (e == hipSuccess) {
+    StageTimer t(st, ST_FINAL);
+    e = launch_prefix_join(pp, pl, ws.p, st);
+  }
+  ws.release(st);
+  if (e != hipSuccess) return fail(TOPK_E_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return TOPK_OK;
+}
+
 }  // namespace
 }  // namespace topk
 
@@ -1068,6 +1249,141 @@ int topk_selftest_mfma_layout(int32_t* rows_out, int32_t* cols_out, void* hip_st
   hipError_t e = launch_mfma_probe(rows_out, cols_out, (hipStream_t)hip_stream);
   if (e != hipSuccess) return fail(TOPK_E_HIP, "probe launch failed: %s", hipGetErrorString(e));
   return TOPK_OK;
+}
+
+int topk_rope(const void* x, void* out, int64_t B, int64_t H, int64_t L, int64_t d, int64_t batch_stride, int64_t head_stride,
+              int64_t token_stride, const topk_rotation* rot, int dtype, void* hip_stream) {
+  g_err.clear();
+  HeadsProblem hp;
+  int rc = heads_shape(&hp, B, L, H, 0, d, 0, 0.f, rot, dtype);
+  if (rc) return rc;
+  if ((rc = elem_ptr(x, "x", dtype)) || (rc = elem_ptr(out, "out", dtype)) ||
+      (rc = stride_ok("x", {batch_stride, head_stride, token_stride})))
+    return rc;
+  hp.x = {(void*)x, batch_stride, head_stride, token_stride};
+  hp.part[0] = plain_heads(out, H, L, d);
+  return run_heads(hp, (hipStream_t)hip_stream);
+}
+
+int topk_qk_norm_rope(const void* qkv, const void* q_weight, const void* k_weight, void* q, void* k, void* v, int64_t B, int64_t L,
+                      int64_t H, int64_t Hkv, int64_t d, int64_t batch_stride, int64_t token_stride, int norm, float eps,
+                      const topk_rotation* rot, int dtype, void* hip_stream) {
+  g_err.clear();
+  HeadsProblem hp;
+  int rc = qkv_problem(&hp, qkv, q_weight, k_weight, B, L, H, Hkv, d, batch_stride, token_stride, norm, eps, rot, dtype);
+  if (rc) return rc;
+  if ((rc = elem_ptr(q, "q", dtype)) || (rc = elem_ptr(k, "k", dtype)) || (rc = elem_ptr(v, "v", dtype))) return rc;
+  hp.part[0] = plain_heads(q, H, L, d);
+  hp.part[1] = plain_heads(k, Hkv, L, d);
+  hp.part[2] = plain_heads(v, Hkv, L, d);
+  return run_heads(hp, (hipStream_t)hip_stream);
+}
+
+int topk_qk_norm_rope_append(const void* qkv, const void* q_weight, const void* k_weight, void* q, void* k_cache, void* v_cache,
+                             const int32_t* lengths, int64_t B, int64_t L, int64_t H, int64_t Hkv, int64_t d, int64_t batch_stride,
+                             int64_t token_stride, int64_t S, int64_t k_batch_stride, int64_t k_head_stride, int64_t k_row_stride,
+                             int64_t v_batch_stride, int64_t v_head_stride, int64_t v_row_stride, int norm, float eps,
+                             const topk_rotation* rot, int dtype, void* hip_stream) {
+  g_err.clear();
+  HeadsProblem hp;
+  int rc = qkv_problem(&hp, qkv, q_weight, k_weight, B, L, H, Hkv, d, batch_stride, token_stride, norm, eps, rot, dtype);
+  if (rc) return rc;
+  if (S < 0) return fail(TOPK_E_INVAL, "S must be >= 0 (got %lld)", (long long)S);
+  if ((rc = elem_ptr(q, "q", dtype)) || (rc = elem_ptr(k_cache, "k_cache", dtype)) || (rc = elem_ptr(v_cache, "v_cache", dtype)) ||
+      (rc = stride_ok("k_cache", {k_batch_stride, k_head_stride, k_row_stride})) ||
+      (rc = stride_ok("v_cache", {v_batch_stride, v_head_stride, v_row_stride})))
+    return rc;
+  if (!lengths) return fail(TOPK_E_NULL, "lengths is NULL");
+  if (((uintptr_t)lengths) % 4) return fail(TOPK_E_ALIGN, "lengths is not 4-byte aligned");
+  hp.part[0] = plain_heads(q, H, L, d);
+  hp.part[1] = {k_cache, k_batch_stride, k_head_stride, k_row_stride};
+  hp.part[2] = {v_cache, v_batch_stride, v_head_stride, v_row_stride};
+  hp.lengths = lengths;
+  hp.S = S;
+  return run_heads(hp, (hipStream_t)hip_stream);
+}
+
+int topk_qk_norm_rope_backward(const void* qkv, const void* q_weight, const void* k_weight, const void* d_q, const void* d_k,
+                               const void* d_v, void* d_qkv, void* d_q_weight, void* d_k_weight, int64_t B, int64_t L, int64_t H,
+                               int64_t Hkv, int64_t d, int64_t batch_stride, int64_t token_stride, int norm, float eps,
+                               const topk_rotation* rot, int dtype, void* hip_stream) {
+  g_err.clear();
+  HeadsProblem hp;
+  int rc = qkv_problem(&hp, qkv, q_weight, k_weight, B, L, H, Hkv, d, batch_stride, token_stride, norm, eps, rot, dtype);
+  if (rc) return rc;
+  if ((rc = elem_ptr(d_q, "d_q", dtype)) || (rc = elem_ptr(d_k, "d_k", dtype)) || (rc = elem_ptr(d_v, "d_v", dtype)) ||
+      (rc = elem_ptr(d_qkv, "d_qkv", dtype)) || (rc = weight_ptr(d_q_weight, "d_q_weight", hp)) ||
+      (rc = weight_ptr(d_k_weight, "d_k_weight", hp)))
+    return rc;
+  hp.part[0] = plain_heads(d_q, H, L, d);
+  hp.part[1] = plain_heads(d_k, Hkv, L, d);
+  hp.part[2] = plain_heads(d_v, Hkv, L, d);
+  const int64_t row = (H + 2 * Hkv) * d;
+  hp.dx = {d_qkv, L * row, d, row};
+  hp.dw[0] = d_q_weight;
+  hp.dw[1] = d_k_weight;
+  hp.rot.inverse ^= 1;
+  hipStream_t st = (hipStream_t)hip_stream;
+  Scratch ws;
+  if ((d_q_weight || d_k_weight) && (rc = ws.get(heads_backward_bytes(hp), "the backward pass", st))) return rc;
+  hp.dw_part = (float*)ws.p;
+  hipError_t e;
+  {
+    StageTimer t(st, ST_BWD);
+    e = launch_heads_backward(hp, st);
+  }
+  ws.release(st);
+  if (e != hipSuccess) return fail(TOPK_E_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return TOPK_OK;
+}
+
+size_t topk_qk_norm_rope_backward_workspace_bytes(int64_t B, int64_t L, int64_t H, int64_t Hkv, int64_t d, int64_t d_rot, int dtype) {
+  HeadsProblem hp;
+  if (heads_shape(&hp, B, L, H, Hkv, d, 1, 0.f, nullptr, dtype) || Hkv < 1 || d_rot < 0 || d_rot > d || d_rot % 2) return 0;
+  hp.rot.half = (int)(d_rot / 2);
+  return heads_backward_bytes(hp);
+}
+
+int topk_attn_prefix(const void* Q, const void* prefix_K, const void* prefix_V, const void* K, const void* V, const int32_t* lengths,
+                     void* out, float* lse, int64_t B, int64_t H, int64_t Hkv, int64_t Lq, int64_t P, int64_t S, int64_t d,
+                     const topk_prefix_strides* strides, int causal, float scale, int dtype, void* hip_stream) {
+  g_err.clear();
+  PrefixProblem pp;
+  int rc = prefix_shape(&pp, B, H, Hkv, Lq, P, S, d, causal, scale, dtype);
+  if (rc) return rc;
+  const topk_prefix_strides t =
+      strides ? *strides : topk_prefix_strides{P * d, d, P * d, d, Hkv * S * d, S * d, d, Hkv * S * d, S * d, d};
+  if ((rc = check_ptr(Q, "Q")) || (rc = check_ptr(out, "out"))) return rc;
+  if (P && ((rc = cache_ptr("prefix_K", prefix_K, {t.prefix_k_head, t.prefix_k_key})) ||
+            (rc = cache_ptr("prefix_V", prefix_V, {t.prefix_v_head, t.prefix_v_key}))))
+    return rc;
+  if (S && ((rc = cache_ptr("K", K, {t.k_batch, t.k_head, t.k_key})) || (rc = cache_ptr("V", V, {t.v_batch, t.v_head, t.v_key})))) return rc;
+  if (((uintptr_t)lengths) % 4 || ((uintptr_t)lse) % 4) return fail(TOPK_E_ALIGN, "lengths or lse is not 4-byte aligned");
+  pp.q = Q;
+  pp.out = out;
+  pp.lse = lse;
+  pp.pk = prefix_K;
+  pp.pv = prefix_V;
+  pp.k = K;
+  pp.v = V;
+  pp.lengths = lengths;
+  pp.pk_sh = t.prefix_k_head;
+  pp.pk_sl = t.prefix_k_key;
+  pp.pv_sh = t.prefix_v_head;
+  pp.pv_sl = t.prefix_v_key;
+  pp.k_sb = t.k_batch;
+  pp.k_sh = t.k_head;
+  pp.k_sl = t.k_key;
+  pp.v_sb = t.v_batch;
+  pp.v_sh = t.v_head;
+  pp.v_sl = t.v_key;
+  return run_prefix(pp, (hipStream_t)hip_stream);
+}
+
+size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t Lq, int64_t P, int64_t S, int64_t d, int dtype) {
+  PrefixProblem pp;
+  if (prefix_shape(&pp, B, H, Hkv, Lq, P, S, d, 0, 1.f, dtype)) return 0;
+  return prefix_bytes(pp, prefix_plan(pp));
 }
 
 }  // extern "C"

@@ -1,0 +1,450 @@
+// What happens to heads between the projection and the attention: the packed [q | k | v] row
+// of each token is taken apart into heads, query and key heads are divided by their root mean
+// square, scaled and rotated by the token's positions.
+//
+//   r = (sum_f x_f^2 / d + eps)^(-1/2),  u = x r,  n = w u  (each a head of d features)
+//   y_a = n_a cos t - n_b sin t,  y_b = n_a sin t + n_b cos t   for each pair (a, b) = p,
+//   t = position[axis(p)] * freq[p]
+// and backward, with m = the rotation by -t of the incoming gradient:
+//   dw = sum over tokens and heads of m u,   dx = r (m w - u mean(m w u)).
+//
+// Bound by memory: every element is read once and written once (backward: x and the gradient
+// read, one gradient written), so the design is about whole cache lines and few instructions.
+// A group of T lanes holds one head, each lane VEC pairs (both features of a pair, so the
+// rotation needs no exchange) by two 16-byte accesses, and stays with its token: the angles
+// are computed once per lane and reused for every head of the workgroup. A workgroup's tokens
+// are consecutive, so that each head it writes is one contiguous run; the packed input is read
+// in runs of d elements. Angles are products in 64 bits, reduced to a turn there (32 bits would
+// lose 0.06 rad at position 10^6), and only the fraction of a turn goes to a 32-bit sine.
+#include "topk_device.h"
+#include "topk_heads.h"
+
+#include <algorithm>
+
+namespace topk {
+namespace {
+
+constexpr int NT = 256;  // threads of a workgroup
+
+template <typename T, int N> struct Vec {
+  T e[N];
+};
+template <typename T> __device__ __forceinline__ float widen(T v);
+template <> __device__ __forceinline__ float widen<float>(float v) { return v; }
+template <> __device__ __forceinline__ float widen<uint16_t>(uint16_t v) { return bf16_to_f32(v); }
+
+// VEC consecutive elements, at an address that is a multiple of their size
+template <typename T, int VEC>
+__device__ __forceinline__ void load_vec(float (&o)[VEC], const T* p) {
+  Vec<T, VEC> v;
+  __builtin_memcpy(&v, __builtin_assume_aligned(p, sizeof(T) * VEC), sizeof(T) * VEC);
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) o[e] = widen(v.e[e]);
+}
+template <int VEC>
+__device__ __forceinline__ void store_vec(float* p, const float (&o)[VEC]) {
+  __builtin_memcpy(__builtin_assume_aligned(p, 4 * VEC), o, 4 * VEC);
+}
+template <int VEC>
+__device__ __forceinline__ void store_vec(uint16_t* p, const float (&o)[VEC]) {
+  typedef __bf16 bf16;
+  bf16 v[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) v[e] = (bf16)o[e];  // nearest-even
+  __builtin_memcpy(__builtin_assume_aligned(p, 2 * VEC), v, 2 * VEC);
+}
+
+struct Grid {
+  int T;             // lanes of a head: a power of two, at least d / (2 VEC NC)
+  int64_t tiles;     // tiles of NT / T tokens
+  int ny[3];         // workgroups that share the heads of q, k, v
+  int per[3];        // heads of each
+};
+
+// A lane's place: its chunks' features and its token.
+template <int VEC, int NC, bool ADJ>
+struct Lane {
+  int lo[NC], hi[NC];  // first features of the two runs of VEC (of pairs p .. p + VEC - 1, or not rotated)
+  bool in[NC], turn[NC];
+  int pair[NC];
+  __device__ Lane(int c0, int T, int d, int half) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int c = c0 + j * T, p = c * VEC;
+      in[j] = 2 * p < d;
+      turn[j] = in[j] && p < half;
+      pair[j] = turn[j] ? p : 0;
+      if (ADJ || p >= half) {
+        lo[j] = in[j] ? 2 * p : 0;
+        hi[j] = lo[j] + (in[j] ? VEC : 0);
+      } else {
+        lo[j] = p;
+        hi[j] = p + half;
+      }
+    }
+  }
+};
+
+// cos and sin of the lane's pairs at token (b, l)
+template <int VEC, int NC, bool ADJ>
+__device__ __forceinline__ void angles(const Rotation& r, const Lane<VEC, NC, ADJ>& ln, int64_t b, int64_t l, float (&co)[NC][VEC],
+                                       float (&si)[NC][VEC]) {
+  const int64_t at = b * r.pos_sb + l * r.pos_sl;
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      co[j][e] = 1.f;
+      si[j][e] = 0.f;
+    }
+    if (!ln.turn[j]) continue;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const int p = ln.pair[j] + e;
+      const int a = (r.axis[p >> 4] >> (2 * (p & 15))) & 3;
+      const int64_t o = at + a * r.pos_sa;
+      const double pos = r.pos64 ? (double)((const int64_t*)r.positions)[o] : (double)((const int32_t*)r.positions)[o];
+      const double turns = pos * r.freqs[p] * 0.15915494309189533577;  // 1 / (2 pi)
+      const float f = 2.f * (float)(turns - rint(turns));              // in half turns, [-1, 1]
+      float s, c;
+      sincospif(f, &s, &c);
+      co[j][e] = c;
+      si[j][e] = r.inverse ? -s : s;
+    }
+  }
+}
+
+// Rotates the lane's pairs by (co, si); features beyond the rotated ones have co = 1, si = 0.
+template <int VEC, bool ADJ>
+__device__ __forceinline__ void turn_pairs(float (&a)[VEC], float (&b)[VEC], const float (&co)[VEC], const float (&si)[VEC]) {
+  float x[2 * VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) x[e] = a[e], x[VEC + e] = b[e];
+  float y[2 * VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    const int i = ADJ ? 2 * e : e, k = ADJ ? 2 * e + 1 : VEC + e;
+    y[i] = fmaf(x[i], co[e], -x[k] * si[e]);
+    y[k] = fmaf(x[i], si[e], x[k] * co[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) a[e] = y[e], b[e] = y[VEC + e];
+}
+
+__device__ __forceinline__ float group_sum(float v, int T) {
+  for (int o = T >> 1; o; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// which of q, k, v a workgroup works on, and its heads
+struct Share {
+  int seg;
+  int64_t h0, h1, first;  // heads [h0, h1) of the part, whose first head is `first` of the packed row
+  __device__ Share(const HeadsProblem& hp, const Grid& g, int y) {
+    seg = 0;
+    first = 0;
+    while (seg < 2 && y >= g.ny[seg]) {
+      first += hp.heads[seg];
+      y -= g.ny[seg++];
+    }
+    h0 = (int64_t)y * g.per[seg];
+    h1 = min(h0 + g.per[seg], hp.heads[seg]);
+  }
+};
+
+// A workgroup takes one part's heads of a tile of NT / T tokens (more tiles only where a grid
+// cannot hold them all).
+template <typename T, int VEC, int NC, bool ADJ>
+__global__ __launch_bounds__(NT) void k_heads(HeadsProblem hp, Grid g) {
+  const Share sh(hp, g, blockIdx.y);
+  const int c0 = threadIdx.x & (g.T - 1);
+  const Lane<VEC, NC, ADJ> ln(c0, g.T, hp.d, hp.rot.half);
+  const bool value = sh.seg == 2;
+  float wa[NC][VEC], wb[NC][VEC];
+  const T* w = value ? nullptr : (const T*)hp.w[sh.seg];
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) wa[j][e] = wb[j][e] = 1.f;
+    if (w && ln.in[j]) {
+      load_vec<T, VEC>(wa[j], w + ln.lo[j]);
+      load_vec<T, VEC>(wb[j], w + ln.hi[j]);
+    }
+  }
+  const float inv_d = 1.f / (float)hp.d;
+  for (int64_t t = blockIdx.x; t < g.tiles; t += gridDim.x) {
+    const int64_t token = t * (NT / g.T) + threadIdx.x / g.T;
+    if (token >= hp.B * hp.L) return;  // (whole groups leave; later tiles lie behind)
+    const int64_t b = token / hp.L, l = token - b * hp.L;
+    int64_t row = l;
+    if (hp.lengths && sh.seg > 0) {
+      row = (int64_t)hp.lengths[b] + l;
+      if (row < 0 || row >= hp.S) continue;  // no place in the cache
+    }
+    float co[NC][VEC], si[NC][VEC];
+    if (!value) angles(hp.rot, ln, b, l, co, si);
+    const T* src = (const T*)hp.x.p + b * hp.x.sb + l * hp.x.sl + (sh.first + sh.h0) * hp.x.sh;
+    const HeadRows& o = hp.part[sh.seg];
+    T* dst = (T*)o.p + b * o.sb + row * o.sl + sh.h0 * o.sh;
+    for (int64_t h = sh.h0; h < sh.h1; ++h, src += hp.x.sh, dst += o.sh) {
+      float a[NC][VEC], c[NC][VEC];
+      float sq = 0.f;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) a[j][e] = c[j][e] = 0.f;
+        if (ln.in[j]) {
+          load_vec<T, VEC>(a[j], src + ln.lo[j]);
+          load_vec<T, VEC>(c[j], src + ln.hi[j]);
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sq = fmaf(a[j][e], a[j][e], fmaf(c[j][e], c[j][e], sq));
+      }
+      if (!value) {
+        const float r = hp.norm ? rsqrtf(fmaf(group_sum(sq, g.T), inv_d, hp.eps)) : 1.f;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            a[j][e] *= r * wa[j][e];
+            c[j][e] *= r * wb[j][e];
+          }
+          turn_pairs<VEC, ADJ>(a[j], c[j], co[j], si[j]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NC; ++j)
+        if (ln.in[j]) {
+          store_vec<VEC>(dst + ln.lo[j], a[j]);
+          store_vec<VEC>(dst + ln.hi[j], c[j]);
+        }
+    }
+  }
+}
+
+// Backward: workgroups walk over tiles of tokens (gridDim.x apart) so that the weights'
+// gradients stay in registers; each writes its own sum, in a fixed order over its groups.
+template <typename T, int VEC, int NC, bool ADJ>
+__global__ __launch_bounds__(NT) void k_heads_backward(HeadsProblem hp, Grid g) {
+  __shared__ float red[NT * NC * VEC];
+  const Share sh(hp, g, blockIdx.y);
+  const int c0 = threadIdx.x & (g.T - 1);
+  const Lane<VEC, NC, ADJ> ln(c0, g.T, hp.d, hp.rot.half);
+  const bool value = sh.seg == 2;
+  float wa[NC][VEC], wb[NC][VEC], ga[NC][VEC], gb[NC][VEC];
+  const T* w = value ? nullptr : (const T*)hp.w[sh.seg];
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      wa[j][e] = wb[j][e] = 1.f;
+      ga[j][e] = gb[j][e] = 0.f;
+    }
+    if (w && ln.in[j]) {
+      load_vec<T, VEC>(wa[j], w + ln.lo[j]);
+      load_vec<T, VEC>(wb[j], w + ln.hi[j]);
+    }
+  }
+  const float inv_d = 1.f / (float)hp.d;
+  for (int64_t t = blockIdx.x; t < g.tiles; t += gridDim.x) {
+    const int64_t token = t * (NT / g.T) + threadIdx.x / g.T;
+    if (token >= hp.B * hp.L) break;  // (whole groups leave; later tiles lie behind)
+    const int64_t b = token / hp.L, l = token - b * hp.L;
+    float co[NC][VEC], si[NC][VEC];
+    if (!value) angles(hp.rot, ln, b, l, co, si);
+    const HeadRows& gr = hp.part[sh.seg];
+    const T* src = (const T*)hp.x.p + b * hp.x.sb + l * hp.x.sl + (sh.first + sh.h0) * hp.x.sh;
+    const T* grad = (const T*)gr.p + b * gr.sb + l * gr.sl + sh.h0 * gr.sh;
+    T* dst = (T*)hp.dx.p + b * hp.dx.sb + l * hp.dx.sl + (sh.first + sh.h0) * hp.dx.sh;
+    for (int64_t h = sh.h0; h < sh.h1; ++h, src += hp.x.sh, grad += gr.sh, dst += hp.dx.sh) {
+      float ma[NC][VEC], mb[NC][VEC];
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) ma[j][e] = mb[j][e] = 0.f;
+        if (ln.in[j]) {
+          load_vec<T, VEC>(ma[j], grad + ln.lo[j]);
+          load_vec<T, VEC>(mb[j], grad + ln.hi[j]);
+        }
+      }
+      if (!value) {
+        float xa[NC][VEC], xb[NC][VEC];
+        float sq = 0.f, dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) xa[j][e] = xb[j][e] = 0.f;
+          if (ln.in[j]) {
+            load_vec<T, VEC>(xa[j], src + ln.lo[j]);
+            load_vec<T, VEC>(xb[j], src + ln.hi[j]);
+          }
+          turn_pairs<VEC, ADJ>(ma[j], mb[j], co[j], si[j]);  // (the launch asks for the opposite angles)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            sq = fmaf(xa[j][e], xa[j][e], fmaf(xb[j][e], xb[j][e], sq));
+            dot = fmaf(ma[j][e] * wa[j][e], xa[j][e], fmaf(mb[j][e] * wb[j][e], xb[j][e], dot));
+          }
+        }
+        float r = 1.f, k = 0.f;  // dx = r m w - k x
+        if (hp.norm) {
+          r = rsqrtf(fmaf(group_sum(sq, g.T), inv_d, hp.eps));
+          k = r * r * r * group_sum(dot, g.T) * inv_d;
+        }
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            ga[j][e] = fmaf(ma[j][e], xa[j][e] * r, ga[j][e]);
+            gb[j][e] = fmaf(mb[j][e], xb[j][e] * r, gb[j][e]);
+            ma[j][e] = fmaf(r * wa[j][e], ma[j][e], -k * xa[j][e]);
+            mb[j][e] = fmaf(r * wb[j][e], mb[j][e], -k * xb[j][e]);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NC; ++j)
+        if (ln.in[j]) {
+          store_vec<VEC>(dst + ln.lo[j], ma[j]);
+          store_vec<VEC>(dst + ln.hi[j], mb[j]);
+        }
+    }
+  }
+  if (value || !hp.dw_part) return;
+  // the groups' sums: [group][lane][NC][VEC], first features then second ones
+  const int y = blockIdx.y - (sh.seg ? g.ny[0] : 0);
+  float* out = hp.dw_part + ((sh.seg ? (int64_t)gridDim.x * g.ny[0] : 0) + (int64_t)y * gridDim.x + blockIdx.x) * hp.d;
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {
+    if (part) __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) red[(j * VEC + e) * NT + threadIdx.x] = part ? gb[j][e] : ga[j][e];
+    __syncthreads();
+    // (one thread per lane place and value; NT threads cover T * NC * VEC values)
+    for (int i = threadIdx.x; i < g.T * NC * VEC; i += NT) {
+      const int c = i % g.T, v = i / g.T, j = v / VEC, e = v % VEC;
+      float s = 0.f;
+      for (int q = c; q < NT; q += g.T) s += red[v * NT + q];
+      const Lane<VEC, 1, ADJ> at(c + j * g.T, 1, hp.d, hp.rot.half);
+      if (at.in[0]) out[(part ? at.hi[0] : at.lo[0]) + e] = s;
+    }
+  }
+}
+
+// One weight gradient per 16 columns: the workgroups' sums, in a fixed order.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_heads_weights(const float* part, T* dw, int64_t n, int d) {
+  __shared__ float red[64][17];
+  const int c = threadIdx.x & 15, q = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
+  float s = 0.f;
+  if (col < d)
+    for (int64_t i = q; i < n; i += 64) s += part[i * d + col];
+  red[q][c] = s;
+  __syncthreads();
+  for (int o = 32; o; o >>= 1) {
+    if (q < o) red[q][c] += red[q + o][c];
+    __syncthreads();
+  }
+  if (q == 0 && col < d) store_elem<T>(dw, col, red[0][c]);
+}
+
+// elements a lane may move at once: 16 bytes where sizes, strides and addresses allow
+bool rows_fit(const HeadRows& r, int vec, int es) {
+  return !r.p || (((uintptr_t)r.p) % (vec * es) == 0 && r.sb % vec == 0 && r.sh % vec == 0 && r.sl % vec == 0);
+}
+int vector_for(const HeadsProblem& hp) {
+  const int es = hp.dtype ? 2 : 4;
+  for (int vec = 16 / es; vec >= 4; vec /= 2) {
+    if (hp.rot.half % vec || (hp.d / 2) % vec) continue;
+    bool ok = rows_fit(hp.x, vec, es) && rows_fit(hp.dx, vec, es);
+    for (int s = 0; s < 3; ++s) ok = ok && rows_fit(hp.part[s], vec, es);
+    for (int s = 0; s < 2; ++s) ok = ok && ((uintptr_t)hp.w[s]) % (vec * es) == 0;
+    if (ok) return vec;
+  }
+  return 1;
+}
+
+Grid grid_for(const HeadsProblem& hp, int vec) {
+  Grid g = {};
+  const int chunks = hp.d / 2 / vec, nc = vec == 1 ? 4 : 1;
+  g.T = 1;
+  while (g.T * nc < chunks && g.T < 64) g.T *= 2;
+  const int64_t tokens = hp.B * hp.L, tile = NT / g.T;
+  g.tiles = (tokens + tile - 1) / tile;
+  // heads of a workgroup: as many as leave eight workgroups a CU (the angles are shared by them)
+  const int64_t want = 2048;
+  int64_t total = hp.heads[0] + hp.heads[1] + hp.heads[2];
+  int64_t per = g.tiles >= want ? total : g.tiles * total / want;
+  per = std::max<int64_t>(1, std::min<int64_t>(per, total));
+  for (int s = 0; s < 3; ++s) {
+    g.ny[s] = (int)((hp.heads[s] + per - 1) / per);
+    g.per[s] = g.ny[s] ? (int)((hp.heads[s] + g.ny[s] - 1) / g.ny[s]) : 1;
+  }
+  return g;
+}
+int backward_blocks(const Grid& g) {
+  const int y = g.ny[0] + g.ny[1] + g.ny[2];
+  return (int)std::max<int64_t>(1, std::min<int64_t>(g.tiles, 2048 / std::max(1, y)));
+}
+
+template <typename T, int VEC, int NC>
+void launch_adj(const HeadsProblem& hp, const Grid& g, dim3 grid, bool backward, hipStream_t st) {
+  if (backward) {
+    if (hp.rot.adjacent) k_heads_backward<T, VEC, NC, true><<<grid, NT, 0, st>>>(hp, g);
+    else k_heads_backward<T, VEC, NC, false><<<grid, NT, 0, st>>>(hp, g);
+  } else {
+    if (hp.rot.adjacent) k_heads<T, VEC, NC, true><<<grid, NT, 0, st>>>(hp, g);
+    else k_heads<T, VEC, NC, false><<<grid, NT, 0, st>>>(hp, g);
+  }
+}
+void launch_any(const HeadsProblem& hp, int vec, const Grid& g, dim3 grid, bool backward, hipStream_t st) {
+  if (hp.dtype) {
+    if (vec == 8) launch_adj<uint16_t, 8, 1>(hp, g, grid, backward, st);
+    else if (vec == 4) launch_adj<uint16_t, 4, 1>(hp, g, grid, backward, st);
+    else launch_adj<uint16_t, 1, 4>(hp, g, grid, backward, st);
+  } else {
+    if (vec == 4) launch_adj<float, 4, 1>(hp, g, grid, backward, st);
+    else launch_adj<float, 1, 4>(hp, g, grid, backward, st);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_heads(const HeadsProblem& hp, hipStream_t st) {
+  const int vec = vector_for(hp);
+  const Grid g = grid_for(hp, vec);
+  launch_any(hp, vec, g, dim3((unsigned)std::min<int64_t>(g.tiles, 1 << 20), g.ny[0] + g.ny[1] + g.ny[2]), false, st);
+  return hipGetLastError();
+}
+
+size_t heads_backward_bytes(const HeadsProblem& hp) {
+  // by the narrowest form, whatever the addresses allow: bounded by backward_blocks
+  size_t most = 0;
+  for (int vec : {8, 4, 1}) {
+    if (vec > 1 && (hp.rot.half % vec || (hp.d / 2) % vec)) continue;
+    const Grid g = grid_for(hp, vec);
+    most = std::max(most, (size_t)backward_blocks(g) * (g.ny[0] + g.ny[1]) * hp.d * 4);
+  }
+  return most;
+}
+
+hipError_t launch_heads_backward(const HeadsProblem& hp, hipStream_t st) {
+  const int vec = vector_for(hp);
+  const Grid g = grid_for(hp, vec);
+  const int gx = backward_blocks(g);
+  launch_any(hp, vec, g, dim3(gx, g.ny[0] + g.ny[1] + g.ny[2]), true, st);
+  const float* part = hp.dw_part;
+  for (int s = 0; s < 2; ++s) {
+    const int64_t n = (int64_t)gx * g.ny[s];
+    if (hp.dw[s]) {
+      const unsigned cols = (hp.d + 15) / 16;
+      if (hp.dtype) k_heads_weights<uint16_t><<<cols, 1024, 0, st>>>(part, (uint16_t*)hp.dw[s], n, hp.d);
+      else k_heads_weights<float><<<cols, 1024, 0, st>>>(part, (float*)hp.dw[s], n, hp.d);
+    }
+    part += n * hp.d;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace topk

@@ -5,15 +5,18 @@ only its inputs and the selected keys with their raw scores, the backward calls
 ``topk_attn_backward`` / ``topk_ffn_backward``.
 
 The projections around the attention are plain GEMMs left to PyTorch (rocBLAS);
-every top-k step runs in libtopk's kernels.
+every top-k step runs in libtopk's kernels, and so do head norms and rotary positions
+(``rotary``, ``norm_rotary_heads``), which the attention layer takes as options.
 """
 from __future__ import annotations
 
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
-from . import attn, attn_backward, attn_dense, ffn, ffn_backward
+from . import (attn, attn_backward, attn_dense, attn_prefix, ffn, ffn_backward, qk_norm_rope, qk_norm_rope_append,
+               qk_norm_rope_backward, rope, rope_axes, rope_frequencies)
 
 
 class TopkAttentionFunction(torch.autograd.Function):
@@ -52,6 +55,57 @@ class TopkFFNFunction(torch.autograd.Function):
         return dx, dw1, dw2, None, None
 
 
+class RotaryFunction(torch.autograd.Function):
+    """out = rope(x, ...), differentiable in x: the gradient turns back."""
+
+    @staticmethod
+    def forward(ctx, x, positions, freqs, axes, adjacent: bool):
+        ctx.save_for_backward(positions, freqs)
+        ctx.axes, ctx.adjacent = axes, adjacent
+        return rope(x, positions, freqs, axes, adjacent)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_out):
+        positions, freqs = ctx.saved_tensors
+        if d_out.stride(-1) != 1:
+            d_out = d_out.contiguous()
+        return rope(d_out, positions, freqs, ctx.axes, ctx.adjacent, inverse=True), None, None, None, None
+
+
+class NormRotaryHeadsFunction(torch.autograd.Function):
+    """q, k, v = qk_norm_rope(qkv, ...), differentiable in qkv and the weights; the backward
+    recomputes from qkv."""
+
+    @staticmethod
+    def forward(ctx, qkv, q_weight, k_weight, positions, freqs, heads, kv_heads, axes, adjacent, eps, norm):
+        ctx.save_for_backward(qkv, q_weight, k_weight, positions, freqs)
+        ctx.how = heads, kv_heads, axes, adjacent, eps, norm
+        return qk_norm_rope(qkv, heads, kv_heads, q_weight, k_weight, positions, freqs, axes, adjacent, eps, norm)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_q, d_k, d_v):
+        qkv, q_weight, k_weight, positions, freqs = ctx.saved_tensors
+        heads, kv_heads, axes, adjacent, eps, norm = ctx.how
+        d_qkv, d_wq, d_wk = qk_norm_rope_backward(
+            qkv, heads, kv_heads, d_q.contiguous(), d_k.contiguous(), d_v.contiguous(), q_weight, k_weight, positions, freqs,
+            axes, adjacent, eps, norm, weights=any(ctx.needs_input_grad[1:3]))
+        return (d_qkv, d_wq, d_wk) + (None,) * 8
+
+
+def rotary(x, positions, freqs, axes=None, adjacent: bool = False):
+    """Differentiable rotary positions on [B, H, L, d] heads; arguments as ``rope``."""
+    return RotaryFunction.apply(x, positions, freqs, axes, bool(adjacent))
+
+
+def norm_rotary_heads(qkv, heads: int, kv_heads: int, q_weight=None, k_weight=None, positions=None, freqs=None, axes=None,
+                      adjacent: bool = False, eps: float = 1e-6, norm: bool = True):
+    """Differentiable q, k, v heads of the packed projection; arguments as ``qk_norm_rope``."""
+    return NormRotaryHeadsFunction.apply(qkv, q_weight, k_weight, positions, freqs, int(heads), int(kv_heads), axes,
+                                         bool(adjacent), float(eps), bool(norm))
+
+
 def topk_attention(q, k, v, topk: int, chunk: int = 0, causal: bool = False, scale: float | None = None):
     """Differentiable top-k attention over contiguous [B, H, L, d] tensors."""
     if scale is None:
@@ -81,10 +135,17 @@ class TopkMultiheadAttention(torch.nn.Module):
     [q | k | v] = x W_qkv^T + b_qkv, head h takes columns h*d_h .. (h+1)*d_h - 1 of
     each; every head runs top-k attention (temperature 1/sqrt(d_h) unless given);
     y = concat(heads) W_o^T + b_o. With topk=None the heads keep every key (query
-    chunking without top-k, the paper's baseline; forward only)."""
+    chunking without top-k, the paper's baseline; forward only).
+
+    With ``qk_norm`` every query and key head is divided by its root mean square and scaled
+    by weights of its own (q_norm, k_norm, [d_h]); with ``rope_theta`` heads are rotated by
+    their positions, by one axis, or by several with ``rope_sections``, the pairs of each
+    (see ``rope_frequencies``, ``rope_axes``, and there ``rope_adjacent``). ``decode`` is the
+    serving form for a batch of requests behind a shared prefix (topk=None, causal)."""
 
     def __init__(self, d_model: int, n_heads: int, topk: int, chunk: int = 1024, causal: bool = False,
-                 bias: bool = True, scale: float | None = None, device=None, dtype=torch.bfloat16):
+                 bias: bool = True, scale: float | None = None, device=None, dtype=torch.bfloat16, qk_norm: bool = False,
+                 rope_theta: float | None = None, rope_sections=None, rope_adjacent: bool = False):
         super().__init__()
         if d_model % n_heads:
             raise ValueError(f"d_model {d_model} is not a multiple of n_heads {n_heads}")
@@ -94,15 +155,73 @@ class TopkMultiheadAttention(torch.nn.Module):
         kw = dict(device=device, dtype=dtype)
         self.qkv = torch.nn.Linear(d_model, 3 * d_model, bias=bias, **kw)
         self.out = torch.nn.Linear(d_model, d_model, bias=bias, **kw)
+        self.qk_norm, self.rope_axes, self.rope_adjacent = bool(qk_norm), None, bool(rope_adjacent)
+        if qk_norm:
+            self.q_norm = torch.nn.Parameter(torch.ones(self.d_head, **kw))
+            self.k_norm = torch.nn.Parameter(torch.ones(self.d_head, **kw))
+        if rope_theta is None and rope_sections is not None:
+            raise ValueError("rope_sections need rope_theta")
+        # the frequencies' bits as integers: a change of the module's type leaves them whole
+        self.register_buffer("rope_bits", None, persistent=False)
+        if rope_theta is not None:
+            pairs = self.d_head // 2 if rope_sections is None else tuple(rope_sections)
+            if rope_sections is not None:
+                self.rope_axes = rope_axes(pairs)
+            freqs = rope_frequencies(pairs, rope_theta, device="cpu")
+            if 2 * freqs.numel() > self.d_head:
+                raise ValueError(f"{freqs.numel()} pairs do not fit into {self.d_head} features")
+            self.rope_bits = freqs.view(torch.int64).to(device)
 
-    def forward(self, x):
+    def _rotation(self, positions, L: int, device):
+        if self.rope_bits is None:
+            if positions is not None:
+                raise ValueError("positions need rope_theta")
+            return dict(norm=self.qk_norm)
+        if positions is None:
+            positions = torch.arange(L, device=device)
+            if self.rope_axes is not None:
+                positions = positions.expand(max(self.rope_axes) + 1, 1, L)
+        return dict(positions=positions, freqs=self.rope_bits.view(torch.float64), axes=self.rope_axes,
+                    adjacent=self.rope_adjacent, norm=self.qk_norm)
+
+    def heads(self, x, positions=None):
+        """q, k, v [B, n_heads, L, d_h] as the attention sees them (the keys and values of a
+        shared prefix are k[0], v[0] of its own call)."""
+        if not self.qk_norm and self.rope_bits is None and positions is None:
+            B, L, D = x.shape
+            p = self.qkv(x).view(B, L, 3, self.n_heads, self.d_head).permute(2, 0, 3, 1, 4)
+            return tuple(p[t].contiguous() for t in range(3))
+        w = (self.q_norm, self.k_norm) if self.qk_norm else (None, None)
+        return norm_rotary_heads(self.qkv(x), self.n_heads, self.n_heads, *w, **self._rotation(positions, x.shape[1], x.device))
+
+    def forward(self, x, positions=None):
+        """x [B, L, d_model]; positions as ``rope`` takes them (default: 0 .. L - 1 on every axis)."""
         B, L, D = x.shape
-        p = self.qkv(x).view(B, L, 3, self.n_heads, self.d_head).permute(2, 0, 3, 1, 4)
-        q, k, v = (p[t].contiguous() for t in range(3))
+        q, k, v = self.heads(x, positions)
         if self.topk is None:
             o = dense_attention(q, k, v, self.chunk, self.causal, self.scale)
         else:
             o = topk_attention(q, k, v, self.topk, self.chunk, self.causal, self.scale)
+        return self.out(o.permute(0, 2, 1, 3).reshape(B, L, D))
+
+    @torch.no_grad()
+    def decode(self, x, prefix_k, prefix_v, k_cache, v_cache, lengths, positions=None):
+        """The next L tokens x [B, L, d_model] of B requests that share the prefix [n_heads, P,
+        d_h] and hold ``lengths[b]`` tokens in their caches [B, n_heads, S, d_h]: their keys and
+        values are appended (the caller advances lengths by L, and leaves room for them), and
+        each attends to the prefix, its own cache and the new tokens up to itself. positions
+        default to P + lengths[b] + 0 .. L - 1 on every axis."""
+        if self.topk is not None or not self.causal:
+            raise ValueError("decode attends to every earlier key: it needs topk=None and causal=True")
+        B, L, D = x.shape
+        if positions is None and self.rope_bits is not None:
+            positions = prefix_k.shape[1] + lengths[:, None] + torch.arange(L, device=x.device, dtype=torch.int32)
+            if self.rope_axes is not None:
+                positions = positions.expand(max(self.rope_axes) + 1, B, L)
+        w = (self.q_norm, self.k_norm) if self.qk_norm else (None, None)
+        q = qk_norm_rope_append(self.qkv(x), self.n_heads, self.n_heads, k_cache, v_cache, lengths, *w,
+                                **self._rotation(positions, L, x.device))
+        o = attn_prefix(q, prefix_k, prefix_v, k_cache, v_cache, lengths + L, True, self.scale)
         return self.out(o.permute(0, 2, 1, 3).reshape(B, L, D))
 
 

@@ -1,0 +1,302 @@
+"""GPU parity of shared-prefix attention against Eq. 1 in 64 bits, and of the layer that uses it.
+
+Tolerance of an output element: half a step of bf16 relative to it, and twice the relative error
+of a weight times sum_j w_j |v_j|. A weight is off by its score's rounding (d products summed in fp32:
+at most (d + 8) 2^-24 sum |q k| scale), by the rounding of the exponent (2^-23 of the largest) and by
+its own on the way into the second product: 2^-16 as the sum of two bf16 numbers, 2^-8 as one, which
+many rows a request may take.
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2106_06899_amd as tk
+from paper_2106_06899_amd import layers
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+@pytest.fixture(autouse=True, scope="module")
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    tk.lib()
+    yield
+
+
+def _inputs(B, H, Hkv, Lq, P, S, d, seed=0, std=2.0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    n = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(BF16)  # noqa: E731
+    q = (torch.randn(B, H, Lq, d, generator=gen, device="cuda") * std).to(BF16)
+    return q, n(Hkv, P, d), n(Hkv, P, d), n(B, Hkv, S, d), n(B, Hkv, S, d)
+
+
+def _check(q, pk, pv, k, v, lengths, causal, scale, out, lse=None):
+    """Every row against the 64-bit sum over exactly the keys it sees."""
+    B, H, Lq, d = q.shape
+    Hkv = (pk if pk is not None else k).shape[-3]
+    P = pk.shape[1] if pk is not None else 0
+    S = k.shape[2] if k is not None else 0
+    G = H // Hkv
+    wstep = 2.0 ** -16 if G * Lq < 64 else 2.0 ** -8
+    worst = 0.0
+    for b in range(B):
+        n = S if lengths is None else min(max(int(lengths[b]), 0), S)
+        for h in range(H):
+            parts = [t for t in ((pk[h // G] if P else None), (k[b, h // G, :n] if n else None)) if t is not None]
+            vals = [t for t in ((pv[h // G] if P else None), (v[b, h // G, :n] if n else None)) if t is not None]
+            if not parts:
+                assert not out[b, h].any()
+                assert lse is None or bool((lse[b, h] == -math.inf).all())
+                continue
+            kk, vv, qq = torch.cat(parts).double(), torch.cat(vals).double(), q[b, h].double()
+            s = qq @ kk.t() * scale
+            last = P + n - Lq + torch.arange(Lq, device="cuda") if causal else torch.full((Lq,), P + n - 1, device="cuda")
+            hidden = torch.arange(P + n, device="cuda") > torch.clamp(last, min=P - 1)[:, None]
+            s = s.masked_fill(hidden, -math.inf)
+            w = torch.softmax(s, -1).nan_to_num(0.0)
+            ref = w @ vv
+            size = (qq.abs() @ kk.abs().t()).masked_fill(hidden, 0).amax(-1, keepdim=True) * scale
+            delta = ((d + 8) * 2.0 ** -24 + 2.0 ** -22) * size + wstep
+            tol = 2.0 ** -8 * ref.abs() + 2 * delta * (w @ vv.abs()) + 1e-37
+            err = (out[b, h].double() - ref).abs()
+            assert bool((err <= tol).all()), f"request {b} head {h}: error {float((err / tol).max()):.2f} of its bound at {int((err / tol).argmax())}"
+            worst = max(worst, float((err / tol).max()))
+            if lse is not None:
+                want = torch.logsumexp(s, -1)
+                both = want == -math.inf
+                assert bool((lse[b, h][both] == -math.inf).all())
+                # (its terms' relative error, and three steps of the logarithm and the sum)
+                assert bool(((lse[b, h].double() - want).abs()[~both] <= (2 * (delta[..., 0] - wstep) + 2.0 ** -21 * (1 + want.abs()))[~both]).all())
+    print(f"[case] worst error {worst:.3f} of its bound", flush=True)
+
+
+CASES = {
+    # name: B, H, Hkv, Lq, P, S, d, causal, lengths
+    "one_of_each": (1, 1, 1, 1, 1, 1, 64, True, None),
+    "prefix_only": (2, 2, 2, 1, 33, 0, 64, True, None),
+    "cache_only": (3, 4, 2, 1, 0, 70, 128, True, [70, 1, 33]),
+    "decode": (4, 12, 12, 1, 500, 130, 64, True, [130, 1, 0, 77]),
+    "decode_shared_heads": (5, 8, 2, 1, 777, 300, 128, True, [300, 31, 32, 33, 299]),
+    "odd_groups": (3, 15, 3, 1, 97, 65, 128, False, [64, 65, 1]),
+    "lengths_out_of_range": (4, 2, 1, 1, 40, 50, 64, True, [-5, 51, 10 ** 9, 0]),
+    "nothing_to_see": (3, 2, 1, 2, 0, 40, 64, True, [0, 1, 40]),
+    "more_queries_than_keys": (3, 4, 2, 9, 0, 40, 128, True, [0, 4, 12]),
+    "more_queries_than_keys_prefix": (3, 4, 2, 9, 17, 40, 64, True, [0, 4, 12]),
+    "verify": (3, 8, 2, 5, 1001, 130, 64, True, [5, 130, 99]),
+    "verify_all_keys": (3, 8, 2, 5, 1001, 130, 64, False, [5, 130, 99]),
+    "thirty_two_rows": (2, 8, 1, 4, 300, 64, 128, True, [64, 4]),
+    "forty_rows": (2, 8, 1, 5, 300, 64, 128, True, [64, 5]),
+    "tile_edges": (2, 2, 2, 16, 256, 257, 128, True, [257, 255]),
+    "chunk": (2, 4, 2, 100, 333, 150, 128, True, [150, 100]),
+    "chunk_d64": (2, 4, 4, 130, 1025, 200, 64, True, [200, 131]),
+    "chunk_all_keys": (2, 4, 2, 65, 64, 65, 128, False, [65, 64]),
+    "chunk_empty_rows": (2, 4, 2, 129, 0, 300, 64, True, [20, 300]),
+    "chunk_groups": (1, 24, 3, 33, 700, 90, 128, True, [88]),
+    "one_long_chunk": (1, 2, 1, 515, 2100, 515, 64, True, [515]),
+    "many_requests": (70, 4, 2, 1, 600, 9, 64, True, [(7 * i) % 10 for i in range(70)]),
+    "long": (2, 2, 1, 1, 9999, 3000, 128, True, [3000, 2049]),
+}
+
+
+@pytest.mark.parametrize("name", sorted(CASES))
+def test_prefix(name):
+    B, H, Hkv, Lq, P, S, d, causal, lens = CASES[name]
+    q, pk, pv, k, v = _inputs(B, H, Hkv, Lq, P, S, d)
+    lengths = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out, lse = tk.attn_prefix(q, pk, pv, k, v, lengths, causal, lse=True)
+    _check(q, pk, pv, k, v, lens, causal, d ** -0.5, out, lse)
+    assert torch.equal(tk.attn_prefix(q, pk, pv, k, v, lengths, causal), out)
+
+
+def test_absent_parts_and_scale():
+    q, pk, pv, k, v = _inputs(3, 4, 2, 2, 90, 40, 64, seed=3)
+    n = torch.tensor([40, 2, 17], dtype=torch.int32, device="cuda")
+    for causal in (True, False):
+        assert torch.equal(tk.attn_prefix(q, pk, pv, causal=causal), tk.attn_prefix(q, pk, pv, k[:, :, :0], v[:, :, :0], causal=causal))
+        assert torch.equal(tk.attn_prefix(q, None, None, k, v, n, causal), tk.attn_prefix(q, pk[:, :0], pv[:, :0], k, v, n, causal))
+    out = tk.attn_prefix(q, pk, pv, k, v, n, scale=0.4)
+    _check(q, pk, pv, k, v, n.tolist(), True, 0.4, out)
+
+
+@pytest.mark.parametrize("Lq", [1, 80])
+def test_what_lies_behind_the_lengths_is_not_used(Lq):
+    q, pk, pv, k, v = _inputs(3, 4, 2, Lq, 70, 200, 128, seed=4)
+    n = torch.tensor([0, 133, 199], dtype=torch.int32, device="cuda")
+    want = tk.attn_prefix(q, pk, pv, k, v, n)
+    for b, m in enumerate(n.tolist()):
+        k[b, :, m:], v[b, :, m:] = math.nan, math.inf
+    assert torch.equal(tk.attn_prefix(q, pk, pv, k, v, n), want)
+
+
+def test_strided_keys():
+    """Caches cut from longer ones, heads behind tokens, prefixes cut from a buffer, one cache for all."""
+    q, pk, pv, k, v = _inputs(3, 4, 2, 1, 90, 40, 64, seed=5)
+    n = torch.tensor([40, 2, 17], dtype=torch.int32, device="cuda")
+    want = tk.attn_prefix(q, pk, pv, k, v, n)
+    cut = lambda t: torch.cat((t, torch.full_like(t, math.nan)), -2)[..., :t.shape[-2], :]  # noqa: E731
+    turned = lambda t: t.transpose(-3, -2).contiguous().transpose(-3, -2)  # noqa: E731
+    for f in (cut, turned, lambda t: torch.stack((t, t), -2)[..., 1, :]):
+        assert torch.equal(tk.attn_prefix(q, f(pk), f(pv), f(k), f(v), n), want)
+    assert torch.equal(tk.attn_prefix(q, pk, pv, k[:1].expand(3, 2, 40, 64), v, n),
+                       tk.attn_prefix(q, pk, pv, k[:1].expand(3, 2, 40, 64).contiguous(), v, n))
+
+
+def test_offsets_past_32_bits():
+    """Keys and values that lie more than 2^32 elements into their buffers."""
+    q, pk, pv, k, v = _inputs(2, 2, 1, 1, 100, 70, 64, seed=6)
+    n = torch.tensor([70, 50], dtype=torch.int32, device="cuda")
+    want = tk.attn_prefix(q, pk, pv, k, v, n)
+    big = torch.empty(2 ** 32 + 2 ** 20, dtype=BF16, device="cuda")
+    far = big.as_strided((2, 1, 70, 64), (2 ** 32, 70 * 64, 64, 1))
+    far.copy_(k)
+    assert torch.equal(tk.attn_prefix(q, pk, pv, far, v, n), want)
+    del big, far
+
+
+def test_extreme_scores():
+    """One key far above the rest; equal keys; weights far below the smallest normal number."""
+    d = 64
+    q, pk, pv, k, v = _inputs(2, 2, 2, 1, 300, 100, d, seed=7)
+    q[..., 0], pk[..., 0], k[..., 0] = 1.0, 0.0, 0.0
+    pk[:, 123, 0] = 3e4
+    out = tk.attn_prefix(q, pk, pv, k, v)
+    assert torch.equal(out, pv[:, 123].expand(2, 2, d)[:, :, None])
+    out, lse = tk.attn_prefix(torch.zeros_like(q), pk, pv, k, v, lse=True)
+    want = (pv.double().sum(1)[None] + v.double().sum(2)) / 400
+    # equal weights are exact; sums of 400 terms in fp32
+    tol = 2.0 ** -8 * want.abs() + 400 * 2.0 ** -24 * (pv.double().abs().sum(1)[None] + v.double().abs().sum(2)) / 400
+    assert bool(((out[:, :, 0].double() - want).abs() <= tol).all())
+    assert bool(((lse.double() - math.log(400)).abs() <= 2.0 ** -21 * 8).all())
+    # a weight of 2^-130 against a value of 2^120, the others' values 0
+    z = torch.zeros(1, 1, 200, d, device="cuda")
+    kk, vv, qq = z.clone(), z.clone(), torch.zeros(1, 1, 1, d, device="cuda")
+    qq[..., 0] = 1
+    kk[..., 0] = -1e4
+    kk[0, 0, 0, 0], kk[0, 0, 150, 0] = 0, -90.0 * 8
+    vv[0, 0, 150] = 2.0 ** 120
+    got = tk.attn_prefix(qq.to(BF16), None, None, kk.to(BF16), vv.to(BF16), scale=0.125).double()
+    ref = math.exp(-90.0) * 2.0 ** 120
+    assert bool(((got - ref).abs() <= (2.0 ** -4 + 2.0 ** -8) * ref).all()), got.flatten()[0]
+
+
+def test_parts_join_by_their_sums():
+    q, pk, pv, k, v = _inputs(3, 6, 3, 1, 400, 90, 128, seed=8)
+    n = torch.tensor([90, 1, 40], dtype=torch.int32, device="cuda")
+    whole, total = tk.attn_prefix(q, pk, pv, k, v, n, lse=True)
+    (a, la), (b, lb) = tk.attn_prefix(q, pk, pv, lse=True), tk.attn_prefix(q, None, None, k, v, n, lse=True)
+    joined = (a.double() * (la - total).double().exp()[..., None] + b.double() * (lb - total).double().exp()[..., None])
+    # each part and the whole rounded to bf16
+    assert bool(((joined - whole.double()).abs() <= 2.0 ** -8 * (whole.double().abs() + a.double().abs() + b.double().abs()) + 1e-5).all())
+
+
+def test_refusals_of_the_binding():
+    q, pk, pv, k, v = _inputs(2, 4, 2, 1, 20, 10, 64)
+    n = torch.zeros(2, dtype=torch.int32, device="cuda")
+    bad = [
+        lambda: tk.attn_prefix(q), lambda: tk.attn_prefix(q, pk), lambda: tk.attn_prefix(q, pk, pv, k), lambda: tk.attn_prefix(q[0], pk, pv),
+        lambda: tk.attn_prefix(q, pk[0], pv), lambda: tk.attn_prefix(q, pk, pv[:, :19]), lambda: tk.attn_prefix(q, pk, pv, k[:1], v[:1]),
+        lambda: tk.attn_prefix(q, pk, pv, k, v[:, :, :9]), lambda: tk.attn_prefix(q, pk, pv, k[0], v[0]), lambda: tk.attn_prefix(q, pk, pv, k, v, n.long()),
+        lambda: tk.attn_prefix(q, pk, pv, k, v, n[:1]), lambda: tk.attn_prefix(q, pk, pv, k, v, n.cpu()), lambda: tk.attn_prefix(q[:, :3].contiguous(), pk, pv),
+        lambda: tk.attn_prefix(q.float(), pk.float(), pv.float()), lambda: tk.attn_prefix(q, pk.float(), pv), lambda: tk.attn_prefix(q, pk, pv, scale=0.0),
+        lambda: tk.attn_prefix(q, pk.transpose(1, 2), pv), lambda: tk.attn_prefix(q[..., :32].contiguous(), pk[..., :32], pv[..., :32]),
+        lambda: tk.attn_prefix(q, torch.zeros(2 * 20 * 68, dtype=BF16, device="cuda").view(2, 20, 68)[..., :64], pv),
+        lambda: tk.attn_prefix(q.expand(2, 4, 1, 64)[:, ::2], pk, pv),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises((ValueError, TypeError, tk.TopkError)):
+            call()
+            print("accepted:", i)
+
+
+def test_small_registered_workspace_is_refused():
+    import ctypes
+    q, pk, pv, k, v = _inputs(2, 2, 2, 1, 90, 40, 64)
+    out, ws, L = torch.empty_like(q), torch.empty(1024, dtype=torch.uint8, device="cuda"), tk.lib()
+    need = tk.attn_prefix_workspace_bytes(2, 2, 2, 1, 90, 40, 64)
+    assert need > 1024
+    args = [t.data_ptr() for t in (q, pk, pv, k, v)] + [None, out.data_ptr(), None, 2, 2, 2, 1, 90, 40, 64, None, 1, 0.125, 1, None]
+    try:
+        assert L.topk_set_workspace(ctypes.c_void_p(ws.data_ptr()), 1024) == 0
+        assert L.topk_attn_prefix(*args) == -5
+    finally:
+        L.topk_set_workspace(None, 0)
+    # none registered: the library allocates its own on the stream
+    assert L.topk_attn_prefix(*args) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out, tk.attn_prefix(q, pk, pv, k, v))
+
+
+@pytest.mark.parametrize("Lq", [1, 96])
+def test_other_streams_and_replayed_graphs(Lq):
+    """Two side streams at once, and two graphs that replay in turn with other lengths."""
+    n = torch.tensor([40, 96, 139], dtype=torch.int32, device="cuda")
+    a, b = _inputs(3, 4, 2, Lq, 600, 140, 64, seed=9), _inputs(3, 4, 2, Lq, 350, 140, 128, seed=10)
+    wa, wb = tk.attn_prefix(*a, n), tk.attn_prefix(*b, n)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(s1):
+            ga = tk.attn_prefix(*a, n)
+        with torch.cuda.stream(s2):
+            gb = tk.attn_prefix(*b, n)
+        torch.cuda.synchronize()
+        assert torch.equal(ga, wa) and torch.equal(gb, wb)
+    g1, g2 = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g1):
+        oa = tk.attn_prefix(*a, n)
+    with torch.cuda.graph(g2, pool=g1.pool()):
+        ob = tk.attn_prefix(*b, n)
+    for rep in range(4):
+        n.copy_(torch.tensor([[40, 96, 139], [96, 0, 140], [1, 100, 3], [140, 140, 140]][rep], dtype=torch.int32))
+        g1.replay()
+        ra = oa.clone()
+        g2.replay()
+        rb = ob.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(ra, tk.attn_prefix(*a, n)) and torch.equal(rb, tk.attn_prefix(*b, n)), f"replay {rep}"
+
+
+def test_layer_trains_with_norm_and_rotation():
+    """The layer's heads are the head call's, its outputs and gradients those of its parts."""
+    torch.manual_seed(0)
+    m = layers.TopkMultiheadAttention(128, 2, 16, 64, True, device="cuda", qk_norm=True, rope_theta=1e4)
+    x = torch.randn(2, 90, 128, device="cuda", dtype=BF16, requires_grad=True)
+    y = m(x)
+    g = torch.randn_like(y)
+    grads = torch.autograd.grad(y, [x, *m.parameters()], g)
+    f = tk.rope_frequencies(32, 1e4)
+    xx = x.detach().clone().requires_grad_()
+    q, k, v = layers.norm_rotary_heads(m.qkv(xx), 2, 2, m.q_norm, m.k_norm, torch.arange(90, device="cuda"), f)
+    o = layers.topk_attention(q, k, v, 16, 64, True, m.scale)
+    z = m.out(o.permute(0, 2, 1, 3).reshape(2, 90, 128))
+    assert torch.equal(y, z)
+    for a, b in zip(grads, torch.autograd.grad(z, [xx, *m.parameters()], g)):
+        assert torch.equal(a, b) and a.isfinite().all()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(qk_norm=True, rope_theta=1e4), dict(rope_theta=1e4, rope_sections=(8, 12, 12), rope_adjacent=True)])
+def test_decode_continues_a_shared_prefix(kw):
+    """A prompt shared by three requests, decoded in steps of 1, 3 and 2 tokens: each step's outputs are
+    the whole sequence's rows, as one dense causal call computes them. Both round q, k, v and the heads'
+    outputs to bf16 at the same places; weights are 2^-8 off in the dense call, which doubled by the
+    norm and summed over 128 columns of the output projection stays below 2^-5 of the largest output."""
+    torch.manual_seed(1)
+    m = layers.TopkMultiheadAttention(128, 2, None, 64, True, device="cuda", **kw)
+    P, steps, B, S = 50, (1, 3, 2), 3, 12
+    x = torch.randn(B, P + sum(steps), 128, device="cuda", dtype=BF16)
+    x[:, :P] = x[:1, :P]
+    with torch.no_grad():
+        want = m(x)
+        _, pk, pv = m.heads(x[:1, :P])
+    kc, vc = (torch.full((B, 2, S, 64), math.nan, device="cuda", dtype=BF16) for _ in range(2))
+    lengths = torch.zeros(B, dtype=torch.int32, device="cuda")
+    at = P
+    for n in steps:
+        y = m.decode(x[:, at:at + n], pk[0], pv[0], kc, vc, lengths)
+        ref = want[:, at:at + n].double()
+        assert bool(((y.double() - ref).abs() <= 2.0 ** -5 * want.double().abs().max()).all())
+        lengths += n
+        at += n
+    assert bool(kc[:, :, at - P:].isnan().all()) and bool(kc[:, :, :at - P].isfinite().all())
