@@ -909,7 +909,7 @@ int cache_ptr(const char* name, const void* p, std::initializer_list<int64_t> st
   for (int64_t s : strides)
     if (s % 8) return fail(TOPK_E_ALIGN, "a stride of %s is not a multiple of 8 elements: %lld", name, (long long)s);
   const int64_t key = *(strides.end() - 1);
-  if (key >= int64_t(1) << 26) return fail(TOPK_E_UNSUPPORTED, "the keys of %s lie 2^26 elements apart or more", name);
+  if (key >= int64_t(1) << 24) return fail(TOPK_E_UNSUPPORTED, "the keys of %s lie 2^24 elements apart or more", name);
   return TOPK_OK;
 }
 

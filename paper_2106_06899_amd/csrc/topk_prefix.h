@@ -20,9 +20,9 @@ struct PrefixProblem {
   float scale;
 };
 
-// How the work is cut: row tiles of RT rows, and key ranges whose partial results are joined.
+// How the work is cut: row tiles, and key ranges whose partial results are joined.
 struct PrefixPlan {
-  int nr;                     // blocks of 16 rows of a workgroup's tile
+  int pblocks, sblocks;       // blocks of 16 rows of a workgroup's tile, on the prefix and on own keys
   int64_t rows;               // B * H * Lq
   int64_t req_rows;           // rows of one request and key head: (H / Hkv) * Lq
   int64_t ptiles, psplits, pkeys;  // prefix: row tiles of a key head, key ranges, keys of a range

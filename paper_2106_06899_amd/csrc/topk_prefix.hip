@@ -30,6 +30,10 @@ namespace topk {
 namespace {
 
 constexpr int NT = 256, WAVES = 4, KT = 32;
+constexpr int JOIN_MAX = 1024;  // key ranges of a row at most,
+constexpr int JOIN_FEW = 16;    // where a workgroup joins several rows
+// s_waitcnt immediate: no vector-memory operation outstanding, the other counters ignored
+constexpr int WAIT_VM0 = (7 << 4) | (15 << 8);
 
 struct PrefixArgs {
   PrefixProblem p;
@@ -50,18 +54,24 @@ struct Item {
   int64_t split;  // where its partial result goes
 };
 
+// A workgroup's LDS: four tile buffers (the few-row form keeps a wave's outputs in each), and the
+// waves' maxima and sums.
+struct Lds {
+  unsigned char *b0, *b1, *b2, *b3;
+  float2 (*ml)[32];
+  __device__ unsigned char* of(int w) const { return w == 0 ? b0 : w == 1 ? b1 : w == 2 ? b2 : b3; }
+};
+
+// 16 NR rows: the waves take key tiles in turn, K and V in registers.
 template <int D, int NR>
-struct Body {
+struct Few {
   static constexpr int NS = D / 32;  // steps over the features of the scores
   static constexpr int NC = D / 16;  // blocks of 16 output features; columns of V a lane reads
   static constexpr int VB = NC * 2;  // their bytes
   static constexpr int LD = D + 4;
-  struct Shared {
-    float o[WAVES][16][LD];
-    float2 ml[WAVES][16 * NR];
-  };
+  typedef float Rows[LD];            // 16 of them a wave
 
-  static __device__ __forceinline__ void run(const PrefixArgs& a, const Item& it, Shared& sh) {
+  static __device__ __forceinline__ void run(const PrefixArgs& a, const Item& it, const Lds& sh) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, g = lane >> 4;
     const int64_t R = a.pl.req_rows, Lq = a.p.Lq, HL = a.p.H * Lq;
     // the lane's rows: where they lie in q and out, and how many keys they see
@@ -213,7 +223,7 @@ struct Body {
 #pragma unroll
       for (int v = 0; v < 4; ++v)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) sh.o[wave][n][(4 * g + v) * NC + c] = o[r][c][v] * f;
+        for (int c = 0; c < NC; ++c) ((Rows*)sh.of(wave))[n][(4 * g + v) * NC + c] = o[r][c][v] * f;
       __syncthreads();
       for (int i = tid; i < 16 * D / 4; i += NT) {
         const int row = i / (D / 4), col = (i % (D / 4)) * 4;
@@ -225,7 +235,7 @@ struct Body {
         float tm = -INFINITY, tl = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-          sum += *(const f32x4*)&sh.o[w][row][col];
+          sum += *(const f32x4*)&((const Rows*)sh.of(w))[row][col];
           tm = fmaxf(tm, sh.ml[w][16 * r + row].x);
         }
 #pragma unroll
@@ -247,13 +257,228 @@ struct Body {
   }
 };
 
-template <int D, int NRP, int NRS>
-__global__ __launch_bounds__(NT, NRP > 2 ? 1 : 2) void k_prefix(PrefixArgs a) {
-  union Both {
-    typename Body<D, NRP>::Shared p;
-    typename Body<D, NRS>::Shared s;
-  };
-  __shared__ __attribute__((aligned(16))) Both sh;
+// 128 rows, 32 a wave: every wave takes every key tile of 64, K and V through LDS.
+//   * S^T = K Q^T by v_mfma_f32_32x32x16_bf16: lane l holds 16 keys' scores of row l % 32 a 32-key
+//     block, keys 8 (v / 4) + 4 (l / 32) + v % 4;
+//   * O^T += V^T P^T by the same instruction: the weights are its operand in the order the lane holds
+//     them, V^T comes from the row-major tile by transposing LDS reads (four keys of a feature each).
+// Tiles come by direct global-to-LDS loads, one ahead; the 16-byte parts of their rows are permuted so
+// that the lanes of one LDS cycle meet different banks. Weights enter the second product rounded to
+// bf16 (relative 2^-8 at most): products bound this form, and a second term would add half as many.
+typedef float f32x16 __attribute__((__vector_size__(64)));
+typedef short s16x4 __attribute__((__vector_size__(8)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+template <int D, bool TWO>
+struct Wide {
+  // Weights are formed as 2^24 times themselves, so that the exponential instruction, which knows no
+  // numbers below 2^-126, keeps every weight that 32 bits can hold.
+  static constexpr float LIFT = 24.f;
+  static constexpr int KEYS = 64;         // of a tile
+  static constexpr int NS = D / 16;       // steps over the features of the scores
+  static constexpr int CH = 2 * D / 16;   // 16-byte parts of a row
+  static constexpr int TILEB = KEYS * 2 * D;
+  static constexpr int LPW = TILEB / 1024 / WAVES;
+  static constexpr int FB = D / 32;       // 32-feature blocks of the output
+
+  static __device__ __forceinline__ int swz_k(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+  static __device__ __forceinline__ int swz_v(int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
+
+  static __device__ __forceinline__ void run(const PrefixArgs& a, const Item& it, const Lds& sh) {
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 31, half = lane >> 5;
+    const int64_t R = a.pl.req_rows, Lq = a.p.Lq, HL = a.p.H * Lq;
+    const bool causal = it.b >= 0 && a.p.causal;
+    const int64_t i = it.r0 + wave * 32 + n;
+    const bool ok = i < it.count;
+    const bool work = it.r0 + wave * 32 < it.count;  // the wave has rows
+    const int64_t ii = ok ? i : it.r0;
+    const int64_t b = it.b >= 0 ? it.b : ii / R, rr = it.b >= 0 ? ii : ii - b * R;
+    const int64_t at = b * HL + it.h * R + rr;
+    int64_t seen = it.len;
+    if (causal) {
+      const int64_t t = it.len - Lq + rr % Lq + 1;
+      seen = t < 0 ? 0 : t;
+    }
+    bf16x8 bq[NS];
+    {
+      const uint16_t* q = (const uint16_t*)a.p.q + at * D + (D / 2) * half;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) bq[s] = *(const bf16x8*)(q + 8 * s);
+    }
+    // keys before all_see are seen by every row, keys from k1 by none of the tile
+    int64_t all_see = it.len, k1 = it.k1;
+    if (causal) {
+      const int64_t r1 = min(it.r0 + 128, it.count) - 1;
+      const bool wraps = r1 / Lq != it.r0 / Lq;
+      all_see = it.len - Lq + (wraps ? 0 : it.r0 % Lq) + 1;
+      k1 = min(k1, it.len - Lq + (wraps ? Lq - 1 : r1 % Lq) + 1);
+    }
+    const int64_t tiles = k1 > it.k0 ? (k1 - it.k0 + KEYS - 1) / KEYS : 0;
+
+    // where the lane's parts of a tile lie, in bytes from its first key
+    uint32_t koff[LPW], voff[LPW];
+#pragma unroll
+    for (int j = 0; j < LPW; ++j) {
+      const int cidx = (wave * LPW + j) * 64 + lane, r = cidx / CH, c = cidx % CH;
+      koff[j] = r * (uint32_t)it.k_sl * 2 + (c ^ swz_k(r)) * 16;
+      voff[j] = r * (uint32_t)it.v_sl * 2 + (c ^ swz_v(r)) * 16;
+    }
+    auto issue = [&](int64_t t, unsigned char* kd, unsigned char* vd) {
+      const int64_t first = it.k0 + t * KEYS;
+      const unsigned char* kt = (const unsigned char*)(it.k + first * it.k_sl);
+      const unsigned char* vt = (const unsigned char*)(it.v + first * it.v_sl);
+      const int left = (int)min((int64_t)KEYS, k1 - first) - 1;
+#pragma unroll
+      for (int j = 0; j < LPW; ++j) {
+        uint32_t ko = koff[j], vo = voff[j];
+        if (left < KEYS - 1) {  // rows past the range load its last one
+          const int r = ((wave * LPW + j) * 64 + lane) / CH, over = r - min(r, left);
+          ko -= over * (uint32_t)it.k_sl * 2;
+          vo -= over * (uint32_t)it.v_sl * 2;
+        }
+        __builtin_amdgcn_global_load_lds((const void*)(kt + ko), (__attribute__((address_space(3))) void*)&kd[(wave * LPW + j) * 1024], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const void*)(vt + vo), (__attribute__((address_space(3))) void*)&vd[(wave * LPW + j) * 1024], 16, 0, 0);
+      }
+    };
+
+    f32x16 o[FB];
+#pragma unroll
+    for (int f = 0; f < FB; ++f) o[f] = (f32x16){};
+    float m = -INFINITY, l = 0.f;
+    // the lane's place in a V tile: row 4 half + (lane & 15) / 4, 8 bytes of it
+    const int va = lane & 15, vrow = 4 * half + (va >> 2);
+    int vat[FB];
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+      vat[f] = vrow * 2 * D + (((f * 4 + ((lane >> 4) & 1) * 2 + ((va & 3) >> 1)) ^ swz_v(vrow)) * 16) + (va & 1) * 8;
+
+    auto tile = [&](auto edge, int64_t t, const unsigned char* kb, const unsigned char* vb) {
+      f32x16 s[2];
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) {
+        const int r = rb * 32 + n;
+        f32x16 acc = {};
+#pragma unroll
+        for (int st = 0; st < NS; ++st) {
+          const bf16x8 av = *(const bf16x8*)(kb + (r * CH + ((half * NS + st) ^ swz_k(r))) * 16);
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bq[st], acc, 0, 0, 0);
+        }
+        s[rb] = acc;
+      }
+      if (decltype(edge)::value) {
+        const int last = (int)max((int64_t)-1, min(min(k1, seen) - it.k0 - t * KEYS, (int64_t)KEYS)) - 4 * half;
+#pragma unroll
+        for (int v = 0; v < 32; ++v)
+          if ((v >> 4) * 32 + 8 * ((v & 15) >> 2) + (v & 3) >= last) s[v >> 4][v & 15] = -INFINITY;
+      }
+      float mt = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < 32; v += 2)
+        mt = __builtin_elementwise_maximum(__builtin_elementwise_maximum(mt, s[v >> 4][v & 15]), s[v >> 4][(v & 15) + 1]);
+      mt = __builtin_elementwise_maximum(mt, __shfl_xor(mt, 32, 64));
+      mt *= a.c;
+      if (__builtin_amdgcn_ballot_w64(!(mt <= m))) {  // (for NaN too; rows whose maximum stays multiply by 1)
+        const float mn = fmaxf(m, mt);
+        const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int f = 0; f < FB; ++f)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[f][v] *= alpha;
+      }
+      const float bias = LIFT - (m == -INFINITY ? 0.f : m);
+#pragma unroll
+      for (int st = 0; st < 4; ++st) {  // 16 keys each
+        bf16x8 pb, pl;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(s[st >> 1][8 * (st & 1) + e], a.c, bias));
+          l += w;
+          pb[e] = (__bf16)w;
+          if (TWO) pl[e] = (__bf16)(w - (float)pb[e]);
+        }
+#pragma unroll
+        for (int f = 0; f < FB; ++f) {
+          const unsigned char* p = vb + vat[f] + st * 16 * 2 * D;
+          const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
+          const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * 2 * D));
+          const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+          o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, pb, o[f], 0, 0, 0);
+          if (TWO) o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, pl, o[f], 0, 0, 0);
+        }
+      }
+    };
+
+    // One tile of lookahead: before tile t is read, this wave's loads of it are complete and the barrier
+    // publishes every wave's part; it also proves that no wave still reads the buffers the next loads
+    // overwrite. (The buffers are named at compile time, so that reads of one pair do not wait for loads
+    // into the other.) Tiles that every row sees whole come first and need no mask.
+    const int64_t whole = min(tiles, max((int64_t)0, min(k1, all_see) - it.k0) / KEYS);
+    auto ready = [&](int64_t t, unsigned char* kn, unsigned char* vn) {
+      __builtin_amdgcn_s_waitcnt(WAIT_VM0);
+      __syncthreads();
+      if (t + 1 < tiles) issue(t + 1, kn, vn);
+    };
+    if (tiles > 0) issue(0, sh.b0, sh.b2);
+    int64_t t = 0;
+    for (; t + 1 < whole; t += 2) {
+      ready(t, sh.b1, sh.b3);
+      if (work) tile(std::false_type{}, t, sh.b0, sh.b2);
+      ready(t + 1, sh.b0, sh.b2);
+      if (work) tile(std::false_type{}, t + 1, sh.b1, sh.b3);
+    }
+    for (; t < tiles; ++t) {
+      const bool odd = t & 1;
+      ready(t, odd ? sh.b0 : sh.b1, odd ? sh.b2 : sh.b3);
+      if (work) tile(std::true_type{}, t, odd ? sh.b1 : sh.b0, odd ? sh.b3 : sh.b2);
+    }
+    m -= LIFT;
+    l += __shfl_xor(l, 32, 64);
+    if (!ok) return;
+    if (a.pl.psplits + a.pl.ssplits == 1) {
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      uint16_t* dst = (uint16_t*)a.p.out + at * D + 4 * half;
+#pragma unroll
+      for (int f = 0; f < FB; ++f)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+          *(uint2*)(dst + 32 * f + 2 * v) = make_uint2(pack_bf16(o[f][v] * inv, o[f][v + 1] * inv), pack_bf16(o[f][v + 2] * inv, o[f][v + 3] * inv));
+      if (a.p.lse && half == 0) a.p.lse[at] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+      return;
+    }
+    float* dst = a.po + (it.split * a.pl.rows + at) * D + 4 * half;
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4) *(f32x4*)(dst + 32 * f + 2 * v) = (f32x4){o[f][v], o[f][v + 1], o[f][v + 2], o[f][v + 3]};
+    if (half == 0) a.ml[it.split * a.pl.rows + at] = make_float2(m, l);
+  }
+};
+
+// NB: blocks of 16 rows of an item; 8 is the wide form
+template <int D, int NB>
+struct Form {
+  typedef Few<D, NB> type;
+};
+template <int D>
+struct Form<D, 8> {
+  typedef Wide<D, false> type;
+};
+template <int D>
+struct Form<D, 9> {
+  typedef Wide<D, true> type;
+};
+
+template <int D, int NBP, int NBS>
+__global__ __launch_bounds__(NT, 2) void k_prefix(PrefixArgs a) {
+  constexpr int BUF = 64 * 2 * D;
+  __shared__ __attribute__((aligned(16))) unsigned char b0[BUF];
+  __shared__ __attribute__((aligned(16))) unsigned char b1[BUF];
+  __shared__ __attribute__((aligned(16))) unsigned char b2[BUF];
+  __shared__ __attribute__((aligned(16))) unsigned char b3[BUF];
+  __shared__ float2 ml[WAVES][32];
+  const Lds sh = {b0, b1, b2, b3, ml};
   const PrefixPlan& pl = a.pl;
   const int64_t np = a.p.Hkv * pl.psplits * pl.ptiles;
   int64_t i = blockIdx.x;
@@ -269,11 +494,11 @@ __global__ __launch_bounds__(NT, NRP > 2 ? 1 : 2) void k_prefix(PrefixArgs a) {
     it.k_sl = a.p.pk_sl;
     it.v_sl = a.p.pv_sl;
     it.count = a.p.B * pl.req_rows;
-    it.r0 = tile * 16 * NRP;
+    it.r0 = tile * 16 * (NBP & ~1 ? NBP & ~1 : 1);
     it.len = a.p.P;
     it.k0 = it.split * pl.pkeys;
     it.k1 = min(it.k0 + pl.pkeys, it.len);
-    Body<D, NRP>::run(a, it, sh.p);
+    Form<D, NBP>::type::run(a, it, sh);
     return;
   }
   i -= np;
@@ -286,37 +511,85 @@ __global__ __launch_bounds__(NT, NRP > 2 ? 1 : 2) void k_prefix(PrefixArgs a) {
   it.k_sl = a.p.k_sl;
   it.v_sl = a.p.v_sl;
   it.count = pl.req_rows;
-  it.r0 = tile * 16 * NRS;
+  it.r0 = tile * 16 * (NBS & ~1 ? NBS & ~1 : 1);
   const int64_t len = a.p.lengths ? a.p.lengths[it.b] : a.p.S;
   it.len = len < 0 ? 0 : min(len, a.p.S);
   it.k0 = min(split * pl.skeys, it.len);
   it.k1 = min(it.k0 + pl.skeys, it.len);
-  Body<D, NRS>::run(a, it, sh.s);
+  Form<D, NBS>::type::run(a, it, sh);
 }
 
-// Joins a row's partial results: D / 4 lanes a row.
-template <int D>
+// Joins a row's partial results. ROWS rows a workgroup: NT / ROWS threads a row, D / 4 columns by
+// as many groups as there are left, each taking every so manieth range; the ranges' factors come
+// first, one thread a range.
+template <int D, int ROWS>
 __global__ __launch_bounds__(NT) void k_prefix_join(PrefixArgs a) {
-  constexpr int LR = D / 4;
-  const int64_t row = (int64_t)blockIdx.x * (NT / LR) + threadIdx.x / LR;
-  const int col = (threadIdx.x % LR) * 4;
-  if (row >= a.pl.rows) return;
+  constexpr int TR = NT / ROWS, LR = D / 4, Q = TR / LR;
+  static_assert(Q >= 1, "a thread has at least one column group");
+  __shared__ float fac[ROWS][ROWS == 1 ? JOIN_MAX : JOIN_FEW];
+  __shared__ f32x4 part[ROWS][Q][LR];
+  const int rl = threadIdx.x / TR, tr = threadIdx.x % TR, q = tr / LR, c = tr % LR;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + rl;
+  const bool ok = row < a.pl.rows;
   const int splits = (int)(a.pl.psplits + a.pl.ssplits);
-  float top = -INFINITY;
-  for (int s = 0; s < splits; ++s) top = fmaxf(top, a.ml[s * a.pl.rows + row].x);
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  float total = 0.f;
-  for (int s = 0; s < splits; ++s) {
-    const float2 x = a.ml[s * a.pl.rows + row];
-    if (x.x == -INFINITY) continue;  // saw no key
-    const float f = exp2f(x.x - top);
-    sum += *(const f32x4*)(a.po + (s * a.pl.rows + row) * D + col) * f;
-    total += x.y * f;
+  float top = -INFINITY, total = 0.f;
+  if (ok) {
+    if (splits <= 4) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if (s < splits) top = fmaxf(top, a.ml[s * a.pl.rows + row].x);
+    } else {
+      for (int s = tr; s < splits; s += TR) top = fmaxf(top, a.ml[s * a.pl.rows + row].x);
+    }
   }
+  if (splits > 4) {  // (TR lanes of a row: 32 or more of one wave, or whole waves)
+    for (int o = 1; o < (TR < 64 ? TR : 64); o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if (TR > 64) {
+      if (threadIdx.x % 64 == 0) fac[rl][threadIdx.x % TR / 64] = top;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < TR / 64; ++w) top = fmaxf(top, fac[rl][w]);
+      __syncthreads();
+    }
+  }
+  if (ok)
+    for (int s = tr; s < splits; s += TR) {
+      const float2 x = a.ml[s * a.pl.rows + row];
+      const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - top);
+      fac[rl][s] = f;
+      total += f * x.y;
+    }
+  for (int o = 1; o < (TR < 64 ? TR : 64); o <<= 1) total += __shfl_xor(total, o, 64);
+  __syncthreads();
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  if (ok) {
+    const float* p = a.po + row * D + 4 * c;
+#pragma unroll 4
+    for (int s = q; s < splits; s += Q) {
+      const float f = fac[rl][s];
+      const f32x4 x = *(const f32x4*)(p + (int64_t)s * a.pl.rows * D);
+      if (f != 0.f) sum += x * f;  // (a range without keys leaves zeros)
+    }
+  }
+  if (Q > 1) {
+    part[rl][q][c] = sum;
+    __shared__ float tot[ROWS][4];
+    if (TR > 64 && threadIdx.x % 64 == 0) tot[rl][threadIdx.x % TR / 64] = total;
+    __syncthreads();
+    if (q > 0) return;
+#pragma unroll
+    for (int k = 1; k < Q; ++k) sum += part[rl][k][c];
+    if (TR > 64) {
+      total = 0.f;
+#pragma unroll
+      for (int w = 0; w < TR / 64; ++w) total += tot[rl][w];
+    }
+  }
+  if (!ok) return;
   const float inv = total > 0.f ? 1.f / total : 0.f;
   const uint2 w = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));
-  *(uint2*)((uint16_t*)a.p.out + row * D + col) = w;
-  if (a.p.lse && col == 0) a.p.lse[row] = total > 0.f ? (top + log2f(total)) * 0.69314718055994531f : -INFINITY;
+  *(uint2*)((uint16_t*)a.p.out + row * D + 4 * c) = w;
+  if (a.p.lse && c == 0) a.p.lse[row] = total > 0.f ? (top + log2f(total)) * 0.69314718055994531f : -INFINITY;
 }
 
 int64_t cdiv(int64_t x, int64_t y) { return (x + y - 1) / y; }
@@ -331,7 +604,7 @@ PrefixArgs args_for(const PrefixProblem& pp, const PrefixPlan& pl, const void* w
   return a;
 }
 
-int blocks_for(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+int blocks_for(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 8; }
 
 }  // namespace
 
@@ -339,13 +612,14 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
   PrefixPlan pl = {};
   pl.rows = pp.B * pp.H * pp.Lq;
   pl.req_rows = pp.H / pp.Hkv * pp.Lq;
-  pl.nr = blocks_for(pp.P ? pp.B * pl.req_rows : pl.req_rows);
-  const int ns = blocks_for(pl.req_rows);
-  pl.ptiles = cdiv(pp.B * pl.req_rows, 16 * pl.nr);
-  pl.stiles = cdiv(pl.req_rows, 16 * ns);
+  pl.sblocks = blocks_for(pl.req_rows);
+  pl.pblocks = pp.P ? blocks_for(pp.B * pl.req_rows) : pl.sblocks;
+  pl.ptiles = cdiv(pp.B * pl.req_rows, 16 * pl.pblocks);
+  pl.stiles = cdiv(pl.req_rows, 16 * pl.sblocks);
   // ranges of equal length, as many as give two workgroups a CU, of 256 keys at least
   const int64_t keys = pp.Hkv * pl.ptiles * pp.P + pp.B * pp.Hkv * pl.stiles * pp.S;
-  const int64_t range = std::max<int64_t>(256, cdiv(cdiv(keys, 512), 128) * 128);
+  int64_t range = std::max<int64_t>(256, cdiv(cdiv(keys, 512), 128) * 128);
+  range = std::max(range, cdiv(std::max(pp.P, pp.S), JOIN_MAX / 2 * 128) * 128);
   pl.psplits = cdiv(pp.P, range);
   pl.ssplits = cdiv(pp.S, range);
   pl.pkeys = pl.psplits ? cdiv(cdiv(pp.P, pl.psplits), 128) * 128 : 128;
@@ -361,13 +635,15 @@ size_t prefix_bytes(const PrefixProblem& pp, const PrefixPlan& pl) {
 }
 
 template <int D>
-static void launch_d(const PrefixArgs& a, int np, int ns, unsigned grid, hipStream_t st) {
+static void launch_d(const PrefixArgs& a, unsigned grid, hipStream_t st) {
+  const int np = a.pl.pblocks, ns = a.pl.sblocks;
   if (np == 1) k_prefix<D, 1, 1><<<grid, NT, 0, st>>>(a);
   else if (np == 2 && ns == 1) k_prefix<D, 2, 1><<<grid, NT, 0, st>>>(a);
   else if (np == 2) k_prefix<D, 2, 2><<<grid, NT, 0, st>>>(a);
-  else if (ns == 1) k_prefix<D, 4, 1><<<grid, NT, 0, st>>>(a);
-  else if (ns == 2) k_prefix<D, 4, 2><<<grid, NT, 0, st>>>(a);
-  else k_prefix<D, 4, 4><<<grid, NT, 0, st>>>(a);
+  else if (ns == 1) k_prefix<D, 9, 1><<<grid, NT, 0, st>>>(a);
+  else if (ns == 2) k_prefix<D, 9, 2><<<grid, NT, 0, st>>>(a);
+  else if (a.pl.req_rows < 64) k_prefix<D, 9, 9><<<grid, NT, 0, st>>>(a);
+  else k_prefix<D, 8, 8><<<grid, NT, 0, st>>>(a);
 }
 
 hipError_t launch_prefix(const PrefixProblem& pp, const PrefixPlan& pl, void* ws, hipStream_t st) {
@@ -375,19 +651,25 @@ hipError_t launch_prefix(const PrefixProblem& pp, const PrefixPlan& pl, void* ws
   if (items > 0xFFFFFF) return hipErrorInvalidValue;
   if (!items) return hipSuccess;
   const PrefixArgs a = args_for(pp, pl, ws);
-  const int ns = blocks_for(pl.req_rows);
-  if (pp.d == 64) launch_d<64>(a, pl.nr, ns, (unsigned)items, st);
-  else launch_d<128>(a, pl.nr, ns, (unsigned)items, st);
+  if (pp.d == 64) launch_d<64>(a, (unsigned)items, st);
+  else launch_d<128>(a, (unsigned)items, st);
   return hipGetLastError();
+}
+
+template <int D>
+static void join_d(const PrefixArgs& a, hipStream_t st) {
+  // one row a workgroup while the rows leave CUs free, or have many ranges
+  constexpr int MANY = NT / (D / 4);
+  if (a.pl.rows <= 2048 || a.pl.psplits + a.pl.ssplits > JOIN_FEW) k_prefix_join<D, 1><<<(unsigned)a.pl.rows, NT, 0, st>>>(a);
+  else k_prefix_join<D, MANY><<<(unsigned)cdiv(a.pl.rows, MANY), NT, 0, st>>>(a);
 }
 
 hipError_t launch_prefix_join(const PrefixProblem& pp, const PrefixPlan& pl, const void* ws, hipStream_t st) {
   if (pl.psplits + pl.ssplits == 1) return hipSuccess;
+  if (pl.rows > 0xFFFFFF) return hipErrorInvalidValue;
   const PrefixArgs a = args_for(pp, pl, ws);
-  const int64_t blocks = cdiv(pl.rows, NT / (pp.d / 4));
-  if (blocks > 0xFFFFFF) return hipErrorInvalidValue;
-  if (pp.d == 64) k_prefix_join<64><<<(unsigned)blocks, NT, 0, st>>>(a);
-  else k_prefix_join<128><<<(unsigned)blocks, NT, 0, st>>>(a);
+  if (pp.d == 64) join_d<64>(a, st);
+  else join_d<128>(a, st);
   return hipGetLastError();
 }
 
