@@ -890,7 +890,7 @@ int prefix_shape(PrefixProblem* pp, int64_t B, int64_t H, int64_t Hkv, int64_t L
   if (dtype != TOPK_BF16 || (d != 64 && d != 128))
     return fail(TOPK_E_UNSUPPORTED, "shared-prefix attention runs on bf16 inputs with d = 64 or 128");
   if (P > 0x7FFFFFFFLL || S > 0x7FFFFFFFLL) return fail(TOPK_E_UNSUPPORTED, "more than 2^31 - 1 keys");
-  if (H > (int64_t(1) << 31) / B || Lq > (int64_t(1) << 31) / (B * H)) return fail(TOPK_E_UNSUPPORTED, "more than 2^31 query rows");
+  if (H > (int64_t(1) << 27) / B || Lq > (int64_t(1) << 27) / (B * H)) return fail(TOPK_E_UNSUPPORTED, "more than 2^27 query rows");
   pp->B = B;
   pp->H = H;
   pp->Hkv = Hkv;
@@ -915,6 +915,7 @@ int cache_ptr(const char* name, const void* p, std::initializer_list<int64_t> st
 
 int run_prefix(const PrefixProblem& pp, hipStream_t st) {
   const PrefixPlan pl = prefix_plan(pp);
+  if (prefix_items(pp, pl) > PREFIX_MAX_ITEMS) return fail(TOPK_E_UNSUPPORTED, "more than 2^24 workgroups: too many requests and heads");
   Scratch ws;
   int rc = ws.get(prefix_bytes(pp, pl), "shared-prefix attention", st);
   if (rc) return rc;

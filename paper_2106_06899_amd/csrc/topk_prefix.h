@@ -22,14 +22,18 @@ struct PrefixProblem {
 
 // How the work is cut: row tiles, and key ranges whose partial results are joined.
 struct PrefixPlan {
-  int pblocks, sblocks;       // blocks of 16 rows of a workgroup's tile, on the prefix and on own keys
-  int64_t rows;               // B * H * Lq
-  int64_t req_rows;           // rows of one request and key head: (H / Hkv) * Lq
+  int pform, sform;        // forms of the items on the prefix and on own keys (see k_prefix)
+  int both;                // items of one request take both, ranges of pkeys of the two as one list
+  int64_t rows;            // B * H * Lq
+  int64_t req_rows;        // rows of one request and key head: (H / Hkv) * Lq
   int64_t ptiles, psplits, pkeys;  // prefix: row tiles of a key head, key ranges, keys of a range
   int64_t stiles, ssplits, skeys;  // own keys: row tiles of a request and key head, ...
+  int64_t splits;          // partial results of a row
 };
 
 PrefixPlan prefix_plan(const PrefixProblem& pp);
+constexpr int64_t PREFIX_MAX_ITEMS = 0xFFFFFF;  // workgroups of a launch
+int64_t prefix_items(const PrefixProblem& pp, const PrefixPlan& pl);
 size_t prefix_bytes(const PrefixProblem& pp, const PrefixPlan& pl);
 hipError_t launch_prefix(const PrefixProblem& pp, const PrefixPlan& pl, void* ws, hipStream_t st);
 hipError_t launch_prefix_join(const PrefixProblem& pp, const PrefixPlan& pl, const void* ws, hipStream_t st);

@@ -43,15 +43,22 @@ struct PrefixArgs {
   float c;     // scale * log2(e)
 };
 
-// One work item: rows [r0, r0 + 16 NR) of a list of `count` rows against keys [k0, k1).
+// A range of keys, of the prefix or of a request's own.
+struct Span {
+  const uint16_t *k, *v;  // its first
+  uint32_t k_sl, v_sl;    // elements from one to the next
+  int n;                  // keys
+  int before;             // (own:) keys of the request before the first one that the row of token 0 does
+                          // not see, from the range's first on; may be negative or beyond n
+};
+
+// One work item: rows from r0 of a list of `count` against keys of the prefix, of a request, or both.
 struct Item {
-  const uint16_t *k, *v;
-  int64_t k_sl, v_sl;
-  int64_t r0, count, k0, k1;
-  int64_t h;      // key head
-  int64_t b;      // request (-1: rows of all requests)
-  int64_t len;    // keys in all
-  int64_t split;  // where its partial result goes
+  Span prefix, own;
+  int r0, count;
+  int h;      // key head
+  int b;      // request (-1: rows of all requests, against the prefix)
+  int split;  // where its partial result goes
 };
 
 // A workgroup's LDS: four tile buffers (the few-row form keeps a wave's outputs in each), and the
@@ -69,32 +76,30 @@ struct Few {
   static constexpr int NC = D / 16;  // blocks of 16 output features; columns of V a lane reads
   static constexpr int VB = NC * 2;  // their bytes
   static constexpr int LD = D + 4;
+  static constexpr int TILE = 16 * NR;
   typedef float Rows[LD];            // 16 of them a wave
 
   static __device__ __forceinline__ void run(const PrefixArgs& a, const Item& it, const Lds& sh) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, g = lane >> 4;
-    const int64_t R = a.pl.req_rows, Lq = a.p.Lq, HL = a.p.H * Lq;
-    // the lane's rows: where they lie in q and out, and how many keys they see
-    int64_t at[NR], seen[NR];
+    const int R = (int)a.pl.req_rows, Lq = (int)a.p.Lq;
+    const Span sp = it.b >= 0 ? it.own : it.prefix;
+    const bool causal = it.b >= 0 && a.p.causal;
+    auto place = [&](int i) {  // of row i in q and out
+      const int b = it.b >= 0 ? it.b : i / R;
+      return b * a.p.H * Lq + it.h * R + (it.b >= 0 ? i : i - b * R);
+    };
+    // how many keys the lane's rows see
+    int seen[NR];
     bf16x8 bq[NR][NS];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-      const int64_t i = it.r0 + 16 * r + n;
-      const bool ok = i < it.count;
-      const int64_t ii = ok ? i : it.r0;
-      const int64_t b = it.b >= 0 ? it.b : ii / R, rr = it.b >= 0 ? ii : ii - b * R;
-      at[r] = b * HL + it.h * R + rr;
-      seen[r] = it.len;
-      if (it.b >= 0 && a.p.causal) {
-        const int64_t t = it.len - Lq + rr % Lq + 1;
-        seen[r] = t < 0 ? 0 : t;
-      }
-      const uint16_t* q = (const uint16_t*)a.p.q + at[r] * D + 8 * g;
+      const int i = it.r0 + 16 * r + n < it.count ? it.r0 + 16 * r + n : it.r0;
+      seen[r] = causal ? min(sp.n, sp.before + i % Lq) : sp.n;
+      const uint16_t* q = (const uint16_t*)a.p.q + place(i) * D + 8 * g;
 #pragma unroll
       for (int s = 0; s < NS; ++s) bq[r][s] = *(const bf16x8*)(q + 32 * s);
-      if (!ok) at[r] = -1;
     }
-    const int64_t all_see = it.b >= 0 && a.p.causal ? it.len - Lq + 1 : it.len;  // keys before this are seen by every row
+    const int all_see = causal ? min(sp.n, sp.before) : sp.n;  // keys before this are seen by every row
 
     f32x4 o[NR][NC];
     float m[NR], l[NR];
@@ -108,36 +113,34 @@ struct Few {
 
     bf16x8 kr[2][NS];
     uint32_t vr[8][NC / 2];
-    const int64_t tiles = (it.k1 - it.k0 + KT - 1) / KT;
+    const int tiles = (sp.n + KT - 1) / KT;
     // keys past the range load its last one: their scores are masked, their values put to 0
-    auto load_k = [&](int64_t t) {
-      const int64_t first = it.k0 + t * KT;
-      const int left = (int)min((int64_t)KT, it.k1 - first) - 1;
-      const uint16_t* p = it.k + first * it.k_sl;
+    auto load_k = [&](int t) {
+      const int left = min(KT, sp.n - t * KT) - 1;
+      const uint16_t* p = sp.k + (int64_t)(t * KT) * sp.k_sl;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        const uint32_t off = (uint32_t)min(16 * kb + n, left) * (uint32_t)it.k_sl + 8 * g;
+        const uint32_t off = (uint32_t)min(16 * kb + n, left) * sp.k_sl + 8 * g;
 #pragma unroll
         for (int s = 0; s < NS; ++s) kr[kb][s] = *(const bf16x8*)(p + off + 32 * s);
       }
     };
-    auto load_v = [&](int64_t t) {
-      const int64_t first = it.k0 + t * KT;
-      const int left = (int)min((int64_t)KT, it.k1 - first) - 1;
-      const uint16_t* p = it.v + first * it.v_sl;
+    auto load_v = [&](int t) {
+      const int left = min(KT, sp.n - t * KT) - 1;
+      const uint16_t* p = sp.v + (int64_t)(t * KT) * sp.v_sl;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint32_t off = (uint32_t)min(16 * (e >> 2) + 4 * g + (e & 3), left) * (uint32_t)it.v_sl + n * NC;
+        const uint32_t off = (uint32_t)min(16 * (e >> 2) + 4 * g + (e & 3), left) * sp.v_sl + n * NC;
         __builtin_memcpy(vr[e], __builtin_assume_aligned(p + off, VB), VB);
       }
     };
-    int64_t t = wave;
+    int t = wave;
     if (t < tiles) {
       load_k(t);
       load_v(t);
     }
     for (; t < tiles; t += WAVES) {
-      const int64_t first = it.k0 + t * KT;
+      const int first = t * KT;
       f32x4 s[NR][2];
 #pragma unroll
       for (int r = 0; r < NR; ++r)
@@ -149,18 +152,15 @@ struct Few {
           s[r][kb] = acc;
         }
       if (t + WAVES < tiles) load_k(t + WAVES);
-      if (first + KT > min(it.k1, all_see)) {
+      if (first + KT > all_see) {
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int64_t j = first + 16 * (e >> 2) + 4 * g + (e & 3);
-            if (j >= it.k1 || j >= seen[r]) s[r][e >> 2][e & 3] = -INFINITY;
-          }
-        const int64_t left = it.k1 - first;
+          for (int e = 0; e < 8; ++e)
+            if (first + 16 * (e >> 2) + 4 * g + (e & 3) >= seen[r]) s[r][e >> 2][e & 3] = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (16 * (e >> 2) + 4 * g + (e & 3) >= left)
+          if (first + 16 * (e >> 2) + 4 * g + (e & 3) >= sp.n)
 #pragma unroll
             for (int w = 0; w < NC / 2; ++w) vr[e][w] = 0;
       }
@@ -212,7 +212,7 @@ struct Few {
       if (g == 0) sh.ml[wave][16 * r + n] = make_float2(m[r], l[r]);
     }
     __syncthreads();
-    const bool last = a.pl.psplits + a.pl.ssplits == 1;
+    const bool last = a.pl.splits == 1;
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       float top = -INFINITY;
@@ -227,10 +227,9 @@ struct Few {
       __syncthreads();
       for (int i = tid; i < 16 * D / 4; i += NT) {
         const int row = i / (D / 4), col = (i % (D / 4)) * 4;
-        const int64_t ri = it.r0 + 16 * r + row;
+        const int ri = it.r0 + 16 * r + row;
         if (ri >= it.count) continue;
-        const int64_t b = it.b >= 0 ? it.b : ri / R, rr = it.b >= 0 ? ri : ri - b * R;
-        const int64_t gr = b * HL + it.h * R + rr;
+        const int64_t gr = place(ri);
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
         float tm = -INFINITY, tl = 0.f;
 #pragma unroll
@@ -269,11 +268,21 @@ typedef float f32x16 __attribute__((__vector_size__(64)));
 typedef short s16x4 __attribute__((__vector_size__(8)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
+// the larger of x and what the lane 32 away holds (NaN if either is)
+__device__ __forceinline__ float other_half_max(float x) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __builtin_elementwise_maximum(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
 template <int D, bool TWO>
 struct Wide {
   // Weights are formed as 2^24 times themselves, so that the exponential instruction, which knows no
   // numbers below 2^-126, keeps every weight that 32 bits can hold.
   static constexpr float LIFT = 24.f;
+  // The maximum that weights are taken against is moved, and the sums with it, only once a score
+  // leads it by 2^8 in weight.
+  static constexpr float LEAD = 8.f;
+  static constexpr int TILE = 32 * WAVES; // rows of a workgroup
   static constexpr int KEYS = 64;         // of a tile
   static constexpr int NS = D / 16;       // steps over the features of the scores
   static constexpr int CH = 2 * D / 16;   // 16-byte parts of a row
@@ -286,61 +295,19 @@ struct Wide {
 
   static __device__ __forceinline__ void run(const PrefixArgs& a, const Item& it, const Lds& sh) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 31, half = lane >> 5;
-    const int64_t R = a.pl.req_rows, Lq = a.p.Lq, HL = a.p.H * Lq;
-    const bool causal = it.b >= 0 && a.p.causal;
-    const int64_t i = it.r0 + wave * 32 + n;
+    const int R = (int)a.pl.req_rows, Lq = (int)a.p.Lq;
+    const int i = it.r0 + wave * 32 + n;
     const bool ok = i < it.count;
     const bool work = it.r0 + wave * 32 < it.count;  // the wave has rows
-    const int64_t ii = ok ? i : it.r0;
-    const int64_t b = it.b >= 0 ? it.b : ii / R, rr = it.b >= 0 ? ii : ii - b * R;
-    const int64_t at = b * HL + it.h * R + rr;
-    int64_t seen = it.len;
-    if (causal) {
-      const int64_t t = it.len - Lq + rr % Lq + 1;
-      seen = t < 0 ? 0 : t;
-    }
+    const int ii = ok ? i : it.r0;
+    const int b = it.b >= 0 ? it.b : ii / R, rr = it.b >= 0 ? ii : ii - b * R;
+    const int64_t at = b * a.p.H * Lq + it.h * R + rr;
     bf16x8 bq[NS];
     {
       const uint16_t* q = (const uint16_t*)a.p.q + at * D + (D / 2) * half;
 #pragma unroll
       for (int s = 0; s < NS; ++s) bq[s] = *(const bf16x8*)(q + 8 * s);
     }
-    // keys before all_see are seen by every row, keys from k1 by none of the tile
-    int64_t all_see = it.len, k1 = it.k1;
-    if (causal) {
-      const int64_t r1 = min(it.r0 + 128, it.count) - 1;
-      const bool wraps = r1 / Lq != it.r0 / Lq;
-      all_see = it.len - Lq + (wraps ? 0 : it.r0 % Lq) + 1;
-      k1 = min(k1, it.len - Lq + (wraps ? Lq - 1 : r1 % Lq) + 1);
-    }
-    const int64_t tiles = k1 > it.k0 ? (k1 - it.k0 + KEYS - 1) / KEYS : 0;
-
-    // where the lane's parts of a tile lie, in bytes from its first key
-    uint32_t koff[LPW], voff[LPW];
-#pragma unroll
-    for (int j = 0; j < LPW; ++j) {
-      const int cidx = (wave * LPW + j) * 64 + lane, r = cidx / CH, c = cidx % CH;
-      koff[j] = r * (uint32_t)it.k_sl * 2 + (c ^ swz_k(r)) * 16;
-      voff[j] = r * (uint32_t)it.v_sl * 2 + (c ^ swz_v(r)) * 16;
-    }
-    auto issue = [&](int64_t t, unsigned char* kd, unsigned char* vd) {
-      const int64_t first = it.k0 + t * KEYS;
-      const unsigned char* kt = (const unsigned char*)(it.k + first * it.k_sl);
-      const unsigned char* vt = (const unsigned char*)(it.v + first * it.v_sl);
-      const int left = (int)min((int64_t)KEYS, k1 - first) - 1;
-#pragma unroll
-      for (int j = 0; j < LPW; ++j) {
-        uint32_t ko = koff[j], vo = voff[j];
-        if (left < KEYS - 1) {  // rows past the range load its last one
-          const int r = ((wave * LPW + j) * 64 + lane) / CH, over = r - min(r, left);
-          ko -= over * (uint32_t)it.k_sl * 2;
-          vo -= over * (uint32_t)it.v_sl * 2;
-        }
-        __builtin_amdgcn_global_load_lds((const void*)(kt + ko), (__attribute__((address_space(3))) void*)&kd[(wave * LPW + j) * 1024], 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((const void*)(vt + vo), (__attribute__((address_space(3))) void*)&vd[(wave * LPW + j) * 1024], 16, 0, 0);
-      }
-    };
-
     f32x16 o[FB];
 #pragma unroll
     for (int f = 0; f < FB; ++f) o[f] = (f32x16){};
@@ -352,7 +319,46 @@ struct Wide {
     for (int f = 0; f < FB; ++f)
       vat[f] = vrow * 2 * D + (((f * 4 + ((lane >> 4) & 1) * 2 + ((va & 3) >> 1)) ^ swz_v(vrow)) * 16) + (va & 1) * 8;
 
-    auto tile = [&](auto edge, int64_t t, const unsigned char* kb, const unsigned char* vb) {
+    for (int part = 0; part < 2; ++part) {
+    const Span sp = part ? it.own : it.prefix;
+    // keys before all_see are seen by every row of the workgroup, keys from keys on by none; the lane's sees `seen`
+    int all_see = sp.n, keys = sp.n, seen = sp.n;
+    if (part && a.p.causal) {
+      const int r1 = min(it.r0 + TILE, it.count) - 1;
+      const bool wraps = r1 / Lq != it.r0 / Lq;
+      all_see = sp.before + (wraps ? 0 : it.r0 % Lq);
+      keys = min(keys, sp.before + (wraps ? Lq - 1 : r1 % Lq));
+      seen = min(keys, sp.before + rr % Lq);
+    }
+    if (keys <= 0) continue;
+    const int tiles = (keys + KEYS - 1) / KEYS;
+    // where the lane's parts of a tile lie, in bytes from its first key
+    uint32_t koff[LPW], voff[LPW];
+#pragma unroll
+    for (int j = 0; j < LPW; ++j) {
+      const int cidx = (wave * LPW + j) * 64 + lane, r = cidx / CH, c = cidx % CH;
+      koff[j] = r * sp.k_sl * 2 + (c ^ swz_k(r)) * 16;
+      voff[j] = r * sp.v_sl * 2 + (c ^ swz_v(r)) * 16;
+    }
+    const unsigned char *kt = (const unsigned char*)sp.k, *vt = (const unsigned char*)sp.v;  // of the next tile to load
+    auto issue = [&](int t, unsigned char* kd, unsigned char* vd) {
+      const int left = min(KEYS, keys - t * KEYS) - 1;
+#pragma unroll
+      for (int j = 0; j < LPW; ++j) {
+        uint32_t ko = koff[j], vo = voff[j];
+        if (left < KEYS - 1) {  // rows past the range load its last one
+          const int r = ((wave * LPW + j) * 64 + lane) / CH, over = r - min(r, left);
+          ko -= over * sp.k_sl * 2;
+          vo -= over * sp.v_sl * 2;
+        }
+        __builtin_amdgcn_global_load_lds((const void*)(kt + ko), (__attribute__((address_space(3))) void*)&kd[(wave * LPW + j) * 1024], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const void*)(vt + vo), (__attribute__((address_space(3))) void*)&vd[(wave * LPW + j) * 1024], 16, 0, 0);
+      }
+      kt += KEYS * 2 * (int64_t)sp.k_sl;
+      vt += KEYS * 2 * (int64_t)sp.v_sl;
+    };
+
+    auto tile = [&](auto edge, int t, const unsigned char* kb, const unsigned char* vb) {
       f32x16 s[2];
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb) {
@@ -366,7 +372,7 @@ struct Wide {
         s[rb] = acc;
       }
       if (decltype(edge)::value) {
-        const int last = (int)max((int64_t)-1, min(min(k1, seen) - it.k0 - t * KEYS, (int64_t)KEYS)) - 4 * half;
+        const int last = seen - t * KEYS - 4 * half;
 #pragma unroll
         for (int v = 0; v < 32; ++v)
           if ((v >> 4) * 32 + 8 * ((v & 15) >> 2) + (v & 3) >= last) s[v >> 4][v & 15] = -INFINITY;
@@ -375,9 +381,8 @@ struct Wide {
 #pragma unroll
       for (int v = 0; v < 32; v += 2)
         mt = __builtin_elementwise_maximum(__builtin_elementwise_maximum(mt, s[v >> 4][v & 15]), s[v >> 4][(v & 15) + 1]);
-      mt = __builtin_elementwise_maximum(mt, __shfl_xor(mt, 32, 64));
-      mt *= a.c;
-      if (__builtin_amdgcn_ballot_w64(!(mt <= m))) {  // (for NaN too; rows whose maximum stays multiply by 1)
+      mt = other_half_max(mt) * a.c;
+      if (__builtin_amdgcn_ballot_w64(!(mt <= m + LEAD))) {  // (for NaN too; rows whose maximum stays multiply by 1)
         const float mn = fmaxf(m, mt);
         const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
         m = mn;
@@ -387,6 +392,7 @@ struct Wide {
 #pragma unroll
           for (int v = 0; v < 16; ++v) o[f][v] *= alpha;
       }
+      __builtin_amdgcn_s_setprio(1);  // the other wave's softmax yields to this one's products
       const float bias = LIFT - (m == -INFINITY ? 0.f : m);
 #pragma unroll
       for (int st = 0; st < 4; ++st) {  // 16 keys each
@@ -408,20 +414,22 @@ struct Wide {
           if (TWO) o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, pl, o[f], 0, 0, 0);
         }
       }
+      __builtin_amdgcn_s_setprio(0);
     };
 
     // One tile of lookahead: before tile t is read, this wave's loads of it are complete and the barrier
     // publishes every wave's part; it also proves that no wave still reads the buffers the next loads
     // overwrite. (The buffers are named at compile time, so that reads of one pair do not wait for loads
     // into the other.) Tiles that every row sees whole come first and need no mask.
-    const int64_t whole = min(tiles, max((int64_t)0, min(k1, all_see) - it.k0) / KEYS);
-    auto ready = [&](int64_t t, unsigned char* kn, unsigned char* vn) {
+    const int whole = max(0, min(keys, all_see)) / KEYS;
+    auto ready = [&](int t, unsigned char* kn, unsigned char* vn) {
       __builtin_amdgcn_s_waitcnt(WAIT_VM0);
       __syncthreads();
       if (t + 1 < tiles) issue(t + 1, kn, vn);
     };
-    if (tiles > 0) issue(0, sh.b0, sh.b2);
-    int64_t t = 0;
+    __syncthreads();  // (the other part's last tile is read)
+    issue(0, sh.b0, sh.b2);
+    int t = 0;
     for (; t + 1 < whole; t += 2) {
       ready(t, sh.b1, sh.b3);
       if (work) tile(std::false_type{}, t, sh.b0, sh.b2);
@@ -433,10 +441,11 @@ struct Wide {
       ready(t, odd ? sh.b0 : sh.b1, odd ? sh.b2 : sh.b3);
       if (work) tile(std::true_type{}, t, odd ? sh.b1 : sh.b0, odd ? sh.b3 : sh.b2);
     }
+    }
     m -= LIFT;
     l += __shfl_xor(l, 32, 64);
     if (!ok) return;
-    if (a.pl.psplits + a.pl.ssplits == 1) {
+    if (a.pl.splits == 1) {
       const float inv = l > 0.f ? 1.f / l : 0.f;
       uint16_t* dst = (uint16_t*)a.p.out + at * D + 4 * half;
 #pragma unroll
@@ -456,21 +465,51 @@ struct Wide {
   }
 };
 
-// NB: blocks of 16 rows of an item; 8 is the wide form
+// A form by its number: 1 and 2 few rows (blocks of 16), 8 and 9 the wide one (with weights as two
+// numbers, as one).
 template <int D, int NB>
 struct Form {
   typedef Few<D, NB> type;
 };
 template <int D>
 struct Form<D, 8> {
-  typedef Wide<D, false> type;
+  typedef Wide<D, true> type;
 };
 template <int D>
 struct Form<D, 9> {
-  typedef Wide<D, true> type;
+  typedef Wide<D, false> type;
 };
 
-template <int D, int NBP, int NBS>
+// keys [k0, k1) of the prefix of key head h, as far as there are
+__device__ __forceinline__ Span prefix_span(const PrefixArgs& a, int h, int64_t k0, int64_t k1) {
+  Span s;
+  k0 = min(k0, a.p.P);
+  s.k = (const uint16_t*)a.p.pk + h * a.p.pk_sh + k0 * a.p.pk_sl;
+  s.v = (const uint16_t*)a.p.pv + h * a.p.pv_sh + k0 * a.p.pv_sl;
+  s.k_sl = (uint32_t)a.p.pk_sl;
+  s.v_sl = (uint32_t)a.p.pv_sl;
+  s.n = (int)(min(k1, a.p.P) - k0);
+  s.before = s.n;
+  return s;
+}
+// keys [k0, k1) of request b's own, as far as it holds them
+__device__ __forceinline__ Span own_span(const PrefixArgs& a, int b, int h, int64_t k0, int64_t k1) {
+  Span s;
+  int64_t len = a.p.lengths ? a.p.lengths[b] : a.p.S;
+  len = max((int64_t)0, min(len, a.p.S));
+  k0 = max((int64_t)0, min(k0, len));
+  s.k = (const uint16_t*)a.p.k + b * a.p.k_sb + h * a.p.k_sh + k0 * a.p.k_sl;
+  s.v = (const uint16_t*)a.p.v + b * a.p.v_sb + h * a.p.v_sh + k0 * a.p.v_sl;
+  s.k_sl = (uint32_t)a.p.k_sl;
+  s.v_sl = (uint32_t)a.p.v_sl;
+  s.n = (int)max((int64_t)0, min(k1, len) - k0);
+  s.before = (int)max((int64_t)-(1 << 30), min(len - a.p.Lq + 1 - k0, (int64_t)(1 << 30)));
+  return s;
+}
+
+// NBP, NBS: the forms of the items on the prefix (row tiles over all requests) and on own keys. BOTH:
+// an item's rows are one request's and take the prefix and its own keys as one list, in form NBS.
+template <int D, int NBP, int NBS, bool BOTH>
 __global__ __launch_bounds__(NT, 2) void k_prefix(PrefixArgs a) {
   constexpr int BUF = 64 * 2 * D;
   __shared__ __attribute__((aligned(16))) unsigned char b0[BUF];
@@ -480,42 +519,51 @@ __global__ __launch_bounds__(NT, 2) void k_prefix(PrefixArgs a) {
   __shared__ float2 ml[WAVES][32];
   const Lds sh = {b0, b1, b2, b3, ml};
   const PrefixPlan& pl = a.pl;
-  const int64_t np = a.p.Hkv * pl.psplits * pl.ptiles;
-  int64_t i = blockIdx.x;
+  const int B = (int)a.p.B, Hkv = (int)a.p.Hkv, ptiles = (int)pl.ptiles, stiles = (int)pl.stiles, psplits = (int)pl.psplits,
+            ssplits = (int)pl.ssplits;
+  int i = blockIdx.x;
   Item it;
+  if (BOTH) {
+    const int n = gridDim.x, splits = (int)pl.splits;
+    if (n % 8 == 0) i = (i % 8) * (n / 8) + i / 8;  // an XCD's workgroups share key ranges
+    const int tile = i % stiles, rest = i / stiles, rest2 = rest / B;
+    it.b = rest % B;
+    it.split = rest2 % splits;
+    it.h = rest2 / splits;
+    it.count = (int)pl.req_rows;
+    it.r0 = tile * Form<D, NBS>::type::TILE;
+    const int64_t k0 = it.split * pl.pkeys;
+    it.prefix = prefix_span(a, it.h, k0, k0 + pl.pkeys);
+    it.own = own_span(a, it.b, it.h, k0 - a.p.P, k0 + pl.pkeys - a.p.P);
+    Form<D, NBS>::type::run(a, it, sh);
+    return;
+  }
+  const int np = Hkv * psplits * ptiles;
   if (i < np) {
-    if (np % 8 == 0) i = (i % 8) * (np / 8) + i / 8;  // an XCD's workgroups share key ranges
-    const int64_t tile = i % pl.ptiles, rest = i / pl.ptiles;
-    it.split = rest % pl.psplits;
-    it.h = rest / pl.psplits;
+    if (np % 8 == 0) i = (i % 8) * (np / 8) + i / 8;
+    const int tile = i % ptiles, rest = i / ptiles;
+    it.split = rest % psplits;
+    it.h = rest / psplits;
     it.b = -1;
-    it.k = (const uint16_t*)a.p.pk + it.h * a.p.pk_sh;
-    it.v = (const uint16_t*)a.p.pv + it.h * a.p.pv_sh;
-    it.k_sl = a.p.pk_sl;
-    it.v_sl = a.p.pv_sl;
-    it.count = a.p.B * pl.req_rows;
-    it.r0 = tile * 16 * (NBP & ~1 ? NBP & ~1 : 1);
-    it.len = a.p.P;
-    it.k0 = it.split * pl.pkeys;
-    it.k1 = min(it.k0 + pl.pkeys, it.len);
+    it.prefix = prefix_span(a, it.h, it.split * pl.pkeys, it.split * pl.pkeys + pl.pkeys);
+    it.own = it.prefix;
+    it.own.n = 0;
+    it.own.before = 0;
+    it.count = (int)(a.p.B * pl.req_rows);
+    it.r0 = tile * Form<D, NBP>::type::TILE;
     Form<D, NBP>::type::run(a, it, sh);
     return;
   }
   i -= np;
-  const int64_t tile = i % pl.stiles, rest = i / pl.stiles, split = rest % pl.ssplits, bh = rest / pl.ssplits;
-  it.b = bh / a.p.Hkv;
-  it.h = bh - it.b * a.p.Hkv;
-  it.split = pl.psplits + split;
-  it.k = (const uint16_t*)a.p.k + it.b * a.p.k_sb + it.h * a.p.k_sh;
-  it.v = (const uint16_t*)a.p.v + it.b * a.p.v_sb + it.h * a.p.v_sh;
-  it.k_sl = a.p.k_sl;
-  it.v_sl = a.p.v_sl;
-  it.count = pl.req_rows;
-  it.r0 = tile * 16 * (NBS & ~1 ? NBS & ~1 : 1);
-  const int64_t len = a.p.lengths ? a.p.lengths[it.b] : a.p.S;
-  it.len = len < 0 ? 0 : min(len, a.p.S);
-  it.k0 = min(split * pl.skeys, it.len);
-  it.k1 = min(it.k0 + pl.skeys, it.len);
+  const int tile = i % stiles, rest = i / stiles, split = rest % ssplits, bh = rest / ssplits;
+  it.b = bh / Hkv;
+  it.h = bh - it.b * Hkv;
+  it.split = psplits + split;
+  it.own = own_span(a, it.b, it.h, split * pl.skeys, split * pl.skeys + pl.skeys);
+  it.prefix = it.own;
+  it.prefix.n = 0;
+  it.count = (int)pl.req_rows;
+  it.r0 = tile * Form<D, NBS>::type::TILE;
   Form<D, NBS>::type::run(a, it, sh);
 }
 
@@ -531,7 +579,7 @@ __global__ __launch_bounds__(NT) void k_prefix_join(PrefixArgs a) {
   const int rl = threadIdx.x / TR, tr = threadIdx.x % TR, q = tr / LR, c = tr % LR;
   const int64_t row = (int64_t)blockIdx.x * ROWS + rl;
   const bool ok = row < a.pl.rows;
-  const int splits = (int)(a.pl.psplits + a.pl.ssplits);
+  const int splits = (int)a.pl.splits;
   float top = -INFINITY, total = 0.f;
   if (ok) {
     if (splits <= 4) {
@@ -599,12 +647,14 @@ PrefixArgs args_for(const PrefixProblem& pp, const PrefixPlan& pl, const void* w
   a.p = pp;
   a.pl = pl;
   a.po = (float*)ws;
-  a.ml = (float2*)((char*)ws + (size_t)(pl.psplits + pl.ssplits) * pl.rows * pp.d * 4);
+  a.ml = (float2*)((char*)ws + (size_t)pl.splits * pl.rows * pp.d * 4);
   a.c = pp.scale * 1.4426950408889634f;
   return a;
 }
 
-int blocks_for(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 8; }
+// the form for so many rows, and its rows
+int form_for(int64_t rows, int wide) { return rows <= 16 ? 1 : rows <= 32 ? 2 : wide; }
+int tile_rows(int form) { return form >= 8 ? 128 : 16 * form; }
 
 }  // namespace
 
@@ -612,43 +662,65 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
   PrefixPlan pl = {};
   pl.rows = pp.B * pp.H * pp.Lq;
   pl.req_rows = pp.H / pp.Hkv * pp.Lq;
-  pl.sblocks = blocks_for(pl.req_rows);
-  pl.pblocks = pp.P ? blocks_for(pp.B * pl.req_rows) : pl.sblocks;
-  pl.ptiles = cdiv(pp.B * pl.req_rows, 16 * pl.pblocks);
-  pl.stiles = cdiv(pl.req_rows, 16 * pl.sblocks);
-  // ranges of equal length, as many as give two workgroups a CU, of 256 keys at least
+  const int wide = pl.req_rows < 64 ? 8 : 9;
+  pl.sform = form_for(pl.req_rows, wide);
+  pl.pform = pp.P ? form_for(pp.B * pl.req_rows, wide) : pl.sform;
+  pl.ptiles = cdiv(pp.B * pl.req_rows, tile_rows(pl.pform));
+  pl.stiles = cdiv(pl.req_rows, tile_rows(pl.sform));
+  // (many rows are joined several a workgroup, from few ranges)
+  const int64_t longest = std::max(pp.P, pp.S), least = cdiv(longest, (pl.rows > 1 << 20 ? JOIN_FEW : JOIN_MAX) / 2 * 128) * 128;
+  pl.both = pl.sform == 9 && pl.stiles * 128 * 8 <= pl.req_rows * 9;
+  if (pl.both) {
+    const int64_t items = pp.Hkv * pp.B * pl.stiles, keys = pp.P + pp.S;
+    double best = 0;
+    for (int64_t s = 1; s <= JOIN_FEW && (s == 1 || cdiv(keys, s) >= 128); ++s) {
+      const int64_t layers = cdiv(items * s, 256), range = std::max(least, cdiv(cdiv(keys, s), 64) * 64);
+      const double tile = pp.d == 64 ? 0.7 : 1.05;  // us of 64 keys where two workgroups share a CU
+      const double us = (layers == 1 ? 1.25 : (double)layers) * tile * (range / 64.0 + 3) + (s > 1 ? 4 + s * pl.rows * pp.d * 2e-6 : 0);
+      if (s == 1 || us < best) {
+        best = us;
+        pl.pkeys = std::max<int64_t>(range, 64);
+      }
+    }
+    pl.splits = std::max<int64_t>(1, cdiv(keys, pl.pkeys));
+    return pl;
+  }
+  // ranges of equal length, as many as give two workgroups a CU, of 128 keys at least
   const int64_t keys = pp.Hkv * pl.ptiles * pp.P + pp.B * pp.Hkv * pl.stiles * pp.S;
-  int64_t range = std::max<int64_t>(256, cdiv(cdiv(keys, 512), 128) * 128);
-  range = std::max(range, cdiv(std::max(pp.P, pp.S), JOIN_MAX / 2 * 128) * 128);
+  const int64_t range = std::max(std::max<int64_t>(128, cdiv(cdiv(keys, 512), 128) * 128), least);
   pl.psplits = cdiv(pp.P, range);
   pl.ssplits = cdiv(pp.S, range);
   pl.pkeys = pl.psplits ? cdiv(cdiv(pp.P, pl.psplits), 128) * 128 : 128;
   pl.skeys = pl.ssplits ? cdiv(cdiv(pp.S, pl.ssplits), 128) * 128 : 128;
   pl.psplits = cdiv(pp.P, pl.pkeys);
   pl.ssplits = cdiv(pp.S, pl.skeys);
+  pl.splits = pl.psplits + pl.ssplits;
   return pl;
 }
 
 size_t prefix_bytes(const PrefixProblem& pp, const PrefixPlan& pl) {
-  const int64_t splits = pl.psplits + pl.ssplits;
-  return splits == 1 ? 0 : (size_t)splits * pl.rows * (pp.d + 2) * 4;
+  return pl.splits == 1 ? 0 : (size_t)pl.splits * pl.rows * (pp.d + 2) * 4;
 }
 
 template <int D>
 static void launch_d(const PrefixArgs& a, unsigned grid, hipStream_t st) {
-  const int np = a.pl.pblocks, ns = a.pl.sblocks;
-  if (np == 1) k_prefix<D, 1, 1><<<grid, NT, 0, st>>>(a);
-  else if (np == 2 && ns == 1) k_prefix<D, 2, 1><<<grid, NT, 0, st>>>(a);
-  else if (np == 2) k_prefix<D, 2, 2><<<grid, NT, 0, st>>>(a);
-  else if (ns == 1) k_prefix<D, 9, 1><<<grid, NT, 0, st>>>(a);
-  else if (ns == 2) k_prefix<D, 9, 2><<<grid, NT, 0, st>>>(a);
-  else if (a.pl.req_rows < 64) k_prefix<D, 9, 9><<<grid, NT, 0, st>>>(a);
-  else k_prefix<D, 8, 8><<<grid, NT, 0, st>>>(a);
+  const int np = a.pl.pform, ns = a.pl.sform;
+  if (a.pl.both) k_prefix<D, 9, 9, true><<<grid, NT, 0, st>>>(a);
+  else if (np == 1) k_prefix<D, 1, 1, false><<<grid, NT, 0, st>>>(a);
+  else if (np == 2 && ns == 1) k_prefix<D, 2, 1, false><<<grid, NT, 0, st>>>(a);
+  else if (np == 2) k_prefix<D, 2, 2, false><<<grid, NT, 0, st>>>(a);
+  else if (ns == 1) k_prefix<D, 8, 1, false><<<grid, NT, 0, st>>>(a);
+  else if (ns == 2) k_prefix<D, 8, 2, false><<<grid, NT, 0, st>>>(a);
+  else if (ns == 8) k_prefix<D, 8, 8, false><<<grid, NT, 0, st>>>(a);
+  else k_prefix<D, 9, 9, false><<<grid, NT, 0, st>>>(a);
+}
+
+int64_t prefix_items(const PrefixProblem& pp, const PrefixPlan& pl) {
+  return pl.both ? pp.Hkv * pp.B * pl.stiles * pl.splits : pp.Hkv * pl.psplits * pl.ptiles + pp.B * pp.Hkv * pl.ssplits * pl.stiles;
 }
 
 hipError_t launch_prefix(const PrefixProblem& pp, const PrefixPlan& pl, void* ws, hipStream_t st) {
-  const int64_t items = pp.Hkv * pl.psplits * pl.ptiles + pp.B * pp.Hkv * pl.ssplits * pl.stiles;
-  if (items > 0xFFFFFF) return hipErrorInvalidValue;
+  const int64_t items = prefix_items(pp, pl);
   if (!items) return hipSuccess;
   const PrefixArgs a = args_for(pp, pl, ws);
   if (pp.d == 64) launch_d<64>(a, (unsigned)items, st);
@@ -660,13 +732,12 @@ template <int D>
 static void join_d(const PrefixArgs& a, hipStream_t st) {
   // one row a workgroup while the rows leave CUs free, or have many ranges
   constexpr int MANY = NT / (D / 4);
-  if (a.pl.rows <= 2048 || a.pl.psplits + a.pl.ssplits > JOIN_FEW) k_prefix_join<D, 1><<<(unsigned)a.pl.rows, NT, 0, st>>>(a);
+  if (a.pl.rows <= 2048 || a.pl.splits > JOIN_FEW) k_prefix_join<D, 1><<<(unsigned)a.pl.rows, NT, 0, st>>>(a);
   else k_prefix_join<D, MANY><<<(unsigned)cdiv(a.pl.rows, MANY), NT, 0, st>>>(a);
 }
 
 hipError_t launch_prefix_join(const PrefixProblem& pp, const PrefixPlan& pl, const void* ws, hipStream_t st) {
-  if (pl.psplits + pl.ssplits == 1) return hipSuccess;
-  if (pl.rows > 0xFFFFFF) return hipErrorInvalidValue;
+  if (pl.splits == 1) return hipSuccess;
   const PrefixArgs a = args_for(pp, pl, ws);
   if (pp.d == 64) join_d<64>(a, st);
   else join_d<128>(a, st);
