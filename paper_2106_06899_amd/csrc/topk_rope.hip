@@ -11,10 +11,11 @@
 // Bound by memory: every element is read once and written once (backward: x and the gradient
 // read, one gradient written), so the design is about whole cache lines and few instructions.
 // A group of T lanes holds one head, each lane VEC pairs (both features of a pair, so the
-// rotation needs no exchange) by two 16-byte accesses, and stays with its token: the angles
-// are computed once per lane and reused for every head of the workgroup. A workgroup's tokens
-// are consecutive, so that each head it writes is one contiguous run; the packed input is read
-// in runs of d elements. Angles are products in 64 bits, reduced to a turn there (32 bits would
+// rotation needs no exchange) by two 16-byte accesses. A workgroup works on `tok` consecutive
+// tokens and `hp` heads at a time, each lane staying with its token and features: the angles of
+// the workgroup's tokens are computed once, by all its lanes, and go through LDS to registers,
+// where every head reuses them. Input is read in runs of hp heads, and each head is written in
+// runs of tok tokens. Angles are products in 64 bits, reduced to a turn there (32 bits would
 // lose 0.06 rad at position 10^6), and only the fraction of a turn goes to a 32-bit sine.
 #include "topk_device.h"
 #include "topk_heads.h"
@@ -41,6 +42,15 @@ __device__ __forceinline__ void load_vec(float (&o)[VEC], const T* p) {
 #pragma unroll
   for (int e = 0; e < VEC; ++e) o[e] = widen(v.e[e]);
 }
+// What a lane holds of a head as it lies in memory: both runs of VEC of each chunk.
+template <typename T, int VEC, int NC> struct Raw {
+  Vec<T, VEC> a[NC], b[NC];
+};
+template <typename T, int VEC>
+__device__ __forceinline__ void widen_vec(float (&o)[VEC], const Vec<T, VEC>& v) {
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) o[e] = widen(v.e[e]);
+}
 template <int VEC>
 __device__ __forceinline__ void store_vec(float* p, const float (&o)[VEC]) {
   __builtin_memcpy(__builtin_assume_aligned(p, 4 * VEC), o, 4 * VEC);
@@ -54,9 +64,13 @@ __device__ __forceinline__ void store_vec(uint16_t* p, const float (&o)[VEC]) {
   __builtin_memcpy(__builtin_assume_aligned(p, 2 * VEC), v, 2 * VEC);
 }
 
+constexpr int64_t WGS = 768;     // workgroups that fill the chip
+
 struct Grid {
   int T;             // lanes of a head: a power of two, at least d / (2 VEC NC)
-  int64_t tiles;     // tiles of NT / T tokens
+  int hp;            // heads at a time (a power of two)
+  int tok;           // tokens of a workgroup: NT / (T hp)
+  int64_t tiles;     // tiles of tok tokens
   int ny[3];         // workgroups that share the heads of q, k, v
   int per[3];        // heads of each
 };
@@ -85,33 +99,48 @@ struct Lane {
   }
 };
 
-// cos and sin of the lane's pairs at token (b, l)
-template <int VEC, int NC, bool ADJ>
-__device__ __forceinline__ void angles(const Rotation& r, const Lane<VEC, NC, ADJ>& ln, int64_t b, int64_t l, float (&co)[NC][VEC],
-                                       float (&si)[NC][VEC]) {
-  const int64_t at = b * r.pos_sb + l * r.pos_sl;
+template <typename T, int VEC, int NC, bool ADJ>
+__device__ __forceinline__ void fetch(Raw<T, VEC, NC>& r, const T* p, const Lane<VEC, NC, ADJ>& ln) {
 #pragma unroll
   for (int j = 0; j < NC; ++j) {
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      co[j][e] = 1.f;
-      si[j][e] = 0.f;
-    }
-    if (!ln.turn[j]) continue;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const int p = ln.pair[j] + e;
-      const int a = (r.axis[p >> 4] >> (2 * (p & 15))) & 3;
-      const int64_t o = at + a * r.pos_sa;
-      const double pos = r.pos64 ? (double)((const int64_t*)r.positions)[o] : (double)((const int32_t*)r.positions)[o];
-      const double turns = pos * r.freqs[p] * 0.15915494309189533577;  // 1 / (2 pi)
-      const float f = 2.f * (float)(turns - rint(turns));              // in half turns, [-1, 1]
-      float s, c;
-      sincospif(f, &s, &c);
-      co[j][e] = c;
-      si[j][e] = r.inverse ? -s : s;
+    r.a[j] = r.b[j] = Vec<T, VEC>{};
+    if (ln.in[j]) {
+      __builtin_memcpy(&r.a[j], __builtin_assume_aligned(p + ln.lo[j], sizeof(T) * VEC), sizeof(T) * VEC);
+      __builtin_memcpy(&r.b[j], __builtin_assume_aligned(p + ln.hi[j], sizeof(T) * VEC), sizeof(T) * VEC);
     }
   }
+}
+
+// cos and sin of all pairs of the workgroup's tokens, from token t0 on, to LDS: [token][pair]
+__device__ __forceinline__ void angles(const HeadsProblem& hp, const Grid& g, int64_t t0, float2* out) {
+  const Rotation& r = hp.rot;
+  const int64_t left = hp.B * hp.L - t0;
+  const int n = (int)min((int64_t)g.tok, left) * r.half;
+  for (int i = threadIdx.x; i < n; i += NT) {
+    const int t = i / r.half, p = i - t * r.half;
+    const int64_t b = (t0 + t) / hp.L, l = t0 + t - b * hp.L;
+    const int a = (r.axis[p >> 4] >> (2 * (p & 15))) & 3;
+    const int64_t o = b * r.pos_sb + l * r.pos_sl + a * r.pos_sa;
+    const double pos = r.pos64 ? (double)((const int64_t*)r.positions)[o] : (double)((const int32_t*)r.positions)[o];
+    const double turns = pos * r.freqs[p] * 0.15915494309189533577;  // 1 / (2 pi)
+    const float f = 2.f * (float)(turns - rint(turns));              // in half turns, [-1, 1]
+    float sn, cs;
+    sincospif(f, &sn, &cs);
+    out[i] = make_float2(cs, r.inverse ? -sn : sn);
+  }
+}
+// the lane's, from there
+template <int VEC, int NC, bool ADJ>
+__device__ __forceinline__ void lane_angles(const Rotation& r, const Lane<VEC, NC, ADJ>& ln, const float2* of_token, float (&co)[NC][VEC],
+                                            float (&si)[NC][VEC]) {
+#pragma unroll
+  for (int j = 0; j < NC; ++j)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const float2 x = ln.turn[j] ? of_token[ln.pair[j] + e] : make_float2(1.f, 0.f);
+      co[j][e] = x.x;
+      si[j][e] = x.y;
+    }
 }
 
 // Rotates the lane's pairs by (co, si); features beyond the rotated ones have co = 1, si = 0.
@@ -152,13 +181,14 @@ struct Share {
   }
 };
 
-// A workgroup takes one part's heads of a tile of NT / T tokens (more tiles only where a grid
-// cannot hold them all).
+// A workgroup takes one part's heads of a tile of tokens (more tiles only where a grid cannot hold
+// them all).
 template <typename T, int VEC, int NC, bool ADJ>
 __global__ __launch_bounds__(NT) void k_heads(HeadsProblem hp, Grid g) {
+  __shared__ __attribute__((aligned(16))) float2 ang[NT * VEC * NC];  // (a lane's pairs are NC chunks of VEC)
   const Share sh(hp, g, blockIdx.y);
-  const int c0 = threadIdx.x & (g.T - 1);
-  const Lane<VEC, NC, ADJ> ln(c0, g.T, hp.d, hp.rot.half);
+  const int lane = threadIdx.x & (g.T - 1), unit = threadIdx.x / g.T, tl = unit & (g.tok - 1), first = unit / g.tok;
+  const Lane<VEC, NC, ADJ> ln(lane, g.T, hp.d, hp.rot.half);
   const bool value = sh.seg == 2;
   float wa[NC][VEC], wb[NC][VEC];
   const T* w = value ? nullptr : (const T*)hp.w[sh.seg];
@@ -173,30 +203,33 @@ __global__ __launch_bounds__(NT) void k_heads(HeadsProblem hp, Grid g) {
   }
   const float inv_d = 1.f / (float)hp.d;
   for (int64_t t = blockIdx.x; t < g.tiles; t += gridDim.x) {
-    const int64_t token = t * (NT / g.T) + threadIdx.x / g.T;
-    if (token >= hp.B * hp.L) return;  // (whole groups leave; later tiles lie behind)
-    const int64_t b = token / hp.L, l = token - b * hp.L;
+    const int64_t token = t * g.tok + tl, b = token / hp.L, l = token - b * hp.L, h0 = sh.h0 + first;
+    bool live = token < hp.B * hp.L && h0 < sh.h1;  // (of whole groups)
     int64_t row = l;
-    if (hp.lengths && sh.seg > 0) {
+    if (live && hp.lengths && sh.seg > 0) {
       row = (int64_t)hp.lengths[b] + l;
-      if (row < 0 || row >= hp.S) continue;  // no place in the cache
+      live = row >= 0 && row < hp.S;  // (otherwise there is no place in the cache)
     }
-    float co[NC][VEC], si[NC][VEC];
-    if (!value) angles(hp.rot, ln, b, l, co, si);
-    const T* src = (const T*)hp.x.p + b * hp.x.sb + l * hp.x.sl + (sh.first + sh.h0) * hp.x.sh;
     const HeadRows& o = hp.part[sh.seg];
-    T* dst = (T*)o.p + b * o.sb + row * o.sl + sh.h0 * o.sh;
-    for (int64_t h = sh.h0; h < sh.h1; ++h, src += hp.x.sh, dst += o.sh) {
+    const T* src = (const T*)hp.x.p + b * hp.x.sb + l * hp.x.sl + (sh.first + h0) * hp.x.sh;
+    T* dst = (T*)o.p + b * o.sb + row * o.sl + h0 * o.sh;
+    float co[NC][VEC], si[NC][VEC];
+    if (!value && hp.rot.half) {
+      if (t != blockIdx.x) __syncthreads();
+      angles(hp, g, t * g.tok, ang);
+      __syncthreads();
+    }
+    if (!value) lane_angles(hp.rot, ln, ang + tl * hp.rot.half, co, si);
+    if (!live) continue;
+    for (int64_t h = h0; h < sh.h1; h += g.hp, src += g.hp * hp.x.sh, dst += g.hp * o.sh) {
+      Raw<T, VEC, NC> raw;
+      fetch(raw, src, ln);
       float a[NC][VEC], c[NC][VEC];
       float sq = 0.f;
 #pragma unroll
       for (int j = 0; j < NC; ++j) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) a[j][e] = c[j][e] = 0.f;
-        if (ln.in[j]) {
-          load_vec<T, VEC>(a[j], src + ln.lo[j]);
-          load_vec<T, VEC>(c[j], src + ln.hi[j]);
-        }
+        widen_vec(a[j], raw.a[j]);
+        widen_vec(c[j], raw.b[j]);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) sq = fmaf(a[j][e], a[j][e], fmaf(c[j][e], c[j][e], sq));
       }
@@ -226,10 +259,11 @@ __global__ __launch_bounds__(NT) void k_heads(HeadsProblem hp, Grid g) {
 // gradients stay in registers; each writes its own sum, in a fixed order over its groups.
 template <typename T, int VEC, int NC, bool ADJ>
 __global__ __launch_bounds__(NT) void k_heads_backward(HeadsProblem hp, Grid g) {
+  __shared__ __attribute__((aligned(16))) float2 ang[NT * VEC * NC];  // (a lane's pairs are NC chunks of VEC)
   __shared__ float red[NT * NC * VEC];
   const Share sh(hp, g, blockIdx.y);
-  const int c0 = threadIdx.x & (g.T - 1);
-  const Lane<VEC, NC, ADJ> ln(c0, g.T, hp.d, hp.rot.half);
+  const int lane = threadIdx.x & (g.T - 1), unit = threadIdx.x / g.T, tl = unit & (g.tok - 1), first = unit / g.tok;
+  const Lane<VEC, NC, ADJ> ln(lane, g.T, hp.d, hp.rot.half);
   const bool value = sh.seg == 2;
   float wa[NC][VEC], wb[NC][VEC], ga[NC][VEC], gb[NC][VEC];
   const T* w = value ? nullptr : (const T*)hp.w[sh.seg];
@@ -247,37 +281,39 @@ __global__ __launch_bounds__(NT) void k_heads_backward(HeadsProblem hp, Grid g) 
   }
   const float inv_d = 1.f / (float)hp.d;
   for (int64_t t = blockIdx.x; t < g.tiles; t += gridDim.x) {
-    const int64_t token = t * (NT / g.T) + threadIdx.x / g.T;
-    if (token >= hp.B * hp.L) break;  // (whole groups leave; later tiles lie behind)
-    const int64_t b = token / hp.L, l = token - b * hp.L;
-    float co[NC][VEC], si[NC][VEC];
-    if (!value) angles(hp.rot, ln, b, l, co, si);
+    const int64_t token = t * g.tok + tl, b = token / hp.L, l = token - b * hp.L, h0 = sh.h0 + first;
+    const bool live = token < hp.B * hp.L && h0 < sh.h1;  // (of whole groups)
     const HeadRows& gr = hp.part[sh.seg];
-    const T* src = (const T*)hp.x.p + b * hp.x.sb + l * hp.x.sl + (sh.first + sh.h0) * hp.x.sh;
-    const T* grad = (const T*)gr.p + b * gr.sb + l * gr.sl + sh.h0 * gr.sh;
-    T* dst = (T*)hp.dx.p + b * hp.dx.sb + l * hp.dx.sl + (sh.first + sh.h0) * hp.dx.sh;
-    for (int64_t h = sh.h0; h < sh.h1; ++h, src += hp.x.sh, grad += gr.sh, dst += hp.dx.sh) {
+    const T* src = (const T*)hp.x.p + b * hp.x.sb + l * hp.x.sl + (sh.first + h0) * hp.x.sh;
+    const T* grad = (const T*)gr.p + b * gr.sb + l * gr.sl + h0 * gr.sh;
+    T* dst = (T*)hp.dx.p + b * hp.dx.sb + l * hp.dx.sl + (sh.first + h0) * hp.dx.sh;
+    float co[NC][VEC], si[NC][VEC];
+    if (!value && hp.rot.half) {
+      if (t != blockIdx.x) __syncthreads();
+      angles(hp, g, t * g.tok, ang);
+      __syncthreads();
+    }
+    if (!value) lane_angles(hp.rot, ln, ang + tl * hp.rot.half, co, si);
+    if (!live) continue;
+    for (int64_t h = h0; h < sh.h1; h += g.hp, dst += g.hp * hp.dx.sh) {
+      Raw<T, VEC, NC> rawx, rawg;
+      fetch(rawg, grad, ln);
+      if (!value) fetch(rawx, src, ln);
+      src += g.hp * hp.x.sh;
+      grad += g.hp * gr.sh;
       float ma[NC][VEC], mb[NC][VEC];
 #pragma unroll
       for (int j = 0; j < NC; ++j) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) ma[j][e] = mb[j][e] = 0.f;
-        if (ln.in[j]) {
-          load_vec<T, VEC>(ma[j], grad + ln.lo[j]);
-          load_vec<T, VEC>(mb[j], grad + ln.hi[j]);
-        }
+        widen_vec(ma[j], rawg.a[j]);
+        widen_vec(mb[j], rawg.b[j]);
       }
       if (!value) {
         float xa[NC][VEC], xb[NC][VEC];
         float sq = 0.f, dot = 0.f;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) xa[j][e] = xb[j][e] = 0.f;
-          if (ln.in[j]) {
-            load_vec<T, VEC>(xa[j], src + ln.lo[j]);
-            load_vec<T, VEC>(xb[j], src + ln.hi[j]);
-          }
+          widen_vec(xa[j], rawx.a[j]);
+          widen_vec(xb[j], rawx.b[j]);
           turn_pairs<VEC, ADJ>(ma[j], mb[j], co[j], si[j]);  // (the launch asks for the opposite angles)
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
@@ -332,14 +368,20 @@ __global__ __launch_bounds__(NT) void k_heads_backward(HeadsProblem hp, Grid g) 
   }
 }
 
-// One weight gradient per 16 columns: the workgroups' sums, in a fixed order.
+// The weights' gradients, 16 columns of one a workgroup: the workgroups' sums, in a fixed order.
 template <typename T>
-__global__ __launch_bounds__(1024) void k_heads_weights(const float* part, T* dw, int64_t n, int d) {
+__global__ __launch_bounds__(1024) void k_heads_weights(const float* part, T* dq, T* dk, int64_t nq, int64_t nk, int d) {
   __shared__ float red[64][17];
+  T* dw = blockIdx.y ? dk : dq;
+  if (!dw) return;
+  const int64_t n = blockIdx.y ? nk : nq;
+  if (blockIdx.y) part += nq * d;
   const int c = threadIdx.x & 15, q = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
   float s = 0.f;
-  if (col < d)
+  if (col < d) {
+#pragma unroll 4
     for (int64_t i = q; i < n; i += 64) s += part[i * d + col];
+  }
   red[q][c] = s;
   __syncthreads();
   for (int o = 32; o; o >>= 1) {
@@ -370,13 +412,17 @@ Grid grid_for(const HeadsProblem& hp, int vec) {
   const int chunks = hp.d / 2 / vec, nc = vec == 1 ? 4 : 1;
   g.T = 1;
   while (g.T * nc < chunks && g.T < 64) g.T *= 2;
-  const int64_t tokens = hp.B * hp.L, tile = NT / g.T;
-  g.tiles = (tokens + tile - 1) / tile;
-  // heads of a workgroup: as many as leave eight workgroups a CU (the angles are shared by them)
-  const int64_t want = 2048;
-  int64_t total = hp.heads[0] + hp.heads[1] + hp.heads[2];
-  int64_t per = g.tiles >= want ? total : g.tiles * total / want;
-  per = std::max<int64_t>(1, std::min<int64_t>(per, total));
+  // four heads at a time, fewer where there are fewer or where a head takes a wave: the angles are
+  // then a small part, and runs stay long
+  g.hp = 1;
+  while (g.hp < 4 && g.hp < hp.heads[0] && g.T * g.hp < NT / 4) g.hp *= 2;
+  g.tok = NT / (g.T * g.hp);
+  const int64_t tokens = hp.B * hp.L;
+  g.tiles = (tokens + g.tok - 1) / g.tok;
+  // heads of a workgroup: as many as leave WGS workgroups
+  const int64_t total = hp.heads[0] + hp.heads[1] + hp.heads[2];
+  int64_t per = g.tiles >= WGS ? total : g.tiles * total / WGS;
+  per = std::max<int64_t>(g.hp, per / g.hp * g.hp);
   for (int s = 0; s < 3; ++s) {
     g.ny[s] = (int)((hp.heads[s] + per - 1) / per);
     g.per[s] = g.ny[s] ? (int)((hp.heads[s] + g.ny[s] - 1) / g.ny[s]) : 1;
@@ -384,8 +430,9 @@ Grid grid_for(const HeadsProblem& hp, int vec) {
   return g;
 }
 int backward_blocks(const Grid& g) {
-  const int y = g.ny[0] + g.ny[1] + g.ny[2];
-  return (int)std::max<int64_t>(1, std::min<int64_t>(g.tiles, 2048 / std::max(1, y)));
+  // each walks over as many tiles as the next, and as leaves about WGS workgroups
+  const int64_t y = g.ny[0] + g.ny[1] + g.ny[2], each = std::max<int64_t>(1, g.tiles * y / WGS);
+  return (int)((g.tiles + each - 1) / each);
 }
 
 template <typename T, int VEC, int NC>
@@ -434,15 +481,11 @@ hipError_t launch_heads_backward(const HeadsProblem& hp, hipStream_t st) {
   const Grid g = grid_for(hp, vec);
   const int gx = backward_blocks(g);
   launch_any(hp, vec, g, dim3(gx, g.ny[0] + g.ny[1] + g.ny[2]), true, st);
-  const float* part = hp.dw_part;
-  for (int s = 0; s < 2; ++s) {
-    const int64_t n = (int64_t)gx * g.ny[s];
-    if (hp.dw[s]) {
-      const unsigned cols = (hp.d + 15) / 16;
-      if (hp.dtype) k_heads_weights<uint16_t><<<cols, 1024, 0, st>>>(part, (uint16_t*)hp.dw[s], n, hp.d);
-      else k_heads_weights<float><<<cols, 1024, 0, st>>>(part, (float*)hp.dw[s], n, hp.d);
-    }
-    part += n * hp.d;
+  if (hp.dw[0] || hp.dw[1]) {
+    const dim3 grid((hp.d + 15) / 16, 2);
+    const int64_t nq = (int64_t)gx * g.ny[0], nk = (int64_t)gx * g.ny[1];
+    if (hp.dtype) k_heads_weights<uint16_t><<<grid, 1024, 0, st>>>(hp.dw_part, (uint16_t*)hp.dw[0], (uint16_t*)hp.dw[1], nq, nk, hp.d);
+    else k_heads_weights<float><<<grid, 1024, 0, st>>>(hp.dw_part, (float*)hp.dw[0], (float*)hp.dw[1], nq, nk, hp.d);
   }
   return hipGetLastError();
 }
