@@ -144,6 +144,13 @@ def _stream_ptr(device):
     return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
 
 
+def _stream_of(device):
+    """The current stream of an indexed device, as an address (without a Stream object, which
+    costs small calls two microseconds)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
 def _with_workspace(nbytes: int, device, fn):
     import torch
     ws = torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
@@ -347,24 +354,32 @@ def ffn_backward(x, w1, w2, idx, dots, d_out):
 
 def _rows(t, name, shape, dtype, device):
     """A tensor whose last dimension is contiguous; the others may have any strides."""
+    if t.device == device and t.dtype == dtype and t.shape == shape and device.type == "cuda" and t.stride()[-1] == 1:
+        return
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.stride(-1) != 1 and t.shape[-1] != 1:
+    if t.shape[-1] != 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
 
 
-def _on(device):
-    """The device's context, for a call on tensors of another device than the current one."""
-    import contextlib
-
+def _launch(device, fn, args, nbytes: int = 0):
+    """fn(*args) with the tensors' device current and a workspace of nbytes; raises on a status."""
     import torch
-    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _launch(device, fn, args, nbytes)
+    if nbytes:
+        _with_workspace(nbytes, device, lambda: fn(*args))
+        return
+    rc = fn(*args)
+    if rc:
+        _raise(rc)
 
 
 def rope_frequencies(sections, theta: float = 10000.0, restart: bool = False, device="cuda"):
@@ -444,9 +459,9 @@ def rope(x, positions, freqs, axes=None, adjacent: bool = False, inverse: bool =
     dt = _dtype_code(x)
     rot = _rotation(positions, freqs, axes, adjacent, inverse, B, L, d, device)
     out = torch.empty((B, H, L, d), dtype=x.dtype, device=device)
-    with _on(device):
-        _raise(lib().topk_rope(x.data_ptr(), out.data_ptr(), B, H, L, d, x.stride(0), x.stride(1), x.stride(2),
-                               rot, dt, _stream_ptr(device)))
+    sb, sh, sl, _ = x.stride()
+    _launch(device, lib().topk_rope,
+            (x.data_ptr(), out.data_ptr(), B, H, L, d, sb, sh, sl, rot, dt, _stream_of(device)))
     return out
 
 
@@ -484,12 +499,12 @@ def qk_norm_rope(qkv, heads: int, kv_heads: int, q_weight=None, k_weight=None, p
     device = qkv.device
     dt = _dtype_code(qkv)
     rot = _rotation(positions, freqs, axes, adjacent, False, B, L, d, device)
-    q = torch.empty((B, heads, L, d), dtype=qkv.dtype, device=device)
-    k, v = (torch.empty((B, kv_heads, L, d), dtype=qkv.dtype, device=device) for _ in range(2))
-    with _on(device):
-        _raise(lib().topk_qk_norm_rope(qkv.data_ptr(), _ptr(q_weight), _ptr(k_weight), q.data_ptr(), k.data_ptr(),
-                                       v.data_ptr(), B, L, heads, kv_heads, d, qkv.stride(0), qkv.stride(1), int(norm),
-                                       eps, rot, dt, _stream_ptr(device)))
+    q, k = qkv.new_empty((B, heads, L, d)), qkv.new_empty((B, kv_heads, L, d))
+    v = torch.empty_like(k)
+    sb, sl, _ = qkv.stride()
+    _launch(device, lib().topk_qk_norm_rope,
+            (qkv.data_ptr(), _ptr(q_weight), _ptr(k_weight), q.data_ptr(), k.data_ptr(), v.data_ptr(), B, L, heads, kv_heads,
+             d, sb, sl, int(norm), float(eps), rot, dt, _stream_of(device)))
     return q, k, v
 
 
@@ -507,7 +522,7 @@ def qk_norm_rope_append(qkv, heads: int, kv_heads: int, k_cache, v_cache, length
     S = k_cache.shape[2] if k_cache.dim() == 4 else 0
     for t, n in ((k_cache, "k_cache"), (v_cache, "v_cache")):
         _rows(t, n, (B, kv_heads, S, d), qkv.dtype, device)
-        if any(t.stride(i) == 0 and t.shape[i] > 1 for i in range(3)):
+        if 0 in t.stride() and any(st == 0 and size > 1 for st, size in zip(t.stride(), t.shape)):
             raise ValueError(f"{n} is written to and must not be expanded")
     if S and k_cache.data_ptr() == v_cache.data_ptr():
         raise ValueError("k_cache and v_cache are the same memory")
@@ -518,12 +533,11 @@ def qk_norm_rope_append(qkv, heads: int, kv_heads: int, k_cache, v_cache, length
     q = torch.empty((B, heads, L, d), dtype=qkv.dtype, device=device)
     if S == 0:  # nothing can be stored; the library wants an address all the same
         k_cache = v_cache = q
-    with _on(device):
-        _raise(lib().topk_qk_norm_rope_append(
-            qkv.data_ptr(), _ptr(q_weight), _ptr(k_weight), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-            lengths.data_ptr(), B, L, heads, kv_heads, d, qkv.stride(0), qkv.stride(1), S, k_cache.stride(0),
-            k_cache.stride(1), k_cache.stride(2), v_cache.stride(0), v_cache.stride(1), v_cache.stride(2), int(norm),
-            eps, rot, dt, _stream_ptr(device)))
+    sb, sl, _ = qkv.stride()
+    _launch(device, lib().topk_qk_norm_rope_append,
+            (qkv.data_ptr(), _ptr(q_weight), _ptr(k_weight), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+             lengths.data_ptr(), B, L, heads, kv_heads, d, sb, sl, S, *k_cache.stride()[:3], *v_cache.stride()[:3],
+             int(norm), float(eps), rot, dt, _stream_of(device)))
     return q
 
 
@@ -545,15 +559,13 @@ def qk_norm_rope_backward(qkv, heads: int, kv_heads: int, d_q, d_k, d_v, q_weigh
     dqkv = torch.empty(qkv.shape, dtype=qkv.dtype, device=device)
     dwq, dwk = (torch.empty_like(w) if weights and w is not None else None for w in (q_weight, k_weight))
     Lb = lib()
-    with _on(device):
-        args = (qkv.data_ptr(), _ptr(q_weight), _ptr(k_weight), d_q.data_ptr(), d_k.data_ptr(), d_v.data_ptr(),
-                dqkv.data_ptr(), _ptr(dwq), _ptr(dwk), B, L, heads, kv_heads, d, qkv.stride(0), qkv.stride(1), int(norm),
-                eps, rot, dt, _stream_ptr(device))
-        if dwq is None and dwk is None:
-            _raise(Lb.topk_qk_norm_rope_backward(*args))
-        else:
-            nbytes = Lb.topk_qk_norm_rope_backward_workspace_bytes(B, L, heads, kv_heads, d, rot.d_rot if rot else 0, dt)
-            _with_workspace(nbytes, device, lambda: Lb.topk_qk_norm_rope_backward(*args))
+    sb, sl, _ = qkv.stride()
+    args = (qkv.data_ptr(), _ptr(q_weight), _ptr(k_weight), d_q.data_ptr(), d_k.data_ptr(), d_v.data_ptr(), dqkv.data_ptr(),
+            _ptr(dwq), _ptr(dwk), B, L, heads, kv_heads, d, sb, sl, int(norm), float(eps), rot, dt, _stream_of(device))
+    nbytes = 0
+    if dwq is not None or dwk is not None:
+        nbytes = Lb.topk_qk_norm_rope_backward_workspace_bytes(B, L, heads, kv_heads, d, rot.d_rot if rot else 0, dt)
+    _launch(device, Lb.topk_qk_norm_rope_backward, args, nbytes)
     return dqkv, dwq, dwk
 
 
@@ -608,13 +620,9 @@ def attn_prefix(q, prefix_k, prefix_v, k=None, v=None, lengths=None, causal: boo
     sums = torch.empty((B, H, Lq), dtype=torch.float32, device=device) if lse else None
     L = lib()
     nbytes = L.topk_attn_prefix_workspace_bytes(B, H, Hkv, Lq, P, S, d, dt)
-    with _on(device):
-        args = (q.data_ptr(), _ptr(prefix_k), _ptr(prefix_v), _ptr(k), _ptr(v), _ptr(lengths), out.data_ptr(), _ptr(sums),
-                B, H, Hkv, Lq, P, S, d, st, int(causal), float(scale), dt, _stream_ptr(device))
-        if nbytes:
-            _with_workspace(nbytes, device, lambda: L.topk_attn_prefix(*args))
-        else:
-            _raise(L.topk_attn_prefix(*args))
+    args = (q.data_ptr(), _ptr(prefix_k), _ptr(prefix_v), _ptr(k), _ptr(v), _ptr(lengths), out.data_ptr(), _ptr(sums),
+            B, H, Hkv, Lq, P, S, d, st, int(causal), float(scale), dt, _stream_of(device))
+    _launch(device, L.topk_attn_prefix, args, nbytes)
     return (out, sums) if lse else out
 
 
