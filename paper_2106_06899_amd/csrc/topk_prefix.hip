@@ -63,10 +63,17 @@ struct Item {
 
 // A workgroup's LDS: four tile buffers (the few-row form keeps a wave's outputs in each), and the
 // waves' maxima and sums.
+// (The few-row form picks its buffer by an LDS address: a generic one would make flat accesses.)
+#define TOPK_LDS __attribute__((address_space(3)))
 struct Lds {
   unsigned char *b0, *b1, *b2, *b3;
-  float2 (*ml)[32];
-  __device__ unsigned char* of(int w) const { return w == 0 ? b0 : w == 1 ? b1 : w == 2 ? b2 : b3; }
+  float2 (*ml)[32], *sum;
+  int64_t* row;
+  __device__ TOPK_LDS unsigned char* of(int w) const {
+    TOPK_LDS unsigned char *p0 = (TOPK_LDS unsigned char*)b0, *p1 = (TOPK_LDS unsigned char*)b1, *p2 = (TOPK_LDS unsigned char*)b2,
+                           *p3 = (TOPK_LDS unsigned char*)b3;
+    return w == 0 ? p0 : w == 1 ? p1 : w == 2 ? p2 : p3;
+  }
 };
 
 // 16 NR rows: the waves take key tiles in turn, K and V in registers.
@@ -75,9 +82,7 @@ struct Few {
   static constexpr int NS = D / 32;  // steps over the features of the scores
   static constexpr int NC = D / 16;  // blocks of 16 output features; columns of V a lane reads
   static constexpr int VB = NC * 2;  // their bytes
-  static constexpr int LD = D + 4;
   static constexpr int TILE = 16 * NR;
-  typedef float Rows[LD];            // 16 of them a wave
 
   static __device__ __forceinline__ void run(const PrefixArgs& a, const Item& it, const Lds& sh) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, g = lane >> 4;
@@ -204,7 +209,8 @@ struct Few {
       if (t + WAVES < tiles) load_v(t + WAVES);
     }
 
-    // join the waves: row by row maxima, then the scaled outputs through LDS
+    // join the waves: every row's maximum and sum, then the scaled outputs through LDS, in parts of four
+    // features whose order in a row is permuted by the row so that its lanes meet different banks
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       l[r] += __shfl_xor(l[r], 16, 64);
@@ -212,45 +218,49 @@ struct Few {
       if (g == 0) sh.ml[wave][16 * r + n] = make_float2(m[r], l[r]);
     }
     __syncthreads();
-    const bool last = a.pl.splits == 1;
+    TOPK_LDS f32x4* mine = (TOPK_LDS f32x4*)sh.of(wave);
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-      float top = -INFINITY;
+      float2 x[WAVES];
+      float top = -INFINITY, total = 0.f;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sh.ml[w][16 * r + n].x);
-      const float f = m[r] == -INFINITY ? 0.f : exp2f(m[r] - top);
-      if (r) __syncthreads();
+      for (int w = 0; w < WAVES; ++w) {
+        x[w] = sh.ml[w][16 * r + n];
+        top = fmaxf(top, x[w].x);
+      }
+      const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) total = fmaf(exp2f(x[w].x - base), x[w].y, total);
+      const float f = exp2f(m[r] - base);  // (m = -inf: 0)
 #pragma unroll
       for (int v = 0; v < 4; ++v)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) ((Rows*)sh.of(wave))[n][(4 * g + v) * NC + c] = o[r][c][v] * f;
-      __syncthreads();
-      for (int i = tid; i < 16 * D / 4; i += NT) {
-        const int row = i / (D / 4), col = (i % (D / 4)) * 4;
-        const int ri = it.r0 + 16 * r + row;
-        if (ri >= it.count) continue;
-        const int64_t gr = place(ri);
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        float tm = -INFINITY, tl = 0.f;
+        for (int c = 0; c < NC; c += 4)
+          mine[(16 * r + n) * (D / 4) + ((((4 * g + v) * NC + c) / 4) ^ n)] =
+              (f32x4){o[r][c][v] * f, o[r][c + 1][v] * f, o[r][c + 2][v] * f, o[r][c + 3][v] * f};
+      if (wave == 0 && g == 0) {
+        const int i = min(it.r0 + 16 * r + n, it.count - 1);
+        sh.row[16 * r + n] = place(i);
+        sh.sum[16 * r + n] = make_float2(top, total);
+      }
+    }
+    __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-          sum += *(const f32x4*)&((const Rows*)sh.of(w))[row][col];
-          tm = fmaxf(tm, sh.ml[w][16 * r + row].x);
-        }
+    for (int u = 0; u < 16 * NR * D / 4 / NT; ++u) {
+      const int i = u * NT + tid, row = i / (D / 4), part = i % (D / 4);
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-          const float2 x = sh.ml[w][16 * r + row];
-          if (x.x != -INFINITY) tl += x.y * exp2f(x.x - tm);
-        }
-        if (last) {
-          const float inv = tl > 0.f ? 1.f / tl : 0.f;
-          const uint2 w = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));
-          *(uint2*)((uint16_t*)a.p.out + gr * D + col) = w;
-          if (a.p.lse && col == 0) a.p.lse[gr] = tl > 0.f ? (tm + log2f(tl)) * 0.69314718055994531f : -INFINITY;
-        } else {
-          *(f32x4*)(a.po + (it.split * a.pl.rows + gr) * D + col) = sum;
-          if (col == 0) a.ml[it.split * a.pl.rows + gr] = make_float2(tm, tl);
-        }
+      for (int w = 0; w < WAVES; ++w) sum += ((const TOPK_LDS f32x4*)sh.of(w))[row * (D / 4) + (part ^ (row & 15))];
+      const int64_t at = sh.row[row];
+      const float2 x = sh.sum[row];
+      if (it.r0 + row >= it.count) continue;
+      if (a.pl.splits == 1) {
+        const float inv = x.y > 0.f ? 1.f / x.y : 0.f;
+        *(uint2*)((uint16_t*)a.p.out + at * D + 4 * part) = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));
+        if (a.p.lse && part == 0) a.p.lse[at] = x.y > 0.f ? (x.x + log2f(x.y)) * 0.69314718055994531f : -INFINITY;
+      } else {
+        *(f32x4*)(a.po + (it.split * a.pl.rows + at) * D + 4 * part) = sum;
+        if (part == 0) a.ml[it.split * a.pl.rows + at] = x;
       }
     }
   }
@@ -266,7 +276,7 @@ struct Few {
 // bf16 (relative 2^-8 at most): products bound this form, and a second term would add half as many.
 typedef float f32x16 __attribute__((__vector_size__(64)));
 typedef short s16x4 __attribute__((__vector_size__(8)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef TOPK_LDS s16x4 lds_s16x4;
 
 // the larger of x and what the lane 32 away holds (NaN if either is)
 __device__ __forceinline__ float other_half_max(float x) {
@@ -351,8 +361,8 @@ struct Wide {
           ko -= over * sp.k_sl * 2;
           vo -= over * sp.v_sl * 2;
         }
-        __builtin_amdgcn_global_load_lds((const void*)(kt + ko), (__attribute__((address_space(3))) void*)&kd[(wave * LPW + j) * 1024], 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((const void*)(vt + vo), (__attribute__((address_space(3))) void*)&vd[(wave * LPW + j) * 1024], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const void*)(kt + ko), (TOPK_LDS void*)&kd[(wave * LPW + j) * 1024], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const void*)(vt + vo), (TOPK_LDS void*)&vd[(wave * LPW + j) * 1024], 16, 0, 0);
       }
       kt += KEYS * 2 * (int64_t)sp.k_sl;
       vt += KEYS * 2 * (int64_t)sp.v_sl;
@@ -516,8 +526,9 @@ __global__ __launch_bounds__(NT, 2) void k_prefix(PrefixArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char b1[BUF];
   __shared__ __attribute__((aligned(16))) unsigned char b2[BUF];
   __shared__ __attribute__((aligned(16))) unsigned char b3[BUF];
-  __shared__ float2 ml[WAVES][32];
-  const Lds sh = {b0, b1, b2, b3, ml};
+  __shared__ float2 ml[WAVES][32], sum[32];
+  __shared__ int64_t row[32];
+  const Lds sh = {b0, b1, b2, b3, ml, sum, row};
   const PrefixPlan& pl = a.pl;
   const int B = (int)a.p.B, Hkv = (int)a.p.Hkv, ptiles = (int)pl.ptiles, stiles = (int)pl.stiles, psplits = (int)pl.psplits,
             ssplits = (int)pl.ssplits;
