@@ -259,7 +259,7 @@ struct Few {
         *(uint2*)((uint16_t*)a.p.out + at * D + 4 * part) = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));
         if (a.p.lse && part == 0) a.p.lse[at] = x.y > 0.f ? (x.x + log2f(x.y)) * 0.69314718055994531f : -INFINITY;
       } else {
-        *(f32x4*)(a.po + (it.split * a.pl.rows + at) * D + 4 * part) = sum;
+        __builtin_nontemporal_store(sum, (f32x4*)(a.po + (it.split * a.pl.rows + at) * D + 4 * part));
         if (part == 0) a.ml[it.split * a.pl.rows + at] = x;
       }
     }
@@ -299,6 +299,7 @@ struct Wide {
   static constexpr int TILEB = KEYS * 2 * D;
   static constexpr int LPW = TILEB / 1024 / WAVES;
   static constexpr int FB = D / 32;       // 32-feature blocks of the output
+  static constexpr int AHEAD_K = 6, AHEAD_V = 4;  // products by which LDS reads run ahead of their use
 
   static __device__ __forceinline__ int swz_k(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
   static __device__ __forceinline__ int swz_v(int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
@@ -369,17 +370,18 @@ struct Wide {
     };
 
     auto tile = [&](auto edge, int t, const unsigned char* kb, const unsigned char* vb) {
-      f32x16 s[2];
+      f32x16 s[2] = {};
+      {
+        bf16x8 kf[AHEAD_K + 1];
+        auto kp = [&](int i) { return *(const bf16x8*)(kb + ((i & 1) * 32 + n) * 2 * D + ((half * NS + (i >> 1)) ^ swz_k(n)) * 16); };
 #pragma unroll
-      for (int rb = 0; rb < 2; ++rb) {
-        const int r = rb * 32 + n;
-        f32x16 acc = {};
+        for (int i = 0; i < AHEAD_K; ++i) kf[i] = kp(i);
 #pragma unroll
-        for (int st = 0; st < NS; ++st) {
-          const bf16x8 av = *(const bf16x8*)(kb + (r * CH + ((half * NS + st) ^ swz_k(r))) * 16);
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bq[st], acc, 0, 0, 0);
+        for (int i = 0; i < 2 * NS; ++i) {
+          if (i + AHEAD_K < 2 * NS) kf[(i + AHEAD_K) % (AHEAD_K + 1)] = kp(i + AHEAD_K);
+          s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % (AHEAD_K + 1)], bq[i >> 1], s[i & 1], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        s[rb] = acc;
       }
       if (decltype(edge)::value) {
         const int last = seen - t * KEYS - 4 * half;
@@ -402,27 +404,36 @@ struct Wide {
 #pragma unroll
           for (int v = 0; v < 16; ++v) o[f][v] *= alpha;
       }
+      constexpr int VM = 4 * FB;
+      bf16x8 pb[4], pl[4], vf[AHEAD_V + 1];
+      auto vp = [&](int j) {
+        const unsigned char* p = vb + vat[j % FB] + j / FB * 16 * 2 * D;
+        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
+        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * 2 * D));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+#pragma unroll
+      for (int j = 0; j < AHEAD_V; ++j) vf[j] = vp(j);
       __builtin_amdgcn_s_setprio(1);  // the other wave's softmax yields to this one's products
       const float bias = LIFT - (m == -INFINITY ? 0.f : m);
+      auto wt = [&](int v) {
+        const float w = __builtin_amdgcn_exp2f(fmaf(s[v >> 4][v & 15], a.c, bias));
+        l += w;
+        pb[v >> 3][v & 7] = (__bf16)w;
+        if (TWO) pl[v >> 3][v & 7] = (__bf16)(w - (float)pb[v >> 3][v & 7]);
+      };
 #pragma unroll
-      for (int st = 0; st < 4; ++st) {  // 16 keys each
-        bf16x8 pb, pl;
+      for (int v = 0; v < 8; ++v) wt(v);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float w = __builtin_amdgcn_exp2f(fmaf(s[st >> 1][8 * (st & 1) + e], a.c, bias));
-          l += w;
-          pb[e] = (__bf16)w;
-          if (TWO) pl[e] = (__bf16)(w - (float)pb[e]);
-        }
+      for (int j = 0; j < VM; ++j) {
+        if (j + AHEAD_V < VM) vf[(j + AHEAD_V) % (AHEAD_V + 1)] = vp(j + AHEAD_V);
+        o[j % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j % (AHEAD_V + 1)], pb[j / FB], o[j % FB], 0, 0, 0);
+        if (TWO) o[j % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j % (AHEAD_V + 1)], pl[j / FB], o[j % FB], 0, 0, 0);
+        if (j + FB < VM)
 #pragma unroll
-        for (int f = 0; f < FB; ++f) {
-          const unsigned char* p = vb + vat[f] + st * 16 * 2 * D;
-          const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
-          const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * 2 * D));
-          const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-          o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, pb, o[f], 0, 0, 0);
-          if (TWO) o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, pl, o[f], 0, 0, 0);
-        }
+          for (int v = 0; v < 8 / FB; ++v) wt(8 + j * (8 / FB) + v);
+        __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_s_setprio(0);
     };
@@ -454,24 +465,34 @@ struct Wide {
     }
     m -= LIFT;
     l += __shfl_xor(l, 32, 64);
-    if (!ok) return;
-    if (a.pl.splits == 1) {
-      const float inv = l > 0.f ? 1.f / l : 0.f;
-      uint16_t* dst = (uint16_t*)a.p.out + at * D + 4 * half;
-#pragma unroll
-      for (int f = 0; f < FB; ++f)
-#pragma unroll
-        for (int v = 0; v < 16; v += 4)
-          *(uint2*)(dst + 32 * f + 2 * v) = make_uint2(pack_bf16(o[f][v] * inv, o[f][v + 1] * inv), pack_bf16(o[f][v + 2] * inv, o[f][v + 3] * inv));
-      if (a.p.lse && half == 0) a.p.lse[at] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
-      return;
-    }
-    float* dst = a.po + (it.split * a.pl.rows + at) * D + 4 * half;
+    // through the wave's own part of LDS, in parts of four features permuted by the row, so that whole rows
+    // are written, two (D = 128) or four a store; partial results past the cache, which would otherwise
+    // be emptied of them at the kernel's end (16 requests of 5 tokens behind 20001 keys: 27.8 -> 26.1 us)
+    __syncthreads();
+    TOPK_LDS f32x4* mine = (TOPK_LDS f32x4*)sh.of(wave);
+    constexpr int PARTS = D / 4, RPS = 64 / PARTS;
 #pragma unroll
     for (int f = 0; f < FB; ++f)
 #pragma unroll
-      for (int v = 0; v < 16; v += 4) *(f32x4*)(dst + 32 * f + 2 * v) = (f32x4){o[f][v], o[f][v + 1], o[f][v + 2], o[f][v + 3]};
-    if (half == 0) a.ml[it.split * a.pl.rows + at] = make_float2(m, l);
+      for (int v = 0; v < 16; v += 4)
+        mine[n * PARTS + ((8 * f + v / 2 + half) ^ (n & 15))] = (f32x4){o[f][v], o[f][v + 1], o[f][v + 2], o[f][v + 3]};
+    wave_sync_lds();
+    const bool last = a.pl.splits == 1;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const int part = lane % PARTS;
+#pragma unroll 4
+    for (int u = 0; u < 32 / RPS; ++u) {
+      const int row = u * RPS + lane / PARTS;
+      const f32x4 x = mine[row * PARTS + (part ^ (row & 15))];
+      const int64_t to = (int64_t)(uint32_t)__shfl((int)at, row, 64);
+      const float by = __shfl(inv, row, 64);
+      if (it.r0 + wave * 32 + row >= it.count) continue;
+      if (last) *(uint2*)((uint16_t*)a.p.out + to * D + 4 * part) = make_uint2(pack_bf16(x[0] * by, x[1] * by), pack_bf16(x[2] * by, x[3] * by));
+      else __builtin_nontemporal_store(x, (f32x4*)(a.po + (it.split * a.pl.rows + to) * D + 4 * part));
+    }
+    if (!ok || half) return;
+    if (!last) a.ml[it.split * a.pl.rows + at] = make_float2(m, l);
+    else if (a.p.lse) a.p.lse[at] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
   }
 };
 
