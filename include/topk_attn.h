@@ -413,7 +413,11 @@ size_t topk_qk_norm_rope_backward_workspace_bytes(int64_t B, int64_t L, int64_t 
  *   out        [B, H, Lq, d]   written; a row that sees no key is 0
  *   lse        NULL, or fp32 [B, H, Lq]: log sum_j exp(scale * s_j), -inf where no key is seen
  *
- * bf16 with d = 64 or 128 (else TOPK_E_UNSUPPORTED). Softmax statistics and sums in fp32.
+ * bf16 with d = 64 or 128, at most 2^27 query rows (else TOPK_E_UNSUPPORTED). Softmax
+ * statistics and sums in fp32, in a fixed order; a row is computed from its own numbers
+ * alone, and values up to 2^90 cannot overflow the sums.
+ * Weights enter the product with V to 16 significant bits, or, with 64 rows a request and
+ * key head ((H / Hkv) * Lq) and more, rounded to bf16 as topk_attn_dense does.
  * Workspace: topk_attn_prefix_workspace_bytes, partial results of key ranges in fp32 (0
  * where none is needed, or for invalid arguments). Stages 0 and 3 of the stage timing.
  */

@@ -43,6 +43,15 @@ struct PrefixArgs {
   float c;     // scale * log2(e)
 };
 
+// the larger, and NaN where either is (a row whose scores hold one is NaN, no other)
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+// a row's factor and its logarithm (to base e) from the sum of its weights, 0 where it saw no key, and the
+// maximum that they were taken against (to base 2)
+__device__ __forceinline__ float row_factor(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+__device__ __forceinline__ float row_log(float top, float sum) {
+  return sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+}
+
 // A range of keys, of the prefix or of a request's own.
 struct Span {
   const uint16_t *k, *v;  // its first
@@ -172,11 +181,11 @@ struct Few {
       bf16x8 hi[NR], lo[NR];
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
-        float mt = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])),
-                         fmaxf(fmaxf(s[r][1][0], s[r][1][1]), fmaxf(s[r][1][2], s[r][1][3])));
-        mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
-        mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
-        const float mn = fmaxf(m[r], mt * a.c);
+        float mt = larger(larger(larger(s[r][0][0], s[r][0][1]), larger(s[r][0][2], s[r][0][3])),
+                          larger(larger(s[r][1][0], s[r][1][1]), larger(s[r][1][2], s[r][1][3])));
+        mt = larger(mt, __shfl_xor(mt, 16, 64));
+        mt = larger(mt, __shfl_xor(mt, 32, 64));
+        const float mn = larger(m[r], mt * a.c);
         const float off = mn == -INFINITY ? 0.f : mn;
         if (__builtin_amdgcn_ballot_w64(mn != m[r])) {
           const float alpha = exp2f(m[r] - off);  // (m = -inf: 0)
@@ -226,7 +235,7 @@ struct Few {
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) {
         x[w] = sh.ml[w][16 * r + n];
-        top = fmaxf(top, x[w].x);
+        top = larger(top, x[w].x);
       }
       const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
@@ -255,9 +264,9 @@ struct Few {
       const float2 x = sh.sum[row];
       if (it.r0 + row >= it.count) continue;
       if (a.pl.splits == 1) {
-        const float inv = x.y > 0.f ? 1.f / x.y : 0.f;
+        const float inv = row_factor(x.y);
         *(uint2*)((uint16_t*)a.p.out + at * D + 4 * part) = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));
-        if (a.p.lse && part == 0) a.p.lse[at] = x.y > 0.f ? (x.x + log2f(x.y)) * 0.69314718055994531f : -INFINITY;
+        if (a.p.lse && part == 0) a.p.lse[at] = row_log(x.x, x.y);
       } else {
         __builtin_nontemporal_store(sum, (f32x4*)(a.po + (it.split * a.pl.rows + at) * D + 4 * part));
         if (part == 0) a.ml[it.split * a.pl.rows + at] = x;
@@ -278,17 +287,14 @@ typedef float f32x16 __attribute__((__vector_size__(64)));
 typedef short s16x4 __attribute__((__vector_size__(8)));
 typedef TOPK_LDS s16x4 lds_s16x4;
 
-// the larger of x and what the lane 32 away holds (NaN if either is)
+// the larger of x and what the lane 32 away holds
 __device__ __forceinline__ float other_half_max(float x) {
   const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __builtin_elementwise_maximum(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  return larger(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
 template <int D, bool TWO>
 struct Wide {
-  // Weights are formed as 2^24 times themselves, so that the exponential instruction, which knows no
-  // numbers below 2^-126, keeps every weight that 32 bits can hold.
-  static constexpr float LIFT = 24.f;
   // The maximum that weights are taken against is moved, and the sums with it, only once a score
   // leads it by 2^8 in weight.
   static constexpr float LEAD = 8.f;
@@ -383,6 +389,10 @@ struct Wide {
           __builtin_amdgcn_sched_barrier(0);
         }
       }
+      float low = INFINITY;  // the tile's lowest score (masked keys' included: they only choose the exponential below)
+#pragma unroll
+      for (int v = 0; v < 32; v += 2)
+        low = __builtin_elementwise_minimum(__builtin_elementwise_minimum(low, s[v >> 4][v & 15]), s[v >> 4][(v & 15) + 1]);
       if (decltype(edge)::value) {
         const int last = seen - t * KEYS - 4 * half;
 #pragma unroll
@@ -392,10 +402,11 @@ struct Wide {
       float mt = -INFINITY;
 #pragma unroll
       for (int v = 0; v < 32; v += 2)
-        mt = __builtin_elementwise_maximum(__builtin_elementwise_maximum(mt, s[v >> 4][v & 15]), s[v >> 4][(v & 15) + 1]);
+        mt = larger(larger(mt, s[v >> 4][v & 15]), s[v >> 4][(v & 15) + 1]);
       mt = other_half_max(mt) * a.c;
-      if (__builtin_amdgcn_ballot_w64(!(mt <= m + LEAD))) {  // (for NaN too; rows whose maximum stays multiply by 1)
-        const float mn = fmaxf(m, mt);
+      const bool leads = !(mt <= m + LEAD);  // (NaN too)
+      if (__builtin_amdgcn_ballot_w64(leads)) {  // (the other rows multiply by 1: a row's result is its own)
+        const float mn = leads ? larger(m, mt) : m;
         const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
         m = mn;
         l *= alpha;
@@ -405,19 +416,40 @@ struct Wide {
           for (int v = 0; v < 16; ++v) o[f][v] *= alpha;
       }
       constexpr int VM = 4 * FB;
-      bf16x8 pb[4], pl[4], vf[AHEAD_V + 1];
-      auto vp = [&](int j) {
+      const float off = m == -INFINITY ? 0.f : m;
+      auto vp = [&](int j) {  // V^T of 16 keys j / FB, features 32 (j % FB) on
         const unsigned char* p = vb + vat[j % FB] + j / FB * 16 * 2 * D;
         const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
         const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * 2 * D));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
       };
+      // Weights below 2^-126, which the exponential instruction alone makes 0, are added by themselves
+      // where the tile has any.
+      if (__builtin_amdgcn_ballot_w64(fmaf(low, a.c, -off) < -126.f)) {
+        float bias = -off;
+        asm volatile("" : "+v"(bias));  // (nothing of this pass is held for the other)
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {
+          bf16x8 pt;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float x = fmaf(s[st >> 1][8 * (st & 1) + e], a.c, bias), w = x < -126.f ? exp2f(x) : 0.f;
+            l += w;
+            pt[e] = (__bf16)w;
+          }
+#pragma unroll
+          for (int f = 0; f < FB; ++f) {
+            o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp(st * FB + f), pt, o[f], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+      bf16x8 pb[4], pl[4], vf[AHEAD_V + 1];
 #pragma unroll
       for (int j = 0; j < AHEAD_V; ++j) vf[j] = vp(j);
       __builtin_amdgcn_s_setprio(1);  // the other wave's softmax yields to this one's products
-      const float bias = LIFT - (m == -INFINITY ? 0.f : m);
       auto wt = [&](int v) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(s[v >> 4][v & 15], a.c, bias));
+        const float w = __builtin_amdgcn_exp2f(fmaf(s[v >> 4][v & 15], a.c, -off));
         l += w;
         pb[v >> 3][v & 7] = (__bf16)w;
         if (TWO) pl[v >> 3][v & 7] = (__bf16)(w - (float)pb[v >> 3][v & 7]);
@@ -463,7 +495,6 @@ struct Wide {
       if (work) tile(std::true_type{}, t, odd ? sh.b1 : sh.b0, odd ? sh.b3 : sh.b2);
     }
     }
-    m -= LIFT;
     l += __shfl_xor(l, 32, 64);
     // through the wave's own part of LDS, in parts of four features permuted by the row, so that whole rows
     // are written, two (D = 128) or four a store; partial results past the cache, which would otherwise
@@ -478,7 +509,7 @@ struct Wide {
         mine[n * PARTS + ((8 * f + v / 2 + half) ^ (n & 15))] = (f32x4){o[f][v], o[f][v + 1], o[f][v + 2], o[f][v + 3]};
     wave_sync_lds();
     const bool last = a.pl.splits == 1;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = row_factor(l);
     const int part = lane % PARTS;
 #pragma unroll 4
     for (int u = 0; u < 32 / RPS; ++u) {
@@ -492,7 +523,7 @@ struct Wide {
     }
     if (!ok || half) return;
     if (!last) a.ml[it.split * a.pl.rows + at] = make_float2(m, l);
-    else if (a.p.lse) a.p.lse[at] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    else if (a.p.lse) a.p.lse[at] = row_log(m, l);
   }
 };
 
@@ -617,18 +648,18 @@ __global__ __launch_bounds__(NT) void k_prefix_join(PrefixArgs a) {
     if (splits <= 4) {
 #pragma unroll
       for (int s = 0; s < 4; ++s)
-        if (s < splits) top = fmaxf(top, a.ml[s * a.pl.rows + row].x);
+        if (s < splits) top = larger(top, a.ml[s * a.pl.rows + row].x);
     } else {
-      for (int s = tr; s < splits; s += TR) top = fmaxf(top, a.ml[s * a.pl.rows + row].x);
+      for (int s = tr; s < splits; s += TR) top = larger(top, a.ml[s * a.pl.rows + row].x);
     }
   }
   if (splits > 4) {  // (TR lanes of a row: 32 or more of one wave, or whole waves)
-    for (int o = 1; o < (TR < 64 ? TR : 64); o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    for (int o = 1; o < (TR < 64 ? TR : 64); o <<= 1) top = larger(top, __shfl_xor(top, o, 64));
     if (TR > 64) {
       if (threadIdx.x % 64 == 0) fac[rl][threadIdx.x % TR / 64] = top;
       __syncthreads();
 #pragma unroll
-      for (int w = 0; w < TR / 64; ++w) top = fmaxf(top, fac[rl][w]);
+      for (int w = 0; w < TR / 64; ++w) top = larger(top, fac[rl][w]);
       __syncthreads();
     }
   }
@@ -666,10 +697,10 @@ __global__ __launch_bounds__(NT) void k_prefix_join(PrefixArgs a) {
     }
   }
   if (!ok) return;
-  const float inv = total > 0.f ? 1.f / total : 0.f;
+  const float inv = row_factor(total);
   const uint2 w = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));
   *(uint2*)((uint16_t*)a.p.out + row * D + 4 * c) = w;
-  if (a.p.lse && c == 0) a.p.lse[row] = total > 0.f ? (top + log2f(total)) * 0.69314718055994531f : -INFINITY;
+  if (a.p.lse && c == 0) a.p.lse[row] = row_log(top, total);
 }
 
 int64_t cdiv(int64_t x, int64_t y) { return (x + y - 1) / y; }

@@ -96,14 +96,14 @@ class NormRotaryHeadsFunction(torch.autograd.Function):
 
 def rotary(x, positions, freqs, axes=None, adjacent: bool = False):
     """Differentiable rotary positions on [B, H, L, d] heads; arguments as ``rope``."""
-    return RotaryFunction.apply(x, positions, freqs, axes, bool(adjacent))
+    return RotaryFunction.apply(x, positions, freqs, None if axes is None else tuple(axes), bool(adjacent))
 
 
 def norm_rotary_heads(qkv, heads: int, kv_heads: int, q_weight=None, k_weight=None, positions=None, freqs=None, axes=None,
                       adjacent: bool = False, eps: float = 1e-6, norm: bool = True):
     """Differentiable q, k, v heads of the packed projection; arguments as ``qk_norm_rope``."""
-    return NormRotaryHeadsFunction.apply(qkv, q_weight, k_weight, positions, freqs, int(heads), int(kv_heads), axes,
-                                         bool(adjacent), float(eps), bool(norm))
+    return NormRotaryHeadsFunction.apply(qkv, q_weight, k_weight, positions, freqs, int(heads), int(kv_heads),
+                                         None if axes is None else tuple(axes), bool(adjacent), float(eps), bool(norm))
 
 
 def topk_attention(q, k, v, topk: int, chunk: int = 0, causal: bool = False, scale: float | None = None):

@@ -97,6 +97,13 @@ CASES = {
     "one_long_chunk": (1, 2, 1, 515, 2100, 515, 64, True, [515]),
     "many_requests": (70, 4, 2, 1, 600, 9, 64, True, [(7 * i) % 10 for i in range(70)]),
     "long": (2, 2, 1, 1, 9999, 3000, 128, True, [3000, 2049]),
+    "no_keys": (2, 4, 2, 3, 0, 0, 64, True, None),
+    "no_keys_chunk": (2, 4, 2, 80, 0, 0, 128, True, None),
+    "whole_tiles": (3, 2, 1, 64, 130, 128, 64, True, [128, 64, 65]),
+    "whole_tiles_d128": (2, 1, 1, 128, 1000, 200, 128, True, [200, 128]),
+    "whole_tiles_all_keys": (2, 2, 2, 256, 65, 300, 128, False, [300, 1]),
+    "whole_tiles_cache_only": (2, 2, 2, 128, 0, 300, 64, True, [300, 100]),
+    "fifty_rows_a_request": (5, 10, 1, 5, 400, 50, 64, True, [50, 5, 6, 49, 33]),
 }
 
 
@@ -300,3 +307,90 @@ def test_decode_continues_a_shared_prefix(kw):
         lengths += n
         at += n
     assert bool(kc[:, :, at - P:].isnan().all()) and bool(kc[:, :, :at - P].isfinite().all())
+
+
+@pytest.mark.parametrize("Lq", [1, 40, 128])
+def test_one_row_of_nan_stays_alone(Lq):
+    q, pk, pv, k, v = _inputs(2, 2, 1, Lq, 300, 150, 64, seed=11)
+    want = tk.attn_prefix(q, pk, pv, k, v)
+    q[1, 0, Lq // 2, 5] = math.nan
+    got = tk.attn_prefix(q, pk, pv, k, v)
+    assert bool(got[1, 0, Lq // 2].isnan().all())
+    keep = torch.ones(2, 2, Lq, dtype=torch.bool, device="cuda")
+    keep[1, 0, Lq // 2] = False
+    assert torch.equal(got[keep], want[keep])
+
+
+@pytest.mark.parametrize("Lq", [4, 40, 128])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_of_minus_infinity_and_tiny_weights(Lq, d):
+    """Whole stretches of keys at -inf, before and after finite ones; and a weight of 2^-130 against a
+    value of 2^120 whose other weights meet zeros (all of it on every form: 4, 40 and 128 rows)."""
+    q, pk, pv, k, v = _inputs(1, 1, 1, Lq, 330, 200, d, seed=12)
+    q[..., 0], pk[..., 0], k[..., 0] = 1.0, 0.0, 0.0
+    away = torch.zeros(330, dtype=torch.bool, device="cuda")
+    away[0:130], away[200:300] = True, True
+    pk[0, away, 0] = -math.inf
+    out = tk.attn_prefix(q, pk, pv, k, v, causal=False)
+    want = tk.attn_prefix(q, pk[:, ~away].contiguous(), pv[:, ~away].contiguous(), k, v, causal=False)
+    # both round to bf16 and their weights by 2^-8 at most
+    assert bool(((out.double() - want.double()).abs() <= 2.0 ** -6 * pv.double().abs().max()).all())
+    z = lambda n: torch.zeros(1, 1, n, d, device="cuda")  # noqa: E731
+    qq, kk, vv = z(Lq), z(200), z(200)
+    qq[..., 0] = 1
+    kk[..., 0] = -1e4
+    kk[0, 0, 3, 0], kk[0, 0, 150, 0] = 0, -90.0 * 8
+    vv[0, 0, 150] = 2.0 ** 120
+    got = tk.attn_prefix(qq.to(BF16), None, None, kk.to(BF16), vv.to(BF16), causal=False, scale=0.125).double()
+    ref = math.exp(-90.0) * 2.0 ** 120
+    assert bool(((got - ref).abs() <= (2.0 ** -4 + 2.0 ** -8) * ref).all()), got.flatten()[0]
+
+
+@pytest.mark.parametrize("Lq", [2, 128])
+def test_large_values_do_not_overflow(Lq):
+    """Values of 2^60 under scores that grow along the keys (each leads the maximum so far)."""
+    d = 64
+    q, pk, pv, k, v = _inputs(1, 2, 2, Lq, 500, 200, d, seed=13)
+    q[..., 0] = 1.0
+    pk[..., 0] = torch.arange(500, device="cuda").to(BF16)
+    k[..., 0] = 500.0
+    big = 2.0 ** 60
+    out = tk.attn_prefix(q, pk, pv * big, k, v * big, scale=0.05)
+    _check(q, pk, pv, k, v, None, True, 0.05, (out.double() / big))
+
+
+def test_rows_by_the_million():
+    """More rows than are joined one a workgroup: every row of three requests against 64 bits."""
+    B, H, Lq, P, S = 300, 64, 64, 300, 64
+    q, pk, pv, k, v = _inputs(B, H, H, Lq, P, S, 64, seed=14)
+    n = torch.arange(B, dtype=torch.int32, device="cuda") % 65
+    out, lse = tk.attn_prefix(q, pk, pv, k, v, n, lse=True)
+    for b in (0, 137, 299):
+        one = slice(b, b + 1)
+        _check(q[one], pk, pv, k[one], v[one], n[one].tolist(), True, 0.125, out[one], lse[one])
+
+
+def test_training_step_captured_and_replayed():
+    """The attention layer's forward and backward with norm and rotation, in a graph, against eager ones."""
+    torch.manual_seed(2)
+    m = layers.TopkMultiheadAttention(128, 2, 16, 64, True, device="cuda", qk_norm=True, rope_theta=1e4)
+    x = torch.randn(2, 70, 128, device="cuda", dtype=BF16, requires_grad=True)
+    g = torch.randn(2, 70, 128, device="cuda", dtype=BF16)
+    pos = torch.arange(70, device="cuda")
+    leaves = [x, m.q_norm, m.k_norm]
+    step = lambda: torch.autograd.grad(m(x, pos), leaves, g)  # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for rep in range(3):
+        with torch.no_grad():
+            x.copy_(torch.randn(2, 70, 128, device="cuda"))
+        graph.replay()
+        got = [t.clone() for t in held]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, step())), f"replay {rep}"
