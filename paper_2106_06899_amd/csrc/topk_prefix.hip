@@ -6,12 +6,23 @@
 // The prefix is read once for a tile of rows of all requests, not once a request: the rows
 // (request, query head of the group, token) of one key head are one long list for the prefix,
 // and one short list a request for the caches. A workgroup takes one row tile and one key
-// range, of the prefix or of one cache, and leaves a partial result (the running maximum, the
-// sum and the unnormalised output, all in 32 bits) which a second kernel joins; where there is
-// one range in all, it writes the output itself. Both kinds of workgroup run in one launch.
+// range, of the prefix or of one cache, and leaves a partial result (the maximum, the sum and
+// the unnormalised output, all in 32 bits) which a second kernel joins; where there is one
+// range in all, it writes the output itself. Both kinds of workgroup run in one launch, so that
+// the prefix's products and the caches' reads overlap. Requests with many rows of their own take
+// prefix and cache as one list of keys instead, which leaves fewer partial results.
 //
-// Within a workgroup four waves take key tiles of 32 in turn, each with a running softmax of
-// its own, joined through LDS at the end. Scores are S^T = K Q^T and the output O^T = V^T P^T by
+// Row tiles come in two forms. Few (up to 32 rows) keeps K and V in registers and is bound by
+// reading them: 8 requests behind 65536 keys, 16 heads of 128, read 571 MB in 98 us (5.8 TB/s; a
+// device copy: 4.94). Wide (128 rows) goes through LDS and is bound by matrix and vector
+// instructions, which this chip runs side by side at falling clocks: 4 requests of 512 tokens, 16
+// heads of 128 on 4 key heads behind 16384 keys, 269 us with the join, 1.04 PFLOP/s (a large
+// library matrix product: 1.38). Short calls are bound by launches and latency, and by the partial
+// results: 64 requests behind 8192 keys, 32 heads of 128 on 8, 30 + 5 us, of which writing and
+// reading 33 MB of them takes about ten.
+//
+// Few rows. Four waves take key tiles of 32 in turn, each with a running softmax of its own, joined
+// through LDS at the end. Scores are S^T = K Q^T and the output O^T = V^T P^T by
 // v_mfma_f32_16x16x32_bf16, so that a lane holds scores, weights and outputs of one row
 // (lane % 16): the weights of 32 keys are the second product's operand as they stand. K and V go
 // from memory to registers: a lane's part of K is the first product's operand as it lies in
@@ -281,8 +292,14 @@ struct Few {
 //   * O^T += V^T P^T by the same instruction: the weights are its operand in the order the lane holds
 //     them, V^T comes from the row-major tile by transposing LDS reads (four keys of a feature each).
 // Tiles come by direct global-to-LDS loads, one ahead; the 16-byte parts of their rows are permuted so
-// that the lanes of one LDS cycle meet different banks. Weights enter the second product rounded to
-// bf16 (relative 2^-8 at most): products bound this form, and a second term would add half as many.
+// that the lanes of one LDS cycle meet different banks. TWO: weights enter the second product as two
+// bf16 numbers, as in the few-row form, which costs 3 to 17 % (5 tokens of 16 requests: 28.7 us, 25.0
+// without); with 64 rows a request and more they are rounded to bf16 (relative 2^-8 at most), which
+// saves a quarter of the products.
+//
+// Measured and left: the scores of the next tile formed between this tile's weights (no faster at
+// sustained clocks, slower on short ranges: 31 us for 25), 64 rows a wave (accumulators spill), eight
+// waves and 256 rows a workgroup (274 us for 276), three tiles ahead (the same).
 typedef float f32x16 __attribute__((__vector_size__(64)));
 typedef short s16x4 __attribute__((__vector_size__(8)));
 typedef TOPK_LDS s16x4 lds_s16x4;
@@ -296,7 +313,7 @@ __device__ __forceinline__ float other_half_max(float x) {
 template <int D, bool TWO>
 struct Wide {
   // The maximum that weights are taken against is moved, and the sums with it, only once a score
-  // leads it by 2^8 in weight.
+  // leads it by 2^8 in weight (291 -> 277 us at 4 x 512 tokens; s_setprio below: 277 -> 270).
   static constexpr float LEAD = 8.f;
   static constexpr int TILE = 32 * WAVES; // rows of a workgroup
   static constexpr int KEYS = 64;         // of a tile
@@ -715,7 +732,10 @@ PrefixArgs args_for(const PrefixProblem& pp, const PrefixPlan& pl, const void* w
   return a;
 }
 
-// the form for so many rows, and its rows
+// The form for so many rows. Measured, 8 key heads of 128: 16 rows behind 30000 keys, 28.4 us as one block
+// of 16 rows, 30.6 as two; 20 rows a request against 16 caches of 1000 to 3000 keys, 37 us as two blocks,
+// 42 as a wide tile; 64 rows behind 30000 keys, 34.4 us as a wide tile, 38.5 as two tiles of 32, and 40 rows
+// against such caches 45 and 57.
 int form_for(int64_t rows, int wide) { return rows <= 16 ? 1 : rows <= 32 ? 2 : wide; }
 int tile_rows(int form) { return form >= 8 ? 128 : 16 * form; }
 
@@ -732,13 +752,17 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
   pl.stiles = cdiv(pl.req_rows, tile_rows(pl.sform));
   // (many rows are joined several a workgroup, from few ranges)
   const int64_t longest = std::max(pp.P, pp.S), least = cdiv(longest, (pl.rows > 1 << 20 ? JOIN_FEW : JOIN_MAX) / 2 * 128) * 128;
+  // one list of prefix and own keys, unless more than an eighth of a tile's rows would be idle on the prefix
+  // (4 x 512 tokens: 277 us, 286 in two lists; 8 requests of 80 rows, of 128: 24.6 us, 21.0 in two lists)
   pl.both = pl.sform == 9 && pl.stiles * 128 * 8 <= pl.req_rows * 9;
   if (pl.both) {
     const int64_t items = pp.Hkv * pp.B * pl.stiles, keys = pp.P + pp.S;
+    // as many ranges as finish soonest: layers of workgroups over 256 CUs, each tile of 64 keys in 1.05 us
+    // (d = 128) where two share a CU, and the join's traffic
     double best = 0;
     for (int64_t s = 1; s <= JOIN_FEW && (s == 1 || cdiv(keys, s) >= 128); ++s) {
       const int64_t layers = cdiv(items * s, 256), range = std::max(least, cdiv(cdiv(keys, s), 64) * 64);
-      const double tile = pp.d == 64 ? 0.7 : 1.05;  // us of 64 keys where two workgroups share a CU
+      const double tile = pp.d == 64 ? 0.7 : 1.05;
       const double us = (layers == 1 ? 1.25 : (double)layers) * tile * (range / 64.0 + 3) + (s > 1 ? 4 + s * pl.rows * pp.d * 2e-6 : 0);
       if (s == 1 || us < best) {
         best = us;
@@ -748,7 +772,8 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
     pl.splits = std::max<int64_t>(1, cdiv(keys, pl.pkeys));
     return pl;
   }
-  // ranges of equal length, as many as give two workgroups a CU, of 128 keys at least
+  // ranges of equal length, as many as give two workgroups a CU, of 128 keys at least (64 requests behind
+  // 8192 keys: 37 us; one and a half a CU 42, four 48)
   const int64_t keys = pp.Hkv * pl.ptiles * pp.P + pp.B * pp.Hkv * pl.stiles * pp.S;
   const int64_t range = std::max(std::max<int64_t>(128, cdiv(cdiv(keys, 512), 128) * 128), least);
   pl.psplits = cdiv(pp.P, range);
