@@ -327,19 +327,20 @@ __global__ __launch_bounds__(NT) void k_heads_backward(HeadsProblem hp, Grid g) 
             dot = fmaf(ma[j][e] * wa[j][e], xa[j][e], fmaf(mb[j][e] * wb[j][e], xb[j][e], dot));
           }
         }
-        float r = 1.f, k = 0.f;  // dx = r m w - k x
+        float r = 1.f, mean = 0.f;  // dx = r (m w - u mean)
         if (hp.norm) {
           r = rsqrtf(fmaf(group_sum(sq, g.T), inv_d, hp.eps));
-          k = r * r * r * group_sum(dot, g.T) * inv_d;
+          mean = r * group_sum(dot, g.T) * inv_d;
         }
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
-            ga[j][e] = fmaf(ma[j][e], xa[j][e] * r, ga[j][e]);
-            gb[j][e] = fmaf(mb[j][e], xb[j][e] * r, gb[j][e]);
-            ma[j][e] = fmaf(r * wa[j][e], ma[j][e], -k * xa[j][e]);
-            mb[j][e] = fmaf(r * wb[j][e], mb[j][e], -k * xb[j][e]);
+            const float ua = xa[j][e] * r, ub = xb[j][e] * r;
+            ga[j][e] = fmaf(ma[j][e], ua, ga[j][e]);
+            gb[j][e] = fmaf(mb[j][e], ub, gb[j][e]);
+            ma[j][e] = r * fmaf(wa[j][e], ma[j][e], -mean * ua);
+            mb[j][e] = r * fmaf(wb[j][e], mb[j][e], -mean * ub);
           }
         }
       }

@@ -383,3 +383,19 @@ def test_other_streams_and_a_replayed_graph():
         eager = (*everything(), kc, vc)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, eager)), f"replay {rep}"
+
+
+def test_gradient_of_empty_tokens_with_a_tiny_eps():
+    """Tokens of zeros (padding): r = eps^(-1/2) = 1e15, whose third power is beyond fp32, and
+    dx = r w times the gradient. r, its products and w: a few e relative each, below 20 e."""
+    H, Hkv, d, L = 2, 1, 64, 5
+    qkv = _randn(21, 1, L, (H + 2 * Hkv) * d)
+    qkv[0, 2:4] = 0
+    w = _randn(22, d, mean=1.0, std=0.1)
+    grads = [_randn(23 + i, 1, h, L, d) for i, h in enumerate((H, Hkv, Hkv))]
+    dx, dwq, dwk = tk.qk_norm_rope_backward(qkv, H, Hkv, *grads, w, w, eps=1e-30)
+    eps = float(torch.tensor(1e-30, dtype=F32).double())
+    for h in range(H + Hkv):
+        ref = (grads[0][0, h] if h < H else grads[1][0, h - H])[2:4].double() * w.double() * eps ** -0.5
+        _close(dx[0, 2:4, h * d:(h + 1) * d], ref, 20 * E * ref.abs(), f"head {h}")
+    assert dx.isfinite().all() and dwq.isfinite().all() and dwk.isfinite().all()
