@@ -405,7 +405,8 @@ size_t topk_qk_norm_rope_backward_workspace_bytes(int64_t B, int64_t L, int64_t 
  *
  *   Q          [B, H, Lq, d]   contiguous
  *   prefix_K, prefix_V [Hkv, P, d]; K, V [B, Hkv, S, d]: strides in elements (NULL:
- *              contiguous), multiples of 8; not read where P = 0 or S = 0
+ *              contiguous), multiples of 8 (any where there is one entry along them); not
+ *              read where P = 0 or S = 0
  *   lengths    device, int32 [B]: request b holds lengths[b] keys (taken into [0, S]; NULL:
  *              S); rows at and behind it are not used, whatever they hold
  *   causal     1: the queries are the request's last Lq positions: query i sees the prefix
@@ -415,7 +416,8 @@ size_t topk_qk_norm_rope_backward_workspace_bytes(int64_t B, int64_t L, int64_t 
  *
  * bf16 with d = 64 or 128, at most 2^27 query rows (else TOPK_E_UNSUPPORTED). Softmax
  * statistics and sums in fp32, in a fixed order; a row is computed from its own numbers
- * alone, and values up to 2^90 cannot overflow the sums.
+ * alone (keys and values it does not see may be infinite or NaN; where it sees such a value
+ * its output is infinite or NaN), and values up to 2^90 cannot overflow the sums.
  * Weights enter the product with V to 16 significant bits, or, with 64 rows a request and
  * key head ((H / Hkv) * Lq) and more, rounded to bf16 as topk_attn_dense does.
  * Workspace: topk_attn_prefix_workspace_bytes, partial results of key ranges in fp32 (0

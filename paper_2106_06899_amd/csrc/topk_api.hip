@@ -1352,8 +1352,13 @@ int topk_attn_prefix(const void* Q, const void* prefix_K, const void* prefix_V, 
   PrefixProblem pp;
   int rc = prefix_shape(&pp, B, H, Hkv, Lq, P, S, d, causal, scale, dtype);
   if (rc) return rc;
-  const topk_prefix_strides t =
+  topk_prefix_strides t =
       strides ? *strides : topk_prefix_strides{P * d, d, P * d, d, Hkv * S * d, S * d, d, Hkv * S * d, S * d, d};
+  // (a stride that leads nowhere may be any)
+  if (B == 1) t.k_batch = t.v_batch = 0;
+  if (Hkv == 1) t.prefix_k_head = t.prefix_v_head = t.k_head = t.v_head = 0;
+  if (P == 1) t.prefix_k_key = t.prefix_v_key = 0;
+  if (S == 1) t.k_key = t.v_key = 0;
   if ((rc = check_ptr(Q, "Q")) || (rc = check_ptr(out, "out"))) return rc;
   if (P && ((rc = cache_ptr("prefix_K", prefix_K, {t.prefix_k_head, t.prefix_k_key})) ||
             (rc = cache_ptr("prefix_V", prefix_V, {t.prefix_v_head, t.prefix_v_key}))))

@@ -43,6 +43,7 @@ namespace {
 constexpr int NT = 256, WAVES = 4, KT = 32;
 constexpr int JOIN_MAX = 1024;  // key ranges of a row at most,
 constexpr int JOIN_FEW = 16;    // where a workgroup joins several rows
+constexpr int64_t RANGE_MAX = int64_t(1) << 30;  // keys of a range (their numbers, and rows on top, are 32 bits)
 // s_waitcnt immediate: no vector-memory operation outstanding, the other counters ignored
 constexpr int WAIT_VM0 = (7 << 4) | (15 << 8);
 
@@ -62,6 +63,9 @@ __device__ __forceinline__ float row_factor(float sum) { return sum == 0.f ? 0.f
 __device__ __forceinline__ float row_log(float top, float sum) {
   return sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
 }
+
+// Of two bf16 numbers, bit 0 and bit 16: is it infinite or NaN?
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) { return (((x & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u; }
 
 // A range of keys, of the prefix or of a request's own.
 struct Span {
@@ -103,6 +107,14 @@ struct Few {
   static constexpr int NC = D / 16;  // blocks of 16 output features; columns of V a lane reads
   static constexpr int VB = NC * 2;  // their bytes
   static constexpr int TILE = 16 * NR;
+
+  // column c of eight keys' numbers, as an operand
+  static __device__ __forceinline__ bf16x8 column(const uint32_t (&x)[8][NC / 2], int c) {
+    const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
+    const int w = c / 2;
+    return __builtin_bit_cast(bf16x8, make_uint4(__builtin_amdgcn_perm(x[1][w], x[0][w], sel), __builtin_amdgcn_perm(x[3][w], x[2][w], sel),
+                                                 __builtin_amdgcn_perm(x[5][w], x[4][w], sel), __builtin_amdgcn_perm(x[7][w], x[6][w], sel)));
+  }
 
   static __device__ __forceinline__ void run(const PrefixArgs& a, const Item& it, const Lds& sh) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, g = lane >> 4;
@@ -188,6 +200,45 @@ struct Few {
           if (first + 16 * (e >> 2) + 4 * g + (e & 3) >= sp.n)
 #pragma unroll
             for (int w = 0; w < NC / 2; ++w) vr[e][w] = 0;
+        // Values that are not finite go to the rows that see their keys, which become NaN there; the others
+        // would meet them as 0 times NaN.
+        uint32_t bad = 0;
+        if (causal && all_see < sp.n) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int w = 0; w < NC / 2; ++w) bad |= not_finite(vr[e][w]);
+        }
+        if (__builtin_amdgcn_ballot_w64(bad)) {
+          int key0 = first + 4 * g;
+          asm volatile("" : "+v"(key0));  // (nothing of this is held from above)
+          bf16x8 sees[NR];
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sees[r][e] = (__bf16)(key0 + 16 * (e >> 2) + (e & 3) < seen[r] ? 1.f : 0.f);
+#pragma unroll
+          for (int w = 0; w < NC / 2; ++w) {
+            uint32_t mark[8][NC / 2];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              uint32_t x = vr[e][w];
+              asm volatile("" : "+v"(x));
+              const uint32_t nf = not_finite(x);
+              mark[e][w] = nf * 0x3F80u;  // 1 of bf16
+              vr[e][w] = x & ~(nf * 0xFFFFu);
+            }
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+              for (int c = 2 * w; c < 2 * w + 2; ++c) {
+                const f32x4 met = __builtin_amdgcn_mfma_f32_16x16x32_bf16(column(mark, c), sees[r], (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                  if (met[v] > 0.f) o[r][c][v] = NAN;
+              }
+          }
+        }
       }
       bf16x8 hi[NR], lo[NR];
 #pragma unroll
@@ -215,11 +266,7 @@ struct Few {
       }
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
-        const int w = c / 2;
-        const uint4 u = make_uint4(__builtin_amdgcn_perm(vr[1][w], vr[0][w], sel), __builtin_amdgcn_perm(vr[3][w], vr[2][w], sel),
-                                   __builtin_amdgcn_perm(vr[5][w], vr[4][w], sel), __builtin_amdgcn_perm(vr[7][w], vr[6][w], sel));
-        const bf16x8 av = __builtin_bit_cast(bf16x8, u);
+        const bf16x8 av = column(vr, c);
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
           o[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, hi[r], o[r][c], 0, 0, 0);
@@ -302,6 +349,7 @@ struct Few {
 // waves and 256 rows a workgroup (274 us for 276), three tiles ahead (the same).
 typedef float f32x16 __attribute__((__vector_size__(64)));
 typedef short s16x4 __attribute__((__vector_size__(8)));
+typedef uint32_t u32x4 __attribute__((__vector_size__(16)));
 typedef TOPK_LDS s16x4 lds_s16x4;
 
 // the larger of x and what the lane 32 away holds
@@ -406,7 +454,7 @@ struct Wide {
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      float low = INFINITY;  // the tile's lowest score (masked keys' included: they only choose the exponential below)
+      float low = INFINITY;  // the tile's lowest score (masked keys' included, NaN too: they only choose the pass below)
 #pragma unroll
       for (int v = 0; v < 32; v += 2)
         low = __builtin_elementwise_minimum(__builtin_elementwise_minimum(low, s[v >> 4][v & 15]), s[v >> 4][(v & 15) + 1]);
@@ -442,7 +490,7 @@ struct Wide {
       };
       // Weights below 2^-126, which the exponential instruction alone makes 0, are added by themselves
       // where the tile has any.
-      if (__builtin_amdgcn_ballot_w64(fmaf(low, a.c, -off) < -126.f)) {
+      if (__builtin_amdgcn_ballot_w64(!(fmaf(low, a.c, -off) >= -126.f))) {
         float bias = -off;
         asm volatile("" : "+v"(bias));  // (nothing of this pass is held for the other)
 #pragma unroll
@@ -506,9 +554,50 @@ struct Wide {
       ready(t + 1, sh.b0, sh.b2);
       if (work) tile(std::false_type{}, t + 1, sh.b1, sh.b3);
     }
+    // Where rows of the workgroup do not see all its keys, values that are not finite go only to the rows that
+    // see theirs, which become NaN there; the others would meet them as 0 times NaN. Each wave looks at its part
+    // of the tile.
+    const bool hides = part && a.p.causal && all_see < keys;
+    auto own_part = [&](unsigned char* vb, int j) { return (TOPK_LDS u32x4*)&vb[(wave * LPW + j) * 1024 + lane * 16]; };
     for (; t < tiles; ++t) {
       const bool odd = t & 1;
+      unsigned char* vb = odd ? sh.b3 : sh.b2;
+      if (hides) {
+        __builtin_amdgcn_s_waitcnt(WAIT_VM0);
+        uint32_t bad = 0;
+#pragma unroll
+        for (int j = 0; j < LPW; ++j) {
+          const u32x4 x = *own_part(vb, j);
+          bad |= not_finite(x[0]) | not_finite(x[1]) | not_finite(x[2]) | not_finite(x[3]);
+        }
+        const bool any = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
+        if (lane == 0) sh.ml[wave][t & 1].x = any ? 1.f : 0.f;  // (read before the next barrier; the next tile's is another)
+      }
       ready(t, odd ? sh.b0 : sh.b1, odd ? sh.b2 : sh.b3);
+      if (hides && sh.ml[0][t & 1].x + sh.ml[1][t & 1].x + sh.ml[2][t & 1].x + sh.ml[3][t & 1].x > 0.f) {
+#pragma unroll 1
+        for (int j = 0; j < KEYS; ++j) {
+          const bool sees = j < seen - t * KEYS;
+#pragma unroll
+          for (int f = 0; f < FB; ++f)
+#pragma unroll
+            for (int v = 0; v < 16; v += 4) {
+              const TOPK_LDS uint32_t* x = (const TOPK_LDS uint32_t*)&vb[j * 2 * D + ((4 * f + v / 4) ^ swz_v(j)) * 16 + 8 * half];
+#pragma unroll
+              for (int w = 0; w < 4; ++w)
+                if (sees && (not_finite(x[w / 2]) >> 16 * (w & 1) & 1)) o[f][v + w] = NAN;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < LPW; ++j) {
+          u32x4 x = *own_part(vb, j);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) x[w] &= ~(not_finite(x[w]) * 0xFFFFu);
+          *own_part(vb, j) = x;
+        }
+        __syncthreads();
+      }
       if (work) tile(std::true_type{}, t, odd ? sh.b1 : sh.b0, odd ? sh.b3 : sh.b2);
     }
     }
@@ -695,8 +784,7 @@ __global__ __launch_bounds__(NT) void k_prefix_join(PrefixArgs a) {
 #pragma unroll 4
     for (int s = q; s < splits; s += Q) {
       const float f = fac[rl][s];
-      const f32x4 x = *(const f32x4*)(p + (int64_t)s * a.pl.rows * D);
-      if (f != 0.f) sum += x * f;  // (a range without keys leaves zeros)
+      sum += *(const f32x4*)(p + (int64_t)s * a.pl.rows * D) * f;  // (a range without keys leaves zeros)
     }
   }
   if (Q > 1) {
@@ -769,13 +857,14 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
         pl.pkeys = std::max<int64_t>(range, 64);
       }
     }
+    pl.pkeys = std::min(pl.pkeys, RANGE_MAX);
     pl.splits = std::max<int64_t>(1, cdiv(keys, pl.pkeys));
     return pl;
   }
   // ranges of equal length, as many as give two workgroups a CU, of 128 keys at least (64 requests behind
   // 8192 keys: 37 us; one and a half a CU 42, four 48)
   const int64_t keys = pp.Hkv * pl.ptiles * pp.P + pp.B * pp.Hkv * pl.stiles * pp.S;
-  const int64_t range = std::max(std::max<int64_t>(128, cdiv(cdiv(keys, 512), 128) * 128), least);
+  const int64_t range = std::min(std::max(std::max<int64_t>(128, cdiv(cdiv(keys, 512), 128) * 128), least), RANGE_MAX);
   pl.psplits = cdiv(pp.P, range);
   pl.ssplits = cdiv(pp.S, range);
   pl.pkeys = pl.psplits ? cdiv(cdiv(pp.P, pl.psplits), 128) * 128 : 128;

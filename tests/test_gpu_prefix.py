@@ -394,3 +394,53 @@ def test_training_step_captured_and_replayed():
         got = [t.clone() for t in held]
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, step())), f"replay {rep}"
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Lq", [2, 5, 10, 40, 128])
+def test_values_that_are_not_finite_reach_only_rows_that_see_them(Lq, d):
+    """2 to 512 rows a request: each form, one list of keys and two."""
+    q, pk, pv, k, v = _inputs(2, 8, 2, Lq, 300, 200, d, seed=14)
+    lengths = [200, Lq + 3]
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    at = {(0, 199, 3): math.nan, (0, 198, d - 1): math.inf, (1, 5, 17): -math.inf, (1, 0, 40): math.nan}
+    for (b, j, c) in at:
+        v[b, 1, j, c] = 0
+    want = tk.attn_prefix(q, pk, pv, k, v, n)
+    for (b, j, c), x in at.items():
+        v[b, 1, j, c] = x
+    got = tk.attn_prefix(q, pk, pv, k, v, n)
+    met = torch.zeros(want.shape, dtype=torch.bool, device="cuda")
+    for b, j, c in at:
+        first = max(0, j - (lengths[b] - Lq))  # query that sees key j
+        met[b, 4:, first:, c] = True
+    assert 0 < int(met.sum()) < met.numel() // 8
+    assert not bool(got[met].isfinite().any())
+    assert torch.equal(got[~met], want[~met])
+
+
+@pytest.mark.parametrize("Lq", [4, 40, 128])
+def test_tiny_weights_do_not_depend_on_what_is_not_seen(Lq):
+    """Weights of 2^-130 beside keys of NaN, behind the length and after a query's place."""
+    z = lambda *s: torch.zeros(1, 1, *s, device="cuda")  # noqa: E731
+    q, k, v = z(Lq, 64), z(200, 64), z(200, 64)
+    q[..., 0] = 1
+    k[..., 0] = -90.0 * 8
+    k[0, 0, 3, 0] = 0
+    v[0, 0, 4:] = 2.0 ** 120
+    q, k, v = q.to(BF16), k.to(BF16), v.to(BF16)
+    n = torch.tensor([150], dtype=torch.int32, device="cuda")
+    want = tk.attn_prefix(q, None, None, k, v, n, scale=0.125)
+    assert float(want.min()) > 0
+    hidden = min(8, Lq - 1)
+    k[:, :, 150 - hidden:], v[:, :, 150 - hidden:] = math.nan, math.nan
+    got = tk.attn_prefix(q, None, None, k, v, n, scale=0.125)
+    assert torch.equal(got[:, :, :Lq - hidden], want[:, :, :Lq - hidden])
+    assert bool(got[:, :, Lq - hidden:].isnan().all())
+
+
+def test_strides_that_lead_nowhere_may_be_any():
+    for B, Hkv, P, S in ((1, 1, 1, 1), (2, 1, 1, 9), (1, 2, 30, 1), (3, 2, 1, 1)):
+        q, pk, pv, k, v = _inputs(B, 2 * Hkv, Hkv, 1, P, S, 64, seed=15)
+        odd = lambda t: t.as_strided(t.shape, [st if n > 1 else 7 for n, st in zip(t.shape[:-1], t.stride())] + [1])  # noqa: E731
+        assert torch.equal(tk.attn_prefix(q, odd(pk), odd(pv), odd(k), odd(v)), tk.attn_prefix(q, pk, pv, k, v))
