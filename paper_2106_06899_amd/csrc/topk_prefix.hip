@@ -18,8 +18,8 @@
 // instructions, which this chip runs side by side at falling clocks: 4 requests of 512 tokens, 16
 // heads of 128 on 4 key heads behind 16384 keys, 269 us with the join, 1.04 PFLOP/s (a large
 // library matrix product: 1.38). Short calls are bound by launches and latency, and by the partial
-// results: 64 requests behind 8192 keys, 32 heads of 128 on 8, 30 + 5 us, of which writing and
-// reading 33 MB of them takes about ten.
+// results, whose join is a launch of its own: 64 requests behind 8192 keys, 32 heads of 128 on 8, 32 +
+// 5 us, where the bytes would take 23.
 //
 // Few rows. Four waves take key tiles of 32 in turn, each with a running softmax of its own, joined
 // through LDS at the end. Scores are S^T = K Q^T and the output O^T = V^T P^T by
@@ -39,6 +39,8 @@
 
 namespace topk {
 namespace {
+
+int64_t cdiv(int64_t x, int64_t y) { return (x + y - 1) / y; }
 
 constexpr int NT = 256, WAVES = 4, KT = 32;
 constexpr int JOIN_MAX = 1024;  // key ranges of a row at most,
@@ -808,8 +810,6 @@ __global__ __launch_bounds__(NT) void k_prefix_join(PrefixArgs a) {
   if (a.p.lse && c == 0) a.p.lse[row] = row_log(top, total);
 }
 
-int64_t cdiv(int64_t x, int64_t y) { return (x + y - 1) / y; }
-
 PrefixArgs args_for(const PrefixProblem& pp, const PrefixPlan& pl, const void* ws) {
   PrefixArgs a;
   a.p = pp;
@@ -826,6 +826,15 @@ PrefixArgs args_for(const PrefixProblem& pp, const PrefixPlan& pl, const void* w
 // against such caches 45 and 57.
 int form_for(int64_t rows, int wide) { return rows <= 16 ? 1 : rows <= 32 ? 2 : wide; }
 int tile_rows(int form) { return form >= 8 ? 128 : 16 * form; }
+// Microseconds of `items` wide tiles of 128 rows against `keys` keys each: as many layers on 256 CUs as it
+// takes, a step of 64 keys in 1.05 us (d = 128) times the workgroups that share a CU, 1.25 alone (d = 64
+// leaves room for a third: 1.65 for two).
+double wide_us(int d, bool two, int64_t items, int64_t keys) {
+  const int64_t layers = cdiv(items, 256);
+  const double step = (d == 64 ? 0.7 : 1.05) * (two ? 1.3 : 1.0);
+  return (layers == 1 ? 1.25 : layers == 2 && d == 64 ? 1.65 : (double)layers) * step * (keys / 64.0 + 3);
+}
+constexpr double JOIN_US = 2e-6;  // of a partial result's number, written and read
 
 }  // namespace
 
@@ -845,13 +854,11 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
   pl.both = pl.sform == 9 && pl.stiles * 128 * 8 <= pl.req_rows * 9;
   if (pl.both) {
     const int64_t items = pp.Hkv * pp.B * pl.stiles, keys = pp.P + pp.S;
-    // as many ranges as finish soonest: layers of workgroups over 256 CUs, each tile of 64 keys in 1.05 us
-    // (d = 128) where two share a CU, and the join's traffic
+    // as many ranges as finish soonest, the join's traffic included
     double best = 0;
     for (int64_t s = 1; s <= JOIN_FEW && (s == 1 || cdiv(keys, s) >= 128); ++s) {
-      const int64_t layers = cdiv(items * s, 256), range = std::max(least, cdiv(cdiv(keys, s), 64) * 64);
-      const double tile = pp.d == 64 ? 0.7 : 1.05;
-      const double us = (layers == 1 ? 1.25 : (double)layers) * tile * (range / 64.0 + 3) + (s > 1 ? 4 + s * pl.rows * pp.d * 2e-6 : 0);
+      const int64_t range = std::max(least, cdiv(cdiv(keys, s), 64) * 64);
+      const double us = wide_us(pp.d, false, items * s, range) + (s > 1 ? 4 + s * pl.rows * pp.d * JOIN_US : 0);
       if (s == 1 || us < best) {
         best = us;
         pl.pkeys = std::max<int64_t>(range, 64);
@@ -861,12 +868,30 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
     pl.splits = std::max<int64_t>(1, cdiv(keys, pl.pkeys));
     return pl;
   }
-  // ranges of equal length, as many as give two workgroups a CU, of 128 keys at least (64 requests behind
-  // 8192 keys: 37 us; one and a half a CU 42, four 48)
+  // ranges of equal length, as many as give two workgroups a CU, of 128 keys at least (4 requests behind 500
+  // keys: 8.6 us, 9.5 with 256 at least)
   const int64_t keys = pp.Hkv * pl.ptiles * pp.P + pp.B * pp.Hkv * pl.stiles * pp.S;
   const int64_t range = std::min(std::max(std::max<int64_t>(128, cdiv(cdiv(keys, 512), 128) * 128), least), RANGE_MAX);
   pl.psplits = cdiv(pp.P, range);
   pl.ssplits = cdiv(pp.S, range);
+  if (pl.pform >= 8 && pl.sform < 8) {
+    // Wide tiles on the prefix beside few rows on the caches: as many ranges as finish soonest beside the
+    // caches' reads (of which the lengths may leave about 0.6), the join's traffic included: 64 requests
+    // behind 8192 keys without caches 27 us, 31 with equal ranges; 128 behind 4096 with caches of 2048, 8 key
+    // heads of 128: 130 and 142.
+    const double own = pp.B * pp.Hkv * pp.S * pp.d * 4 * 0.6 / 5e6;
+    double best = 0;
+    for (int64_t s = 1; s <= JOIN_MAX / 2 && (s == 1 || cdiv(pp.P, s) >= 128); s += std::max<int64_t>(1, s / 8)) {
+      const int64_t part = std::max(cdiv(cdiv(pp.P, s), 128) * 128, least), n = cdiv(pp.P, part);
+      const double wide_t = wide_us(pp.d, wide == 8, pp.Hkv * pl.ptiles * n, part);
+      const double us = std::max(wide_t, own) + 0.25 * std::min(wide_t, own) + n * pl.rows * pp.d * JOIN_US;
+      if (best == 0 || us < best) {
+        best = us;
+        pl.psplits = n;
+      }
+    }
+    pl.psplits = std::max(pl.psplits, cdiv(pp.P, RANGE_MAX));
+  }
   pl.pkeys = pl.psplits ? cdiv(cdiv(pp.P, pl.psplits), 128) * 128 : 128;
   pl.skeys = pl.ssplits ? cdiv(cdiv(pp.S, pl.ssplits), 128) * 128 : 128;
   pl.psplits = cdiv(pp.P, pl.pkeys);
