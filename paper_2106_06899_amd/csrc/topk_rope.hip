@@ -21,8 +21,9 @@
 //
 // Measured (a device copy reaches 4.94 TB/s): 4 x 8192 tokens of 16 + 16 + 16 heads of 128, bf16,
 // 169 us (4.8 TB/s); rotation of 2 x 16 heads of 8192 tokens, three axes, 29 us (4.6 TB/s); 8 x 512
-// tokens of 12 + 12 + 12 heads of 64, where latency counts, 11 us forward (3.4 TB/s), 19 + 4 us
-// backward. With the angles formed by each lane for itself, one head at a time: 188, 30, 16, 31 + 9.
+// tokens of 12 + 12 + 12 heads of 64, where latency counts, 11 us forward (3.4 TB/s), 16 + 4 us
+// backward (4 x 8192: 91 + 5, 5.0 TB/s). With the angles formed by each lane for itself, one head at a
+// time: 188, 30, 16, 31 + 9.
 #include "topk_device.h"
 #include "topk_heads.h"
 
@@ -435,8 +436,10 @@ Grid grid_for(const HeadsProblem& hp, int vec) {
   return g;
 }
 int backward_blocks(const Grid& g) {
-  // each walks over as many tiles as the next, and as leaves about WGS workgroups
-  const int64_t y = g.ny[0] + g.ny[1] + g.ny[2], each = std::max<int64_t>(1, g.tiles * y / WGS);
+  // each walks over as many tiles as the next, and as leaves 4096 workgroups: parts differ in heads, and values
+  // take less (2 x 8192 tokens of 48 heads of 128, 32 of them queries: 127 us, 186 with 1024, 230 with 768; 2 x 1511
+  // of 8 heads of 96 in fp32: 13.4, 12.0 with 1024)
+  const int64_t y = g.ny[0] + g.ny[1] + g.ny[2], each = std::max<int64_t>(1, g.tiles * y / 4096);
   return (int)((g.tiles + each - 1) / each);
 }
 
