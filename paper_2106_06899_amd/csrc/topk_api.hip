@@ -1352,8 +1352,8 @@ int topk_attn_prefix(const void* Q, const void* prefix_K, const void* prefix_V, 
   PrefixProblem pp;
   int rc = prefix_shape(&pp, B, H, Hkv, Lq, P, S, d, causal, scale, dtype);
   if (rc) return rc;
-  topk_prefix_strides t =
-      strides ? *strides : topk_prefix_strides{P * d, d, P * d, d, Hkv * S * d, S * d, d, Hkv * S * d, S * d, d};
+  const int64_t cache = S && Hkv > STRIDE_MAX / (S * d) ? STRIDE_MAX : Hkv * S * d;
+  topk_prefix_strides t = strides ? *strides : topk_prefix_strides{P * d, d, P * d, d, cache, S * d, d, cache, S * d, d};
   // (a stride that leads nowhere may be any)
   if (B == 1) t.k_batch = t.v_batch = 0;
   if (Hkv == 1) t.prefix_k_head = t.prefix_v_head = t.k_head = t.v_head = 0;

@@ -879,7 +879,7 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
     // caches' reads (of which the lengths may leave about 0.6), the join's traffic included: 64 requests
     // behind 8192 keys without caches 27 us, 31 with equal ranges; 128 behind 4096 with caches of 2048, 8 key
     // heads of 128: 130 and 142.
-    const double own = pp.B * pp.Hkv * pp.S * pp.d * 4 * 0.6 / 5e6;
+    const double own = (double)pp.S * pp.B * pp.Hkv * pp.d * 4 * 0.6 / 5e6;
     double best = 0;
     for (int64_t s = 1; s <= JOIN_MAX / 2 && (s == 1 || cdiv(pp.P, s) >= 128); s += std::max<int64_t>(1, s / 8)) {
       const int64_t part = std::max(cdiv(cdiv(pp.P, s), 128) * 128, least), n = cdiv(pp.P, part);
