@@ -16,10 +16,10 @@
 // reading them: 8 requests behind 65536 keys, 16 heads of 128, read 571 MB in 98 us (5.8 TB/s; a
 // device copy: 4.94). Wide (128 rows) goes through LDS and is bound by matrix and vector
 // instructions, which this chip runs side by side at falling clocks: 4 requests of 512 tokens, 16
-// heads of 128 on 4 key heads behind 16384 keys, 269 us with the join, 1.04 PFLOP/s (a large
+// heads of 128 on 4 key heads behind 16384 keys, 273 us with the join, 1.02 PFLOP/s (a large
 // library matrix product: 1.38). Short calls are bound by launches and latency, and by the partial
-// results, whose join is a launch of its own: 64 requests behind 8192 keys, 32 heads of 128 on 8, 32 +
-// 5 us, where the bytes would take 23.
+// results, whose join is a launch of its own: 64 requests behind 8192 keys, 32 heads of 128 on 8, 28 +
+// 6 us, where the bytes would take 23. Calls with few keys in all take one range instead.
 //
 // Few rows. Four waves take key tiles of 32 in turn, each with a running softmax of its own, joined
 // through LDS at the end. Scores are S^T = K Q^T and the output O^T = V^T P^T by
@@ -102,8 +102,9 @@ struct Lds {
   }
 };
 
-// 16 NR rows: the waves take key tiles in turn, K and V in registers.
-template <int D, int NR>
+// 16 NR rows: the waves take key tiles in turn, K and V in registers. BOTH: of the prefix and of the request's
+// own keys, as one list.
+template <int D, int NR, bool BOTH>
 struct Few {
   static constexpr int NS = D / 32;  // steps over the features of the scores
   static constexpr int NC = D / 16;  // blocks of 16 output features; columns of V a lane reads
@@ -121,24 +122,18 @@ struct Few {
   static __device__ __forceinline__ void run(const PrefixArgs& a, const Item& it, const Lds& sh) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, g = lane >> 4;
     const int R = (int)a.pl.req_rows, Lq = (int)a.p.Lq;
-    const Span sp = it.b >= 0 ? it.own : it.prefix;
-    const bool causal = it.b >= 0 && a.p.causal;
     auto place = [&](int i) {  // of row i in q and out
       const int b = it.b >= 0 ? it.b : i / R;
       return b * a.p.H * Lq + it.h * R + (it.b >= 0 ? i : i - b * R);
     };
-    // how many keys the lane's rows see
-    int seen[NR];
+    auto lane_row = [&](int r) { return it.r0 + 16 * r + n < it.count ? it.r0 + 16 * r + n : it.r0; };
     bf16x8 bq[NR][NS];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-      const int i = it.r0 + 16 * r + n < it.count ? it.r0 + 16 * r + n : it.r0;
-      seen[r] = causal ? min(sp.n, sp.before + i % Lq) : sp.n;
-      const uint16_t* q = (const uint16_t*)a.p.q + place(i) * D + 8 * g;
+      const uint16_t* q = (const uint16_t*)a.p.q + place(lane_row(r)) * D + 8 * g;
 #pragma unroll
       for (int s = 0; s < NS; ++s) bq[r][s] = *(const bf16x8*)(q + 32 * s);
     }
-    const int all_see = causal ? min(sp.n, sp.before) : sp.n;  // keys before this are seen by every row
 
     f32x4 o[NR][NC];
     float m[NR], l[NR];
@@ -149,6 +144,19 @@ struct Few {
 #pragma unroll
       for (int c = 0; c < NC; ++c) o[r][c] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
+
+    int turn = wave;  // the wave's next tile
+    // (code of its own for each part is faster, 5.1 us for 5.6 with 100 + 60 keys, where registers last)
+    constexpr int COPIES = D * NR > 128 ? 1 : 2;
+#pragma unroll COPIES
+    for (int part = 0; part < (BOTH ? 2 : 1); ++part) {
+    const Span sp = (BOTH ? part == 1 : it.b >= 0) ? it.own : it.prefix;
+    const bool causal = (BOTH ? part == 1 : it.b >= 0) && a.p.causal;
+    // how many keys the lane's rows see; keys before all_see are seen by every row
+    int seen[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) seen[r] = causal ? min(sp.n, sp.before + lane_row(r) % Lq) : sp.n;
+    const int all_see = causal ? min(sp.n, sp.before) : sp.n;
 
     bf16x8 kr[2][NS];
     uint32_t vr[8][NC / 2];
@@ -173,7 +181,7 @@ struct Few {
         __builtin_memcpy(vr[e], __builtin_assume_aligned(p + off, VB), VB);
       }
     };
-    int t = wave;
+    int t = turn;
     if (t < tiles) {
       load_k(t);
       load_v(t);
@@ -276,6 +284,8 @@ struct Few {
         }
       }
       if (t + WAVES < tiles) load_v(t + WAVES);
+    }
+    turn = t - tiles;
     }
 
     // join the waves: every row's maximum and sum, then the scaled outputs through LDS, in parts of four
@@ -637,16 +647,16 @@ struct Wide {
 
 // A form by its number: 1 and 2 few rows (blocks of 16), 8 and 9 the wide one (with weights as two
 // numbers, as one).
-template <int D, int NB>
+template <int D, int NB, bool BOTH = false>
 struct Form {
-  typedef Few<D, NB> type;
+  typedef Few<D, NB, BOTH> type;
 };
-template <int D>
-struct Form<D, 8> {
+template <int D, bool BOTH>
+struct Form<D, 8, BOTH> {
   typedef Wide<D, true> type;
 };
-template <int D>
-struct Form<D, 9> {
+template <int D, bool BOTH>
+struct Form<D, 9, BOTH> {
   typedef Wide<D, false> type;
 };
 
@@ -702,11 +712,12 @@ __global__ __launch_bounds__(NT, 2) void k_prefix(PrefixArgs a) {
     it.split = rest2 % splits;
     it.h = rest2 / splits;
     it.count = (int)pl.req_rows;
-    it.r0 = tile * Form<D, NBS>::type::TILE;
+    typedef typename Form<D, NBS, true>::type F;
+    it.r0 = tile * F::TILE;
     const int64_t k0 = it.split * pl.pkeys;
     it.prefix = prefix_span(a, it.h, k0, k0 + pl.pkeys);
     it.own = own_span(a, it.b, it.h, k0 - a.p.P, k0 + pl.pkeys - a.p.P);
-    Form<D, NBS>::type::run(a, it, sh);
+    F::run(a, it, sh);
     return;
   }
   const int np = Hkv * psplits * ptiles;
@@ -834,6 +845,7 @@ double wide_us(int d, bool two, int64_t items, int64_t keys) {
   const double step = (d == 64 ? 0.7 : 1.05) * (two ? 1.3 : 1.0);
   return (layers == 1 ? 1.25 : layers == 2 && d == 64 ? 1.65 : (double)layers) * step * (keys / 64.0 + 3);
 }
+constexpr int64_t ONE_ITEMS = 512, ONE_KEYS = 1024;  // requests and key heads, keys of 64 features, of calls in one range
 constexpr double JOIN_US = 2e-6;  // of a partial result's number, written and read
 
 }  // namespace
@@ -849,6 +861,16 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
   pl.stiles = cdiv(pl.req_rows, tile_rows(pl.sform));
   // (many rows are joined several a workgroup, from few ranges)
   const int64_t longest = std::max(pp.P, pp.S), least = cdiv(longest, (pl.rows > 1 << 20 ? JOIN_FEW : JOIN_MAX) / 2 * 128) * 128;
+  // Few rows and few keys: one workgroup a request and key head takes all its keys, and nothing is left to join.
+  // (12 heads of 64, 4 requests, 500 + 130 keys: 7.8 us either way, 700 + 300: 9.3 and 8.1, but a launch less for
+  // the host, 5 us; 32 heads on 8, 16 requests, 500 + 130: 8.0 and 13.0, at d = 128 with 1000 + 500 22 and 17; 64
+  // requests of d = 64 with 700 + 300 16.4 and 15.7, 128 with 400 + 100 16.7 and 14.3.)
+  if (pl.sform < 8 && pp.B * pp.Hkv <= ONE_ITEMS && pp.P + pp.S > 0 && (pp.P + pp.S) * pp.d <= ONE_KEYS * 64) {
+    pl.both = true;
+    pl.pkeys = pp.P + pp.S;
+    pl.splits = 1;
+    return pl;
+  }
   // one list of prefix and own keys, unless more than an eighth of a tile's rows would be idle on the prefix
   // (4 x 512 tokens: 277 us, 286 in two lists; 8 requests of 80 rows, of 128: 24.6 us, 21.0 in two lists)
   pl.both = pl.sform == 9 && pl.stiles * 128 * 8 <= pl.req_rows * 9;
@@ -907,7 +929,9 @@ size_t prefix_bytes(const PrefixProblem& pp, const PrefixPlan& pl) {
 template <int D>
 static void launch_d(const PrefixArgs& a, unsigned grid, hipStream_t st) {
   const int np = a.pl.pform, ns = a.pl.sform;
-  if (a.pl.both) k_prefix<D, 9, 9, true><<<grid, NT, 0, st>>>(a);
+  if (a.pl.both && ns == 1) k_prefix<D, 1, 1, true><<<grid, NT, 0, st>>>(a);
+  else if (a.pl.both && ns == 2) k_prefix<D, 2, 2, true><<<grid, NT, 0, st>>>(a);
+  else if (a.pl.both) k_prefix<D, 9, 9, true><<<grid, NT, 0, st>>>(a);
   else if (np == 1) k_prefix<D, 1, 1, false><<<grid, NT, 0, st>>>(a);
   else if (np == 2 && ns == 1) k_prefix<D, 2, 1, false><<<grid, NT, 0, st>>>(a);
   else if (np == 2) k_prefix<D, 2, 2, false><<<grid, NT, 0, st>>>(a);

@@ -219,11 +219,11 @@ def test_refusals_of_the_binding():
 
 def test_small_registered_workspace_is_refused():
     import ctypes
-    q, pk, pv, k, v = _inputs(2, 2, 2, 1, 90, 40, 64)
+    q, pk, pv, k, v = _inputs(2, 2, 2, 1, 2000, 40, 64)
     out, ws, L = torch.empty_like(q), torch.empty(1024, dtype=torch.uint8, device="cuda"), tk.lib()
-    need = tk.attn_prefix_workspace_bytes(2, 2, 2, 1, 90, 40, 64)
+    need = tk.attn_prefix_workspace_bytes(2, 2, 2, 1, 2000, 40, 64)
     assert need > 1024
-    args = [t.data_ptr() for t in (q, pk, pv, k, v)] + [None, out.data_ptr(), None, 2, 2, 2, 1, 90, 40, 64, None, 1, 0.125, 1, None]
+    args = [t.data_ptr() for t in (q, pk, pv, k, v)] + [None, out.data_ptr(), None, 2, 2, 2, 1, 2000, 40, 64, None, 1, 0.125, 1, None]
     try:
         assert L.topk_set_workspace(ctypes.c_void_p(ws.data_ptr()), 1024) == 0
         assert L.topk_attn_prefix(*args) == -5
@@ -444,3 +444,17 @@ def test_strides_that_lead_nowhere_may_be_any():
         q, pk, pv, k, v = _inputs(B, 2 * Hkv, Hkv, 1, P, S, 64, seed=15)
         odd = lambda t: t.as_strided(t.shape, [st if n > 1 else 7 for n, st in zip(t.shape[:-1], t.stride())] + [1])  # noqa: E731
         assert torch.equal(tk.attn_prefix(q, odd(pk), odd(pv), odd(k), odd(v)), tk.attn_prefix(q, pk, pv, k, v))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,G,Lq", [(5, 1, 1), (5, 4, 4), (3, 5, 5)])
+def test_calls_in_one_range_and_in_several(B, G, Lq, d):
+    """Up to 65536 / d keys in all are taken by one workgroup (without workspace), more in ranges; rows
+    of 1, 16 and 25; keys split anyhow between prefix and caches."""
+    n = 65536 // d
+    for P, S in ((n - 1, 1), (n - 33, 33), (1, n - 1), (n, 0), (0, n), (n - 32, 33), (n + 1, 0), (37, n)):
+        q, pk, pv, k, v = _inputs(B, 2 * G, 2, Lq, P, S, d, seed=16)
+        assert (tk.attn_prefix_workspace_bytes(B, 2 * G, 2, Lq, P, S, d) == 0) == (P + S <= n)
+        for lengths in (None, torch.randint(-2, S + 3, (B,), generator=torch.Generator().manual_seed(S)).to(torch.int32).cuda()):
+            out, lse = tk.attn_prefix(q, pk, pv, k, v, lengths, lse=True)
+            _check(q, pk, pv, k, v, lengths, True, 1 / math.sqrt(d), out, lse)
