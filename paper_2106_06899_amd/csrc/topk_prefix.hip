@@ -838,12 +838,14 @@ PrefixArgs args_for(const PrefixProblem& pp, const PrefixPlan& pl, const void* w
 int form_for(int64_t rows, int wide) { return rows <= 16 ? 1 : rows <= 32 ? 2 : wide; }
 int tile_rows(int form) { return form >= 8 ? 128 : 16 * form; }
 // Microseconds of `items` wide tiles of 128 rows against `keys` keys each: as many layers on 256 CUs as it
-// takes, a step of 64 keys in 1.05 us (d = 128) times the workgroups that share a CU, 1.25 alone (d = 64
-// leaves room for a third: 1.65 for two).
-double wide_us(int d, bool two, int64_t items, int64_t keys) {
+// takes, a step of 64 keys in 1.05 us (d = 128) times the workgroups that share a CU; 1.25 alone, 1.45 where
+// hundreds of caches' workgroups (crowded) find no CU free of them, and 1.65 for two whose registers or weights as
+// two numbers leave the units idle.
+double wide_us(int d, bool two, bool crowded, int64_t items, int64_t keys) {
   const int64_t layers = cdiv(items, 256);
   const double step = (d == 64 ? 0.7 : 1.05) * (two ? 1.3 : 1.0);
-  return (layers == 1 ? 1.25 : layers == 2 && d == 64 ? 1.65 : (double)layers) * step * (keys / 64.0 + 3);
+  const double share = layers == 1 ? (crowded && items > 208 ? 1.45 : 1.25) : layers == 2 && (two || d == 64) ? 1.65 : (double)layers;
+  return share * step * (keys / 64.0 + 3);
 }
 constexpr int64_t ONE_ITEMS = 512, ONE_KEYS = 1024;  // requests and key heads, keys of 64 features, of calls in one range
 constexpr double JOIN_US = 2e-6;  // of a partial result's number, written and read
@@ -880,7 +882,7 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
     double best = 0;
     for (int64_t s = 1; s <= JOIN_FEW && (s == 1 || cdiv(keys, s) >= 128); ++s) {
       const int64_t range = std::max(least, cdiv(cdiv(keys, s), 64) * 64);
-      const double us = wide_us(pp.d, false, items * s, range) + (s > 1 ? 4 + s * pl.rows * pp.d * JOIN_US : 0);
+      const double us = wide_us(pp.d, false, false, items * s, range) + (s > 1 ? 4 + s * pl.rows * pp.d * JOIN_US : 0);
       if (s == 1 || us < best) {
         best = us;
         pl.pkeys = std::max<int64_t>(range, 64);
@@ -899,13 +901,13 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
   if (pl.pform >= 8 && pl.sform < 8) {
     // Wide tiles on the prefix beside few rows on the caches: as many ranges as finish soonest beside the
     // caches' reads (of which the lengths may leave about 0.6), the join's traffic included: 64 requests
-    // behind 8192 keys without caches 27 us, 31 with equal ranges; 128 behind 4096 with caches of 2048, 8 key
-    // heads of 128: 130 and 142.
+    // behind 8192 keys without caches 28 us, 32 with equal ranges; 128 behind 4096 with caches of 2048, 8 key
+    // heads of 128: 125 and 143; 256 behind 1000 with caches of 1000, 8 of 64: 66 and 64.
     const double own = (double)pp.S * pp.B * pp.Hkv * pp.d * 4 * 0.6 / 5e6;
     double best = 0;
     for (int64_t s = 1; s <= JOIN_MAX / 2 && (s == 1 || cdiv(pp.P, s) >= 128); s += std::max<int64_t>(1, s / 8)) {
       const int64_t part = std::max(cdiv(cdiv(pp.P, s), 128) * 128, least), n = cdiv(pp.P, part);
-      const double wide_t = wide_us(pp.d, wide == 8, pp.Hkv * pl.ptiles * n, part);
+      const double wide_t = wide_us(pp.d, wide == 8, pp.B * pp.Hkv >= 256, pp.Hkv * pl.ptiles * n, part);
       const double us = std::max(wide_t, own) + 0.25 * std::min(wide_t, own) + n * pl.rows * pp.d * JOIN_US;
       if (best == 0 || us < best) {
         best = us;
