@@ -414,7 +414,7 @@ size_t topk_qk_norm_rope_backward_workspace_bytes(int64_t B, int64_t L, int64_t 
  *   out        [B, H, Lq, d]   written; a row that sees no key is 0
  *   lse        NULL, or fp32 [B, H, Lq]: log sum_j exp(scale * s_j), -inf where no key is seen
  *
- * bf16 with d = 64 or 128, at most 2^27 query rows (else TOPK_E_UNSUPPORTED). Softmax
+ * bf16 with d = 64 or 128, at most 2^26 query rows (else TOPK_E_UNSUPPORTED). Softmax
  * statistics and sums in fp32, in a fixed order; a row is computed from its own numbers
  * alone (keys and values it does not see may be infinite or NaN; where it sees such a value
  * its output is infinite or NaN), and values up to 2^90 cannot overflow the sums.

@@ -890,7 +890,8 @@ int prefix_shape(PrefixProblem* pp, int64_t B, int64_t H, int64_t Hkv, int64_t L
   if (dtype != TOPK_BF16 || (d != 64 && d != 128))
     return fail(TOPK_E_UNSUPPORTED, "shared-prefix attention runs on bf16 inputs with d = 64 or 128");
   if (P > 0x7FFFFFFFLL || S > 0x7FFFFFFFLL) return fail(TOPK_E_UNSUPPORTED, "more than 2^31 - 1 keys");
-  if (H > (int64_t(1) << 27) / B || Lq > (int64_t(1) << 27) / (B * H)) return fail(TOPK_E_UNSUPPORTED, "more than 2^27 query rows");
+  // (the join's grid of eight rows a workgroup has to stay below 2^32 threads)
+  if (H > (int64_t(1) << 26) / B || Lq > (int64_t(1) << 26) / (B * H)) return fail(TOPK_E_UNSUPPORTED, "more than 2^26 query rows");
   pp->B = B;
   pp->H = H;
   pp->Hkv = Hkv;

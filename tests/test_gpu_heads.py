@@ -399,3 +399,15 @@ def test_gradient_of_empty_tokens_with_a_tiny_eps():
         ref = (grads[0][0, h] if h < H else grads[1][0, h - H])[2:4].double() * w.double() * eps ** -0.5
         _close(dx[0, 2:4, h * d:(h + 1) * d], ref, 20 * E * ref.abs(), f"head {h}")
     assert dx.isfinite().all() and dwq.isfinite().all() and dwk.isfinite().all()
+
+
+def test_more_tiles_than_a_grid_and_offsets_past_31_bits():
+    """2^22 + 5 tokens of 512 features: a workgroup takes a second tile of tokens, elements lie past 2^31."""
+    L, d = 2 ** 22 + 5, 512
+    x = torch.empty(1, 1, L, d, dtype=BF16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(31))
+    pos, f = torch.arange(L, device="cuda"), tk.rope_frequencies(d // 2)
+    y = tk.rope(x, pos, f)
+    for a, b in ((0, 9), (L // 2 - 3, L // 2 + 4), (2 ** 22 - 6, L)):
+        assert torch.equal(y[:, :, a:b], tk.rope(x[:, :, a:b], pos[a:b], f))
+    ref, size = _turn(x[:, :, -7:].double(), pos[None, None, -7:], f, (0,) * (d // 2), False)
+    _close(y[:, :, -7:], ref, 10 * E * size, "last rows")

@@ -136,3 +136,9 @@ def test_layer_options():
         layers.TopkMultiheadAttention(128, 2, 8, rope_sections=(8, 8))
     with pytest.raises(ValueError):
         layers.TopkMultiheadAttention(128, 2, 8).decode(*[torch.zeros(1, 1, 128)] * 6)
+
+
+@pytest.mark.parametrize("B,H,Lq", [(1, 1, (1 << 26) + 1), (1 << 26, 2, 1), (3, 1 << 25, 1)])
+def test_more_rows_than_a_launch_holds_are_refused(B, H, Lq):
+    assert _prefix(B=B, H=H, Hkv=1, Lq=Lq) == E_UNSUPPORTED
+    assert tk.attn_prefix_workspace_bytes(B, H, 1, Lq, 100, 10, 64) == 0
