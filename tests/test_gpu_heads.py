@@ -411,3 +411,16 @@ def test_more_tiles_than_a_grid_and_offsets_past_31_bits():
         assert torch.equal(y[:, :, a:b], tk.rope(x[:, :, a:b], pos[a:b], f))
     ref, size = _turn(x[:, :, -7:].double(), pos[None, None, -7:], f, (0,) * (d // 2), False)
     _close(y[:, :, -7:], ref, 10 * E * size, "last rows")
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("d,pairs", [(128, 64), (70, 11)])
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_rope_over_its_input(dt, d, pairs, adjacent):
+    """The C call with out = x, by whole accesses and by single elements."""
+    x = _randn(41, 2, 3, 301, d, dtype=dt)
+    pos, f = torch.arange(301, device="cuda") * 3, tk.rope_frequencies(pairs)
+    want = tk.rope(x, pos, f, adjacent=adjacent)
+    rot = tk._Rotation(pos.data_ptr(), f.data_ptr(), None, 2 * pairs, 0, 0, 1, 1, 8, int(adjacent), 0)
+    rc = tk.lib().topk_rope(x.data_ptr(), x.data_ptr(), 2, 3, 301, d, *x.stride()[:3], rot, int(dt is BF16), torch.cuda.current_stream().cuda_stream)
+    assert rc == 0 and torch.equal(x, want)
