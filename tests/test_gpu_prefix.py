@@ -458,3 +458,14 @@ def test_calls_in_one_range_and_in_several(B, G, Lq, d):
         for lengths in (None, torch.randint(-2, S + 3, (B,), generator=torch.Generator().manual_seed(S)).to(torch.int32).cuda()):
             out, lse = tk.attn_prefix(q, pk, pv, k, v, lengths, lse=True)
             _check(q, pk, pv, k, v, lengths, True, 1 / math.sqrt(d), out, lse)
+
+
+@pytest.mark.parametrize("name,B,H,Hkv,Lq,P,S,d", [("few_tiles", 1, 4, 2, 64, 9001, 64, 128), ("one_tile", 1, 1, 1, 128, 20000, 200, 64),
+                                                   ("thousands_of_rows", 1, 8, 1, 320, 30011, 320, 64)])
+def test_one_request_behind_a_long_prefix(name, B, H, Hkv, Lq, P, S, d):
+    """Few row tiles, whose one list of keys is cut into many ranges."""
+    q, pk, pv, k, v = _inputs(B, H, Hkv, Lq, P, S, d, seed=17)
+    assert tk.attn_prefix_workspace_bytes(B, H, Hkv, Lq, P, S, d) >= 10 * B * H * Lq * (d + 2) * 4
+    n = torch.tensor([S - 3], dtype=torch.int32, device="cuda")
+    out, lse = tk.attn_prefix(q, pk, pv, k, v, n, lse=True)
+    _check(q, pk, pv, k, v, n, True, 1 / math.sqrt(d), out, lse)
