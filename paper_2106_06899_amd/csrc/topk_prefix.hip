@@ -883,11 +883,11 @@ PrefixPlan prefix_plan(const PrefixProblem& pp) {
     double best = 0;
     const int64_t most = pl.rows > 1 << 20 ? JOIN_FEW : JOIN_MAX / 2;
     for (int64_t s = 1; s <= most && (s == 1 || cdiv(keys, s) >= 128); s += std::max<int64_t>(1, s / 8)) {
-      const int64_t range = std::max(least, cdiv(cdiv(keys, s), 64) * 64), n = std::max<int64_t>(1, cdiv(keys, range));
+      const int64_t range = std::max<int64_t>({64, least, cdiv(cdiv(keys, s), 64) * 64}), n = std::max<int64_t>(1, cdiv(keys, range));
       const double us = wide_us(pp.d, false, false, items * n, range) + (n > 1 ? 4 + n * pl.rows * pp.d * JOIN_US : 0);
       if (s == 1 || us < best) {
         best = us;
-        pl.pkeys = std::max<int64_t>(range, 64);
+        pl.pkeys = range;
       }
     }
     pl.pkeys = std::min(pl.pkeys, RANGE_MAX);

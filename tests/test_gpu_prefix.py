@@ -469,3 +469,13 @@ def test_one_request_behind_a_long_prefix(name, B, H, Hkv, Lq, P, S, d):
     n = torch.tensor([S - 3], dtype=torch.int32, device="cuda")
     out, lse = tk.attn_prefix(q, pk, pv, k, v, n, lse=True)
     _check(q, pk, pv, k, v, n, True, 1 / math.sqrt(d), out, lse)
+
+
+@pytest.mark.parametrize("Lq", [1, 20, 40, 80, 128])
+def test_no_keys_on_every_form(Lq):
+    q, pk, pv, k, v = _inputs(2, 2, 2, Lq, 0, 0, 64, seed=18)
+    out, lse = tk.attn_prefix(q, pk, pv, k, v, lse=True)
+    assert not out.any() and bool((lse == -math.inf).all())
+    _, _, _, k, v = _inputs(2, 2, 2, Lq, 0, 70, 64, seed=18)
+    out, lse = tk.attn_prefix(q, None, None, k, v, torch.zeros(2, dtype=torch.int32, device="cuda"), lse=True)
+    assert not out.any() and bool((lse == -math.inf).all())

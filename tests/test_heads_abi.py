@@ -142,3 +142,9 @@ def test_layer_options():
 def test_more_rows_than_a_launch_holds_are_refused(B, H, Lq):
     assert _prefix(B=B, H=H, Hkv=1, Lq=Lq) == E_UNSUPPORTED
     assert tk.attn_prefix_workspace_bytes(B, H, 1, Lq, 100, 10, 64) == 0
+
+
+@pytest.mark.parametrize("Lq", [1, 20, 40, 80, 128, 1024])
+def test_calls_without_keys_are_planned(Lq):
+    for d in (64, 128):
+        assert tk.attn_prefix_workspace_bytes(2, 2, 2, Lq, 0, 0, d) == 0
