@@ -150,7 +150,8 @@ __device__ __forceinline__ void lane_angles(const Rotation& r, const Lane<VEC, N
     }
 }
 
-// Rotates the lane's pairs by (co, si); features beyond the rotated ones have co = 1, si = 0.
+// Rotates the lane's pairs by (co, si). Chunks that are not rotated do not come here: x 1 - x' 0 is
+// NaN where x' is not finite.
 template <int VEC, bool ADJ>
 __device__ __forceinline__ void turn_pairs(float (&a)[VEC], float (&b)[VEC], const float (&co)[VEC], const float (&si)[VEC]) {
   float x[2 * VEC];
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(NT) void k_heads(HeadsProblem hp, Grid g) {
             a[j][e] *= r * wa[j][e];
             c[j][e] *= r * wb[j][e];
           }
-          turn_pairs<VEC, ADJ>(a[j], c[j], co[j], si[j]);
+          if (ln.turn[j]) turn_pairs<VEC, ADJ>(a[j], c[j], co[j], si[j]);
         }
       }
 #pragma unroll
@@ -321,7 +322,7 @@ __global__ __launch_bounds__(NT) void k_heads_backward(HeadsProblem hp, Grid g) 
         for (int j = 0; j < NC; ++j) {
           widen_vec(xa[j], rawx.a[j]);
           widen_vec(xb[j], rawx.b[j]);
-          turn_pairs<VEC, ADJ>(ma[j], mb[j], co[j], si[j]);  // (the launch asks for the opposite angles)
+          if (ln.turn[j]) turn_pairs<VEC, ADJ>(ma[j], mb[j], co[j], si[j]);  // (the launch asks for the opposite angles)
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
             sq = fmaf(xa[j][e], xa[j][e], fmaf(xb[j][e], xb[j][e], sq));

@@ -8,6 +8,8 @@ Tolerances, element by element, with e = 2^-24 (half a step of fp32):
   below 20 e relative, and as much again for the second sum of the backward pass;
 * weight gradients: N terms of the above in fp32, below (N + 40) e times the sum of their sizes.
 """
+import math
+
 import pytest
 import torch
 
@@ -424,3 +426,64 @@ def test_rope_over_its_input(dt, d, pairs, adjacent):
     rot = tk._Rotation(pos.data_ptr(), f.data_ptr(), None, 2 * pairs, 0, 0, 1, 1, 8, int(adjacent), 0)
     rc = tk.lib().topk_rope(x.data_ptr(), x.data_ptr(), 2, 3, 301, d, *x.stride()[:3], rot, int(dt is BF16), torch.cuda.current_stream().cuda_stream)
     assert rc == 0 and torch.equal(x, want)
+
+
+def _same(a, b):
+    """Equal, with the sign of zeros; NaN equals NaN."""
+    return bool((((a == b) & (a.signbit() == b.signbit())) | (a.isnan() & b.isnan())).all())
+
+
+PASSING = [(80, 20, False), (80, 20, True), (70, 11, False), (70, 11, True), (64, 0, False), (70, 0, False), (512, 128, False)]
+# features behind the rotated ones: places in (B, H, L) and what stands there
+ODD = {(0, 0, 0): math.inf, (1, 1, 4): -math.inf, (0, 1, 2): math.nan, (1, 0, 3): -0.0}
+
+
+def _spoil(t, first):
+    """t [B, h, L, d] with ODD in its features from `first` on (one each)."""
+    t = t.clone()
+    for i, (at, x) in enumerate(ODD.items()):
+        t[at[0], at[1] % t.shape[1], at[2], first + (5 * i) % (t.shape[-1] - first)] = x
+    return t
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("d,pairs,adjacent", PASSING)
+def test_features_that_are_not_rotated_stay_alone(dt, d, pairs, adjacent):
+    """What is infinite, NaN or minus zero behind the rotated features comes out as it went in, and meets
+    no other feature."""
+    x = _randn(100, 2, 2, 5, d, dtype=dt)
+    odd = _spoil(x, 2 * pairs)
+    pos, f = torch.arange(5, device="cuda") + 3, tk.rope_frequencies(pairs) if pairs else torch.zeros(0, dtype=torch.float64, device="cuda")
+    for inverse in (False, True):
+        y, plain = (tk.rope(t, pos, f, adjacent=adjacent, inverse=inverse) for t in (odd, x))
+        assert _same(y[..., 2 * pairs:], odd[..., 2 * pairs:])
+        assert torch.equal(y[..., :2 * pairs], plain[..., :2 * pairs])
+    # the packed form without a norm: the same numbers
+    rot = dict(positions=pos, freqs=f, adjacent=adjacent) if pairs else {}
+    packed = torch.cat((odd, x[:, :1].roll(1, 2), odd[:, 1:]), 1)
+    q, k, v = tk.qk_norm_rope(packed.transpose(1, 2).reshape(2, 5, 4 * d), 2, 1, norm=False, **rot)
+    assert _same(q, tk.rope(odd, pos, f, adjacent=adjacent)) and _same(v, odd[:, 1:])
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("d,pairs,adjacent", [p for p in PASSING if p[1]])
+def test_infinite_features_beside_a_norm(dt, d, pairs, adjacent):
+    """An infinite feature makes its head's root mean square infinite: it becomes NaN, the others 0. An
+    infinite gradient of a feature that is not rotated reaches the gradient of that feature's weight alone."""
+    rot = dict(positions=torch.arange(5, device="cuda") + 3, freqs=tk.rope_frequencies(pairs), adjacent=adjacent)
+    x = _randn(102, 2, 5, 4, d, dtype=dt)
+    w = _randn(103, d, dtype=dt, mean=1.0)
+    odd, at = x.clone(), 2 * pairs + 3
+    odd[1, 2, 0, at] = math.inf
+    q, k, v = tk.qk_norm_rope(odd.view(2, 5, 4 * d), 2, 1, w, w, **rot)
+    want = tk.qk_norm_rope(x.view(2, 5, 4 * d), 2, 1, w, w, **rot)
+    assert bool(q[1, 0, 2, at].isnan())
+    rest = torch.arange(d, device="cuda") != at
+    assert not q[1, 0, 2, rest].any()
+    q[1, 0, 2] = want[0][1, 0, 2]
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(v, want[2])
+    g = [_randn(104 + i, 2, h, 5, d, dtype=dt) for i, h in enumerate((2, 1, 1))]
+    dwq = tk.qk_norm_rope_backward(x.view(2, 5, 4 * d), 2, 1, *g, w, w, **rot)[1]
+    g[0][1, 0, 2, at] = math.inf
+    got = tk.qk_norm_rope_backward(x.view(2, 5, 4 * d), 2, 1, *g, w, w, **rot)[1]
+    assert not bool(got[at].isfinite()) and torch.equal(got[rest], dwq[rest])
