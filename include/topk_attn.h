@@ -386,7 +386,7 @@ int topk_qk_norm_rope_append(const void* qkv, const void* q_weight, const void* 
  * Gradients of topk_qk_norm_rope, recomputed from its input: d_q [B, H, L, d], d_k, d_v
  * [B, Hkv, L, d] (contiguous) to d_qkv [B, L, (H + 2 Hkv) d] (contiguous) and, where not
  * NULL, d_q_weight and d_k_weight [d], sums over every token and head in a fixed order.
- * rot as in the forward call. Workspace for the weights' gradients:
+ * rot as in the forward call; with norm = 0 qkv is not read. Workspace for the weights' gradients:
  * topk_qk_norm_rope_backward_workspace_bytes (0 for invalid arguments).
  */
 int topk_qk_norm_rope_backward(const void* qkv, const void* q_weight, const void* k_weight,

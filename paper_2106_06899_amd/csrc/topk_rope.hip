@@ -7,6 +7,7 @@
 //   t = position[axis(p)] * freq[p]
 // and backward, with m = the rotation by -t of the incoming gradient:
 //   dw = sum over tokens and heads of m u,   dx = r (m w - u mean(m w u)).
+// Without a norm dx = m, which x has no part in (an infinite x would make 0 x of it NaN).
 //
 // Bound by memory: every element is read once and written once (backward: x and the gradient
 // read, one gradient written), so the design is about whole cache lines and few instructions.
@@ -22,7 +23,7 @@
 // Measured (a device copy reaches 4.94 TB/s): 4 x 8192 tokens of 16 + 16 + 16 heads of 128, bf16,
 // 169 us (4.8 TB/s); rotation of 2 x 16 heads of 8192 tokens, three axes, 29 us (4.6 TB/s); 8 x 512
 // tokens of 12 + 12 + 12 heads of 64, where latency counts, 11 us forward (3.4 TB/s), 16 + 4 us
-// backward (4 x 8192: 91 + 5, 5.0 TB/s). With the angles formed by each lane for itself, one head at a
+// backward (4 x 8192: 91 + 5, 5.0 TB/s; without a norm 73 in all, 84 where x was read all the same). With the angles formed by each lane for itself, one head at a
 // time: 188, 30, 16, 31 + 9.
 #include "topk_device.h"
 #include "topk_heads.h"
@@ -272,7 +273,7 @@ __global__ __launch_bounds__(NT) void k_heads_backward(HeadsProblem hp, Grid g) 
   const Share sh(hp, g, blockIdx.y);
   const int lane = threadIdx.x & (g.T - 1), unit = threadIdx.x / g.T, tl = unit & (g.tok - 1), first = unit / g.tok;
   const Lane<VEC, NC, ADJ> ln(lane, g.T, hp.d, hp.rot.half);
-  const bool value = sh.seg == 2;
+  const bool value = sh.seg == 2, norm = !value && hp.norm;  // (the gradient depends on x through the norm alone)
   float wa[NC][VEC], wb[NC][VEC], ga[NC][VEC], gb[NC][VEC];
   const T* w = value ? nullptr : (const T*)hp.w[sh.seg];
 #pragma unroll
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(NT) void k_heads_backward(HeadsProblem hp, Grid g) 
     for (int64_t h = h0; h < sh.h1; h += g.hp, dst += g.hp * hp.dx.sh) {
       Raw<T, VEC, NC> rawx, rawg;
       fetch(rawg, grad, ln);
-      if (!value) fetch(rawx, src, ln);
+      if (norm) fetch(rawx, src, ln);
       src += g.hp * hp.x.sh;
       grad += g.hp * gr.sh;
       float ma[NC][VEC], mb[NC][VEC];
@@ -314,30 +315,26 @@ __global__ __launch_bounds__(NT) void k_heads_backward(HeadsProblem hp, Grid g) 
       for (int j = 0; j < NC; ++j) {
         widen_vec(ma[j], rawg.a[j]);
         widen_vec(mb[j], rawg.b[j]);
+        if (!value && ln.turn[j]) turn_pairs<VEC, ADJ>(ma[j], mb[j], co[j], si[j]);  // (the launch asks for the opposite angles)
       }
-      if (!value) {
+      if (norm) {
         float xa[NC][VEC], xb[NC][VEC];
         float sq = 0.f, dot = 0.f;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
           widen_vec(xa[j], rawx.a[j]);
           widen_vec(xb[j], rawx.b[j]);
-          if (ln.turn[j]) turn_pairs<VEC, ADJ>(ma[j], mb[j], co[j], si[j]);  // (the launch asks for the opposite angles)
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
             sq = fmaf(xa[j][e], xa[j][e], fmaf(xb[j][e], xb[j][e], sq));
             dot = fmaf(ma[j][e] * wa[j][e], xa[j][e], fmaf(mb[j][e] * wb[j][e], xb[j][e], dot));
           }
         }
-        float r = 1.f, mean = 0.f;  // dx = r (m w - u mean)
-        if (hp.norm) {
-          r = rsqrtf(fmaf(group_sum(sq, g.T), inv_d, hp.eps));
-          mean = r * group_sum(dot, g.T) * inv_d;
-        }
+        const float r = rsqrtf(fmaf(group_sum(sq, g.T), inv_d, hp.eps)), mean = r * group_sum(dot, g.T) * inv_d;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) {
+          for (int e = 0; e < VEC; ++e) {  // dx = r (m w - u mean)
             const float ua = xa[j][e] * r, ub = xb[j][e] * r;
             ga[j][e] = fmaf(ma[j][e], ua, ga[j][e]);
             gb[j][e] = fmaf(mb[j][e], ub, gb[j][e]);

@@ -487,3 +487,21 @@ def test_infinite_features_beside_a_norm(dt, d, pairs, adjacent):
     g[0][1, 0, 2, at] = math.inf
     got = tk.qk_norm_rope_backward(x.view(2, 5, 4 * d), 2, 1, *g, w, w, **rot)[1]
     assert not bool(got[at].isfinite()) and torch.equal(got[rest], dwq[rest])
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("d,pairs,adjacent", PASSING)
+def test_gradient_of_a_rotation_does_not_depend_on_its_input(dt, d, pairs, adjacent):
+    """Without a norm the gradient is the turned one, to the sign of its zeros, whatever the projection holds."""
+    rot = dict(positions=torch.arange(5, device="cuda") + 3, freqs=tk.rope_frequencies(pairs), adjacent=adjacent) if pairs else {}
+    g = [_randn(110 + i, 2, h, 5, d, dtype=dt) for i, h in enumerate((2, 1, 1))]
+    qkv = _randn(113, 2, 5, 4 * d, dtype=dt)
+    want = tk.qk_norm_rope_backward(qkv, 2, 1, *g, norm=False, **rot)[0]
+    for x in (math.inf, -math.inf, math.nan):
+        assert _same(tk.qk_norm_rope_backward(torch.full_like(qkv, x), 2, 1, *g, norm=False, **rot)[0], want)
+    pos, f = torch.arange(5, device="cuda") + 3, tk.rope_frequencies(pairs) if pairs else torch.zeros(0, dtype=torch.float64, device="cuda")
+    g = [_spoil(t, 2 * pairs) for t in g]
+    back = tk.qk_norm_rope_backward(qkv, 2, 1, *g, norm=False, **rot)[0].view(2, 5, 4, d).transpose(1, 2)
+    for t, at in zip(g[:2], (0, 2)):
+        assert _same(back[:, at:at + t.shape[1]], tk.rope(t, pos, f, adjacent=adjacent, inverse=True))
+    assert _same(back[:, 3:], g[2])
