@@ -75,11 +75,11 @@ class RotaryFunction(torch.autograd.Function):
 
 class NormRotaryHeadsFunction(torch.autograd.Function):
     """q, k, v = qk_norm_rope(qkv, ...), differentiable in qkv and the weights; the backward
-    recomputes from qkv."""
+    recomputes from qkv, which it needs, and keeps, for the norm alone."""
 
     @staticmethod
     def forward(ctx, qkv, q_weight, k_weight, positions, freqs, heads, kv_heads, axes, adjacent, eps, norm):
-        ctx.save_for_backward(qkv, q_weight, k_weight, positions, freqs)
+        ctx.save_for_backward(qkv if norm else None, q_weight, k_weight, positions, freqs)
         ctx.how = heads, kv_heads, axes, adjacent, eps, norm
         return qk_norm_rope(qkv, heads, kv_heads, q_weight, k_weight, positions, freqs, axes, adjacent, eps, norm)
 
@@ -88,6 +88,9 @@ class NormRotaryHeadsFunction(torch.autograd.Function):
     def backward(ctx, d_q, d_k, d_v):
         qkv, q_weight, k_weight, positions, freqs = ctx.saved_tensors
         heads, kv_heads, axes, adjacent, eps, norm = ctx.how
+        if qkv is None:  # (not read: one row stands for all)
+            B, _, L, d = d_q.shape
+            qkv = d_q.new_empty((heads + 2 * kv_heads) * d).expand(B, L, -1)
         d_qkv, d_wq, d_wk = qk_norm_rope_backward(
             qkv, heads, kv_heads, d_q.contiguous(), d_k.contiguous(), d_v.contiguous(), q_weight, k_weight, positions, freqs,
             axes, adjacent, eps, norm, weights=any(ctx.needs_input_grad[1:3]))

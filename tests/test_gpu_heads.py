@@ -505,3 +505,17 @@ def test_gradient_of_a_rotation_does_not_depend_on_its_input(dt, d, pairs, adjac
     for t, at in zip(g[:2], (0, 2)):
         assert _same(back[:, at:at + t.shape[1]], tk.rope(t, pos, f, adjacent=adjacent, inverse=True))
     assert _same(back[:, 3:], g[2])
+
+
+def test_rotation_alone_keeps_no_input():
+    """Nothing of the projection is held for the gradient where there is no norm: it may be overwritten."""
+    pos, f = torch.arange(9, device="cuda"), tk.rope_frequencies(32)
+    leaf = _randn(120, 2, 9, 4 * 64, dtype=BF16).requires_grad_()
+    g = [_randn(121 + i, 2, h, 9, 64, dtype=BF16) for i, h in enumerate((2, 1, 1))]
+    for kw in (dict(positions=pos, freqs=f), dict()):
+        qkv = leaf * 2
+        outs = layers.norm_rotary_heads(qkv, 2, 1, norm=False, **kw)
+        want = tk.qk_norm_rope_backward(qkv.detach().clone(), 2, 1, *g, norm=False, **kw)[0] * 2
+        with torch.no_grad():
+            qkv.fill_(math.nan)
+        assert torch.equal(torch.autograd.grad(outs, leaf, g)[0], want)
