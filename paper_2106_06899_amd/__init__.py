@@ -390,7 +390,7 @@ def rope_frequencies(sections, theta: float = 10000.0, restart: bool = False, de
     if not parts or min(parts) < 0:
         raise ValueError(f"sections must be pair counts, got {sections}")
     runs = parts if restart else [sum(parts)]
-    return torch.cat([float(theta) ** (-torch.arange(n, dtype=torch.float64) / max(n, 1)) for n in runs]).to(device)
+    return torch.cat([float(theta) ** (-torch.arange(n, dtype=torch.float64, device="cpu") / max(n, 1)) for n in runs]).to(device)
 
 
 def rope_axes(sections, interleaved: bool = False) -> tuple:

@@ -170,16 +170,30 @@ class TopkMultiheadAttention(torch.nn.Module):
             pairs = self.d_head // 2 if rope_sections is None else tuple(rope_sections)
             if rope_sections is not None:
                 self.rope_axes = rope_axes(pairs)
-            freqs = rope_frequencies(pairs, rope_theta, device="cpu")
-            if 2 * freqs.numel() > self.d_head:
-                raise ValueError(f"{freqs.numel()} pairs do not fit into {self.d_head} features")
-            self.rope_bits = freqs.view(torch.int64).to(device)
+            self.rope_of = pairs, float(rope_theta)
+            bits = self._rope_bits()
+            if 2 * bits.numel() > self.d_head:
+                raise ValueError(f"{bits.numel()} pairs do not fit into {self.d_head} features")
+            self.rope_bits = bits.to(self.qkv.weight.device)
+
+    def _rope_bits(self):
+        return rope_frequencies(*self.rope_of, device="cpu").view(torch.int64)
+
+    def _apply(self, fn, recurse=True):
+        # (a layer built without memory gets it here; the frequencies are in no state_dict)
+        bare = self.rope_bits is not None and self.rope_bits.is_meta
+        super()._apply(fn, recurse)
+        if bare and not self.rope_bits.is_meta:
+            self.rope_bits.copy_(self._rope_bits())
+        return self
 
     def _rotation(self, positions, L: int, device):
         if self.rope_bits is None:
             if positions is not None:
                 raise ValueError("positions need rope_theta")
             return dict(norm=self.qk_norm)
+        if self.rope_bits.is_meta:  # (weights that were assigned to a layer without memory)
+            self.rope_bits = self._rope_bits().to(device)
         if positions is None:
             positions = torch.arange(L, device=device)
             if self.rope_axes is not None:

@@ -479,3 +479,21 @@ def test_no_keys_on_every_form(Lq):
     _, _, _, k, v = _inputs(2, 2, 2, Lq, 0, 70, 64, seed=18)
     out, lse = tk.attn_prefix(q, None, None, k, v, torch.zeros(2, dtype=torch.int32, device="cuda"), lse=True)
     assert not out.any() and bool((lse == -math.inf).all())
+
+
+def test_layer_built_under_a_default_device():
+    x = torch.randn(2, 20, 128, device="cuda", dtype=BF16)
+    kw = dict(qk_norm=True, rope_theta=1e4, rope_sections=(8, 12, 12))
+    named = layers.TopkMultiheadAttention(128, 2, None, 64, True, device="cuda", **kw)
+    with torch.device("cuda"):
+        m = layers.TopkMultiheadAttention(128, 2, None, 64, True, **kw)
+    with torch.device("meta"):
+        late = layers.TopkMultiheadAttention(128, 2, None, 64, True, **kw)
+        given = layers.TopkMultiheadAttention(128, 2, None, 64, True, **kw)
+    for t in (m, late.to_empty(device="cuda")):
+        t.load_state_dict(named.state_dict())
+    given.load_state_dict(named.state_dict(), assign=True)
+    with torch.no_grad():
+        want = named(x)
+        for t in (m, late, given):
+            assert torch.equal(t(x), want)

@@ -148,3 +148,30 @@ def test_more_rows_than_a_launch_holds_are_refused(B, H, Lq):
 def test_calls_without_keys_are_planned(Lq):
     for d in (64, 128):
         assert tk.attn_prefix_workspace_bytes(2, 2, 2, Lq, 0, 0, d) == 0
+
+
+def _turning(**kw):
+    return layers.TopkMultiheadAttention(128, 2, 8, rope_theta=1e4, rope_sections=(8, 12, 12), **kw)
+
+
+def test_layers_built_without_memory():
+    """Under a default device without memory, or on it by name: the frequencies are made where the weights
+    are, and are there once the layer has memory, however it comes by it."""
+    want = tk.rope_frequencies(32, 1e4, device="cpu")
+    for named in (False, True):
+        if named:
+            m = _turning(device="meta")
+        else:
+            with torch.device("meta"):
+                m = _turning()
+                assert torch.equal(tk.rope_frequencies(32, 1e4, device="cpu"), want)
+        assert m.qkv.weight.is_meta and m.rope_bits.is_meta
+        whole = torch.nn.Sequential(m).to_empty(device="cpu")
+        assert torch.equal(whole[0].rope_bits.view(torch.float64), want)
+        m.load_state_dict(_turning().state_dict())
+        assert torch.equal(m.rope_bits.view(torch.float64), want)
+    m = _turning(device="meta")
+    m.load_state_dict(_turning().state_dict(), assign=True)
+    assert torch.equal(m._rotation(None, 3, torch.device("cpu"))["freqs"], want)
+    before = m.rope_bits
+    assert m.to(torch.float32).rope_bits is before  # (what a captured graph reads stays)
