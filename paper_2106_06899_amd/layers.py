@@ -179,6 +179,9 @@ class TopkMultiheadAttention(torch.nn.Module):
     def _rope_bits(self):
         return rope_frequencies(*self.rope_of, device="cpu").view(torch.int64)
 
+    def _axes(self):
+        return max(self.rope_axes, default=0) + 1
+
     def _apply(self, fn, recurse=True):
         # (a layer built without memory gets it here; the frequencies are in no state_dict)
         bare = self.rope_bits is not None and self.rope_bits.is_meta
@@ -197,7 +200,7 @@ class TopkMultiheadAttention(torch.nn.Module):
         if positions is None:
             positions = torch.arange(L, device=device)
             if self.rope_axes is not None:
-                positions = positions.expand(max(self.rope_axes) + 1, 1, L)
+                positions = positions.expand(self._axes(), 1, L)
         return dict(positions=positions, freqs=self.rope_bits.view(torch.float64), axes=self.rope_axes,
                     adjacent=self.rope_adjacent, norm=self.qk_norm)
 
@@ -234,7 +237,7 @@ class TopkMultiheadAttention(torch.nn.Module):
         if positions is None and self.rope_bits is not None:
             positions = prefix_k.shape[1] + lengths[:, None] + torch.arange(L, device=x.device, dtype=torch.int32)
             if self.rope_axes is not None:
-                positions = positions.expand(max(self.rope_axes) + 1, B, L)
+                positions = positions.expand(self._axes(), B, L)
         w = (self.q_norm, self.k_norm) if self.qk_norm else (None, None)
         q = qk_norm_rope_append(self.qkv(x), self.n_heads, self.n_heads, k_cache, v_cache, lengths, *w,
                                 **self._rotation(positions, L, x.device))

@@ -175,3 +175,10 @@ def test_layers_built_without_memory():
     assert torch.equal(m._rotation(None, 3, torch.device("cpu"))["freqs"], want)
     before = m.rope_bits
     assert m.to(torch.float32).rope_bits is before  # (what a captured graph reads stays)
+
+
+def test_layer_of_sections_without_pairs():
+    """Sections of no pairs at all: nothing turns, by the default positions too."""
+    m = layers.TopkMultiheadAttention(128, 2, 8, rope_theta=1e4, rope_sections=(0,))
+    rot = m._rotation(None, 3, torch.device("cpu"))
+    assert rot["freqs"].numel() == 0 and rot["positions"].shape == (1, 1, 3)
