@@ -484,7 +484,7 @@ struct Wide {
       const bool leads = !(mt <= m + LEAD);  // (NaN too)
       if (__builtin_amdgcn_ballot_w64(leads)) {  // (the other rows multiply by 1: a row's result is its own)
         const float mn = leads ? larger(m, mt) : m;
-        const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+        const float alpha = mn == -INFINITY ? 1.f : exp2f(m - mn);  // (below 2^-126 too: see the weights)
         m = mn;
         l *= alpha;
 #pragma unroll

@@ -497,3 +497,20 @@ def test_layer_built_under_a_default_device():
         want = named(x)
         for t in (m, late, given):
             assert torch.equal(t(x), want)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Lq", [4, 40, 80, 128])
+@pytest.mark.parametrize("at", [0, 70, 127, 199])
+def test_tiny_weights_before_and_after_their_maximum(Lq, d, at):
+    """Keys of weight 2^-130 around one that leads them: those before it count like those behind it. (As a bf16
+    number such a weight is a multiple of 2^-133, off by 2^-4 at most; the output's rounding 2^-8.)"""
+    q, k, v = (torch.zeros(1, 1, n, d, device="cuda") for n in (Lq, 200, 200))
+    q[..., 0] = 1
+    k[..., 0] = -90.0 * 8
+    k[0, 0, at, 0] = 0
+    v[:] = 2.0 ** 90
+    v[0, 0, at] = 0
+    out = tk.attn_prefix(q.to(BF16), None, None, k.to(BF16), v.to(BF16), causal=False, scale=0.125).double()
+    want = 199 * math.exp(-90.0) * 2.0 ** 90
+    assert bool(((out - want).abs() <= (2.0 ** -4 + 2.0 ** -8) * want).all()), out.flatten()[0] / want
