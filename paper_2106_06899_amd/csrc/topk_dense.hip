@@ -156,7 +156,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_dense_attn(DenseArgs a
     // (not <=: for NaN too; queries whose maximum stays multiply by 1)
     if (__builtin_amdgcn_ballot_w64(!(mt <= m_run))) {
       const float m_new = fmaxf(m_run, mt);
-      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run - m_new) * cexp);  // m_run = -inf -> 0
+      const float alpha = m_new == -INFINITY ? 1.f : exp2f((m_run - m_new) * cexp);  // m_run = -inf -> 0; below 2^-126 too, as the weights
       m_run = m_new;
       l_run *= alpha;
 #pragma unroll

@@ -127,3 +127,19 @@ def test_dense_infinities(d, causal):
         s = s.masked_fill(~torch.ones(L, L, dtype=torch.bool, device="cuda").tril(), -float("inf"))
     ref = torch.softmax(s, -1) @ v[0, 0].double()
     assert bool(((out - ref).abs().amax(-1) <= parity.RTOL[wl.BF16] * ref.abs().amax(-1)).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("at", [0, 64, 130, 299])
+def test_dense_tiny_weights_before_and_after_their_maximum(d, at):
+    """Keys of weight 2^-130 around one that leads them: those before it count like those behind it (each a
+    multiple of 2^-133 as a bf16 number, off by 2^-4 at most; the output's rounding 2^-8)."""
+    q, k, v = (torch.zeros(1, 1, n, d, device="cuda") for n in (200, 300, 300))
+    q[..., 0] = 1
+    k[..., 0] = -90.0 * 8
+    k[0, 0, at, 0] = 0
+    v[:] = 2.0 ** 90
+    v[0, 0, at] = 0
+    out = tk.attn_dense(q.bfloat16(), k.bfloat16(), v.bfloat16(), 0, False, 0.125).double()
+    want = 299 * np.exp(-90.0) * 2.0 ** 90
+    assert bool(((out - want).abs() <= (2.0 ** -4 + 2.0 ** -8) * want).all()), out.flatten()[0] / want
