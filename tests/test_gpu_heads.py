@@ -519,3 +519,34 @@ def test_rotation_alone_keeps_no_input():
         with torch.no_grad():
             qkv.fill_(math.nan)
         assert torch.equal(torch.autograd.grad(outs, leaf, g)[0], want)
+
+
+LOOPS = {
+    # name: dtype, L, H, Hkv, d, pairs of each axis, adjacent (each with two tiles of tokens a workgroup in the
+    # backward pass, the last workgroup's second tile missing, the last tile ragged)
+    "rotated": (BF16, 11003, 3, 3, 128, (64,), False),
+    "single_features": (F32, 11003, 3, 3, 70, (7, 3), True),
+    "not_rotated": (BF16, 24004, 3, 3, 64, (), False),
+    "half_rotated": (BF16, 21861, 2, 1, 128, (32,), True),
+}
+
+
+@pytest.mark.parametrize("name", sorted(LOOPS))
+def test_backward_over_several_tiles_a_workgroup(name):
+    dt, L, H, Hkv, d, sections, adjacent = LOOPS[name]
+    qkv = _randn(130, 1, L, (H + 2 * Hkv) * d, dtype=dt, std=1.5)
+    wq, wk = (_randn(s, d, dtype=dt, std=0.2, mean=1.0) for s in (131, 132))
+    kw = dict(norm=True)
+    if sections:
+        pos = torch.randint(0, 100000, (len(sections), 1, L), generator=torch.Generator(device="cuda").manual_seed(133), device="cuda")
+        kw.update(positions=pos, freqs=tk.rope_frequencies(sections), axes=tk.rope_axes(sections), adjacent=adjacent)
+    grads = [_randn(134 + i, 1, h, L, d, dtype=dt) for i, h in enumerate((H, Hkv, Hkv))]
+    dx, tol, dw = _grad_reference(qkv, H, Hkv, wq, wk, kw, grads)
+    got = tk.qk_norm_rope_backward(qkv, H, Hkv, *grads, wq, wk, **kw)
+    _close(got[0], dx, tol, "d_qkv")
+    for g, r, n in zip(got[1:], dw, ("d_q_weight", "d_k_weight")):
+        _close(g, r[0], r[1], n)
+    if sections:
+        got = tk.qk_norm_rope_backward(qkv, H, Hkv, *grads, **dict(kw, norm=False))
+        dx, tol, _ = _grad_reference(qkv, H, Hkv, None, None, dict(kw, norm=False), grads)
+        _close(got[0], dx, tol, "d_qkv without a norm")
