@@ -514,3 +514,155 @@ def test_tiny_weights_before_and_after_their_maximum(Lq, d, at):
     out = tk.attn_prefix(q.to(BF16), None, None, k.to(BF16), v.to(BF16), causal=False, scale=0.125).double()
     want = 199 * math.exp(-90.0) * 2.0 ** 90
     assert bool(((out - want).abs() <= (2.0 ** -4 + 2.0 ** -8) * want).all()), out.flatten()[0] / want
+
+
+# Every pair of forms that a call in several ranges takes (on the prefix, on the caches; 8 heads on 2): requests, tokens of each
+FORMS = {
+    "blocks_1_1": (2, 2), "blocks_2_1": (4, 2), "blocks_2_2": (1, 5), "wide_1": (9, 2), "wide_2": (2, 5), "wide_two_numbers": (2, 10),
+    "wide_one_number": (2, 20), "one_list": (2, 32),
+}
+LONG = 2100  # keys of the prefix: several ranges at either d
+
+
+def _form(name, d, seed, S=300):
+    """(inputs, lengths as a list and on the GPU) of a call whose partial results are joined."""
+    B, Lq = FORMS[name]
+    q, pk, pv, k, v = _inputs(B, 8, 2, Lq, LONG, S, d, seed=seed)
+    assert tk.attn_prefix_workspace_bytes(B, 8, 2, Lq, LONG, S, d) >= 2 * B * 8 * Lq * (d + 2) * 4
+    n = [(S, Lq + 3, 131, 257)[b % 4] for b in range(B)]
+    return (q, pk, pv, k, v), n, torch.tensor(n, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("name", sorted(FORMS))
+def test_forms_in_several_ranges(name, d):
+    """Against 64 bits, causal and not; what lies behind the lengths, strides and a row of NaN change nothing else."""
+    (q, pk, pv, k, v), lens, n = _form(name, d, 20)
+    B, Lq = FORMS[name]
+    for causal in (True, False):
+        out, lse = tk.attn_prefix(q, pk, pv, k, v, n, causal, lse=True)
+        _check(q, pk, pv, k, v, lens, causal, d ** -0.5, out, lse)
+    want = tk.attn_prefix(q, pk, pv, k, v, n)
+    cut = lambda t: torch.cat((t, torch.full_like(t, math.nan)), -2)[..., :t.shape[-2], :]  # noqa: E731
+    turned = lambda t: t.transpose(-3, -2).contiguous().transpose(-3, -2)  # noqa: E731
+    for f in (cut, turned, lambda t: torch.stack((t, t), -2)[..., 1, :]):
+        assert torch.equal(tk.attn_prefix(q, f(pk), f(pv), f(k), f(v), n), want)
+    kk, vv = k.clone(), v.clone()
+    for b, m in enumerate(lens):
+        kk[b, :, m:], vv[b, :, m:] = math.nan, math.inf
+    assert torch.equal(tk.attn_prefix(q, pk, pv, kk, vv, n), want)
+    qq = q.clone()
+    qq[B - 1, 3, Lq // 2, 5] = math.nan
+    got = tk.attn_prefix(qq, pk, pv, k, v, n)
+    assert bool(got[B - 1, 3, Lq // 2].isnan().all())
+    got[B - 1, 3, Lq // 2] = want[B - 1, 3, Lq // 2]
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("name", sorted(FORMS))
+def test_forms_in_several_ranges_and_values_that_are_not_finite(name, d):
+    """In the caches they reach only rows that see them, in the prefix every row of their key head."""
+    (q, pk, pv, k, v), lens, n = _form(name, d, 21)
+    B, Lq = FORMS[name]
+    last, other = B - 1, 0
+    at = {(last, lens[last] - 1, 3): math.nan, (last, lens[last] - 2, d - 1): math.inf, (other, 5, 17): -math.inf, (other, 0, 40): math.nan}
+    for b, j, c in at:
+        v[b, 1, j, c] = 0
+    pv[0, 1700, 9] = 0
+    want = tk.attn_prefix(q, pk, pv, k, v, n)
+    for (b, j, c), x in at.items():
+        v[b, 1, j, c] = x
+    pv[0, 1700, 9] = math.inf
+    got = tk.attn_prefix(q, pk, pv, k, v, n)
+    met = torch.zeros(want.shape, dtype=torch.bool, device="cuda")
+    for b, j, c in at:
+        met[b, 4:, max(0, j - (lens[b] - Lq)):, c] = True
+    met[:, :4, :, 9] = True
+    assert not bool(got[met].isfinite().any())
+    assert torch.equal(got[~met], want[~met])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("name", sorted(FORMS))
+def test_forms_in_several_ranges_and_extreme_scores(name, d):
+    """One key far above the rest, in a range of its own; whole ranges at -inf; and weights of 2^-130 against
+    values of 2^90 (rounded like the few-key ones: a number below 2^-126 keeps 2^-4 of itself as bf16)."""
+    (q, pk, pv, k, v), lens, n = _form(name, d, 22)
+    B, Lq = FORMS[name]
+    q[..., 0], pk[..., 0], k[..., 0] = 1.0, 0.0, 0.0
+    pk[:, 1999, 0] = 3e4
+    out = tk.attn_prefix(q, pk, pv, k, v, n)
+    assert torch.equal(out, pv[:, 1999].repeat_interleave(4, 0)[None, :, None].expand_as(out))
+    pk[:, 1999, 0] = 0
+    away = torch.zeros(LONG, dtype=torch.bool, device="cuda")
+    away[0:1300], away[1500:2000] = True, True
+    pk[:, away, 0] = -math.inf
+    out, lse = tk.attn_prefix(q, pk, pv, k, v, n, lse=True)
+    _check(q, pk[:, ~away], pv[:, ~away], k, v, lens, True, d ** -0.5, out, lse)
+    z = lambda t: torch.zeros_like(t)  # noqa: E731
+    q, pk, pv, k, v = z(q), z(pk), z(pv), z(k), z(v)
+    q[..., 0], pk[..., 0], k[..., 0] = 1, -90.0 * 8, -90.0 * 8
+    k[:, :, 1, 0] = 0
+    pv[:], v[:] = 2.0 ** 90, 2.0 ** 90
+    v[:, :, 1] = 0
+    got = tk.attn_prefix(q, pk, pv, k, v, n, scale=0.125).double()
+    seen = LONG - 1 + n.double()[:, None] - (Lq - 1) + torch.arange(Lq, device="cuda")  # of weight e^-90
+    ref = (seen * math.exp(-90.0) * 2.0 ** 90)[:, None, :, None]
+    assert bool(((got - ref).abs() <= (2.0 ** -4 + 2.0 ** -8) * ref).all())
+
+
+@pytest.mark.parametrize("name", sorted(FORMS))
+def test_forms_in_several_ranges_on_streams_and_in_graphs(name):
+    """Two side streams at once, and two graphs of one memory pool that replay in turn with other lengths."""
+    (a, lens, n), (b, _, _) = _form(name, 64, 23), _form(name, 128, 24)
+    wa, wb = tk.attn_prefix(*a, n), tk.attn_prefix(*b, n)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(s1):
+            ga = tk.attn_prefix(*a, n)
+        with torch.cuda.stream(s2):
+            gb = tk.attn_prefix(*b, n)
+        torch.cuda.synchronize()
+        assert torch.equal(ga, wa) and torch.equal(gb, wb)
+    g1, g2 = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g1):
+        oa = tk.attn_prefix(*a, n)
+    with torch.cuda.graph(g2, pool=g1.pool()):
+        ob = tk.attn_prefix(*b, n)
+    first = n.clone()
+    for rep in range(4):
+        n.copy_((first * (rep + 1)) % 301)
+        g1.replay()
+        ra = oa.clone()
+        g2.replay()
+        rb = ob.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(ra, tk.attn_prefix(*a, n)) and torch.equal(rb, tk.attn_prefix(*b, n)), f"replay {rep}"
+
+
+def test_offsets_past_32_bits_in_several_ranges():
+    """A long cache whose second request lies 2^32 elements behind the first."""
+    q, pk, pv, k, v = _inputs(2, 2, 1, 1, 100, 2000, 64, seed=25)
+    assert tk.attn_prefix_workspace_bytes(2, 2, 1, 1, 100, 2000, 64) > 0
+    n = torch.tensor([2000, 1503], dtype=torch.int32, device="cuda")
+    want = tk.attn_prefix(q, pk, pv, k, v, n)
+    _check(q, pk, pv, k, v, n.tolist(), True, 0.125, want)
+    big = torch.empty(2 ** 32 + 2 ** 20, dtype=BF16, device="cuda")
+    far = big.as_strided((2, 1, 2000, 64), (2 ** 32, 2000 * 64, 64, 1))
+    far.copy_(k)
+    assert torch.equal(tk.attn_prefix(q, pk, pv, far, v, n), want)
+    del big, far
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_thousands_of_rows_from_a_few_ranges(d):
+    """Rows that are joined several a workgroup, the last workgroup not full."""
+    B, H, Hkv, Lq, P, S = 1, 21, 3, 131, 5000, 200
+    q, pk, pv, k, v = _inputs(B, H, Hkv, Lq, P, S, d, seed=26)
+    splits = tk.attn_prefix_workspace_bytes(B, H, Hkv, Lq, P, S, d) // (B * H * Lq * (d + 2) * 4)
+    assert B * H * Lq > 2048 and B * H * Lq % 16 and 2 <= splits <= 16
+    n = torch.tensor([167], dtype=torch.int32, device="cuda")
+    out, lse = tk.attn_prefix(q, pk, pv, k, v, n, lse=True)
+    _check(q, pk, pv, k, v, n.tolist(), True, d ** -0.5, out, lse)
