@@ -343,9 +343,10 @@ typedef struct {
  * topk_rope -- rotary positions on heads. x [B, H, L, d] with head row (b, h, l) at
  * b * batch_stride + h * head_stride + l * token_stride elements; out contiguous
  * [B, H, L, d], not overlapping x unless it is x itself with the same strides. Any
- * even d up to 512; tensors need the alignment of their elements only (16 bytes, and
- * strides and pairs that are multiples of 16 bytes, run fastest). Its gradient is the
- * same call with `inverse` changed.
+ * even d up to 512; tensors need the alignment of their elements only (addresses and
+ * strides that are multiples of four elements, with d of eight and pairs of four, run
+ * fastest). Features behind the d_rot first come out as they are, whatever they hold. Its
+ * gradient is the same call with `inverse` changed.
  */
 int topk_rope(const void* x, void* out, int64_t B, int64_t H, int64_t L, int64_t d,
               int64_t batch_stride, int64_t head_stride, int64_t token_stride,
@@ -359,7 +360,8 @@ int topk_rope(const void* x, void* out, int64_t B, int64_t H, int64_t L, int64_t
  * and rotated (rot NULL: not); value heads are copied. Squares are summed in fp32.
  *
  *   q_weight, k_weight   [d], in dtype; NULL: ones
- *   q [B, H, L, d], k, v [B, Hkv, L, d]   written, contiguous: what topk_attn takes
+ *   q [B, H, L, d], k, v [B, Hkv, L, d]   written, contiguous: what topk_attn_prefix
+ *                        takes, and topk_attn and topk_attn_dense where Hkv = H
  *
  * d and alignment as topk_rope.
  */
@@ -420,6 +422,9 @@ size_t topk_qk_norm_rope_backward_workspace_bytes(int64_t B, int64_t L, int64_t 
  * its output is infinite or NaN), and values up to 2^90 cannot overflow the sums.
  * Weights enter the product with V to 16 significant bits, or, with 64 rows a request and
  * key head ((H / Hkv) * Lq) and more, rounded to bf16 as topk_attn_dense does.
+ * Key ranges are planned for S keys a request, since lengths lie on the device: caches with
+ * far more rows than any request holds are best passed with an S that covers the longest
+ * (the strides say where the rows lie), or a long prefix gets few ranges.
  * Workspace: topk_attn_prefix_workspace_bytes, partial results of key ranges in fp32 (0
  * where none is needed, or for invalid arguments). Stages 0 and 3 of the stage timing.
  */

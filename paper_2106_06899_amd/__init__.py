@@ -493,7 +493,8 @@ def qk_norm_rope(qkv, heads: int, kv_heads: int, q_weight=None, k_weight=None, p
     """(q [B, heads, L, d], k, v [B, kv_heads, L, d]) from the packed projection qkv
     [B, L, (heads + 2 kv_heads) d]: query and key heads divided by their root mean square
     (``norm``), scaled by q_weight / k_weight [d] and rotated as ``rope`` says (freqs None:
-    not); values as they are. One pass; what ``attn`` and ``attn_dense`` take."""
+    not); values as they are. One pass; what ``attn_prefix`` takes, and with kv_heads ==
+    heads ``attn`` and ``attn_dense``."""
     import torch
     B, L, d = _qkv(qkv, heads, kv_heads, q_weight, k_weight, norm)
     device = qkv.device
@@ -585,7 +586,11 @@ def attn_prefix(q, prefix_k, prefix_v, k=None, v=None, lengths=None, causal: boo
     Returns out [B, H, Lq, d]; with ``lse`` also the fp32 [B, H, Lq] logarithm of the sum of
     exp(scale * score), by which results over different keys can be joined. Keys and values
     may have any strides but for the last dimension (caches cut from larger ones), multiples
-    of 8; None stands for no keys. bf16, d = 64 or 128. Forward only."""
+    of 8; None stands for no keys. bf16, d = 64 or 128. Forward only.
+
+    The work is divided for S keys a request. Where caches have far more rows than any
+    request holds, pass them cut (``k[:, :, :n]``, n at least the longest length): behind 65536
+    shared keys 8 requests of up to 1000 take 105 us so, 354 with caches of 131072 rows."""
     import torch
     device = q.device
     _check(q, "q", 4, q.dtype, device)

@@ -15,8 +15,8 @@
 // Row tiles come in two forms. Few (up to 32 rows) keeps K and V in registers and is bound by
 // reading them: 8 requests behind 65536 keys, 16 heads of 128, read 571 MB in 98 us (5.8 TB/s; a
 // device copy: 4.94). Wide (128 rows) goes through LDS and is bound by matrix and vector
-// instructions, which this chip runs side by side at falling clocks: 4 requests of 512 tokens, 16
-// heads of 128 on 4 key heads behind 16384 keys, 273 us with the join, 1.02 PFLOP/s (a large
+// instructions, which run side by side: 4 requests of 512 tokens, 16
+// heads of 128 on 4 key heads behind 16384 keys, 277 us with the join, 1.0 PFLOP/s (a large
 // library matrix product: 1.38). Short calls are bound by launches and latency, and by the partial
 // results, whose join is a launch of its own: 64 requests behind 8192 keys, 32 heads of 128 on 8, 28 +
 // 6 us, where the bytes would take 23. Calls with few keys in all take one range instead.
@@ -772,7 +772,7 @@ __global__ __launch_bounds__(NT) void k_prefix_join(PrefixArgs a) {
       for (int s = tr; s < splits; s += TR) top = larger(top, a.ml[s * a.pl.rows + row].x);
     }
   }
-  if (splits > 4) {  // (TR lanes of a row: 32 or more of one wave, or whole waves)
+  if (splits > 4) {  // (TR lanes of a row: 16 or 32 of one wave, or whole waves)
     for (int o = 1; o < (TR < 64 ? TR : 64); o <<= 1) top = larger(top, __shfl_xor(top, o, 64));
     if (TR > 64) {
       if (threadIdx.x % 64 == 0) fac[rl][threadIdx.x % TR / 64] = top;

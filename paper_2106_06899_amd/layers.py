@@ -230,7 +230,8 @@ class TopkMultiheadAttention(torch.nn.Module):
         d_h] and hold ``lengths[b]`` tokens in their caches [B, n_heads, S, d_h]: their keys and
         values are appended (the caller advances lengths by L, and leaves room for them), and
         each attends to the prefix, its own cache and the new tokens up to itself. positions
-        default to P + lengths[b] + 0 .. L - 1 on every axis."""
+        default to P + lengths[b] + 0 .. L - 1 on every axis. Caches may be cut from longer ones
+        (see ``attn_prefix``)."""
         if self.topk is not None or not self.causal:
             raise ValueError("decode attends to every earlier key: it needs topk=None and causal=True")
         B, L, D = x.shape
