@@ -440,6 +440,74 @@ size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64
                                         int64_t d, int dtype);
 
 /*
+ * Pages of a cache. Keys and values of requests lie in pages of page_rows rows (any number >= 1)
+ * of a common pool: row r of page p, head h, layer l at l * layer + p * page + h * head + r * row
+ * elements, d of them, 16-byte aligned. A table [B, M] (row b at b * table_stride) holds each
+ * request's pages in order: row i of request b lies in page table[b][i / page_rows], at row
+ * i % page_rows; -1 where it holds none. refs[p] counts the entries that hold page p; a page with
+ * 0 is free (a caller who sets one aside counts 1 for that). lengths[b] rows are in use.
+ * Tables, refs, lengths: device, int32; all calls are enqueued, read nothing back and can be
+ * captured. An entry that names no page of the pool counts as none, and nothing is read or
+ * written for it.
+ *
+ * topk_pages_reserve makes room for `rows` more rows of each request (rows_each[b] where not
+ * NULL; none where lengths[b] < 0): entries of the rows lengths[b] .. lengths[b] + rows - 1 that
+ * hold no page take the free pages of the lowest numbers, in the order of requests and rows, and
+ * a page among them that others hold too is left for such a page, with a copy of the rows
+ * in use, in all layers. (Where all that hold a page ask at once, the first of them keeps it.)
+ * Rows behind the table's end get no room. *missing: 0, or how many pages the pool lacks, and
+ * then nothing has changed. Workspace: topk_pages_reserve_workspace_bytes.
+ *
+ * topk_pages_append writes k, v [layers, B, heads, T, d] (strides layer, batch, head, token) to
+ * rows lengths[b] + t, or, with offsets (device, int32 [B + 1], not decreasing), tokens
+ * offsets[b] .. offsets[b + 1] - 1 of k, v [layers, heads, T, d] of request b. Rows without a page
+ * are dropped. lengths are read, not advanced, and should be as topk_pages_reserve had them.
+ *
+ * topk_pages_keep keeps the accepted ones of drafted rows: row lengths[b] + kept[b][i] goes to row
+ * lengths[b] + i, for i up to the first negative entry of kept (device, int32 [B, A], A <= 64,
+ * row b at b * kept_stride), in all layers, and new_lengths[b] is lengths[b] and their number. A row
+ * without a page is not moved.
+ *
+ * topk_pages_fork makes request b go on from request parents[b] (device, int32 [B]): it holds the
+ * pages of its parent's rows, shared, and has its length; its former pages are given back. All at
+ * once, so that parents may change places. parents[b] = b or >= B: no change; < 0: the request ends
+ * (no pages, length 0). Workspace: topk_pages_fork_workspace_bytes.
+ *
+ * topk_pages_release gives back the pages behind those that lengths[b] rows need.
+ *
+ * topk_pages_compact copies the used pages, in order, to the first ones of another pool (of n_to
+ * pages, same heads, rows and layers, not overlapping), and writes what the books are there:
+ * new_table [B, M] (contiguous) and new_refs [n_to]. *missing: 0, or how many pages do not fit, and
+ * then new_table is -1, new_refs 0 and nothing copied. Workspace:
+ * topk_pages_compact_workspace_bytes.
+ */
+typedef struct {
+  void *k, *v;
+  int64_t layers, pages, heads, page_rows, d;
+  int64_t k_layer, k_page, k_head, k_row, v_layer, v_page, v_head, v_row;
+} topk_pages;
+int topk_pages_reserve(const topk_pages* pool, int32_t* table, int64_t table_stride, int64_t B, int64_t M, int32_t* refs,
+                       const int32_t* lengths, const int32_t* rows_each, int64_t rows, int32_t* missing, int dtype,
+                       void* hip_stream);
+size_t topk_pages_reserve_workspace_bytes(int64_t pages, int64_t B, int64_t M);
+int topk_pages_append(const void* k, const void* v, int64_t k_layer, int64_t k_batch, int64_t k_head, int64_t k_token,
+                      int64_t v_layer, int64_t v_batch, int64_t v_head, int64_t v_token, int64_t T, const int32_t* offsets,
+                      const topk_pages* pool, const int32_t* table, int64_t table_stride, int64_t B, int64_t M,
+                      const int32_t* lengths, int dtype, void* hip_stream);
+int topk_pages_keep(const topk_pages* pool, const int32_t* table, int64_t table_stride, int64_t B, int64_t M,
+                    const int32_t* lengths, const int32_t* kept, int64_t kept_stride, int64_t A, int32_t* new_lengths,
+                    int dtype, void* hip_stream);
+int topk_pages_fork(int32_t* table, int64_t table_stride, int64_t B, int64_t M, int32_t* refs, int64_t pages,
+                    int32_t* lengths, const int32_t* parents, int64_t page_rows, void* hip_stream);
+size_t topk_pages_fork_workspace_bytes(int64_t B, int64_t M);
+int topk_pages_release(int32_t* table, int64_t table_stride, int64_t B, int64_t M, int32_t* refs, int64_t pages,
+                       const int32_t* lengths, int64_t page_rows, void* hip_stream);
+int topk_pages_compact(const topk_pages* pool, const topk_pages* to, const int32_t* table, int64_t table_stride, int64_t B,
+                       int64_t M, const int32_t* refs, int32_t* new_table, int32_t* new_refs, int32_t* missing, int dtype,
+                       void* hip_stream);
+size_t topk_pages_compact_workspace_bytes(int64_t pages, int64_t n_to);
+
+/*
  * Test hook: the number of query rows that the last topk_attn_debug /
  * topk_ffn_debug call on the calling thread selected through a fallback path
  * (rows whose sampled threshold or candidate buffers could not prove the

@@ -24,7 +24,8 @@ import os
 __all__ = ["attn", "attn_dense", "scan_ablation", "probe_mfma", "ffn", "attn_workspace_bytes", "ffn_workspace_bytes", "attn_path", "ffn_path",
            "mfma_layout", "lib", "TopkError", "LIB_PATH", "profile_begin", "profile_end", "STAGES",
            "attn_backward", "ffn_backward", "rope", "rope_frequencies", "rope_axes", "qk_norm_rope", "qk_norm_rope_append",
-           "qk_norm_rope_backward", "attn_prefix", "attn_prefix_workspace_bytes", "set_backward_lists", "set_memory_budget", "last_fallback_rows"]
+           "qk_norm_rope_backward", "attn_prefix", "attn_prefix_workspace_bytes",
+           "pages_reserve", "pages_append", "pages_keep", "pages_fork", "pages_release", "pages_compact", "set_backward_lists", "set_memory_budget", "last_fallback_rows"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtopk.so")
 
@@ -49,6 +50,11 @@ class _PrefixStrides(ctypes.Structure):  # topk_prefix_strides
                                               "k_head", "k_key", "v_batch", "v_head", "v_key")]
 
 
+class _Pages(ctypes.Structure):  # topk_pages
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in (
+        "layers", "pages", "heads", "page_rows", "d", "k_layer", "k_page", "k_head", "k_row", "v_layer", "v_page", "v_head", "v_row")]
+
+
 class TopkError(RuntimeError):
     """A non-OK status from libtopk; ``status`` holds the code."""
 
@@ -66,6 +72,7 @@ def lib() -> ctypes.CDLL:
         raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2106_06899_amd.build`")
     L = ctypes.CDLL(LIB_PATH)
     i64, vp, i32, f32 = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_float
+    pool = ctypes.POINTER(_Pages)
     attn_args = [vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, i64, i32, f32, i32, vp]
     ffn_args = [vp, vp, vp, vp, i64, i64, i64, i64, i64, i32, vp]
     sigs = {
@@ -98,6 +105,15 @@ def lib() -> ctypes.CDLL:
         "topk_qk_norm_rope_backward_workspace_bytes": ([i64] * 6 + [i32], ctypes.c_size_t),
         "topk_attn_prefix": ([vp] * 8 + [i64] * 7 + [ctypes.POINTER(_PrefixStrides), i32, f32, i32, vp], i32),
         "topk_attn_prefix_workspace_bytes": ([i64] * 7 + [i32], ctypes.c_size_t),
+        "topk_pages_reserve": ([pool, vp] + [i64] * 3 + [vp] * 3 + [i64, vp, i32, vp], i32),
+        "topk_pages_reserve_workspace_bytes": ([i64] * 3, ctypes.c_size_t),
+        "topk_pages_append": ([vp] * 2 + [i64] * 9 + [vp, pool, vp] + [i64] * 3 + [vp, i32, vp], i32),
+        "topk_pages_keep": ([pool, vp] + [i64] * 3 + [vp] * 2 + [i64] * 2 + [vp, i32, vp], i32),
+        "topk_pages_fork": ([vp] + [i64] * 3 + [vp, i64, vp, vp, i64, vp], i32),
+        "topk_pages_fork_workspace_bytes": ([i64] * 2, ctypes.c_size_t),
+        "topk_pages_release": ([vp] + [i64] * 3 + [vp, i64, vp, i64, vp], i32),
+        "topk_pages_compact": ([pool, pool, vp] + [i64] * 3 + [vp] * 4 + [i32, vp], i32),
+        "topk_pages_compact_workspace_bytes": ([i64] * 2, ctypes.c_size_t),
         "topk_selftest_mfma_layout": ([vp, vp, vp], i32),
         "topk_scan_ablation": ([vp, vp] + [i64] * 7 + [i32, vp], i32),
         "topk_probe_mfma": ([ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), vp], i32),
@@ -629,6 +645,198 @@ def attn_prefix(q, prefix_k, prefix_v, k=None, v=None, lengths=None, causal: boo
             B, H, Hkv, Lq, P, S, d, st, int(causal), float(scale), dt, _stream_of(device))
     _launch(device, L.topk_attn_prefix, args, nbytes)
     return (out, sums) if lse else out
+
+
+def _written(t, name):
+    """A tensor whose entries are written must not hold one twice."""
+    if 0 in t.stride() and any(st == 0 and size > 1 for st, size in zip(t.stride(), t.shape)):
+        raise ValueError(f"{name} is written to and must not be expanded")
+
+
+def _pool(k_pages, v_pages, writes: bool = True):
+    """topk_pages of a pool [pages, heads, rows, d], or of all layers' [layers, pages, heads, rows, d]."""
+    shape = k_pages.shape
+    if len(shape) not in (4, 5) or 0 in shape:
+        raise ValueError(f"k_pages must be [pages, heads, rows, d] or [layers, pages, heads, rows, d], got {tuple(shape)}")
+    for t, n in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        _rows(t, n, shape, k_pages.dtype, k_pages.device)
+        if writes:
+            _written(t, n)
+    if k_pages.data_ptr() == v_pages.data_ptr():
+        raise ValueError("k_pages and v_pages are the same memory")
+    ks, vs = k_pages.stride()[:-1], v_pages.stride()[:-1]
+    if len(shape) == 4:
+        shape, ks, vs = (1, *shape), (0, *ks), (0, *vs)
+    return _Pages(k_pages.data_ptr(), v_pages.data_ptr(), *shape, *ks, *vs)
+
+
+def _page_table(table, device, writes: bool = True):
+    """(address, row stride, B, M) of a table of pages."""
+    if table.dim() != 2 or 0 in table.shape:
+        raise ValueError(f"table must be [requests, pages], got {tuple(table.shape)}")
+    import torch
+    _rows(table, "table", table.shape, torch.int32, device)
+    if writes:
+        _written(table, "table")
+    elif table.shape[0] > 1 and table.stride(0) < table.shape[1]:
+        table = table.contiguous()
+    B, M = table.shape
+    return table, (table.data_ptr(), table.stride(0) if B > 1 else M, B, M)
+
+
+def _ints(t, name, n, device):
+    import torch
+    _check(t, name, 1, torch.int32, device)
+    if t.shape[0] != n:
+        raise ValueError(f"{name} must have {n} entries, got {t.shape[0]}")
+    return t.data_ptr()
+
+
+def pages_reserve(k_pages, v_pages, table, refs, lengths, rows):
+    """Room for ``rows`` more rows of every request (an int, or int32 [B] on the GPU) behind the
+    ``lengths[b]`` that it has (none where that is negative), in a cache of pages.
+
+    k_pages, v_pages [pages, heads, page_rows, d], or [layers, pages, ...] where the layers
+    share one table (any strides but for the last dimension, in multiples of 16 bytes; bf16 or
+    fp32); ``table`` int32 [B, M]: the pages of each request in order, -1 where it holds none;
+    ``refs`` int32 [pages]: how many table entries hold a page, 0 for a free one. Entries of the new
+    rows that hold no page take the free ones of the lowest numbers, in order; a page among
+    them that others hold too is left for a copy of its rows in use (where all its holders ask
+    at once the first keeps it). Rows behind the table's end get no room.
+
+    Changes table, refs and the copied pages in place. Returns int32 [], on the GPU: 0, or how many
+    pages the pool lacks, and then nothing has changed. Reads nothing back."""
+    import torch
+    device = k_pages.device
+    pool = _pool(k_pages, v_pages)
+    _dtype_code(k_pages)
+    table, at = _page_table(table, device)
+    B = at[2]
+    refs_ptr, len_ptr = _ints(refs, "refs", pool.pages, device), _ints(lengths, "lengths", B, device)
+    each = None
+    if isinstance(rows, torch.Tensor):
+        each, rows = _ints(rows, "rows", B, device), 0
+    missing = torch.empty((), dtype=torch.int32, device=device)
+    L = lib()
+    _launch(device, L.topk_pages_reserve,
+            (pool, *at, refs_ptr, len_ptr, each, int(rows), missing.data_ptr(), _dtype_code(k_pages), _stream_of(device)),
+            L.topk_pages_reserve_workspace_bytes(pool.pages, B, at[3]))
+    return missing
+
+
+def pages_append(k, v, k_pages, v_pages, table, lengths, offsets=None):
+    """Writes keys and values k, v [B, heads, T, d] to the rows ``lengths[b] + t`` of each request,
+    or, with ``offsets`` (int32 [B + 1] on the GPU), packed ones [heads, N, d] as ``attn_packed`` takes
+    them: tokens offsets[b] .. offsets[b + 1] - 1 to rows of request b. With pools of all layers k
+    and v have the layers in front too. Rows without a page (see ``pages_reserve``) and tokens
+    outside every request are dropped; ``lengths`` is not advanced."""
+    device = k_pages.device
+    pool = _pool(k_pages, v_pages)
+    table, at = _page_table(table, device, writes=False)
+    B = at[2]
+    len_ptr = _ints(lengths, "lengths", B, device)
+    layers = k_pages.shape[:-4]
+    if k.dim() != len(layers) + (4 if offsets is None else 3):
+        raise ValueError(f"k of shape {tuple(k.shape)} does not go with pools of shape {tuple(k_pages.shape)}")
+    T = k.shape[-2]
+    for t, n in ((k, "k"), (v, "v")):
+        _rows(t, n, (*layers, *(() if offsets is not None else (B,)), pool.heads, T, pool.d), k_pages.dtype, device)
+    off = None if offsets is None else _ints(offsets, "offsets", B + 1, device)
+    if T == 0:
+        return
+
+    def strides(t):
+        st = t.stride()[:-1]
+        st = (0, *st) if not layers else st
+        return st if offsets is None else (st[0], 0, *st[1:])
+
+    _launch(device, lib().topk_pages_append,
+            (k.data_ptr(), v.data_ptr(), *strides(k), *strides(v), T, off, pool, *at, len_ptr, _dtype_code(k_pages), _stream_of(device)))
+
+
+def pages_keep(k_pages, v_pages, table, lengths, kept):
+    """Keeps the accepted drafts: row ``lengths[b] + kept[b, i]`` moves to row ``lengths[b] + i``, for
+    i up to the first negative entry of ``kept`` (int32 [B, A] on the GPU, A at most 64), in all
+    layers. Returns the new lengths, int32 [B]: ``lengths`` and how many were kept. (What is behind
+    them goes back by ``pages_release``.) A row without a page is not moved."""
+    import torch
+    device = k_pages.device
+    pool = _pool(k_pages, v_pages)
+    table, at = _page_table(table, device, writes=False)
+    B = at[2]
+    len_ptr = _ints(lengths, "lengths", B, device)
+    if kept.dim() != 2:
+        raise ValueError(f"kept must be [requests, drafts], got {tuple(kept.shape)}")
+    A = kept.shape[1]
+    if A == 0:
+        _rows(kept, "kept", (B, 0), torch.int32, device)
+        return lengths.clone()
+    _rows(kept, "kept", (B, A), torch.int32, device)
+    new = torch.empty(B, dtype=torch.int32, device=device)
+    _launch(device, lib().topk_pages_keep,
+            (pool, *at, len_ptr, kept.data_ptr(), kept.stride(0), A, new.data_ptr(), _dtype_code(k_pages), _stream_of(device)))
+    return new
+
+
+def pages_fork(table, refs, lengths, parents, page_rows: int):
+    """Every request b goes on from request ``parents[b]`` (int32 [B] on the GPU): it takes its
+    length and shares the pages of its rows; its former pages are given back. ``parents[b] == b``
+    (or past the last) changes nothing, a negative one ends the request. All at once, so that
+    beams may change places. Changes table, refs and lengths in place; ``pages_reserve`` copies
+    a shared page when it is to be written."""
+    device = table.device
+    table, at = _page_table(table, device)
+    B = at[2]
+    L = lib()
+    _launch(device, L.topk_pages_fork,
+            (*at, _ints(refs, "refs", refs.shape[0] if refs.dim() == 1 else 0, device), refs.numel(), _ints(lengths, "lengths", B, device),
+             _ints(parents, "parents", B, device), int(page_rows), _stream_of(device)),
+            L.topk_pages_fork_workspace_bytes(B, at[3]))
+
+
+def pages_release(table, refs, lengths, page_rows: int):
+    """Gives back the pages behind those that ``lengths[b]`` rows need (all of them where it is 0);
+    changes table and refs in place."""
+    device = table.device
+    table, at = _page_table(table, device)
+    _launch(device, lib().topk_pages_release,
+            (*at, _ints(refs, "refs", refs.shape[0] if refs.dim() == 1 else 0, device), refs.numel(), _ints(lengths, "lengths", at[2], device),
+             int(page_rows), _stream_of(device)))
+
+
+def _span(t):
+    """First and last byte of a tensor's memory."""
+    end = sum((n - 1) * st for n, st in zip(t.shape, t.stride()))
+    return t.data_ptr(), t.data_ptr() + (end + 1) * t.element_size() - 1
+
+
+def pages_compact(k_pages, v_pages, table, refs, k_to, v_to):
+    """Copies the used pages (``refs > 0``), in order, to the first ones of the pools k_to, v_to
+    (of any number of pages, memory of their own): a pool that is to grow or shrink, or to be
+    saved. Returns (table, refs, missing) of the new pool; missing, int32 [], is 0, or how many
+    pages do not fit, and then nothing is copied and the new table is -1 throughout."""
+    import torch
+    device = k_pages.device
+    pool, to = _pool(k_pages, v_pages, writes=False), _pool(k_to, v_to)
+    if k_to.dim() != k_pages.dim() or k_to.shape[:-4] != k_pages.shape[:-4] or k_to.shape[-3:] != k_pages.shape[-3:]:
+        raise ValueError(f"pools of shapes {tuple(k_pages.shape)} and {tuple(k_to.shape)} differ in more than their pages")
+    if k_to.dtype != k_pages.dtype or k_to.device != device:
+        raise TypeError(f"the new pool is {k_to.dtype} on {k_to.device}, the old one {k_pages.dtype} on {device}")
+    for a in (k_to, v_to):
+        for b in (k_pages, v_pages):
+            (a0, a1), (b0, b1) = _span(a), _span(b)
+            if a0 <= b1 and b0 <= a1:
+                raise ValueError("the new pool overlaps the old one")
+    table, at = _page_table(table, device, writes=False)
+    refs_ptr = _ints(refs, "refs", pool.pages, device)
+    new_table = torch.empty(at[2:], dtype=torch.int32, device=device)
+    new_refs = torch.empty(to.pages, dtype=torch.int32, device=device)
+    missing = torch.empty((), dtype=torch.int32, device=device)
+    L = lib()
+    _launch(device, L.topk_pages_compact,
+            (pool, to, *at, refs_ptr, new_table.data_ptr(), new_refs.data_ptr(), missing.data_ptr(), _dtype_code(k_pages), _stream_of(device)),
+            L.topk_pages_compact_workspace_bytes(pool.pages, to.pages))
+    return new_table, new_refs, missing
 
 
 STAGES = ("score", "select", "redo", "finalize", "backward")

@@ -4,6 +4,7 @@
 #include "topk_attn.h"
 #include "topk_heads.h"
 #include "topk_internal.h"
+#include "topk_pages.h"
 #include "topk_prefix.h"
 
 #include <math.h>
@@ -934,6 +935,68 @@ int run_prefix(const PrefixProblem& pp, hipStream_t st) {
   return TOPK_OK;
 }
 
+// ---------------------------------------------------------------- pages
+constexpr int64_t MAX_WGS = 0xFFFFFF;  // workgroups of a launch (of 256 threads, fewer than 2^32 in all)
+
+int int_ptr(const void* p, const char* name) {
+  if (!p) return fail(TOPK_E_NULL, "%s is NULL", name);
+  if (((uintptr_t)p) % 4) return fail(TOPK_E_ALIGN, "%s is not 4-byte aligned", name);
+  return TOPK_OK;
+}
+
+int pages_table(PageTable* t, const int32_t* table, int64_t stride, int64_t B, int64_t M) {
+  if (B < 1 || M < 1) return fail(TOPK_E_INVAL, "a table needs B >= 1 and M >= 1 (got %lld, %lld)", (long long)B, (long long)M);
+  if (B > MAX_WGS || M > 0x7FFFFFFFLL / B) return fail(TOPK_E_UNSUPPORTED, "a table of more than 2^31 - 1 entries or 2^24 - 1 requests");
+  if (B > 1 && (stride < M || stride >= STRIDE_MAX)) return fail(TOPK_E_INVAL, "table_stride %lld is out of range", (long long)stride);
+  *t = {(int32_t*)table, B > 1 ? stride : 0, (int)B, (int)M};
+  return int_ptr(table, "table");
+}
+
+int page_numbers(int64_t pages, int64_t page_rows) {
+  if (pages < 1 || page_rows < 1) return fail(TOPK_E_INVAL, "need pages >= 1 and page_rows >= 1 (got %lld, %lld)", (long long)pages, (long long)page_rows);
+  if (pages > 0x7FFFFFFFLL || page_rows > 0x7FFFFFFFLL) return fail(TOPK_E_UNSUPPORTED, "more than 2^31 - 1 pages or rows");
+  return TOPK_OK;
+}
+
+// a stride in elements that leads from one 16-byte aligned row to another, or nowhere
+int page_stride(const char* name, int64_t n, int64_t* s, int es) {
+  if (n == 1) *s = 0;
+  int rc = stride_ok(name, {*s});
+  if (!rc && *s % (16 / es)) return fail(TOPK_E_ALIGN, "a stride of %s is not a multiple of 16 bytes: %lld elements", name, (long long)*s);
+  return rc;
+}
+
+int page_pool(PagePool* pp, PageShape* s, const topk_pages* in, const char* what, int dtype) {
+  if (!in) return fail(TOPK_E_NULL, "%s is NULL", what);
+  if (dtype != TOPK_F32 && dtype != TOPK_BF16) return fail(TOPK_E_INVAL, "dtype must be TOPK_F32 or TOPK_BF16");
+  const int es = dtype == TOPK_BF16 ? 2 : 4;
+  int rc = page_numbers(in->pages, in->page_rows);
+  if (rc) return rc;
+  if (in->layers < 1 || in->heads < 1 || in->d < 1)
+    return fail(TOPK_E_INVAL, "sizes of %s must be >= 1 (got layers = %lld, heads = %lld, d = %lld)", what, (long long)in->layers,
+                (long long)in->heads, (long long)in->d);
+  if (in->d > 1024 || in->d * es % 16) return fail(TOPK_E_UNSUPPORTED, "feature size %lld: pages hold rows of whole 16 bytes, at most 1024 features", (long long)in->d);
+  if (in->layers > 65536 || in->heads > 16384 || in->page_rows > (int64_t(1) << 30) / (in->heads * (in->d * es / 16)))
+    return fail(TOPK_E_UNSUPPORTED, "%s: more than 65536 layers, 16384 heads or 2^34 bytes a page", what);
+  if ((rc = check_ptr(in->k, "the keys' pool")) || (rc = check_ptr(in->v, "the values' pool"))) return rc;
+  *pp = {{in->k, in->v}, {in->k_layer, in->v_layer}, {in->k_page, in->v_page}, {in->k_head, in->v_head}, {in->k_row, in->v_row}};
+  for (int i = 0; i < 2; ++i)
+    if ((rc = page_stride(what, in->layers, &pp->layer[i], es)) || (rc = page_stride(what, in->pages, &pp->page[i], es)) ||
+        (rc = page_stride(what, in->heads, &pp->head[i], es)) || (rc = page_stride(what, in->page_rows, &pp->row[i], es)))
+      return rc;
+  *s = {in->layers, in->heads, in->pages, (int)in->page_rows, (int)(in->d * es / 16), es};
+  return TOPK_OK;
+}
+
+int too_many_wgs(int64_t n) {
+  return n > MAX_WGS ? fail(TOPK_E_UNSUPPORTED, "more than 2^24 - 1 workgroups: too many requests, layers and heads") : TOPK_OK;
+}
+
+int pages_done(hipError_t e) {
+  if (e != hipSuccess) return fail(TOPK_E_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return TOPK_OK;
+}
+
 }  // namespace
 }  // namespace topk
 
@@ -1391,6 +1454,156 @@ size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64
   PrefixProblem pp;
   if (prefix_shape(&pp, B, H, Hkv, Lq, P, S, d, 0, 1.f, dtype)) return 0;
   return prefix_bytes(pp, prefix_plan(pp));
+}
+
+int topk_pages_reserve(const topk_pages* pool, int32_t* table, int64_t table_stride, int64_t B, int64_t M, int32_t* refs,
+                       const int32_t* lengths, const int32_t* rows_each, int64_t rows, int32_t* missing, int dtype, void* hip_stream) {
+  g_err.clear();
+  ReserveArgs a = {};
+  int rc;
+  if ((rc = page_pool(&a.pool, &a.s, pool, "the pool", dtype)) || (rc = pages_table(&a.t, table, table_stride, B, M)) ||
+      (rc = int_ptr(refs, "refs")) || (rc = int_ptr(lengths, "lengths")) || (rc = int_ptr(missing, "missing")))
+    return rc;
+  if (rows_each && (rc = int_ptr(rows_each, "rows_each"))) return rc;
+  if (rows < 0 || rows > 0x7FFFFFFFLL) return fail(TOPK_E_INVAL, "rows must be 0 to 2^31 - 1 (got %lld)", (long long)rows);
+  if (B > MAX_WGS / (pages_workgroups(a.s, 1))) return too_many_wgs(MAX_WGS + 1);
+  a.refs = refs;
+  a.missing = missing;
+  a.lengths = lengths;
+  a.rows_each = rows_each;
+  a.rows = rows;
+  hipStream_t st = (hipStream_t)hip_stream;
+  Scratch ws;
+  if ((rc = ws.get(reserve_bytes(a.s, a.t), "the reservation", st))) return rc;
+  const hipError_t e = launch_reserve(a, ws.p, st);
+  ws.release(st);
+  return pages_done(e);
+}
+
+size_t topk_pages_reserve_workspace_bytes(int64_t pages, int64_t B, int64_t M) {
+  PageTable t;
+  const int32_t some = 0;
+  if (page_numbers(pages, 1) || pages_table(&t, &some, M, B, M)) return 0;
+  PageShape s = {};
+  s.n_pages = pages;
+  return reserve_bytes(s, t);
+}
+
+int topk_pages_append(const void* k, const void* v, int64_t k_layer, int64_t k_batch, int64_t k_head, int64_t k_token, int64_t v_layer,
+                      int64_t v_batch, int64_t v_head, int64_t v_token, int64_t T, const int32_t* offsets, const topk_pages* pool,
+                      const int32_t* table, int64_t table_stride, int64_t B, int64_t M, const int32_t* lengths, int dtype, void* hip_stream) {
+  g_err.clear();
+  AppendArgs a = {};
+  int rc;
+  if ((rc = page_pool(&a.pool, &a.s, pool, "the pool", dtype)) || (rc = pages_table(&a.t, table, table_stride, B, M)) ||
+      (rc = int_ptr(lengths, "lengths")) || (rc = check_ptr(k, "k")) || (rc = check_ptr(v, "v")))
+    return rc;
+  if (offsets && (rc = int_ptr(offsets, "offsets"))) return rc;
+  if (T < 1) return fail(TOPK_E_INVAL, "T must be >= 1 (got %lld)", (long long)T);
+  a.from = {{(void*)k, (void*)v}, {k_layer, v_layer}, {k_batch, v_batch}, {k_head, v_head}, {k_token, v_token}};
+  for (int i = 0; i < 2; ++i) {
+    const char* n = i ? "v" : "k";
+    if ((rc = page_stride(n, a.s.layers, &a.from.layer[i], a.s.es)) || (rc = page_stride(n, offsets ? 1 : B, &a.from.page[i], a.s.es)) ||
+        (rc = page_stride(n, a.s.heads, &a.from.head[i], a.s.es)) || (rc = page_stride(n, T, &a.from.row[i], a.s.es)))
+      return rc;
+  }
+  if (T > MAX_WGS / a.s.layers / (offsets ? 1 : B)) return too_many_wgs(MAX_WGS + 1);
+  a.lengths = lengths;
+  a.offsets = offsets;
+  a.T = T;
+  return pages_done(launch_append(a, (hipStream_t)hip_stream));
+}
+
+int topk_pages_keep(const topk_pages* pool, const int32_t* table, int64_t table_stride, int64_t B, int64_t M, const int32_t* lengths,
+                    const int32_t* kept, int64_t kept_stride, int64_t A, int32_t* new_lengths, int dtype, void* hip_stream) {
+  g_err.clear();
+  KeepArgs a = {};
+  int rc;
+  if ((rc = page_pool(&a.pool, &a.s, pool, "the pool", dtype)) || (rc = pages_table(&a.t, table, table_stride, B, M)) ||
+      (rc = int_ptr(lengths, "lengths")) || (rc = int_ptr(kept, "kept")) || (rc = int_ptr(new_lengths, "new_lengths")))
+    return rc;
+  if (A < 1) return fail(TOPK_E_INVAL, "need at least one column of kept (got %lld)", (long long)A);
+  if (A > KEEP_MAX) return fail(TOPK_E_UNSUPPORTED, "more than %d kept drafts a request", KEEP_MAX);
+  if (B > 1 && (kept_stride < 0 || kept_stride >= STRIDE_MAX)) return fail(TOPK_E_INVAL, "kept_stride %lld is out of range", (long long)kept_stride);
+  if (B > MAX_WGS / (a.s.layers * a.s.heads * 2)) return too_many_wgs(MAX_WGS + 1);
+  a.lengths = lengths;
+  a.kept = kept;
+  a.kept_stride = kept_stride;
+  a.A = (int)A;
+  a.new_lengths = new_lengths;
+  return pages_done(launch_keep(a, (hipStream_t)hip_stream));
+}
+
+int topk_pages_fork(int32_t* table, int64_t table_stride, int64_t B, int64_t M, int32_t* refs, int64_t pages, int32_t* lengths,
+                    const int32_t* parents, int64_t page_rows, void* hip_stream) {
+  g_err.clear();
+  ForkArgs a = {};
+  int rc;
+  if ((rc = pages_table(&a.t, table, table_stride, B, M)) || (rc = page_numbers(pages, page_rows)) || (rc = int_ptr(refs, "refs")) ||
+      (rc = int_ptr(lengths, "lengths")) || (rc = int_ptr(parents, "parents")))
+    return rc;
+  a.refs = refs;
+  a.lengths = lengths;
+  a.parents = parents;
+  a.n_pages = pages;
+  a.page_rows = (int)page_rows;
+  hipStream_t st = (hipStream_t)hip_stream;
+  Scratch ws;
+  if ((rc = ws.get(fork_bytes(a.t), "the fork", st))) return rc;
+  const hipError_t e = launch_fork(a, ws.p, st);
+  ws.release(st);
+  return pages_done(e);
+}
+
+size_t topk_pages_fork_workspace_bytes(int64_t B, int64_t M) {
+  PageTable t;
+  const int32_t some = 0;
+  return pages_table(&t, &some, M, B, M) ? 0 : fork_bytes(t);
+}
+
+int topk_pages_release(int32_t* table, int64_t table_stride, int64_t B, int64_t M, int32_t* refs, int64_t pages, const int32_t* lengths,
+                       int64_t page_rows, void* hip_stream) {
+  g_err.clear();
+  PageTable t;
+  int rc;
+  if ((rc = pages_table(&t, table, table_stride, B, M)) || (rc = page_numbers(pages, page_rows)) || (rc = int_ptr(refs, "refs")) ||
+      (rc = int_ptr(lengths, "lengths")))
+    return rc;
+  return pages_done(launch_release(t, refs, lengths, pages, (int)page_rows, (hipStream_t)hip_stream));
+}
+
+int topk_pages_compact(const topk_pages* pool, const topk_pages* to, const int32_t* table, int64_t table_stride, int64_t B, int64_t M,
+                       const int32_t* refs, int32_t* new_table, int32_t* new_refs, int32_t* missing, int dtype, void* hip_stream) {
+  g_err.clear();
+  CompactArgs a = {};
+  PageShape s_to;
+  int rc;
+  if ((rc = page_pool(&a.pool, &a.s, pool, "the pool", dtype)) || (rc = page_pool(&a.to, &s_to, to, "the new pool", dtype)) ||
+      (rc = pages_table(&a.t, table, table_stride, B, M)) || (rc = int_ptr(refs, "refs")) || (rc = int_ptr(new_table, "new_table")) ||
+      (rc = int_ptr(new_refs, "new_refs")) || (rc = int_ptr(missing, "missing")))
+    return rc;
+  if (a.s.layers != s_to.layers || a.s.heads != s_to.heads || a.s.page_rows != s_to.page_rows || a.s.pieces != s_to.pieces)
+    return fail(TOPK_E_INVAL, "the pools differ in layers, heads, rows of a page or features");
+  if (pool->k == to->k || pool->v == to->v) return fail(TOPK_E_INVAL, "the new pool is the old one's memory");
+  if (std::min(s_to.n_pages, a.s.n_pages) > (MAX_WGS - B * M / 256 - 1) / pages_workgroups(a.s, 1)) return too_many_wgs(MAX_WGS + 1);
+  a.refs = refs;
+  a.new_table = new_table;
+  a.new_refs = new_refs;
+  a.missing = missing;
+  a.n_to = s_to.n_pages;
+  hipStream_t st = (hipStream_t)hip_stream;
+  Scratch ws;
+  if ((rc = ws.get(compact_bytes(a.s, a.n_to), "the move", st))) return rc;
+  const hipError_t e = launch_compact(a, ws.p, st);
+  ws.release(st);
+  return pages_done(e);
+}
+
+size_t topk_pages_compact_workspace_bytes(int64_t pages, int64_t n_to) {
+  if (page_numbers(pages, 1) || page_numbers(n_to, 1)) return 0;
+  PageShape s = {};
+  s.n_pages = pages;
+  return compact_bytes(s, n_to);
 }
 
 }  // extern "C"

@@ -1,0 +1,475 @@
+// A cache in pages: keys and values of requests lie in pages of page_rows rows of a common pool, and a
+// table says which pages hold a request's rows, in order. refs[p] counts the table entries that hold page
+// p; a page with 0 is free. That array and the tables are the whole state: a call that needs pages takes
+// the free ones of the lowest numbers, in the order of requests and rows, so that results do not
+// depend on scheduling, and nothing is kept between calls.
+//
+// The books (tables, counts) are a few kilobytes and bound by latency: one workgroup decides who gets
+// which page, with prefix sums over requests and over the counts. Rows of keys and values move in a
+// launch of their own, by many workgroups, in 16-byte pieces, and are bound by memory.
+#include "topk_device.h"
+#include "topk_pages.h"
+
+#include <limits.h>
+
+#include <algorithm>
+
+namespace topk {
+namespace {
+
+constexpr int BOOK = 1024;       // threads of a workgroup on the books
+constexpr int NT = 256;          // on rows
+constexpr int PIECES = 8 * NT;   // 16-byte pieces that a workgroup copies
+
+int64_t cdiv(int64_t x, int64_t y) { return (x + y - 1) / y; }
+size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+// (counts change by atomics, which pass the vector cache by; so do these reads)
+__device__ __forceinline__ int count_of(const int32_t* refs, int p) { return __hip_atomic_load(refs + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void count_add(int32_t* refs, int p, int by) {
+  __hip_atomic_fetch_add(refs + p, by, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// every access of the workgroup before this is seen by all of it behind
+__device__ __forceinline__ void book_sync() {
+  __threadfence();
+  __syncthreads();
+}
+
+// Inclusive prefix sum over the workgroup; *total: of all. `sums`: one entry a wave.
+__device__ __forceinline__ uint32_t book_scan(uint32_t x, uint32_t* sums, uint32_t* total) {
+  const int wave = threadIdx.x >> 6;
+  x = wave_incl_scan_full(x);
+  if ((threadIdx.x & 63) == 63) sums[wave] = x;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < BOOK / 64; ++w) {
+    const uint32_t s = sums[w];
+    before += w < wave ? s : 0;
+    all += s;
+  }
+  __syncthreads();
+  *total = all;
+  return before + x;
+}
+
+// The rows [lengths[b], lengths[b] + rows) of each request, as table entries in the order of requests: the
+// workgroup takes BOOK requests at a time, each adding its entries to one list.
+struct Entries {
+  const ReserveArgs& a;
+  uint32_t *ends, *sums;
+  int32_t* firsts;
+  uint32_t total;
+
+  __device__ void load(int base) {
+    const int b = base + threadIdx.x;
+    int64_t n = 0, first = 0;
+    if (b < a.t.B) {
+      const int64_t len = a.lengths[b], rows = a.rows_each ? a.rows_each[b] : a.rows;
+      if (len >= 0 && rows > 0) {
+        first = min(len / a.s.page_rows, (int64_t)a.t.M);
+        n = min((len + rows + a.s.page_rows - 1) / a.s.page_rows, (int64_t)a.t.M) - first;
+      }
+    }
+    __syncthreads();
+    ends[threadIdx.x] = book_scan((uint32_t)n, sums, &total);
+    firsts[threadIdx.x] = (int32_t)first;
+    __syncthreads();
+  }
+  // f(is there one, request, entry), by the whole workgroup
+  template <typename F>
+  __device__ void each(F f) {
+    for (int base = 0; base < a.t.B; base += BOOK) {
+      if (a.t.B > BOOK) load(base);
+      for (uint32_t i0 = 0; i0 < total; i0 += BOOK) {
+        const uint32_t i = i0 + threadIdx.x;
+        int lo = 0, hi = BOOK - 1;  // the first request whose entries end behind i
+        while (lo < hi) {
+          const int mid = (lo + hi) / 2;
+          if (ends[mid] > i) hi = mid;
+          else lo = mid + 1;
+        }
+        f(i < total, base + lo, firsts[lo] + (int)(i - (lo ? ends[lo - 1] : 0)));
+      }
+    }
+  }
+};
+
+// What becomes of an entry: it stays; it takes a free page; it is one of several that hold its page and is
+// to leave it for a copy.
+enum { STAYS = 0, FRESH = 1, SHARED = 2, LEAVES = 3, KEEPS = 4 };
+
+__global__ __launch_bounds__(BOOK) void k_pages_reserve(ReserveArgs a) {
+  __shared__ uint32_t ends[BOOK], sums[BOOK / 64];
+  __shared__ int32_t firsts[BOOK];
+  const int tid = threadIdx.x, n_pages = (int)a.s.n_pages;
+  Entries en = {a, ends, sums, firsts, 0};
+  if (a.t.B <= BOOK) en.load(0);
+  for (int b = tid; b < a.t.B; b += BOOK) a.copies[b] = make_int4(0, 0, 0, 0);
+  auto entry = [&](int b, int e) { return a.t.at + b * a.t.stride + e; };
+  auto kind = [&](int b, int e) { return a.kind + (int64_t)b * a.t.M + e; };
+  en.each([&](bool ok, int b, int e) {
+    if (!ok) return;
+    const int p = *entry(b, e);
+    *kind(b, e) = (uint32_t)p >= (uint32_t)n_pages ? FRESH : count_of(a.refs, p) > 1 ? SHARED : STAYS;
+  });
+  book_sync();
+  // Those that leave a page take themselves off its count. Where that leaves nobody, the first (in the order
+  // of requests) stays: it is found as the smallest of their numbers, written into the count itself as a
+  // negative one.
+  en.each([&](bool ok, int b, int e) {
+    if (ok && *kind(b, e) == SHARED) count_add(a.refs, *entry(b, e), -1);
+  });
+  book_sync();
+  en.each([&](bool ok, int b, int e) {
+    if (ok && *kind(b, e) == SHARED && count_of(a.refs, *entry(b, e)) <= 0)
+      __hip_atomic_fetch_min(a.refs + *entry(b, e), INT_MIN + (int)((int64_t)b * a.t.M + e), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  });
+  book_sync();
+  uint32_t need = 0;
+  en.each([&](bool ok, int b, int e) {
+    int k = STAYS;
+    if (ok) {
+      k = *kind(b, e);
+      if (k == SHARED) {
+        k = count_of(a.refs, *entry(b, e)) == INT_MIN + (int)((int64_t)b * a.t.M + e) ? KEEPS : LEAVES;
+        *kind(b, e) = k;
+      }
+    }
+    uint32_t n;
+    book_scan(k == FRESH || k == LEAVES, sums, &n);
+    need += n;
+  });
+  book_sync();
+  en.each([&](bool ok, int b, int e) {  // (a page that its first keeps: 1)
+    if (ok && *kind(b, e) == KEEPS) a.refs[*entry(b, e)] = 1;
+  });
+  book_sync();
+  // the free pages of the lowest numbers, as many as are needed
+  uint32_t have = 0;
+  for (int64_t base = 0; base < n_pages && have < need; base += 4 * BOOK) {
+    bool free[4];
+    uint32_t c = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t p = base + 4 * tid + u;
+      free[u] = p < n_pages && count_of(a.refs, (int)min(p, (int64_t)n_pages - 1)) == 0;
+      c += free[u];
+    }
+    uint32_t n, at = have + book_scan(c, sums, &n) - c;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (free[u] && at < need) a.free_list[at++] = (int)(base + 4 * tid + u);
+    have += n;
+  }
+  book_sync();
+  if (have < need) {  // nothing is changed: those that left are counted again
+    if (tid == 0) *a.missing = (int)(need - have);
+    en.each([&](bool ok, int b, int e) {
+      if (ok && *kind(b, e) == KEEPS) a.refs[*entry(b, e)] = 0;
+    });
+    book_sync();
+    en.each([&](bool ok, int b, int e) {
+      if (ok && *kind(b, e) >= LEAVES) count_add(a.refs, *entry(b, e), 1);
+    });
+    return;
+  }
+  if (tid == 0) *a.missing = 0;
+  uint32_t taken = 0;
+  en.each([&](bool ok, int b, int e) {
+    const int k = ok ? *kind(b, e) : STAYS;
+    const bool takes = k == FRESH || k == LEAVES;
+    uint32_t n;
+    const uint32_t at = taken + book_scan(takes, sums, &n) - 1;
+    taken += n;
+    if (!takes) return;
+    const int p = *entry(b, e), to = a.free_list[at], len = a.lengths[b];
+    const int left = len - e * a.s.page_rows;  // rows of the page that the request has already
+    if (k == LEAVES && left > 0) a.copies[b] = make_int4(p, to, left, 0);
+    *entry(b, e) = to;
+    a.refs[to] = 1;
+  });
+}
+
+// Where piece i of `rows` rows of a page's heads lies, in elements from the page's first.
+__device__ __forceinline__ int64_t piece_at(const PagePool& pool, int kv, int i, int pieces, int rows, int es) {
+  const int c = i % pieces, r = i / pieces, row = r % rows, head = r / rows;
+  return head * pool.head[kv] + row * pool.row[kv] + c * (16 / es);
+}
+__device__ __forceinline__ uint4* piece_ptr(const PagePool& pool, int kv, int64_t layer, int64_t page, int64_t at, int es) {
+  return (uint4*)((char*)pool.p[kv] + (layer * pool.layer[kv] + page * pool.page[kv] + at) * es);
+}
+
+// Copies the first `rows` rows of page `from` to page `to`, one part of PIECES pieces of them.
+__device__ __forceinline__ void copy_page(const PagePool& pa, const PagePool& pb, const PageShape& s, int kv, int64_t layer, int part,
+                                          int64_t from, int64_t to, int rows) {
+  const int total = (int)s.heads * rows * s.pieces, i0 = part * PIECES + threadIdx.x;
+  uint4 x[PIECES / NT];
+#pragma unroll
+  for (int u = 0; u < PIECES / NT; ++u) {
+    const int i = i0 + u * NT;
+    if (i < total) x[u] = *piece_ptr(pa, kv, layer, from, piece_at(pa, kv, i, s.pieces, rows, s.es), s.es);
+  }
+#pragma unroll
+  for (int u = 0; u < PIECES / NT; ++u) {
+    const int i = i0 + u * NT;
+    if (i < total) *piece_ptr(pb, kv, layer, to, piece_at(pb, kv, i, s.pieces, rows, s.es), s.es) = x[u];
+  }
+}
+
+struct CopyPlace {
+  int64_t page, layer;
+  int part, kv;
+};
+// the page, layer, pool and part of copying workgroup i
+__device__ __forceinline__ CopyPlace copy_place(const PageShape& s, int64_t i) {
+  const int64_t parts = (s.heads * s.page_rows * s.pieces + PIECES - 1) / PIECES;
+  CopyPlace c;
+  c.part = (int)(i % parts);
+  i /= parts;
+  c.kv = (int)(i & 1);
+  i >>= 1;
+  c.layer = i % s.layers;
+  c.page = i / s.layers;
+  return c;
+}
+
+__global__ __launch_bounds__(NT) void k_pages_copy(ReserveArgs a) {
+  const CopyPlace c = copy_place(a.s, blockIdx.x);
+  const int4 x = a.copies[c.page];
+  if (x.z) copy_page(a.pool, a.pool, a.s, c.kv, c.layer, c.part, x.x, x.y, x.z);
+}
+
+// One token of one layer a workgroup: its keys and values to row lengths[b] + its place in the request.
+__global__ __launch_bounds__(NT) void k_pages_append(AppendArgs a) {
+  const int64_t layer = blockIdx.x % a.s.layers, i = blockIdx.x / a.s.layers;
+  int64_t b, t, from;
+  if (a.offsets) {  // the last request whose first token is not behind i
+    int lo = 0, hi = a.t.B;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (a.offsets[mid] <= i) lo = mid;
+      else hi = mid;
+    }
+    b = lo;
+    t = i - a.offsets[b];
+    if (t < 0 || i >= a.offsets[b + 1]) return;
+    from = 0;
+  } else {
+    b = i / a.T;
+    t = i - b * a.T;
+    from = b;
+  }
+  const int64_t len = a.lengths[b], r = len + t, e = r / a.s.page_rows;
+  if (len < 0 || e >= a.t.M) return;
+  const int p = a.t.at[b * a.t.stride + e];
+  if ((uint32_t)p >= (uint32_t)a.s.n_pages) return;
+  const int row = (int)(r - e * a.s.page_rows), each = (int)a.s.heads * a.s.pieces;
+  const int64_t token = a.offsets ? i : t;
+  for (int x = threadIdx.x; x < 2 * each; x += NT) {
+    const int kv = x >= each, y = x - kv * each, head = y / a.s.pieces, c = (y - head * a.s.pieces) * (16 / a.s.es);
+    *piece_ptr(a.pool, kv, layer, p, head * a.pool.head[kv] + row * a.pool.row[kv] + c, a.s.es) =
+        *piece_ptr(a.from, kv, layer, from, head * a.from.head[kv] + token * a.from.row[kv] + c, a.s.es);
+  }
+}
+
+// Rows lengths[b] + kept[b][i] of one head, layer and pool go to rows lengths[b] + i: all of a slab of
+// columns is read before any of it is written, so that the order of `kept` does not matter.
+__global__ __launch_bounds__(NT) void k_pages_keep(KeepArgs a) {
+  __shared__ int2 from[KEEP_MAX], to[KEEP_MAX];  // page (-1: none), row
+  __shared__ int count;
+  int64_t i = blockIdx.x;
+  const int kv = (int)(i & 1);
+  i >>= 1;
+  const int64_t head = i % a.s.heads, layer = i / a.s.heads % a.s.layers, b = i / a.s.heads / a.s.layers;
+  const int64_t len = a.lengths[b];
+  if (threadIdx.x < 64) {
+    const int x = threadIdx.x < a.A ? a.kept[b * a.kept_stride + threadIdx.x] : -1;
+    const uint64_t over = __builtin_amdgcn_ballot_w64(x < 0);
+    const int n = len < 0 ? 0 : over ? __builtin_ctzll(over) : 64;
+    if (threadIdx.x == 0) {
+      count = n;
+      if (blockIdx.x % (2 * a.s.heads * a.s.layers) == 0) a.new_lengths[b] = (int32_t)(len + n);
+    }
+    auto place = [&](int64_t r) {
+      const int64_t e = r / a.s.page_rows;
+      const int p = e < a.t.M ? a.t.at[b * a.t.stride + e] : -1;
+      return make_int2((uint32_t)p < (uint32_t)a.s.n_pages ? p : -1, (int)(r - e * a.s.page_rows));
+    };
+    if ((int)threadIdx.x < n) {
+      int2 f = place(len + x);
+      const int2 t = place(len + threadIdx.x);
+      if (t.x < 0) f.x = -1;
+      from[threadIdx.x] = f;
+      to[threadIdx.x] = t;
+    }
+  }
+  __syncthreads();
+  constexpr int U = 4;
+  const int n = count;
+  if (!n) return;
+  const int cols = min(a.s.pieces, U * NT / n);  // columns of a slab
+  for (int c0 = 0; c0 < a.s.pieces; c0 += cols) {
+    uint4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = threadIdx.x + u * NT, r = k / cols, c = c0 + k % cols;
+      if (r < n && c < a.s.pieces && from[r].x >= 0)
+        x[u] = *piece_ptr(a.pool, kv, layer, from[r].x, head * a.pool.head[kv] + from[r].y * a.pool.row[kv] + c * (16 / a.s.es), a.s.es);
+    }
+    __syncthreads();  // (waits for the loads, too)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = threadIdx.x + u * NT, r = k / cols, c = c0 + k % cols;
+      if (r < n && c < a.s.pieces && from[r].x >= 0)
+        *piece_ptr(a.pool, kv, layer, to[r].x, head * a.pool.head[kv] + to[r].y * a.pool.row[kv] + c * (16 / a.s.es), a.s.es) = x[u];
+    }
+  }
+}
+
+__device__ __forceinline__ int64_t pages_of(int64_t len, int rows) { return len <= 0 ? 0 : (len + rows - 1) / rows; }
+
+// A request's new row of the table, and its old and new pages' counts. The tables change in a launch of
+// their own, when nothing reads the old ones any more.
+__global__ __launch_bounds__(NT) void k_pages_fork(ForkArgs a) {
+  const int b = blockIdx.x;
+  const int par = a.parents[b];
+  if (par == b || par >= a.t.B) return;
+  int32_t* tmp = a.tmp + (int64_t)b * (a.t.M + 1);
+  const int len = par < 0 ? 0 : a.lengths[par];
+  const int64_t n = pages_of(len, a.page_rows);
+  for (int e = threadIdx.x; e < a.t.M; e += NT) {
+    const int old = a.t.at[b * a.t.stride + e];
+    int p = par >= 0 && e < n ? a.t.at[par * a.t.stride + e] : -1;
+    if ((uint32_t)p >= (uint32_t)a.n_pages) p = -1;
+    if ((uint32_t)old < (uint32_t)a.n_pages) count_add(a.refs, old, -1);
+    if (p >= 0) count_add(a.refs, p, 1);
+    tmp[e] = p;
+  }
+  if (threadIdx.x == 0) tmp[a.t.M] = len;
+}
+__global__ __launch_bounds__(NT) void k_pages_forked(ForkArgs a) {
+  const int b = blockIdx.x;
+  const int par = a.parents[b];
+  if (par == b || par >= a.t.B) return;
+  const int32_t* tmp = a.tmp + (int64_t)b * (a.t.M + 1);
+  for (int e = threadIdx.x; e < a.t.M; e += NT) a.t.at[b * a.t.stride + e] = tmp[e];
+  if (threadIdx.x == 0) a.lengths[b] = tmp[a.t.M];
+}
+
+__global__ __launch_bounds__(NT) void k_pages_release(PageTable t, int32_t* refs, const int32_t* lengths, int64_t n_pages, int page_rows) {
+  const int b = blockIdx.x;
+  for (int64_t e = pages_of(lengths[b], page_rows) + threadIdx.x; e < t.M; e += NT) {
+    int32_t* at = t.at + b * t.stride + e;
+    const int p = *at;
+    if (p == -1) continue;
+    if ((uint32_t)p < (uint32_t)n_pages) count_add(refs, p, -1);
+    *at = -1;
+  }
+}
+
+// The used pages' new numbers, in the order of their old ones.
+__global__ __launch_bounds__(BOOK) void k_pages_number(CompactArgs a) {
+  __shared__ uint32_t sums[BOOK / 64];
+  const int tid = threadIdx.x;
+  const int64_t n_pages = a.s.n_pages;
+  uint32_t have = 0;
+  for (int64_t base = 0; base < n_pages; base += 4 * BOOK) {
+    int r[4];
+    uint32_t c = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t p = base + 4 * tid + u;
+      r[u] = p < n_pages ? a.refs[p] : 0;
+      c += r[u] > 0;
+    }
+    uint32_t n, at = have + book_scan(c, sums, &n) - c;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t p = base + 4 * tid + u;
+      if (p < n_pages) a.number[p] = r[u] > 0 ? (int)at : -1;
+      if (r[u] > 0) {
+        if (at < a.n_to) {
+          a.live[at] = (int)p;
+          a.new_refs[at] = r[u];
+        }
+        ++at;
+      }
+    }
+    have += n;
+  }
+  const bool fits = have <= a.n_to;
+  if (tid == 0) {
+    a.live[a.n_to] = fits ? (int)have : 0;
+    *a.missing = fits ? 0 : (int)(have - a.n_to);
+  }
+  __syncthreads();
+  for (int64_t p = (fits ? have : 0) + tid; p < a.n_to; p += BOOK) a.new_refs[p] = 0;
+}
+__global__ __launch_bounds__(NT) void k_pages_move(CompactArgs a, int64_t table_wgs) {
+  const int live = a.live[a.n_to];
+  if (blockIdx.x < table_wgs) {
+    const int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x;
+    if (i >= (int64_t)a.t.B * a.t.M) return;
+    const int p = a.t.at[i / a.t.M * a.t.stride + i % a.t.M];
+    a.new_table[i] = live && (uint32_t)p < (uint32_t)a.s.n_pages ? a.number[p] : -1;
+    return;
+  }
+  const CopyPlace c = copy_place(a.s, blockIdx.x - table_wgs);
+  if (c.page < live) copy_page(a.pool, a.to, a.s, c.kv, c.layer, c.part, a.live[c.page], c.page, a.s.page_rows);
+}
+
+}  // namespace
+
+int64_t pages_workgroups(const PageShape& s, int64_t pages) {
+  return pages * s.layers * 2 * cdiv(s.heads * s.page_rows * s.pieces, PIECES);
+}
+
+size_t reserve_bytes(const PageShape& s, const PageTable& t) {
+  const int64_t entries = (int64_t)t.B * t.M;
+  return up(t.B * sizeof(int4)) + up(entries * 4) + std::min(entries, s.n_pages) * 4;
+}
+hipError_t launch_reserve(ReserveArgs a, void* ws, hipStream_t st) {
+  a.copies = (int4*)ws;
+  a.kind = (int32_t*)((char*)ws + up(a.t.B * sizeof(int4)));
+  a.free_list = (int32_t*)((char*)a.kind + up((size_t)a.t.B * a.t.M * 4));
+  k_pages_reserve<<<1, BOOK, 0, st>>>(a);
+  k_pages_copy<<<(unsigned)pages_workgroups(a.s, a.t.B), NT, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_append(const AppendArgs& a, hipStream_t st) {
+  const int64_t tokens = a.offsets ? a.T : a.T * a.t.B;
+  if (tokens) k_pages_append<<<(unsigned)(tokens * a.s.layers), NT, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_keep(const KeepArgs& a, hipStream_t st) {
+  k_pages_keep<<<(unsigned)(a.t.B * a.s.layers * a.s.heads * 2), NT, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+size_t fork_bytes(const PageTable& t) { return (size_t)t.B * (t.M + 1) * 4; }
+hipError_t launch_fork(ForkArgs a, void* ws, hipStream_t st) {
+  a.tmp = (int32_t*)ws;
+  k_pages_fork<<<a.t.B, NT, 0, st>>>(a);
+  k_pages_forked<<<a.t.B, NT, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_release(const PageTable& t, int32_t* refs, const int32_t* lengths, int64_t n_pages, int page_rows, hipStream_t st) {
+  k_pages_release<<<t.B, NT, 0, st>>>(t, refs, lengths, n_pages, page_rows);
+  return hipGetLastError();
+}
+
+size_t compact_bytes(const PageShape& s, int64_t n_to) { return up(s.n_pages * 4) + (n_to + 1) * 4; }
+hipError_t launch_compact(CompactArgs a, void* ws, hipStream_t st) {
+  a.number = (int32_t*)ws;
+  a.live = (int32_t*)((char*)ws + up(a.s.n_pages * 4));
+  const int64_t table_wgs = cdiv((int64_t)a.t.B * a.t.M, NT);
+  k_pages_number<<<1, BOOK, 0, st>>>(a);
+  k_pages_move<<<(unsigned)(table_wgs + pages_workgroups(a.s, std::min(a.n_to, a.s.n_pages))), NT, 0, st>>>(a, table_wgs);
+  return hipGetLastError();
+}
+
+}  // namespace topk
