@@ -25,7 +25,7 @@ __all__ = ["attn", "attn_dense", "scan_ablation", "probe_mfma", "ffn", "attn_wor
            "mfma_layout", "lib", "TopkError", "LIB_PATH", "profile_begin", "profile_end", "STAGES",
            "attn_backward", "ffn_backward", "rope", "rope_frequencies", "rope_axes", "qk_norm_rope", "qk_norm_rope_append",
            "qk_norm_rope_backward", "attn_prefix", "attn_prefix_workspace_bytes",
-           "pages_reserve", "pages_append", "pages_keep", "pages_fork", "pages_release", "pages_compact", "set_backward_lists", "set_memory_budget", "last_fallback_rows"]
+           "attn_packed", "pages_reserve", "pages_append", "pages_keep", "pages_fork", "pages_release", "pages_compact", "set_backward_lists", "set_memory_budget", "last_fallback_rows"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtopk.so")
 
@@ -48,6 +48,10 @@ class _Rotation(ctypes.Structure):  # topk_rotation
 class _PrefixStrides(ctypes.Structure):  # topk_prefix_strides
     _fields_ = [(n, ctypes.c_int64) for n in ("prefix_k_head", "prefix_k_key", "prefix_v_head", "prefix_v_key", "k_batch",
                                               "k_head", "k_key", "v_batch", "v_head", "v_key")]
+
+
+class _PackedStrides(ctypes.Structure):  # topk_packed_strides
+    _fields_ = [(f"{n}_{s}", ctypes.c_int64) for n in ("q", "k", "v", "out", "d_out", "d_q", "d_k", "d_v") for s in ("head", "token")]
 
 
 class _Pages(ctypes.Structure):  # topk_pages
@@ -105,6 +109,7 @@ def lib() -> ctypes.CDLL:
         "topk_qk_norm_rope_backward_workspace_bytes": ([i64] * 6 + [i32], ctypes.c_size_t),
         "topk_attn_prefix": ([vp] * 8 + [i64] * 7 + [ctypes.POINTER(_PrefixStrides), i32, f32, i32, vp], i32),
         "topk_attn_prefix_workspace_bytes": ([i64] * 7 + [i32], ctypes.c_size_t),
+        "topk_attn_packed": ([vp] * 6 + [i64] * 5 + [ctypes.POINTER(_PackedStrides), i32, f32, i32, vp], i32),
         "topk_pages_reserve": ([pool, vp] + [i64] * 3 + [vp] * 3 + [i64, vp, i32, vp], i32),
         "topk_pages_reserve_workspace_bytes": ([i64] * 3, ctypes.c_size_t),
         "topk_pages_append": ([vp] * 2 + [i64] * 9 + [vp, pool, vp] + [i64] * 3 + [vp, i32, vp], i32),
@@ -644,6 +649,45 @@ def attn_prefix(q, prefix_k, prefix_v, k=None, v=None, lengths=None, causal: boo
     args = (q.data_ptr(), _ptr(prefix_k), _ptr(prefix_v), _ptr(k), _ptr(v), _ptr(lengths), out.data_ptr(), _ptr(sums),
             B, H, Hkv, Lq, P, S, d, st, int(causal), float(scale), dt, _stream_of(device))
     _launch(device, L.topk_attn_prefix, args, nbytes)
+    return (out, sums) if lse else out
+
+
+def _packed(q, k, v, offsets):
+    """Checks of packed heads; (H, Hkv, N, d, address of the offsets, sequences)."""
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError(f"q and k must be [heads, tokens, d], got {tuple(q.shape)} and {tuple(k.shape)}")
+    H, N, d = q.shape
+    Hkv = k.shape[0]
+    _rows(q, "q", (H, N, d), q.dtype, q.device)
+    for t, n in ((k, "k"), (v, "v")):
+        _rows(t, n, (Hkv, N, d), q.dtype, q.device)
+    if offsets.dim() != 1 or offsets.shape[0] < 2:
+        raise ValueError(f"offsets must be one entry more than there are sequences, got {tuple(offsets.shape)}")
+    return H, Hkv, N, d, _ints(offsets, "offsets", offsets.shape[0], q.device), offsets.shape[0] - 1
+
+
+def attn_packed(q, k, v, offsets, causal: bool = True, scale: float | None = None, lse: bool = False):
+    """Attention over every valid key (Eq. 1) of packed sequences: q [H, N, d], k, v [Hkv, N, d], in
+    which tokens offsets[s] .. offsets[s + 1] - 1 are sequence s (int32 [n + 1] on the GPU, not
+    decreasing). A query sees the keys of its own sequence, ``causal``: up to itself. H / Hkv query
+    heads share a key head.
+
+    Returns out [H, N, d], laid out as q (0 for tokens of no sequence); with ``lse`` also the fp32
+    [H, N] logarithm of the sum of exp(scale * score). Heads may have any strides but for the last
+    dimension, multiples of 8 (``x.view(N, heads, d).transpose(0, 1)`` of a projection, or one
+    entry of ``qk_norm_rope``'s). bf16, d = 64 or 128; differentiable as ``layers.packed_attention``."""
+    import torch
+    H, Hkv, N, d, off, n = _packed(q, k, v, offsets)
+    device, dt = q.device, _dtype_code(q)
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    out = torch.empty_like(q)
+    sums = torch.empty((H, N), dtype=torch.float32, device=device) if lse else None
+    st = _PackedStrides(*q.stride()[:2], *k.stride()[:2], *v.stride()[:2], *out.stride()[:2])
+    if N:
+        _launch(device, lib().topk_attn_packed,
+                (q.data_ptr(), k.data_ptr(), v.data_ptr(), off, out.data_ptr(), _ptr(sums), n, N, H, Hkv, d, st, int(causal), float(scale),
+                 dt, _stream_of(device)))
     return (out, sums) if lse else out
 
 

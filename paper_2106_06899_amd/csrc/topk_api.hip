@@ -4,6 +4,7 @@
 #include "topk_attn.h"
 #include "topk_heads.h"
 #include "topk_internal.h"
+#include "topk_packed.h"
 #include "topk_pages.h"
 #include "topk_prefix.h"
 
@@ -935,7 +936,7 @@ int run_prefix(const PrefixProblem& pp, hipStream_t st) {
   return TOPK_OK;
 }
 
-// ---------------------------------------------------------------- pages
+// ---------------------------------------------------------------- packed sequences
 constexpr int64_t MAX_WGS = 0xFFFFFF;  // workgroups of a launch (of 256 threads, fewer than 2^32 in all)
 
 int int_ptr(const void* p, const char* name) {
@@ -944,6 +945,61 @@ int int_ptr(const void* p, const char* name) {
   return TOPK_OK;
 }
 
+int too_many_wgs(int64_t n) {
+  return n > MAX_WGS ? fail(TOPK_E_UNSUPPORTED, "more than 2^24 - 1 workgroups: too many tokens or requests, layers and heads") : TOPK_OK;
+}
+
+int packed_shape(PackedProblem* pp, int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d, int causal, float scale, int dtype) {
+  *pp = PackedProblem{};
+  if (n < 1 || N < 1 || H < 1 || Hkv < 1 || d < 1)
+    return fail(TOPK_E_INVAL, "sizes must be >= 1 (got n = %lld, N = %lld, H = %lld, Hkv = %lld, d = %lld)", (long long)n, (long long)N,
+                (long long)H, (long long)Hkv, (long long)d);
+  if (H % Hkv) return fail(TOPK_E_INVAL, "%lld query heads do not share %lld key heads evenly", (long long)H, (long long)Hkv);
+  if (causal != 0 && causal != 1) return fail(TOPK_E_INVAL, "causal must be 0 or 1");
+  if (!(isfinite(scale) && scale > 0.f)) return fail(TOPK_E_INVAL, "scale must be finite and > 0");
+  if (dtype != TOPK_F32 && dtype != TOPK_BF16) return fail(TOPK_E_INVAL, "dtype must be TOPK_F32 or TOPK_BF16");
+  if (dtype != TOPK_BF16 || (d != 64 && d != 128)) return fail(TOPK_E_UNSUPPORTED, "packed attention runs on bf16 inputs with d = 64 or 128");
+  if (N > int64_t(1) << 30 || n > int64_t(1) << 30) return fail(TOPK_E_UNSUPPORTED, "more than 2^30 tokens or sequences");
+  pp->n = (int)n;
+  pp->N = N;
+  if (H > MAX_WGS / packed_tiles(*pp)) return too_many_wgs(MAX_WGS + 1);
+  pp->H = (int)H;
+  pp->Hkv = (int)Hkv;
+  pp->d = (int)d;
+  pp->causal = causal;
+  pp->scale = scale;
+  return TOPK_OK;
+}
+
+int packed_rows(PackedRows* r, const char* name, const void* p, int64_t head, int64_t token, int64_t heads, int64_t N) {
+  if (heads == 1) head = 0;
+  if (N == 1) token = 0;
+  *r = {(void*)p, head, token};
+  int rc = check_ptr(p, name);
+  if (rc || (rc = stride_ok(name, {head, token}))) return rc;
+  if (head % 8 || token % 8) return fail(TOPK_E_ALIGN, "a stride of %s is not a multiple of 8 elements: %lld, %lld", name, (long long)head, (long long)token);
+  if (token >= int64_t(1) << 24) return fail(TOPK_E_UNSUPPORTED, "the tokens of %s lie 2^24 elements apart or more", name);
+  return TOPK_OK;
+}
+
+int packed_problem(PackedProblem* pp, const void* Q, const void* K, const void* V, const int32_t* offsets, const void* out, const float* lse,
+                   int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d, topk_packed_strides* st, const topk_packed_strides* strides,
+                   int causal, float scale, int dtype) {
+  int rc = packed_shape(pp, n, N, H, Hkv, d, causal, scale, dtype);
+  if (rc) return rc;
+  const int64_t hd = N * d;
+  *st = strides ? *strides : topk_packed_strides{hd, d, hd, d, hd, d, hd, d, hd, d, hd, d, hd, d, hd, d};
+  if ((rc = packed_rows(&pp->q, "Q", Q, st->q_head, st->q_token, H, N)) || (rc = packed_rows(&pp->k, "K", K, st->k_head, st->k_token, Hkv, N)) ||
+      (rc = packed_rows(&pp->v, "V", V, st->v_head, st->v_token, Hkv, N)) ||
+      (rc = packed_rows(&pp->out, "out", out, st->out_head, st->out_token, H, N)) || (rc = int_ptr(offsets, "offsets")))
+    return rc;
+  if (((uintptr_t)lse) % 4) return fail(TOPK_E_ALIGN, "lse is not 4-byte aligned");
+  pp->offsets = offsets;
+  pp->lse = (float*)lse;
+  return TOPK_OK;
+}
+
+// ---------------------------------------------------------------- pages
 int pages_table(PageTable* t, const int32_t* table, int64_t stride, int64_t B, int64_t M) {
   if (B < 1 || M < 1) return fail(TOPK_E_INVAL, "a table needs B >= 1 and M >= 1 (got %lld, %lld)", (long long)B, (long long)M);
   if (B > MAX_WGS || M > 0x7FFFFFFFLL / B) return fail(TOPK_E_UNSUPPORTED, "a table of more than 2^31 - 1 entries or 2^24 - 1 requests");
@@ -986,10 +1042,6 @@ int page_pool(PagePool* pp, PageShape* s, const topk_pages* in, const char* what
       return rc;
   *s = {in->layers, in->heads, in->pages, (int)in->page_rows, (int)(in->d * es / 16), es};
   return TOPK_OK;
-}
-
-int too_many_wgs(int64_t n) {
-  return n > MAX_WGS ? fail(TOPK_E_UNSUPPORTED, "more than 2^24 - 1 workgroups: too many requests, layers and heads") : TOPK_OK;
 }
 
 int pages_done(hipError_t e) {
@@ -1454,6 +1506,18 @@ size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64
   PrefixProblem pp;
   if (prefix_shape(&pp, B, H, Hkv, Lq, P, S, d, 0, 1.f, dtype)) return 0;
   return prefix_bytes(pp, prefix_plan(pp));
+}
+
+int topk_attn_packed(const void* Q, const void* K, const void* V, const int32_t* offsets, void* out, float* lse, int64_t n, int64_t N,
+                     int64_t H, int64_t Hkv, int64_t d, const topk_packed_strides* strides, int causal, float scale, int dtype, void* hip_stream) {
+  g_err.clear();
+  PackedProblem pp;
+  topk_packed_strides t;
+  int rc = packed_problem(&pp, Q, K, V, offsets, out, lse, n, N, H, Hkv, d, &t, strides, causal, scale, dtype);
+  if (rc) return rc;
+  hipStream_t st = (hipStream_t)hip_stream;
+  StageTimer timer(st, ST_SCORE);
+  return pages_done(launch_packed(pp, st));
 }
 
 int topk_pages_reserve(const topk_pages* pool, int32_t* table, int64_t table_stride, int64_t B, int64_t M, int32_t* refs,

@@ -1,0 +1,32 @@
+// Internal interface of packed attention (topk_packed.hip, topk_packed_bwd.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace topk {
+
+// Heads of packed tokens: head h, token t at h * head + t * token elements.
+struct PackedRows {
+  void* p;
+  int64_t head, token;
+};
+
+struct PackedProblem {
+  PackedRows q, k, v, out;
+  PackedRows d_out, dq, dk, dv;  // (backward)
+  float* lse;                    // [H, N], contiguous; NULL: not written
+  const int32_t* offsets;        // [n + 1]
+  int64_t N;
+  int n, H, Hkv, d, causal;
+  float scale;
+  float2* stat;  // (backward) workspace [H, N]: lse to base 2, sum of d_out * out
+};
+
+constexpr int PACKED_TILE = 128;  // rows of a workgroup
+int64_t packed_tiles(const PackedProblem& p);  // workgroups of a head at most, and one for the tokens of no sequence
+size_t packed_backward_bytes(const PackedProblem& p);
+hipError_t launch_packed(const PackedProblem& p, hipStream_t st);
+hipError_t launch_packed_backward(const PackedProblem& p, hipStream_t st);
+
+}  // namespace topk

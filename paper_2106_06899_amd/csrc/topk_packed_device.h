@@ -1,0 +1,130 @@
+// Shared by the forward and the backward pass of packed attention: which rows a workgroup takes, and how
+// tiles of rows come to LDS and are read there.
+#pragma once
+
+#include "topk_device.h"
+#include "topk_packed.h"
+
+namespace topk {
+
+#define TOPK_LDS __attribute__((address_space(3)))
+typedef float f32x16 __attribute__((__vector_size__(64)));
+typedef short s16x4 __attribute__((__vector_size__(8)));
+typedef uint32_t u32x4 __attribute__((__vector_size__(16)));
+typedef TOPK_LDS s16x4 lds_s16x4;
+
+// s_waitcnt immediate: no vector-memory operation outstanding, the other counters ignored
+constexpr int PACKED_WAIT_VM0 = (7 << 4) | (15 << 8);
+
+// the larger, and NaN where either is
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+// the larger of x and what the lane 32 away holds
+__device__ __forceinline__ float other_half_max(float x) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return larger(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+// Of two bf16 numbers, bit 0 and bit 16: is it infinite or NaN?
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) { return (((x & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u; }
+
+// A workgroup's tile: tile `tile` of the sequence of n tokens from token `first` on; n = 0: none.
+struct PackedPlace {
+  int64_t first;
+  int n, tile;
+};
+
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan_full(x), 63); }
+
+// Tile number t of all sequences' tiles of `rows` tokens. levels: up to 64 sequences' tiles are numbered by
+// their place in their sequence, the last places (or, from_end, the first) first: under a causal mask these
+// have the most to do. Every wave finds it by itself.
+__device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int t, int rows, bool levels, bool from_end) {
+  const int lane = threadIdx.x & 63;
+  PackedPlace at = {0, 0, 0};
+  auto bounds = [&](int s, int* a, int* len) {
+    const int N = (int)p.N;
+    *a = min(max(p.offsets[s], 0), N);
+    *len = min(max(p.offsets[s + 1], 0), N) - *a;
+    if (*len < 0) *len = 0;
+  };
+  int s = -1;
+  if (levels && p.n <= 64) {
+    int a, len = 0;
+    if (lane < p.n) bounds(lane, &a, &len);
+    const int nt = (len + rows - 1) / rows;
+    auto longer = [&](int c) { return (int)wave_sum((uint32_t)max(nt - c, 0)); };  // tiles in places from c on
+    if (longer(0) <= t) return at;
+    int lo = 0, hi = (int)((p.N + rows - 1) / rows);  // longer(lo) > t >= longer(hi)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (longer(mid) > t) lo = mid;
+      else hi = mid;
+    }
+    const uint64_t those = __builtin_amdgcn_ballot_w64(nt > lo);
+    const int r = t - longer(lo + 1);
+    const uint64_t mine = __builtin_amdgcn_ballot_w64(nt > lo && (int)lanes_below(those) == r);
+    s = __builtin_ctzll(mine);
+    at.tile = lo;
+  } else {
+    uint32_t before = 0;
+    for (int s0 = 0; s0 < p.n && s < 0; s0 += 64) {
+      int a, len = 0;
+      if (s0 + lane < p.n) bounds(s0 + lane, &a, &len);
+      const uint32_t nt = (len + rows - 1) / rows, end = before + wave_incl_scan_full(nt);
+      const uint64_t those = __builtin_amdgcn_ballot_w64(end > (uint32_t)t);
+      if (those) {
+        const int l = __builtin_ctzll(those);
+        s = s0 + l;
+        at.tile = t - (__builtin_amdgcn_readlane((int)end, l) - __builtin_amdgcn_readlane((int)nt, l));
+      }
+      before = (uint32_t)__builtin_amdgcn_readlane((int)end, 63);
+    }
+    if (s < 0) return at;
+  }
+  int a, len;
+  bounds(s, &a, &len);
+  at.first = __builtin_amdgcn_readfirstlane(a);
+  at.n = __builtin_amdgcn_readfirstlane(len);
+  at.tile = __builtin_amdgcn_readfirstlane(at.tile);
+  if (levels && p.n <= 64 ? from_end : false) at.tile = (at.n + rows - 1) / rows - 1 - at.tile;
+  return at;
+}
+
+// The head and tile number of a workgroup: all heads of a tile number before the next, so that the long
+// tiles of every head start first; where 8 divides the heads, an XCD (every eighth workgroup) takes
+// neighbouring ones, which share key heads.
+__device__ __forceinline__ int2 packed_item(int heads) {
+  const int t = blockIdx.x / heads, r = blockIdx.x % heads;
+  return make_int2(heads % 8 == 0 ? (r % 8) * (heads / 8) + r / 8 : r, t);
+}
+
+// A tile of KEYS rows of D features in LDS, as it lies in memory but for its rows' 16-byte parts, part c of
+// row r at place c ^ swz(r): sixteen rows' equal parts lie in different banks, for reads of whole parts, and four
+// rows' equal halves of pairs of parts, for transposing reads.
+template <int D>
+struct PackedTile {
+  static constexpr int CH = 2 * D / 16;  // parts of a row
+  static __device__ __forceinline__ int swz(int r) {
+    return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  }
+  // sixteen bytes: part c of row r
+  static __device__ __forceinline__ bf16x8 part(const unsigned char* b, int r, int c) {
+    return *(const bf16x8*)(b + r * 2 * D + (c ^ swz(r)) * 16);
+  }
+  // The lane's place for transposing reads of the 32 features f * 32 on: row 4 half + (lane & 15) / 4, 8 bytes of it.
+  static __device__ __forceinline__ int place(int f) {
+    const int lane = threadIdx.x & 63, va = lane & 15, r = 4 * (lane >> 5) + (va >> 2);
+    return r * 2 * D + (((f * 4 + ((lane >> 4) & 1) * 2 + ((va & 3) >> 1)) ^ swz(r)) * 16) + (va & 1) * 8;
+  }
+  // Rows 16 j .. 16 j + 15 of 32 features, transposed: feature lane % 32, rows 8 (e / 4) + 4 (lane / 32) + e % 4.
+  // (swz of rows 8 and 16 further on differs from the lane's by what `hop` says)
+  static __device__ __forceinline__ bf16x8 columns(const unsigned char* b, int place, int j) {
+    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(b + hop(place, 16 * j)));
+    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(b + hop(place, 16 * j + 8)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+  // the place `rows` (a multiple of 8) further on: swz is linear in the bits of r, and rows 8, 16 and 32 add
+  // their bits to it
+  static __device__ __forceinline__ int hop(int place, int rows) { return (place ^ (swz(rows) * 16)) + rows * 2 * D; }
+};
+
+}  // namespace topk

@@ -1,0 +1,216 @@
+"""GPU parity of attention over packed sequences against Eq. 1 in 64 bits.
+
+Tolerance of an output element: half a step of bf16 relative to it, and twice the relative error
+of a weight times sum_j w_j |v_j|. A weight is off by its score's rounding (d products summed in fp32:
+at most (d + 8) 2^-24 sum |q k| scale), by the rounding of the exponent (2^-22 of the largest) and by
+its own to bf16 (2^-8 at most; half a step is 2^-9, and the sum that it is divided by is not rounded).
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2106_06899_amd as tk
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+@pytest.fixture(autouse=True, scope="module")
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    tk.lib()
+    yield
+
+
+def _int(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _inputs(offsets, N, H, Hkv, d, seed=0, std=2.0, tokens=False):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+
+    def normal(heads, std):
+        x = (torch.randn(N, heads, d, generator=gen, device="cuda") * std).to(BF16).transpose(0, 1)
+        return x if tokens else x.contiguous()
+
+    return normal(H, std), normal(Hkv, 1.0), normal(Hkv, 1.0), _int(offsets)
+
+
+def _sequence(q, k, causal, scale):
+    """Scores of one sequence and head in 64 bits, what is hidden, and the size of the scores' terms."""
+    s = q.double() @ k.double().t() * scale
+    n = len(q)
+    hidden = torch.ones(n, n, dtype=torch.bool, device="cuda").triu_(1) if causal else torch.zeros(n, n, dtype=torch.bool, device="cuda")
+    size = (q.double().abs() @ k.double().abs().t()).masked_fill(hidden, 0).amax(-1, keepdim=True) * scale
+    return s.masked_fill(hidden, -math.inf), hidden, size
+
+
+def _check(q, k, v, offsets, causal, scale, out, lse=None):
+    H, N, d = q.shape
+    G = H // k.shape[0]
+    off, worst = offsets.tolist(), 0.0
+    outside = torch.ones(N, dtype=torch.bool, device="cuda")
+    for a, z in zip(off, off[1:]):
+        outside[a:z] = False
+        for h in range(H if z > a else 0):
+            vv = v[h // G, a:z].double()
+            s, hidden, size = _sequence(q[h, a:z], k[h // G, a:z], causal, scale)
+            w = torch.softmax(s, -1)
+            ref = w @ vv
+            delta = ((d + 8) * 2.0 ** -24 + 2.0 ** -22) * size
+            tol = 2.0 ** -8 * ref.abs() + 2 * (delta + 2.0 ** -9) * (w @ vv.abs()) + 1e-37
+            err = (out[h, a:z].double() - ref).abs()
+            assert bool((err <= tol).all()), f"sequence {a}:{z} head {h}: error {float((err / tol).max()):.2f} of its bound"
+            worst = max(worst, float((err / tol).max()))
+            if lse is not None:
+                want = torch.logsumexp(s, -1)
+                assert bool(((lse[h, a:z].double() - want).abs() <= 2 * delta[:, 0] + 2.0 ** -21 * (1 + want.abs())).all())
+    assert not out[:, outside].any()
+    assert lse is None or bool((lse[:, outside] == -math.inf).all())
+    print(f"[case] worst error {worst:.3f} of its bound", flush=True)
+
+
+CASES = {
+    # name: offsets, N, H, Hkv, d, causal
+    "one_token": ([0, 1], 1, 1, 1, 64, True),
+    "one_token_each": ([0, 1, 2, 3], 3, 2, 1, 128, False),
+    "two_tokens": ([0, 2], 2, 8, 8, 128, True),
+    "empty_ones": ([0, 0, 5, 5, 5, 12, 12], 12, 4, 2, 64, True),
+    "only_empty": ([3, 3, 3], 7, 2, 2, 128, True),
+    "outside": ([5, 40, 90], 133, 3, 1, 64, True),
+    "outside_all_keys": ([1, 300], 301, 2, 2, 128, False),
+    "tile_edges": ([0, 63, 127, 255, 256, 320, 449, 705], 705, 2, 1, 64, True),
+    "tile_edges_d128": ([0, 64, 192, 320, 449, 641], 641, 2, 1, 128, True),
+    "tile_edges_all_keys": ([0, 64, 129, 256, 449, 641], 641, 2, 1, 128, False),
+    "odd_groups": ([0, 77, 300], 300, 15, 3, 64, True),
+    "eight_heads": ([0, 130, 201, 700], 700, 16, 4, 128, True),
+    "many": ([i * (i + 1) // 2 for i in range(64)], 2016, 2, 1, 64, True),
+    "more_than_a_wave_of_them": ([i * 7 for i in range(150)], 1043, 2, 2, 64, True),
+    "more_all_keys": ([i * 13 for i in range(70)], 897, 1, 1, 128, False),
+    "long": ([0, 2000, 5003], 5003, 2, 1, 128, True),
+    "long_d64": ([0, 3001, 3002, 5000], 5000, 2, 2, 64, True),
+    "long_all_keys": ([0, 1500, 3333], 3333, 2, 1, 64, False),
+}
+
+
+@pytest.mark.parametrize("name", sorted(CASES))
+@pytest.mark.parametrize("tokens", [False, True])
+def test_packed(name, tokens):
+    offsets, N, H, Hkv, d, causal = CASES[name]
+    q, k, v, off = _inputs(offsets, N, H, Hkv, d, tokens=tokens)
+    out, lse = tk.attn_packed(q, k, v, off, causal, lse=True)
+    assert out.stride() == q.stride()
+    _check(q, k, v, off, causal, d ** -0.5, out, lse)
+    same = torch.equal(tk.attn_packed(q, k, v, off, causal), out)
+    assert same
+
+
+def test_scale_and_large_scores():
+    q, k, v, off = _inputs([0, 200, 333], 333, 2, 1, 64, std=8.0)
+    for scale in (1e-3, 0.7):
+        _check(q, k, v, off, True, scale, *tk.attn_packed(q, k, v, off, scale=scale, lse=True))
+
+
+def test_cut_from_a_projection():
+    """q, k and v as columns of one packed projection; the result as contiguous heads would give it."""
+    H, Hkv, d, N = 4, 2, 64, 300
+    x = torch.randn(N, (H + 2 * Hkv) * d, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(BF16)
+    q, k, v = x.view(N, H + 2 * Hkv, d).transpose(0, 1).split((H, Hkv, Hkv))
+    off = _int([0, 111, 300])
+    out = tk.attn_packed(q, k, v, off)
+    same = torch.equal(out, tk.attn_packed(q.contiguous(), k.contiguous(), v.contiguous(), off))
+    assert same
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("d", [64, 128])
+def test_hidden_rows_may_hold_anything(bad, d):
+    """Later tokens, other sequences and tokens of none hold numbers that are not finite: rows that
+    do not see them are as if they were not there."""
+    off, N = [0, 150, 200, 420], 430
+    q, k, v, o = _inputs(off, N, 2, 1, d, seed=3)
+    want, wl = tk.attn_packed(q, k, v, o, lse=True)
+    k2, v2 = k.clone(), v.clone()
+    for t in (149, 100, 330, 425):
+        v2[0, t, t % d] = bad
+    k2[0, 427] = v2[0, 428] = bad
+    got, gl = tk.attn_packed(q, k2, v2, o, lse=True)
+    same = torch.equal(gl, wl)
+    assert same
+    for a, z, ts in ((0, 150, (100, 149)), (150, 200, ()), (200, 420, (330,))):
+        for i in range(a, z):
+            cols = {t % d for t in ts if t <= i}
+            clean = [f for f in range(d) if f not in cols]
+            assert torch.equal(got[:, i, clean], want[:, i, clean]), i
+            assert all(not got[:, i, f].isfinite().any() for f in cols), i
+    assert not got[:, 420:].any()
+    k3 = k.clone()
+    k3[0, 300] = bad  # a key: rows before it are untouched
+    same = torch.equal(tk.attn_packed(q, k3, v, o)[:, :300], want[:, :300])
+    assert same
+
+
+def test_tiny_weights_and_a_late_maximum():
+    """Weights below 2^-126 still count against large values, before and behind a maximum that leads
+    them by far."""
+    d, n = 64, 200
+    q = torch.zeros(1, n, d, device="cuda", dtype=BF16)
+    k, v = torch.zeros_like(q), torch.zeros_like(q)
+    q[..., 0] = 1
+    for at in (10, 190):
+        k[:] = 0
+        k[0, at, 0] = 88.5
+        v[:] = 2.0 ** 100
+        v[0, at] = 1.0
+        off = _int([0, n])
+        out = tk.attn_packed(q, k, v, off, causal=False, scale=1.0)
+        s = q[0].double() @ k[0].double().t()
+        ref = torch.softmax(s, -1) @ v[0].double()
+        assert bool(((out[0].double() - ref).abs() <= 2.0 ** -7 * ref.abs()).all()), at
+
+
+def test_streams_and_graphs():
+    q, k, v, off = _inputs([0, 90, 400], 400, 4, 2, 128, seed=5)
+    want = tk.attn_packed(q, k, v, off)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = tk.attn_packed(q, k, v, off)
+    torch.cuda.current_stream().wait_stream(s)
+    same = torch.equal(got, want)
+    assert same
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = tk.attn_packed(q, k, v, off)
+    for o in ([0, 90, 400], [0, 5, 300], [7, 333, 400]):
+        off.copy_(_int(o))
+        g.replay()
+        torch.cuda.synchronize()
+        same = torch.equal(out, tk.attn_packed(q, k, v, off))
+        assert same
+
+
+def test_offsets_that_decrease_stay_inside():
+    """No meaningful result, but nothing outside the tensors is read or written."""
+    q, k, v, off = _inputs([0, 200, 100, 300], 300, 2, 1, 64)
+    for o in ([0, 200, 100, 300], [-50, 100, 1000, 3], [2 ** 31 - 1, -2 ** 31, 300, 300]):
+        off.copy_(_int(o))
+        out = tk.attn_packed(q, k, v, off, lse=True)
+        torch.cuda.synchronize()
+        assert out[0].shape == q.shape
+
+
+def test_refused_on_the_gpu():
+    q, k, v, off = _inputs([0, 50], 50, 4, 2, 64)
+    for args in ((q[0], k, v, off), (q, k[:, :40], v, off), (q, k, v, off[:1]), (q, k, v[..., ::2], off), (q.cpu(), k, v, off)):
+        with pytest.raises(ValueError):
+            tk.attn_packed(*args)
+    with pytest.raises(TypeError):
+        tk.attn_packed(q, k, v, off.long())
+    with pytest.raises(TypeError):
+        tk.attn_packed(q, k.float(), v, off)
+    for args in ((q.float(), k.float(), v.float(), off), (q[:3], k, v, off), (q[..., :32], k[..., :32], v[..., :32], off)):
+        with pytest.raises(tk.TopkError):
+            tk.attn_packed(*args)
+    assert tk.attn_packed(q[:, :0], k[:, :0], v[:, :0], off).shape == (4, 0, 64)
