@@ -25,7 +25,7 @@ __all__ = ["attn", "attn_dense", "scan_ablation", "probe_mfma", "ffn", "attn_wor
            "mfma_layout", "lib", "TopkError", "LIB_PATH", "profile_begin", "profile_end", "STAGES",
            "attn_backward", "ffn_backward", "rope", "rope_frequencies", "rope_axes", "qk_norm_rope", "qk_norm_rope_append",
            "qk_norm_rope_backward", "attn_prefix", "attn_prefix_workspace_bytes",
-           "attn_packed", "pages_reserve", "pages_append", "pages_keep", "pages_fork", "pages_release", "pages_compact", "set_backward_lists", "set_memory_budget", "last_fallback_rows"]
+           "attn_packed", "attn_packed_backward", "pages_reserve", "pages_append", "pages_keep", "pages_fork", "pages_release", "pages_compact", "set_backward_lists", "set_memory_budget", "last_fallback_rows"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtopk.so")
 
@@ -110,6 +110,8 @@ def lib() -> ctypes.CDLL:
         "topk_attn_prefix": ([vp] * 8 + [i64] * 7 + [ctypes.POINTER(_PrefixStrides), i32, f32, i32, vp], i32),
         "topk_attn_prefix_workspace_bytes": ([i64] * 7 + [i32], ctypes.c_size_t),
         "topk_attn_packed": ([vp] * 6 + [i64] * 5 + [ctypes.POINTER(_PackedStrides), i32, f32, i32, vp], i32),
+        "topk_attn_packed_backward": ([vp] * 10 + [i64] * 5 + [ctypes.POINTER(_PackedStrides), i32, f32, i32, vp], i32),
+        "topk_attn_packed_backward_workspace_bytes": ([i64] * 5 + [i32], ctypes.c_size_t),
         "topk_pages_reserve": ([pool, vp] + [i64] * 3 + [vp] * 3 + [i64, vp, i32, vp], i32),
         "topk_pages_reserve_workspace_bytes": ([i64] * 3, ctypes.c_size_t),
         "topk_pages_append": ([vp] * 2 + [i64] * 9 + [vp, pool, vp] + [i64] * 3 + [vp, i32, vp], i32),
@@ -689,6 +691,31 @@ def attn_packed(q, k, v, offsets, causal: bool = True, scale: float | None = Non
                 (q.data_ptr(), k.data_ptr(), v.data_ptr(), off, out.data_ptr(), _ptr(sums), n, N, H, Hkv, d, st, int(causal), float(scale),
                  dt, _stream_of(device)))
     return (out, sums) if lse else out
+
+
+def attn_packed_backward(q, k, v, offsets, out, lse, d_out, causal: bool = True, scale: float | None = None):
+    """Gradients (d_q, d_k, d_v) of ``attn_packed``, laid out as q, k and v, from its inputs, what it
+    returned with ``lse`` and the gradient of out (any strides but for the last dimension,
+    multiples of 8). 0 for tokens of no sequence."""
+    import torch
+    H, Hkv, N, d, off, n = _packed(q, k, v, offsets)
+    device, dt = q.device, _dtype_code(q)
+    for t, name in ((out, "out"), (d_out, "d_out")):
+        _rows(t, name, (H, N, d), q.dtype, device)
+    _check(lse, "lse", 2, torch.float32, device)
+    if tuple(lse.shape) != (H, N):
+        raise ValueError(f"lse must have shape {(H, N)}, got {tuple(lse.shape)}")
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    if N:
+        st = _PackedStrides(*(s for t in (q, k, v, out, d_out, dq, dk, dv) for s in t.stride()[:2]))
+        L = lib()
+        _launch(device, L.topk_attn_packed_backward,
+                (q.data_ptr(), k.data_ptr(), v.data_ptr(), off, out.data_ptr(), lse.data_ptr(), d_out.data_ptr(), dq.data_ptr(),
+                 dk.data_ptr(), dv.data_ptr(), n, N, H, Hkv, d, st, int(causal), float(scale), dt, _stream_of(device)),
+                L.topk_attn_packed_backward_workspace_bytes(n, N, H, Hkv, d, dt))
+    return dq, dk, dv
 
 
 def _written(t, name):

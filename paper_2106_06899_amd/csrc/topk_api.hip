@@ -1520,6 +1520,37 @@ int topk_attn_packed(const void* Q, const void* K, const void* V, const int32_t*
   return pages_done(launch_packed(pp, st));
 }
 
+int topk_attn_packed_backward(const void* Q, const void* K, const void* V, const int32_t* offsets, const void* out, const float* lse,
+                              const void* d_out, void* d_Q, void* d_K, void* d_V, int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d,
+                              const topk_packed_strides* strides, int causal, float scale, int dtype, void* hip_stream) {
+  g_err.clear();
+  PackedProblem pp;
+  topk_packed_strides t;
+  int rc = packed_problem(&pp, Q, K, V, offsets, out, lse, n, N, H, Hkv, d, &t, strides, causal, scale, dtype);
+  if (rc) return rc;
+  if ((rc = int_ptr(lse, "lse")) || (rc = packed_rows(&pp.d_out, "d_out", d_out, t.d_out_head, t.d_out_token, H, N)) ||
+      (rc = packed_rows(&pp.dq, "d_Q", d_Q, t.d_q_head, t.d_q_token, H, N)) ||
+      (rc = packed_rows(&pp.dk, "d_K", d_K, t.d_k_head, t.d_k_token, Hkv, N)) ||
+      (rc = packed_rows(&pp.dv, "d_V", d_V, t.d_v_head, t.d_v_token, Hkv, N)))
+    return rc;
+  hipStream_t st = (hipStream_t)hip_stream;
+  Scratch ws;
+  if ((rc = ws.get(packed_backward_bytes(pp), "the backward pass", st))) return rc;
+  pp.stat = (float*)ws.p;
+  hipError_t e;
+  {
+    StageTimer timer(st, ST_BWD);
+    e = launch_packed_backward(pp, st);
+  }
+  ws.release(st);
+  return pages_done(e);
+}
+
+size_t topk_attn_packed_backward_workspace_bytes(int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d, int dtype) {
+  PackedProblem pp;
+  return packed_shape(&pp, n, N, H, Hkv, d, 0, 1.f, dtype) ? 0 : packed_backward_bytes(pp);
+}
+
 int topk_pages_reserve(const topk_pages* pool, int32_t* table, int64_t table_stride, int64_t B, int64_t M, int32_t* refs,
                        const int32_t* lengths, const int32_t* rows_each, int64_t rows, int32_t* missing, int dtype, void* hip_stream) {
   g_err.clear();

@@ -20,7 +20,7 @@ struct PackedProblem {
   int64_t N;
   int n, H, Hkv, d, causal;
   float scale;
-  float2* stat;  // (backward) workspace [H, N]: lse to base 2, sum of d_out * out
+  float* stat;  // (backward) workspace [2, H, N]: lse to base 2; sum of d_out * out
 };
 
 constexpr int PACKED_TILE = 128;  // rows of a workgroup

@@ -77,9 +77,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
 #pragma unroll
   for (int f = 0; f < FB; ++f) o[f] = (f32x16){};
   float m = -INFINITY, l = 0.f;
-  int vat[FB];
-#pragma unroll
-  for (int f = 0; f < FB; ++f) vat[f] = Tile::place(f);
+  const uint32_t kbase = Tile::straight_base(), vbase = Tile::across_base();
 
   // keys that some row of the workgroup sees; those that every row sees; those that the lane's does
   const int keys = CAUSAL ? min(at.n, at.tile * PACKED_TILE + PACKED_TILE) : at.n;
@@ -117,7 +115,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     f32x16 s[2] = {};
     {
       bf16x8 kf[AHEAD_K + 1];
-      auto kp = [&](int i) { return Tile::part(kb + (i & 1) * 32 * 2 * D, n, half * NS + (i >> 1)); };
+      auto kp = [&](int i) { return Tile::straight((const TOPK_LDS unsigned char*)kb, kbase, i & 1, i >> 1); };
 #pragma unroll
       for (int i = 0; i < AHEAD_K; ++i) kf[i] = kp(i);
 #pragma unroll
@@ -155,7 +153,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     }
     constexpr int VM = 4 * FB;
     const float off = m == -INFINITY ? 0.f : m;
-    auto vp = [&](int j) { return Tile::columns(vb, vat[j % FB], j / FB); };  // V^T of 16 keys j / FB, features 32 (j % FB) on
+    auto vp = [&](int j) { return Tile::across((const TOPK_LDS unsigned char*)vb, vbase, j % FB, j / FB); };  // V^T of 16 keys j / FB, features 32 (j % FB) on
     // Weights below 2^-126, which the exponential instruction alone makes 0, are added by themselves where
     // the tile has any.
     if (__builtin_amdgcn_ballot_w64(!(fmaf(low, a.c, -off) >= -126.f))) {

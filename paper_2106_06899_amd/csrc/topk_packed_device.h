@@ -106,25 +106,26 @@ struct PackedTile {
   static __device__ __forceinline__ int swz(int r) {
     return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
   }
-  // sixteen bytes: part c of row r
-  static __device__ __forceinline__ bf16x8 part(const unsigned char* b, int r, int c) {
-    return *(const bf16x8*)(b + r * 2 * D + (c ^ swz(r)) * 16);
+  // Where the lane's reads lie, in bytes from the tile's first: one number each, from which the others
+  // follow by flipping bits, since swz is linear in the bits of a row's number.
+  // Straight: features (D / 2) (lane / 32) + 8 i .. + 7 of row 32 rb + lane % 32, for i and rb that are known.
+  static __device__ __forceinline__ uint32_t straight_base() {
+    const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
+    return n * 2 * D + ((half * (D / 16)) ^ swz(n)) * 16;
   }
-  // The lane's place for transposing reads of the 32 features f * 32 on: row 4 half + (lane & 15) / 4, 8 bytes of it.
-  static __device__ __forceinline__ int place(int f) {
+  static __device__ __forceinline__ bf16x8 straight(const TOPK_LDS unsigned char* b, uint32_t base, int rb, int i) {
+    return *(const TOPK_LDS bf16x8*)(b + (base ^ (i * 16)) + rb * 32 * 2 * D);
+  }
+  // Transposed: feature 32 f + lane % 32 of rows 16 j + 8 (e / 4) + 4 (lane / 32) + e % 4.
+  static __device__ __forceinline__ uint32_t across_base() {
     const int lane = threadIdx.x & 63, va = lane & 15, r = 4 * (lane >> 5) + (va >> 2);
-    return r * 2 * D + (((f * 4 + ((lane >> 4) & 1) * 2 + ((va & 3) >> 1)) ^ swz(r)) * 16) + (va & 1) * 8;
+    return r * 2 * D + (((((lane >> 4) & 1) * 2 + ((va & 3) >> 1)) ^ swz(r)) * 16) + (va & 1) * 8;
   }
-  // Rows 16 j .. 16 j + 15 of 32 features, transposed: feature lane % 32, rows 8 (e / 4) + 4 (lane / 32) + e % 4.
-  // (swz of rows 8 and 16 further on differs from the lane's by what `hop` says)
-  static __device__ __forceinline__ bf16x8 columns(const unsigned char* b, int place, int j) {
-    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(b + hop(place, 16 * j)));
-    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(b + hop(place, 16 * j + 8)));
+  static __device__ __forceinline__ bf16x8 across(const TOPK_LDS unsigned char* b, uint32_t base, int f, int j) {
+    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(b + (base ^ (f * 64) ^ (swz(16 * j) * 16)) + 16 * j * 2 * D));
+    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(b + (base ^ (f * 64) ^ (swz(16 * j + 8) * 16)) + (16 * j + 8) * 2 * D));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
   }
-  // the place `rows` (a multiple of 8) further on: swz is linear in the bits of r, and rows 8, 16 and 32 add
-  // their bits to it
-  static __device__ __forceinline__ int hop(int place, int rows) { return (place ^ (swz(rows) * 16)) + rows * 2 * D; }
 };
 
 }  // namespace topk

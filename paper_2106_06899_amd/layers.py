@@ -15,7 +15,7 @@ import math
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import (attn, attn_backward, attn_dense, attn_prefix, ffn, ffn_backward, qk_norm_rope, qk_norm_rope_append,
+from . import (attn, attn_backward, attn_dense, attn_packed, attn_packed_backward, attn_prefix, ffn, ffn_backward, qk_norm_rope, qk_norm_rope_append,
                qk_norm_rope_backward, rope, rope_axes, rope_frequencies)
 
 
@@ -95,6 +95,33 @@ class NormRotaryHeadsFunction(torch.autograd.Function):
             qkv, heads, kv_heads, d_q.contiguous(), d_k.contiguous(), d_v.contiguous(), q_weight, k_weight, positions, freqs,
             axes, adjacent, eps, norm, weights=any(ctx.needs_input_grad[1:3]))
         return (d_qkv, d_wq, d_wk) + (None,) * 8
+
+
+class PackedAttentionFunction(torch.autograd.Function):
+    """out = attn_packed(q, k, v, offsets), differentiable in q, k and v; the backward recomputes the
+    weights from the inputs and each row's logarithm of their sum."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, offsets, causal: bool, scale: float):
+        out, lse = attn_packed(q, k, v, offsets, causal, scale, lse=True)
+        ctx.save_for_backward(q, k, v, offsets, out, lse)
+        ctx.how = causal, scale
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_out):
+        q, k, v, offsets, out, lse = ctx.saved_tensors
+        if d_out.stride(-1) != 1 or any(s % 8 for s in d_out.stride()[:-1]) or d_out.data_ptr() % 16:
+            d_out = d_out.contiguous()
+        return (*attn_packed_backward(q, k, v, offsets, out, lse, d_out, *ctx.how), None, None, None)
+
+
+def packed_attention(q, k, v, offsets, causal: bool = True, scale: float | None = None):
+    """Differentiable attention over packed sequences; arguments as ``attn_packed``."""
+    if scale is None:
+        scale = 1.0 / math.sqrt(q.shape[-1])
+    return PackedAttentionFunction.apply(q, k, v, offsets, bool(causal), float(scale))
 
 
 def rotary(x, positions, freqs, axes=None, adjacent: bool = False):

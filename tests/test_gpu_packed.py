@@ -3,7 +3,15 @@
 Tolerance of an output element: half a step of bf16 relative to it, and twice the relative error
 of a weight times sum_j w_j |v_j|. A weight is off by its score's rounding (d products summed in fp32:
 at most (d + 8) 2^-24 sum |q k| scale), by the rounding of the exponent (2^-22 of the largest) and by
-its own to bf16 (2^-8 at most; half a step is 2^-9, and the sum that it is divided by is not rounded).
+its own to bf16 (2^-9 at most: the sum that it is divided by is not rounded).
+
+Tolerances of the gradients. With u = 2^-9 (half a step of bf16 relative to the number), w the weights,
+a = d_out v^T and D = d_out . out: a recomputed weight is off by delta' = delta and the rounding of lse
+(2^-21 (1 + |lse|), as tested), D by u |d_out| . |out| (out is stored in bf16) and sums' rounding, and
+ds = w (a - D) by its own rounding u besides; so with e = delta' and A = (d + 8) 2^-24 |d_out| |v|^T
+    dv: half a step of the result, and (u + e) w^T |d_out|
+    dq: half a step, and scale (u + e) |ds| |k| + scale (w (A + u |d_out| . |out| + its sums)) |k|, dk likewise with |q|.
+Every bound is doubled for terms of second order.
 """
 import math
 
@@ -11,6 +19,7 @@ import pytest
 import torch
 
 import paper_2106_06899_amd as tk
+from paper_2106_06899_amd import layers
 
 pytestmark = pytest.mark.gpu
 BF16 = torch.bfloat16
@@ -214,3 +223,181 @@ def test_refused_on_the_gpu():
         with pytest.raises(tk.TopkError):
             tk.attn_packed(*args)
     assert tk.attn_packed(q[:, :0], k[:, :0], v[:, :0], off).shape == (4, 0, 64)
+
+
+def _grad_check(q, k, v, offsets, g, causal, scale, grads, n_heads=None):
+    H, N, d = q.shape
+    Hkv = k.shape[0]
+    G = H // Hkv
+    dq, dk, dv = grads
+    u = 2.0 ** -9
+    outside = torch.ones(N, dtype=torch.bool, device="cuda")
+    off, worst = offsets.tolist(), 0.0
+    for a, z in zip(off, off[1:]):
+        outside[a:z] = False
+        if z <= a:
+            continue
+        for hk in range(Hkv):
+            kk, vv = k[hk, a:z].double(), v[hk, a:z].double()
+            want = [torch.zeros(z - a, d, dtype=torch.float64, device="cuda") for _ in range(2)]
+            tol = [torch.zeros_like(want[0]) for _ in range(2)]
+            for h in range(hk * G, hk * G + G):
+                qq, gg = q[h, a:z].double(), g[h, a:z].double()
+                s, hidden, size = _sequence(q[h, a:z], k[hk, a:z], causal, scale)
+                w = torch.softmax(s, -1)
+                lse = torch.logsumexp(s, -1, keepdim=True)
+                out = w @ vv
+                x = gg @ vv.t()
+                D = (gg * out).sum(-1, keepdim=True)
+                ds = w * (x - D)
+                # (out is off by its weights too: their bound is part of D's)
+                e = 2 * ((d + 8) * 2.0 ** -24 + 2.0 ** -22) * size + 2.0 ** -21 * (1 + lse.abs())
+                out_off = 2.0 ** -9 * out.abs() + 2 * (e + u) * (w @ vv.abs())
+                D_off = (gg.abs() * out_off).sum(-1, keepdim=True) + d * 2.0 ** -24 * (gg.abs() * out.abs()).sum(-1, keepdim=True)
+                A = (d + 8) * 2.0 ** -24 * (gg.abs() @ vv.abs().t())
+                ds_off = ((u + e) * ds.abs() + w * (A + D_off)).masked_fill(hidden, 0)
+                for name, got, ref, t in (("dq", dq[h, a:z], scale * ds @ kk, 2 * scale * ds_off @ kk.abs()),):
+                    t = t + 2.0 ** -8 * ref.abs() + 1e-37
+                    err = (got.double() - ref).abs()
+                    assert bool((err <= t).all()), f"{name} of sequence {a}:{z} head {h}: error {float((err / t).max()):.2f} of its bound"
+                    worst = max(worst, float((err / t).max()))
+                want[0] += scale * ds.t() @ qq
+                tol[0] += 2 * scale * ds_off.t() @ qq.abs()
+                want[1] += w.t() @ gg
+                tol[1] += 2 * ((u + e) * w).t() @ gg.abs()
+            for name, got, ref, t in (("dk", dk[hk, a:z], want[0], tol[0]), ("dv", dv[hk, a:z], want[1], tol[1])):
+                t = t + 2.0 ** -8 * ref.abs() + 1e-37
+                err = (got.double() - ref).abs()
+                assert bool((err <= t).all()), f"{name} of sequence {a}:{z} head {hk}: error {float((err / t).max()):.2f} of its bound"
+                worst = max(worst, float((err / t).max()))
+    for t in grads:
+        assert not t[:, outside].any()
+    print(f"[case] worst gradient error {worst:.3f} of its bound", flush=True)
+
+
+def _gradient(q, k, v, off, causal=True, scale=None, seed=9, tokens=False):
+    g = torch.randn(q.shape[1], q.shape[0], q.shape[2], generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").to(BF16).transpose(0, 1)
+    if not tokens:
+        g = g.contiguous()
+    out, lse = tk.attn_packed(q, k, v, off, causal, scale, lse=True)
+    return g, tk.attn_packed_backward(q, k, v, off, out, lse, g, causal, scale)
+
+
+@pytest.mark.parametrize("name", sorted(CASES))
+@pytest.mark.parametrize("tokens", [False, True])
+def test_packed_backward(name, tokens):
+    offsets, N, H, Hkv, d, causal = CASES[name]
+    q, k, v, off = _inputs(offsets, N, H, Hkv, d, tokens=tokens)
+    g, grads = _gradient(q, k, v, off, causal, tokens=tokens)
+    assert [t.stride() for t in grads] == [t.stride() for t in (q, k, v)]
+    _grad_check(q, k, v, off, g, causal, d ** -0.5, grads)
+    same = all(torch.equal(a, b) for a, b in zip(grads, _gradient(q, k, v, off, causal, tokens=tokens)[1]))
+    assert same
+
+
+def test_gradients_against_differences():
+    """Central differences of the 64-bit definition in a few directions: what the tests above take for the
+    gradient is the gradient."""
+    d, off = 64, [0, 9, 30]
+    q, k, v, o = _inputs(off, 30, 2, 1, d, std=1.0)
+    g, grads = _gradient(q, k, v, o)
+
+    def loss(q, k, v):
+        total = 0.0
+        for a, z in zip(off, off[1:]):
+            for h in range(2):
+                s = q[h, a:z] @ k[0, a:z].t() / 8
+                s = s.masked_fill(torch.ones_like(s, dtype=torch.bool).triu_(1), -math.inf)
+                total += float((torch.softmax(s, -1) @ v[0, a:z] * g[h, a:z].double()).sum())
+        return total
+
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x = [t.double() for t in (q, k, v)]
+    for i in range(3):
+        for _ in range(3):
+            u = torch.randn(x[i].shape, generator=gen, device="cuda", dtype=torch.float64)
+            step = 1e-5
+            up, down = ([t + s * step * u if j == i else t for j, t in enumerate(x)] for s in (1, -1))
+            slope = (loss(*up) - loss(*down)) / (2 * step)
+            got = float((grads[i].double() * u).sum())
+            # each element is within 2^-6 of its size at most, and independent: their sum stays within 2^-6 of the whole
+            assert abs(got - slope) <= 2.0 ** -6 * float((grads[i].double() * u).norm()) + 1e-6, (i, got, slope)
+
+
+def test_autograd_on_layouts_and_broadcast_gradients():
+    """Leaves as tokens, a gradient that is one number expanded, and values that need no gradient."""
+    N, H, Hkv, d = 200, 4, 2, 64
+    off = _int([0, 70, 200])
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(N, H + 2 * Hkv, d, generator=gen, device="cuda").to(BF16).requires_grad_()
+    q, k, v = x.transpose(0, 1).split((H, Hkv, Hkv))
+    out = layers.packed_attention(q, k, v, off)
+    out.sum().backward()
+    ones = torch.ones(H, N, d, dtype=BF16, device="cuda")
+    o, lse = tk.attn_packed(q.detach(), k.detach(), v.detach(), off, lse=True)
+    want = torch.cat(tk.attn_packed_backward(q.detach(), k.detach(), v.detach(), off, o, lse, ones)).transpose(0, 1)
+    same = torch.equal(x.grad, want)
+    assert same
+    y = x.detach().transpose(0, 1)[:H].requires_grad_()
+    (dq,) = torch.autograd.grad(layers.packed_attention(y, k.detach(), v.detach(), off).float().sum(), y)
+    same = torch.equal(dq, want.transpose(0, 1)[:H])
+    assert same
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradients_of_hidden_rows(bad, d):
+    """Numbers that are not finite reach the gradients of what meets them, no other."""
+    off, N = [0, 150, 290], 300
+    q, k, v, o = _inputs(off, N, 2, 1, d, seed=3)
+    g, want = _gradient(q, k, v, o)
+    out, lse = tk.attn_packed(q, k, v, o, lse=True)
+    # d_out of token 100: dq of that token, dk and dv of the keys that it sees
+    g2 = g.clone()
+    g2[:, 100, 5] = bad
+    g2[:, 295] = bad
+    got = tk.attn_packed_backward(q, k, v, o, out, lse, g2)
+    rows = [t for t in range(N) if t != 100]
+    assert torch.equal(got[0][:, rows], want[0][:, rows]) and not got[0][:, 100].isfinite().any()
+    for i in (1, 2):
+        assert torch.equal(got[i][:, 101:], want[i][:, 101:])
+    assert not got[2][:, :101, 5].isfinite().any()
+    cols = [f for f in range(d) if f != 5]
+    assert torch.equal(got[2][:, :, cols], want[2][:, :, cols])
+    # a query of token 100: its output and logarithm with it
+    q2 = q.clone()
+    q2[:, 100, 3] = bad
+    out2, lse2 = tk.attn_packed(q2, k, v, o, lse=True)
+    got = tk.attn_packed_backward(q2, k, v, o, out2, lse2, g)
+    for i in (1, 2):
+        assert torch.equal(got[i][:, 101:], want[i][:, 101:])
+    assert torch.equal(got[0][:, rows], want[0][:, rows])
+    # a key and a value of token 100: rows that do not see them
+    for which in (0, 1):
+        kv = [k.clone(), v.clone()]
+        kv[which][0, 100, 7] = bad
+        out2, lse2 = tk.attn_packed(q, *kv, o, lse=True)
+        got = tk.attn_packed_backward(q, *kv, o, out2, lse2, g)
+        seen = list(range(100)) + list(range(150, N))
+        assert torch.equal(got[0][:, seen], want[0][:, seen])
+        assert torch.equal(got[1][:, 150:], want[1][:, 150:]) and torch.equal(got[2][:, 150:], want[2][:, 150:])
+
+
+def test_backward_in_graphs_and_streams():
+    q, k, v, off = _inputs([0, 90, 400], 400, 4, 2, 128, seed=5)
+    g = _gradient(q, k, v, off)[0]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        _gradient(q, k, v, off)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = tk.attn_packed(q, k, v, off, lse=True)
+        grads = tk.attn_packed_backward(q, k, v, off, out, lse, g)
+    for o in ([0, 90, 400], [0, 5, 300], [7, 333, 400]):
+        off.copy_(_int(o))
+        graph.replay()
+        torch.cuda.synchronize()
+        same = all(torch.equal(a, b) for a, b in zip(grads, _gradient(q, k, v, off)[1]))
+        assert same
