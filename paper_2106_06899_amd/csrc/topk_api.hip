@@ -962,7 +962,7 @@ int packed_shape(PackedProblem* pp, int64_t n, int64_t N, int64_t H, int64_t Hkv
   if (N > int64_t(1) << 30 || n > int64_t(1) << 30) return fail(TOPK_E_UNSUPPORTED, "more than 2^30 tokens or sequences");
   pp->n = (int)n;
   pp->N = N;
-  if (H > MAX_WGS / packed_tiles(*pp)) return too_many_wgs(MAX_WGS + 1);
+  if (H > MAX_WGS / 8 / packed_tiles(*pp)) return too_many_wgs(MAX_WGS + 1);  // (8: the most shares of the backward pass)
   pp->H = (int)H;
   pp->Hkv = (int)Hkv;
   pp->d = (int)d;
@@ -1536,11 +1536,10 @@ int topk_attn_packed_backward(const void* Q, const void* K, const void* V, const
   hipStream_t st = (hipStream_t)hip_stream;
   Scratch ws;
   if ((rc = ws.get(packed_backward_bytes(pp), "the backward pass", st))) return rc;
-  pp.stat = (float*)ws.p;
   hipError_t e;
   {
     StageTimer timer(st, ST_BWD);
-    e = launch_packed_backward(pp, st);
+    e = launch_packed_backward(pp, ws.p, st);
   }
   ws.release(st);
   return pages_done(e);
@@ -1548,7 +1547,7 @@ int topk_attn_packed_backward(const void* Q, const void* K, const void* V, const
 
 size_t topk_attn_packed_backward_workspace_bytes(int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d, int dtype) {
   PackedProblem pp;
-  return packed_shape(&pp, n, N, H, Hkv, d, 0, 1.f, dtype) ? 0 : packed_backward_bytes(pp);
+  return packed_shape(&pp, n, N, H, Hkv, d, 1, 1.f, dtype) ? 0 : packed_backward_bytes(pp);  // (causal: the larger)
 }
 
 int topk_pages_reserve(const topk_pages* pool, int32_t* table, int64_t table_stride, int64_t B, int64_t M, int32_t* refs,

@@ -20,13 +20,16 @@ struct PackedProblem {
   int64_t N;
   int n, H, Hkv, d, causal;
   float scale;
-  float* stat;  // (backward) workspace [2, H, N]: lse to base 2; sum of d_out * out
+  // (backward) workspace
+  float* stat;  // [2, H, N]: lse to base 2; sum of d_out * out
+  float* part;  // splits > 1: [splits, 2, Hkv, N, d] shares of dK and dV
+  int splits;
 };
 
 constexpr int PACKED_TILE = 128;  // rows of a workgroup
 int64_t packed_tiles(const PackedProblem& p);  // workgroups of a head at most, and one for the tokens of no sequence
 size_t packed_backward_bytes(const PackedProblem& p);
 hipError_t launch_packed(const PackedProblem& p, hipStream_t st);
-hipError_t launch_packed_backward(const PackedProblem& p, hipStream_t st);
+hipError_t launch_packed_backward(PackedProblem p, void* ws, hipStream_t st);
 
 }  // namespace topk

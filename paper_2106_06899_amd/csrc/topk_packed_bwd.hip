@@ -126,8 +126,9 @@ __device__ __forceinline__ void apply_marks(f32x16 (&o)[D / 32], const TOPK_LDS 
 }
 
 // 32 rows of a wave, times `by`, through its 16 (D = 128) or 8 KiB of LDS to rows first .. of `to`, those before n.
-template <int D>
-__device__ __forceinline__ void store_rows(const f32x16 (&o)[D / 32], float by, TOPK_LDS f32x4* mine, uint16_t* to, int64_t token, int first, int n) {
+// (T float: as they are, past the cache.)
+template <int D, typename T>
+__device__ __forceinline__ void store_rows(const f32x16 (&o)[D / 32], float by, TOPK_LDS f32x4* mine, T* to, int64_t token, int first, int n) {
   const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
   constexpr int PARTS = D / 4, RPS = 64 / PARTS;
 #pragma unroll
@@ -141,7 +142,9 @@ __device__ __forceinline__ void store_rows(const f32x16 (&o)[D / 32], float by, 
   for (int u = 0; u < 32 / RPS; ++u) {
     const int r = u * RPS + lane / PARTS;
     const f32x4 x = mine[r * PARTS + (part ^ (r & 15))];
-    if (first + r < n) *(uint2*)(to + (first + r) * token + 4 * part) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+    if (first + r >= n) continue;
+    if constexpr (std::is_same<T, float>::value) __builtin_nontemporal_store(x, (f32x4*)(to + (first + r) * token + 4 * part));
+    else *(uint2*)(to + (first + r) * token + 4 * part) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
   }
   wave_sync_lds();
 }
@@ -287,9 +290,11 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dkv(BackwardArgs a) {
   __shared__ __attribute__((aligned(16))) float s1[2 * ROWS];
   __shared__ int flag[WAVES][2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 31, half = lane >> 5;
-  const int2 item = packed_item(a.p.Hkv);
-  const int hk = item.x;
-  if (blockIdx.x >= gridDim.x - a.p.Hkv) {
+  const int splits = a.p.splits;
+  const int2 item = packed_item(a.p.Hkv * splits);
+  const int hk = item.x / splits, split = item.x - hk * splits;
+  if (blockIdx.x >= gridDim.x - a.p.Hkv * splits) {
+    if (splits > 1) return;  // (the sums' launch does it)
     clear_outside<D>(a.p, a.p.dk, hk);
     return clear_outside<D>(a.p, a.p.dv, hk);
   }
@@ -319,15 +324,19 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dkv(BackwardArgs a) {
 #pragma unroll
   for (int f = 0; f < FB; ++f) dk[f] = dv[f] = (f32x16){};
 
-  // query tiles of each head, from the first that sees a key of the workgroup on; all heads' as one list
-  const int first = CAUSAL ? at.tile * (PACKED_TILE / ROWS) : 0, per = (at.n + ROWS - 1) / ROWS - first, tiles = per * G;
+  // query tiles of each head, from the first that sees a key of the workgroup on; of all heads' as one list the
+  // workgroup's share
+  const int first = CAUSAL ? at.tile * (PACKED_TILE / ROWS) : 0, per = (at.n + ROWS - 1) / ROWS - first;
+  const int begin = (int)((int64_t)per * G * split / splits), tiles = (int)((int64_t)per * G * (split + 1) / splits) - begin;
   const Loader<D, LPW> load_q(a.p.q.token), load_g(a.p.d_out.token);
   // the next tile to load: its place in its head, and where its rows lie
-  int next_t = first;
-  const int64_t token = at.first + first * ROWS;
-  const unsigned char* qp = (const unsigned char*)((const uint16_t*)a.p.q.p + hk * G * a.p.q.head + token * a.p.q.token);
-  const unsigned char* gp = (const unsigned char*)((const uint16_t*)a.p.d_out.p + hk * G * a.p.d_out.head + token * a.p.d_out.token);
-  const float* sp = a.p.stat + ((wave & 1) * a.p.H + hk * G) * a.p.N + token;  // lse by the first wave, D by the second
+  const int h = hk * G + begin / per;
+  int next_t = first + begin % per;
+  int t = next_t;  // the current tile's place in its head
+  const int64_t token = at.first + next_t * ROWS;
+  const unsigned char* qp = (const unsigned char*)((const uint16_t*)a.p.q.p + h * a.p.q.head + token * a.p.q.token);
+  const unsigned char* gp = (const unsigned char*)((const uint16_t*)a.p.d_out.p + h * a.p.d_out.head + token * a.p.d_out.token);
+  const float* sp = a.p.stat + ((int64_t)(wave & 1) * a.p.H + h) * a.p.N + token;  // lse by the first wave, D by the second
   auto issue = [&](unsigned char* qd, unsigned char* gd, float* sd) TOPK_INLINE {
     const int left = min(ROWS, at.n - next_t * ROWS) - 1;
     load_q(qp, qd, left, wave);
@@ -409,7 +418,6 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dkv(BackwardArgs a) {
       }
     }
   };
-  int t = first;  // the current tile's place in its head
   // tile i of the list, in the buffers that it is in; the next one's loads go to the others
   __shared__ uint64_t marks[CAUSAL ? NT : 1];
   TOPK_LDS uint64_t* mark = (TOPK_LDS uint64_t*)&marks[tid];
@@ -451,8 +459,36 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dkv(BackwardArgs a) {
                          *p3 = (TOPK_LDS unsigned char*)g1;
   TOPK_LDS f32x4* mine = (TOPK_LDS f32x4*)(wave == 0 ? p0 : wave == 1 ? p1 : wave == 2 ? p2 : p3);
   const int r0 = at.tile * PACKED_TILE + wave * 32;
+  if (splits > 1) {
+    float* part = a.p.part + ((int64_t)(2 * split) * a.p.Hkv + hk) * a.p.N * D + at.first * D;
+    store_rows<D>(dk, a.p.scale, mine, part, D, r0, at.n);
+    store_rows<D>(dv, 1.f, mine, part + a.p.Hkv * a.p.N * D, D, r0, at.n);
+    return;
+  }
   store_rows<D>(dk, a.p.scale, mine, (uint16_t*)a.p.dk.p + hk * a.p.dk.head + at.first * a.p.dk.token, a.p.dk.token, r0, at.n);
   store_rows<D>(dv, 1.f, mine, (uint16_t*)a.p.dv.p + hk * a.p.dv.head + at.first * a.p.dv.token, a.p.dv.token, r0, at.n);
+}
+
+// The sums of a key tile's shares: eight features a thread.
+template <int D>
+__global__ __launch_bounds__(NT) void k_packed_sum(BackwardArgs a) {
+  const int64_t all = a.p.Hkv * a.p.N * (D / 8), i0 = (int64_t)blockIdx.x * NT + threadIdx.x;
+  if (i0 >= 2 * all) return;
+  const bool is_v = i0 >= all;
+  const int64_t i = is_v ? i0 - all : i0, hk = i / (a.p.N * (D / 8)), r = i - hk * (a.p.N * (D / 8)), t = r / (D / 8);
+  const int c = (int)(r % (D / 8)) * 8, N = (int)a.p.N;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+  const int z0 = min(max(a.p.offsets[0], 0), N), z1 = max(z0, min(max(a.p.offsets[a.p.n], 0), N));
+  if (t >= z0 && t < z1) {
+    const float* p = a.p.part + ((is_v ? a.p.Hkv : 0) + hk) * a.p.N * D + t * D + c;
+    for (int s = 0; s < a.p.splits; ++s, p += 2 * a.p.Hkv * a.p.N * D) {
+      x += *(const f32x4*)p;
+      y += *(const f32x4*)(p + 4);
+    }
+  }
+  const PackedRows& to = is_v ? a.p.dv : a.p.dk;
+  *(uint4*)((uint16_t*)to.p + hk * to.head + t * to.token + c) =
+      make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
 }
 
 template <int D, bool CAUSAL>
@@ -460,14 +496,33 @@ void launch_d(const BackwardArgs& a, hipStream_t st) {
   const int64_t rows = a.p.H * a.p.N, per = NT / (D / 8);
   k_packed_stat<D><<<(unsigned)((rows + per - 1) / per), NT, 0, st>>>(a);
   k_packed_dq<D, CAUSAL><<<(unsigned)(packed_tiles(a.p) * a.p.H), NT, 0, st>>>(a);
-  k_packed_dkv<D, CAUSAL><<<(unsigned)(packed_tiles(a.p) * a.p.Hkv), NT, 0, st>>>(a);
+  k_packed_dkv<D, CAUSAL><<<(unsigned)(packed_tiles(a.p) * a.p.Hkv * a.p.splits), NT, 0, st>>>(a);
+  if (a.p.splits > 1) k_packed_sum<D><<<(unsigned)((2 * a.p.Hkv * a.p.N * (D / 8) + NT - 1) / NT), NT, 0, st>>>(a);
 }
 
 }  // namespace
 
-size_t packed_backward_bytes(const PackedProblem& p) { return (size_t)p.H * p.N * 2 * sizeof(float); }
+// Shares of a key tile's queries. With sequences of N / n tokens the longest workgroup goes over (N / n) / 64 tiles
+// of each of G heads, and the chip's 512 (two a CU) over H n (N / n)^2 / 8192 in all, half of it where causal;
+// a tile is shared out until the longest has no more than three quarters of the average, or into SPLITS.
+static int packed_splits(const PackedProblem& p) {
+  constexpr int SPLITS = 8;
+  const double L = (double)p.N / p.n, longest = L / ROWS * (p.H / p.Hkv), all = p.H * p.n * L * L / (ROWS * PACKED_TILE) / (p.causal ? 2 : 1) / 512;
+  int s = 1;
+  while (s < SPLITS && longest / s > 0.75 * all && longest / s > 8) ++s;
+  return s;
+}
 
-hipError_t launch_packed_backward(const PackedProblem& p, hipStream_t st) {
+static size_t stat_bytes(const PackedProblem& p) { return ((size_t)p.H * p.N * 2 * sizeof(float) + 255) / 256 * 256; }
+size_t packed_backward_bytes(const PackedProblem& p) {
+  const int s = packed_splits(p);
+  return stat_bytes(p) + (s > 1 ? (size_t)s * 2 * p.Hkv * p.N * p.d * sizeof(float) : 0);
+}
+
+hipError_t launch_packed_backward(PackedProblem p, void* ws, hipStream_t st) {
+  p.splits = packed_splits(p);
+  p.stat = (float*)ws;
+  p.part = (float*)((char*)ws + stat_bytes(p));
   const BackwardArgs a = {p, p.scale * 1.4426950408889634f};
   if (p.d == 64 && p.causal) launch_d<64, true>(a, st);
   else if (p.d == 64) launch_d<64, false>(a, st);

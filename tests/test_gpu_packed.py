@@ -99,6 +99,9 @@ CASES = {
     "more_all_keys": ([i * 13 for i in range(70)], 897, 1, 1, 128, False),
     "long": ([0, 2000, 5003], 5003, 2, 1, 128, True),
     "long_d64": ([0, 3001, 3002, 5000], 5000, 2, 2, 64, True),
+    "shared_out": ([0, 1100, 1133, 2300], 2310, 4, 1, 128, True),
+    "shared_out_d64": ([3, 1500], 1500, 6, 2, 64, True),
+    "shared_out_all_keys": ([0, 900, 900], 905, 5, 1, 128, False),
     "long_all_keys": ([0, 1500, 3333], 3333, 2, 1, 64, False),
 }
 
