@@ -544,6 +544,38 @@ int topk_pages_compact(const topk_pages* pool, const topk_pages* to, const int32
 size_t topk_pages_compact_workspace_bytes(int64_t pages, int64_t n_to);
 
 /*
+ * topk_attn_tree -- attention (every key that a row sees, Eq. 1) of T drafted tokens of each request over
+ * a cache in pages (see topk_pages). Request b's cache holds lengths[b] rows, the last T of which
+ * are its drafts; a draft sees the rows before the drafts, itself and the drafts that it follows.
+ * With T = 1 that is the step of a single token. H / Hkv query heads share a key head.
+ *
+ *   Q          [B, H, T, d]   contiguous
+ *   pool       keys and values, one layer; read only; heads = Hkv
+ *   table      device, int32 [B, M], row b at b * table_stride: row i of request b lies in page
+ *              table[b][i / page_rows]; NULL: in page b (a cache of one long page a request; M is
+ *              not read). Rows whose entry names no page of the pool are not seen
+ *   lengths    device, int32 [B] (taken into [0, M * page_rows]); the drafts are counted
+ *   parents    device, int32 [B, T], row b at b * parents_stride (0: one tree for all): the draft that
+ *              draft i follows, before it (0 <= p < i); any other number: the text itself. NULL: each
+ *              draft follows the one before it
+ *   out        [B, H, T, d]   written; a row that sees no key is 0
+ *   lse        NULL, or fp32 [B, H, T]: log sum_j exp(scale * s_j), -inf where no key is seen
+ *
+ * bf16 with d = 64 or 128, T <= 64, fewer than 2^24 workgroups (else TOPK_E_UNSUPPORTED). Softmax
+ * statistics and sums in fp32, in a fixed order; a row is computed from its own numbers alone
+ * (drafts that it does not see, and rows behind the request's, may be infinite or NaN). Weights enter
+ * the product with V to 16 significant bits, or, with 64 rows a request and key head ((H / Hkv) * T)
+ * and more, rounded to bf16. The work is laid out on the device by the lengths, so a table may be
+ * wider than any request needs. Workspace: topk_attn_tree_workspace_bytes (M = 1 without a table).
+ * Stages 0 and 3 of the stage timing.
+ */
+int topk_attn_tree(const void* Q, const topk_pages* pool, const int32_t* table, int64_t table_stride, const int32_t* lengths,
+                   const int32_t* parents, int64_t parents_stride, void* out, float* lse, int64_t B, int64_t M, int64_t H,
+                   int64_t T, float scale, int dtype, void* hip_stream);
+size_t topk_attn_tree_workspace_bytes(int64_t B, int64_t M, int64_t page_rows, int64_t H, int64_t Hkv, int64_t T,
+                                      int64_t d, int dtype);
+
+/*
  * Test hook: the number of query rows that the last topk_attn_debug /
  * topk_ffn_debug call on the calling thread selected through a fallback path
  * (rows whose sampled threshold or candidate buffers could not prove the

@@ -25,7 +25,7 @@ __all__ = ["attn", "attn_dense", "scan_ablation", "probe_mfma", "ffn", "attn_wor
            "mfma_layout", "lib", "TopkError", "LIB_PATH", "profile_begin", "profile_end", "STAGES",
            "attn_backward", "ffn_backward", "rope", "rope_frequencies", "rope_axes", "qk_norm_rope", "qk_norm_rope_append",
            "qk_norm_rope_backward", "attn_prefix", "attn_prefix_workspace_bytes",
-           "attn_packed", "attn_packed_backward", "pages_reserve", "pages_append", "pages_keep", "pages_fork", "pages_release", "pages_compact", "set_backward_lists", "set_memory_budget", "last_fallback_rows"]
+           "attn_packed", "attn_packed_backward", "attn_tree", "pages_reserve", "pages_append", "pages_keep", "pages_fork", "pages_release", "pages_compact", "set_backward_lists", "set_memory_budget", "last_fallback_rows"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtopk.so")
 
@@ -112,6 +112,8 @@ def lib() -> ctypes.CDLL:
         "topk_attn_packed": ([vp] * 6 + [i64] * 5 + [ctypes.POINTER(_PackedStrides), i32, f32, i32, vp], i32),
         "topk_attn_packed_backward": ([vp] * 10 + [i64] * 5 + [ctypes.POINTER(_PackedStrides), i32, f32, i32, vp], i32),
         "topk_attn_packed_backward_workspace_bytes": ([i64] * 5 + [i32], ctypes.c_size_t),
+        "topk_attn_tree": ([vp, pool, vp, i64, vp, vp, i64, vp, vp] + [i64] * 4 + [f32, i32, vp], i32),
+        "topk_attn_tree_workspace_bytes": ([i64] * 7 + [i32], ctypes.c_size_t),
         "topk_pages_reserve": ([pool, vp] + [i64] * 3 + [vp] * 3 + [i64, vp, i32, vp], i32),
         "topk_pages_reserve_workspace_bytes": ([i64] * 3, ctypes.c_size_t),
         "topk_pages_append": ([vp] * 2 + [i64] * 9 + [vp, pool, vp] + [i64] * 3 + [vp, i32, vp], i32),
@@ -873,6 +875,53 @@ def pages_release(table, refs, lengths, page_rows: int):
     _launch(device, lib().topk_pages_release,
             (*at, _ints(refs, "refs", refs.shape[0] if refs.dim() == 1 else 0, device), refs.numel(), _ints(lengths, "lengths", at[2], device),
              int(page_rows), _stream_of(device)))
+
+
+def attn_tree(q, k_pages, v_pages, lengths, table=None, parents=None, scale: float | None = None, lse: bool = False):
+    """Attention (Eq. 1) of T drafted tokens q [B, H, T, d] of each request over a cache in pages
+    k_pages, v_pages [pages, Hkv, page_rows, d], of which request b holds ``lengths[b]`` rows (int32
+    [B] on the GPU), the last T of them its drafts. A draft sees the rows before the drafts, itself
+    and the drafts that it follows: ``parents``, int32 [T] or [B, T] on the GPU, names for each the
+    draft before it (anything else than an earlier draft: the text); None: each follows the one before
+    it. T = 1 is the step of a single token. H / Hkv query heads share a key head.
+
+    ``table`` int32 [B, M]: the pages of each request in order (see ``pages_reserve``; it may be wider
+    than any request needs); rows whose entry names no page are not seen. None: request b's rows are
+    page b, as in a cache [B, Hkv, S, d] of one long page a request.
+
+    Returns out [B, H, T, d]; with ``lse`` also the fp32 [B, H, T] logarithm of the sum of exp(scale *
+    score). Pools may have any strides but for the last dimension, multiples of 8. bf16, d = 64 or
+    128, T at most 64. Forward only."""
+    import torch
+    device = q.device
+    _check(q, "q", 4, q.dtype, device)
+    B, H, T, d = q.shape
+    dt = _dtype_code(q)
+    if k_pages.dim() != 4 or k_pages.dtype != q.dtype or k_pages.device != device or k_pages.shape[-1] != d:
+        raise ValueError(f"k_pages must be [pages, heads, rows, {d}] of {q.dtype} on {device}, got {tuple(k_pages.shape)} of {k_pages.dtype} on {k_pages.device}")
+    pool = _pool(k_pages, v_pages, writes=False)
+    if table is None:
+        if pool.pages < B:
+            raise ValueError(f"without a table there must be a page for each of {B} requests, got {pool.pages}")
+        at = (None, 0, B, 1)
+    else:
+        table, at = _page_table(table, device, writes=False)
+        if at[2] != B:
+            raise ValueError(f"table must have {B} rows, got {at[2]}")
+    par, par_stride = None, 0
+    if parents is not None:
+        _rows(parents, "parents", (T,) if parents.dim() == 1 else (B, T), torch.int32, device)
+        par, par_stride = parents.data_ptr(), parents.stride(0) if parents.dim() == 2 and B > 1 else 0
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    out = torch.empty_like(q)
+    sums = torch.empty((B, H, T), dtype=torch.float32, device=device) if lse else None
+    L = lib()
+    _launch(device, L.topk_attn_tree,
+            (q.data_ptr(), pool, at[0], at[1], _ints(lengths, "lengths", B, device), par, par_stride, out.data_ptr(), _ptr(sums), B, at[3], H, T,
+             float(scale), dt, _stream_of(device)),
+            L.topk_attn_tree_workspace_bytes(B, at[3], pool.page_rows, H, pool.heads, T, d, dt))
+    return (out, sums) if lse else out
 
 
 def _span(t):

@@ -23,7 +23,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SOURCES = ["csrc/topk_kernels.hip", "csrc/topk_rows.hip", "csrc/topk_cells.hip", "csrc/topk_few.hip", "csrc/topk_keep.hip",
            "csrc/topk_dense.hip", "csrc/topk_rope.hip", "csrc/topk_prefix.hip",
-           "csrc/topk_packed.hip", "csrc/topk_packed_bwd.hip", "csrc/topk_pages.hip", "csrc/topk_api.hip"]
+           "csrc/topk_packed.hip", "csrc/topk_packed_bwd.hip", "csrc/topk_pages.hip", "csrc/topk_tree.hip", "csrc/topk_api.hip"]
 LIB = os.path.join(PKG, "libtopk.so")
 LIB_CHECK = os.path.join(PKG, "libtopk_check.so")
 LIB_SAN = os.path.join(PKG, "libtopk_san.so")

@@ -7,6 +7,7 @@
 #include "topk_packed.h"
 #include "topk_pages.h"
 #include "topk_prefix.h"
+#include "topk_tree.h"
 
 #include <math.h>
 #include <stdarg.h>
@@ -1049,6 +1050,49 @@ int pages_done(hipError_t e) {
   return TOPK_OK;
 }
 
+// ---------------------------------------------------------------- drafted tokens
+int tree_shape(TreeProblem* tp, int64_t B, int64_t M, int64_t page_rows, int64_t H, int64_t Hkv, int64_t T, int64_t d, float scale, int dtype) {
+  *tp = TreeProblem{};
+  if (B < 1 || M < 1 || page_rows < 1 || H < 1 || Hkv < 1 || T < 1 || d < 1)
+    return fail(TOPK_E_INVAL, "sizes must be >= 1 (got B = %lld, M = %lld, page_rows = %lld, H = %lld, Hkv = %lld, T = %lld, d = %lld)", (long long)B,
+                (long long)M, (long long)page_rows, (long long)H, (long long)Hkv, (long long)T, (long long)d);
+  if (H % Hkv) return fail(TOPK_E_INVAL, "%lld query heads do not share %lld key heads evenly", (long long)H, (long long)Hkv);
+  if (!(isfinite(scale) && scale > 0.f)) return fail(TOPK_E_INVAL, "scale must be finite and > 0");
+  if (dtype != TOPK_F32 && dtype != TOPK_BF16) return fail(TOPK_E_INVAL, "dtype must be TOPK_F32 or TOPK_BF16");
+  if (dtype != TOPK_BF16 || (d != 64 && d != 128)) return fail(TOPK_E_UNSUPPORTED, "attention over pages runs on bf16 inputs with d = 64 or 128");
+  if (T > TREE_MAX) return fail(TOPK_E_UNSUPPORTED, "more than %d drafts a request", TREE_MAX);
+  if (B > MAX_WGS || H > MAX_WGS || M > 0x7FFFFFFFLL || page_rows > 0x7FFFFFFFLL) return fail(TOPK_E_UNSUPPORTED, "more than 2^24 - 1 requests or heads, or 2^31 - 1 pages or rows");
+  tp->B = B;
+  tp->M = M;
+  tp->page_rows = page_rows;
+  tp->H = (int)H;
+  tp->Hkv = (int)Hkv;
+  tp->T = (int)T;
+  tp->d = (int)d;
+  tp->scale = scale;
+  // (the join takes a workgroup a row at most)
+  if (H * T > MAX_WGS / B || tree_workgroups(*tp, tree_plan(*tp)) > MAX_WGS) return too_many_wgs(MAX_WGS + 1);
+  return TOPK_OK;
+}
+
+int run_tree(const TreeProblem& tp, hipStream_t st) {
+  const TreePlan pl = tree_plan(tp);
+  Scratch ws;
+  int rc = ws.get(tree_bytes(tp, pl), "attention over pages", st);
+  if (rc) return rc;
+  hipError_t e;
+  {
+    StageTimer t(st, ST_SCORE);
+    e = launch_tree(tp, pl, ws.p, st);
+  }
+  if (e == hipSuccess) {
+    StageTimer t(st, ST_FINAL);
+    e = launch_tree_join(tp, pl, ws.p, st);
+  }
+  ws.release(st);
+  return pages_done(e);
+}
+
 }  // namespace
 }  // namespace topk
 
@@ -1698,6 +1742,51 @@ size_t topk_pages_compact_workspace_bytes(int64_t pages, int64_t n_to) {
   PageShape s = {};
   s.n_pages = pages;
   return compact_bytes(s, n_to);
+}
+
+int topk_attn_tree(const void* Q, const topk_pages* pool, const int32_t* table, int64_t table_stride, const int32_t* lengths,
+                   const int32_t* parents, int64_t parents_stride, void* out, float* lse, int64_t B, int64_t M, int64_t H, int64_t T,
+                   float scale, int dtype, void* hip_stream) {
+  g_err.clear();
+  TreeProblem tp;
+  PagePool pp;
+  PageShape s;
+  int rc = page_pool(&pp, &s, pool, "the pool", dtype);
+  if (rc) return rc;
+  if (s.layers != 1) return fail(TOPK_E_INVAL, "attention reads one layer's pages (got %lld layers)", (long long)s.layers);
+  if (!table) M = 1;
+  if ((rc = tree_shape(&tp, B, M, s.page_rows, H, s.heads, T, pool->d, scale, dtype))) return rc;
+  if ((rc = check_ptr(Q, "Q")) || (rc = check_ptr(out, "out")) || (rc = int_ptr(lengths, "lengths"))) return rc;
+  if (table) {
+    PageTable t;
+    if ((rc = pages_table(&t, table, table_stride, B, M))) return rc;
+    tp.table = table;
+    tp.table_stride = t.stride;
+  }
+  if (parents) {
+    if ((rc = int_ptr(parents, "parents"))) return rc;
+    if (B > 1 && (parents_stride < 0 || parents_stride >= STRIDE_MAX)) return fail(TOPK_E_INVAL, "parents_stride %lld is out of range", (long long)parents_stride);
+    tp.parents = parents;
+    tp.parents_stride = B > 1 ? parents_stride : 0;
+  }
+  if (((uintptr_t)lse) % 4) return fail(TOPK_E_ALIGN, "lse is not 4-byte aligned");
+  tp.q = Q;
+  tp.out = out;
+  tp.lse = lse;
+  for (int i = 0; i < 2; ++i) {
+    tp.pool[i] = pp.p[i];
+    tp.page[i] = pp.page[i];
+    tp.head[i] = pp.head[i];
+    tp.row[i] = pp.row[i];
+  }
+  tp.lengths = lengths;
+  tp.n_pages = s.n_pages;
+  return run_tree(tp, (hipStream_t)hip_stream);
+}
+
+size_t topk_attn_tree_workspace_bytes(int64_t B, int64_t M, int64_t page_rows, int64_t H, int64_t Hkv, int64_t T, int64_t d, int dtype) {
+  TreeProblem tp;
+  return tree_shape(&tp, B, M, page_rows, H, Hkv, T, d, 1.f, dtype) ? 0 : tree_bytes(tp, tree_plan(tp));
 }
 
 }  // extern "C"
