@@ -735,12 +735,12 @@ def _pool(k_pages, v_pages, writes: bool = True):
         _rows(t, n, shape, k_pages.dtype, k_pages.device)
         if writes:
             _written(t, n)
-    if k_pages.data_ptr() == v_pages.data_ptr():
+    k, v, ks, vs = k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride()[:-1], v_pages.stride()[:-1]
+    if k == v:
         raise ValueError("k_pages and v_pages are the same memory")
-    ks, vs = k_pages.stride()[:-1], v_pages.stride()[:-1]
     if len(shape) == 4:
-        shape, ks, vs = (1, *shape), (0, *ks), (0, *vs)
-    return _Pages(k_pages.data_ptr(), v_pages.data_ptr(), *shape, *ks, *vs)
+        return _Pages(k, v, 1, *shape, 0, *ks, 0, *vs)
+    return _Pages(k, v, *shape, *ks, *vs)
 
 
 def _page_table(table, device, writes: bool = True):
@@ -748,20 +748,25 @@ def _page_table(table, device, writes: bool = True):
     if table.dim() != 2 or 0 in table.shape:
         raise ValueError(f"table must be [requests, pages], got {tuple(table.shape)}")
     import torch
-    _rows(table, "table", table.shape, torch.int32, device)
-    if writes:
-        _written(table, "table")
-    elif table.shape[0] > 1 and table.stride(0) < table.shape[1]:
-        table = table.contiguous()
-    B, M = table.shape
-    return table, (table.data_ptr(), table.stride(0) if B > 1 else M, B, M)
+    B, M = shape = table.shape
+    _rows(table, "table", shape, torch.int32, device)
+    stride = table.stride()[0]
+    if B == 1:
+        stride = M
+    elif stride < M:
+        if writes:
+            raise ValueError("table is written to and must not be expanded")
+        table, stride = table.contiguous(), M
+    return table, (table.data_ptr(), stride, B, M)
 
 
 def _ints(t, name, n, device):
+    """Address of n int32 on the GPU."""
     import torch
-    _check(t, name, 1, torch.int32, device)
-    if t.shape[0] != n:
-        raise ValueError(f"{name} must have {n} entries, got {t.shape[0]}")
+    if not (t.dtype == torch.int32 and t.shape == (n,) and t.device == device and device.type == "cuda" and t.is_contiguous()):
+        _check(t, name, 1, torch.int32, device)
+        if t.shape[0] != n:
+            raise ValueError(f"{name} must have {n} entries, got {t.shape[0]}")
     return t.data_ptr()
 
 

@@ -29,9 +29,11 @@ __device__ __forceinline__ int count_of(const int32_t* refs, int p) { return __h
 __device__ __forceinline__ void count_add(int32_t* refs, int p, int by) {
   __hip_atomic_fetch_add(refs + p, by, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// every access of the workgroup before this is seen by all of it behind
+// Every access of the workgroup before this is done, and seen by all of it behind: they share one vector cache,
+// which stores write through, and atomics are done where they are acknowledged. (A fence for the whole GPU would
+// write its caches back: 27 us a reservation in place of 15.)
 __device__ __forceinline__ void book_sync() {
-  __threadfence();
+  __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // no vector-memory operation outstanding
   __syncthreads();
 }
 
@@ -53,19 +55,26 @@ __device__ __forceinline__ uint32_t book_scan(uint32_t x, uint32_t* sums, uint32
   return before + x;
 }
 
-// The rows [lengths[b], lengths[b] + rows) of each request, as table entries in the order of requests: the
-// workgroup takes BOOK requests at a time, each adding its entries to one list.
+// What becomes of an entry: it stays; it takes a free page; it is one of several that hold its page and is
+// to leave it for a copy.
+enum { STAYS = 0, FRESH = 1, SHARED = 2, LEAVES = 3, KEEPS = 4 };
+
+// The entries of the rows [lengths[b], lengths[b] + rows) of each request, in the order of requests: the workgroup
+// takes BOOK requests at a time, each adding its entries to one list. Where that is one list of at most BOOK
+// entries, each thread has one and keeps it, otherwise their kinds lie in memory.
 struct Entries {
   const ReserveArgs& a;
   uint32_t *ends, *sums;
   int32_t* firsts;
   uint32_t total;
+  bool one;
+  int b, e, page, kind, left;  // one: request (-1: none), entry, its page, what becomes of it, rows in use behind its start
 
   __device__ void load(int base) {
-    const int b = base + threadIdx.x;
+    const int r = base + threadIdx.x;
     int64_t n = 0, first = 0;
-    if (b < a.t.B) {
-      const int64_t len = a.lengths[b], rows = a.rows_each ? a.rows_each[b] : a.rows;
+    if (r < a.t.B) {
+      const int64_t len = a.lengths[r], rows = a.rows_each ? a.rows_each[r] : a.rows;
       if (len >= 0 && rows > 0) {
         first = min(len / a.s.page_rows, (int64_t)a.t.M);
         n = min((len + rows + a.s.page_rows - 1) / a.s.page_rows, (int64_t)a.t.M) - first;
@@ -76,76 +85,105 @@ struct Entries {
     firsts[threadIdx.x] = (int32_t)first;
     __syncthreads();
   }
-  // f(is there one, request, entry), by the whole workgroup
+  __device__ void find(uint32_t i, int base, int* to_b, int* to_e) const {
+    int lo = 0, hi = BOOK - 1;  // the first request whose entries end behind i
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (ends[mid] > i) hi = mid;
+      else lo = mid + 1;
+    }
+    *to_b = base + lo;
+    *to_e = firsts[lo] + (int)(i - (lo ? ends[lo - 1] : 0));
+  }
+  __device__ void begin() {
+    one = false;
+    if (a.t.B > BOOK) return;
+    load(0);
+    one = total <= BOOK;
+    b = -1;
+    if (one && threadIdx.x < total) {
+      find(threadIdx.x, 0, &b, &e);
+      page = a.t.at[b * a.t.stride + e];
+      left = a.lengths[b] - e * a.s.page_rows;
+    }
+  }
+  // f(is there one, its number, its page, its kind to be read and changed, ...), by the whole workgroup
   template <typename F>
   __device__ void each(F f) {
+    if (one) {
+      f(b >= 0, (int)((int64_t)b * a.t.M + e), b, e, page, &kind, left);
+      return;
+    }
     for (int base = 0; base < a.t.B; base += BOOK) {
       if (a.t.B > BOOK) load(base);
       for (uint32_t i0 = 0; i0 < total; i0 += BOOK) {
-        const uint32_t i = i0 + threadIdx.x;
-        int lo = 0, hi = BOOK - 1;  // the first request whose entries end behind i
-        while (lo < hi) {
-          const int mid = (lo + hi) / 2;
-          if (ends[mid] > i) hi = mid;
-          else lo = mid + 1;
+        const bool ok = i0 + threadIdx.x < total;
+        int fb = 0, fe = 0, k = STAYS, p = -1;
+        int64_t number = 0;
+        if (ok) {
+          find(i0 + threadIdx.x, base, &fb, &fe);
+          number = (int64_t)fb * a.t.M + fe;
+          p = a.t.at[fb * a.t.stride + fe];
+          k = a.kind[number];
         }
-        f(i < total, base + lo, firsts[lo] + (int)(i - (lo ? ends[lo - 1] : 0)));
+        const int was = k;
+        f(ok, (int)number, fb, fe, p, &k, ok ? a.lengths[fb] - fe * a.s.page_rows : 0);
+        if (ok && k != was) a.kind[number] = k;
       }
     }
   }
 };
 
-// What becomes of an entry: it stays; it takes a free page; it is one of several that hold its page and is
-// to leave it for a copy.
-enum { STAYS = 0, FRESH = 1, SHARED = 2, LEAVES = 3, KEEPS = 4 };
-
 __global__ __launch_bounds__(BOOK) void k_pages_reserve(ReserveArgs a) {
   __shared__ uint32_t ends[BOOK], sums[BOOK / 64];
-  __shared__ int32_t firsts[BOOK];
+  __shared__ int32_t firsts[BOOK], found[BOOK];
+  __shared__ int any_shared;
   const int tid = threadIdx.x, n_pages = (int)a.s.n_pages;
-  Entries en = {a, ends, sums, firsts, 0};
-  if (a.t.B <= BOOK) en.load(0);
+  Entries en = {a, ends, sums, firsts};
+  if (tid == 0) any_shared = 0;
   for (int b = tid; b < a.t.B; b += BOOK) a.copies[b] = make_int4(0, 0, 0, 0);
-  auto entry = [&](int b, int e) { return a.t.at + b * a.t.stride + e; };
-  auto kind = [&](int b, int e) { return a.kind + (int64_t)b * a.t.M + e; };
-  en.each([&](bool ok, int b, int e) {
-    if (!ok) return;
-    const int p = *entry(b, e);
-    *kind(b, e) = (uint32_t)p >= (uint32_t)n_pages ? FRESH : count_of(a.refs, p) > 1 ? SHARED : STAYS;
-  });
-  book_sync();
-  // Those that leave a page take themselves off its count. Where that leaves nobody, the first (in the order
-  // of requests) stays: it is found as the smallest of their numbers, written into the count itself as a
-  // negative one.
-  en.each([&](bool ok, int b, int e) {
-    if (ok && *kind(b, e) == SHARED) count_add(a.refs, *entry(b, e), -1);
-  });
-  book_sync();
-  en.each([&](bool ok, int b, int e) {
-    if (ok && *kind(b, e) == SHARED && count_of(a.refs, *entry(b, e)) <= 0)
-      __hip_atomic_fetch_min(a.refs + *entry(b, e), INT_MIN + (int)((int64_t)b * a.t.M + e), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  });
-  book_sync();
+  en.begin();
+  __syncthreads();
   uint32_t need = 0;
-  en.each([&](bool ok, int b, int e) {
-    int k = STAYS;
+  en.each([&](bool ok, int, int, int, int p, int* k, int) {
+    *k = -1;  // (whatever is in memory is written over)
     if (ok) {
-      k = *kind(b, e);
-      if (k == SHARED) {
-        k = count_of(a.refs, *entry(b, e)) == INT_MIN + (int)((int64_t)b * a.t.M + e) ? KEEPS : LEAVES;
-        *kind(b, e) = k;
-      }
+      *k = (uint32_t)p >= (uint32_t)n_pages ? FRESH : count_of(a.refs, p) > 1 ? SHARED : STAYS;
+      if (*k == SHARED) any_shared = 1;
     }
     uint32_t n;
-    book_scan(k == FRESH || k == LEAVES, sums, &n);
+    book_scan(*k == FRESH, sums, &n);
     need += n;
   });
   book_sync();
-  en.each([&](bool ok, int b, int e) {  // (a page that its first keeps: 1)
-    if (ok && *kind(b, e) == KEEPS) a.refs[*entry(b, e)] = 1;
-  });
-  book_sync();
+  const bool shared = any_shared;
+  if (shared) {
+    // Those that leave a page take themselves off its count. Where that leaves nobody, the first (in the order
+    // of requests) stays: it is found as the smallest of their numbers, written into the count itself as a
+    // negative one.
+    en.each([&](bool ok, int, int, int, int p, int* k, int) {
+      if (ok && *k == SHARED) count_add(a.refs, p, -1);
+    });
+    book_sync();
+    en.each([&](bool ok, int number, int, int, int p, int* k, int) {
+      if (ok && *k == SHARED && count_of(a.refs, p) <= 0)
+        __hip_atomic_fetch_min(a.refs + p, INT_MIN + number, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    });
+    book_sync();
+    en.each([&](bool ok, int number, int, int, int p, int* k, int) {
+      if (ok && *k == SHARED) *k = count_of(a.refs, p) == INT_MIN + number ? KEEPS : LEAVES;
+      uint32_t n;
+      book_scan(ok && *k == LEAVES, sums, &n);
+      need += n;
+    });
+    book_sync();
+    en.each([&](bool ok, int, int, int, int p, int* k, int) {  // (a page that its first keeps: 1)
+      if (ok && *k == KEEPS) a.refs[p] = 1;
+    });
+    book_sync();
+  }
   // the free pages of the lowest numbers, as many as are needed
+  const bool few = need <= BOOK;
   uint32_t have = 0;
   for (int64_t base = 0; base < n_pages && have < need; base += 4 * BOOK) {
     bool free[4];
@@ -159,112 +197,144 @@ __global__ __launch_bounds__(BOOK) void k_pages_reserve(ReserveArgs a) {
     uint32_t n, at = have + book_scan(c, sums, &n) - c;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (free[u] && at < need) a.free_list[at++] = (int)(base + 4 * tid + u);
+      if (free[u] && at < need) {
+        if (few) found[at++] = (int)(base + 4 * tid + u);
+        else a.free_list[at++] = (int)(base + 4 * tid + u);
+      }
     have += n;
   }
   book_sync();
   if (have < need) {  // nothing is changed: those that left are counted again
     if (tid == 0) *a.missing = (int)(need - have);
-    en.each([&](bool ok, int b, int e) {
-      if (ok && *kind(b, e) == KEEPS) a.refs[*entry(b, e)] = 0;
+    if (!shared) return;
+    en.each([&](bool ok, int, int, int, int p, int* k, int) {
+      if (ok && *k == KEEPS) a.refs[p] = 0;
     });
     book_sync();
-    en.each([&](bool ok, int b, int e) {
-      if (ok && *kind(b, e) >= LEAVES) count_add(a.refs, *entry(b, e), 1);
+    en.each([&](bool ok, int, int, int, int p, int* k, int) {
+      if (ok && *k >= LEAVES) count_add(a.refs, p, 1);
     });
     return;
   }
   if (tid == 0) *a.missing = 0;
   uint32_t taken = 0;
-  en.each([&](bool ok, int b, int e) {
-    const int k = ok ? *kind(b, e) : STAYS;
-    const bool takes = k == FRESH || k == LEAVES;
+  en.each([&](bool ok, int, int b, int e, int p, int* k, int left) {
+    const bool takes = ok && (*k == FRESH || *k == LEAVES);
     uint32_t n;
     const uint32_t at = taken + book_scan(takes, sums, &n) - 1;
     taken += n;
     if (!takes) return;
-    const int p = *entry(b, e), to = a.free_list[at], len = a.lengths[b];
-    const int left = len - e * a.s.page_rows;  // rows of the page that the request has already
-    if (k == LEAVES && left > 0) a.copies[b] = make_int4(p, to, left, 0);
-    *entry(b, e) = to;
+    const int to = few ? found[at] : a.free_list[at];
+    if (*k == LEAVES && left > 0) a.copies[b] = make_int4(p, to, left, 0);  // (`left` rows of the page are in use)
+    a.t.at[b * a.t.stride + e] = to;
     a.refs[to] = 1;
   });
 }
 
-// Where piece i of `rows` rows of a page's heads lies, in elements from the page's first.
-__device__ __forceinline__ int64_t piece_at(const PagePool& pool, int kv, int i, int pieces, int rows, int es) {
-  const int c = i % pieces, r = i / pieces, row = r % rows, head = r / rows;
-  return head * pool.head[kv] + row * pool.row[kv] + c * (16 / es);
-}
-__device__ __forceinline__ uint4* piece_ptr(const PagePool& pool, int kv, int64_t layer, int64_t page, int64_t at, int es) {
-  return (uint4*)((char*)pool.p[kv] + (layer * pool.layer[kv] + page * pool.page[kv] + at) * es);
+__device__ __forceinline__ f32x4* piece_ptr(const PagePool& pool, int kv, int64_t layer, int64_t page, int64_t at, int es) {
+  return (f32x4*)((char*)pool.p[kv] + (layer * pool.layer[kv] + page * pool.page[kv] + at) * es);
 }
 
-// Copies the first `rows` rows of page `from` to page `to`, one part of PIECES pieces of them.
-__device__ __forceinline__ void copy_page(const PagePool& pa, const PagePool& pb, const PageShape& s, int kv, int64_t layer, int part,
-                                          int64_t from, int64_t to, int rows) {
-  const int total = (int)s.heads * rows * s.pieces, i0 = part * PIECES + threadIdx.x;
-  uint4 x[PIECES / NT];
+// Copies the first `rows` rows of every head of page `from` to page `to`, one part of PIECES pieces of them. Piece i is
+// piece i % s.pieces of row i / s.pieces % rows of a head; FLAT: all of a page that lies in one piece in both pools.
+template <bool FLAT>
+__device__ __forceinline__ void copy_page(const PagePool& pa, const PagePool& pb, const PageShape& s, int kv, int layer, int part, int from,
+                                          int to, int rows) {
+  constexpr int U = PIECES / NT;
+  const uint32_t total = (uint32_t)s.heads * rows * s.pieces, i0 = part * PIECES + threadIdx.x;
+  if (part * PIECES >= total) return;
+  const f32x4* src = piece_ptr(pa, kv, layer, from, 0, s.es);
+  f32x4* dst = piece_ptr(pb, kv, layer, to, 0, s.es);
+  const bool whole = (part + 1) * PIECES <= total;
+  if (FLAT) {
+    if (!whole) {
+      for (uint32_t i = i0; i < total; i += NT) dst[i] = src[i];
+      return;
+    }
+    f32x4 x[U];
 #pragma unroll
-  for (int u = 0; u < PIECES / NT; ++u) {
-    const int i = i0 + u * NT;
-    if (i < total) x[u] = *piece_ptr(pa, kv, layer, from, piece_at(pa, kv, i, s.pieces, rows, s.es), s.es);
+    for (int u = 0; u < U; ++u) x[u] = src[i0 + u * NT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) __builtin_nontemporal_store(x[u], dst + i0 + u * NT);
+    return;
+  }
+  // the place of the first piece by division, of the others by steps of NT pieces
+  const uint32_t step_c = NT % s.pieces, step_r = NT / s.pieces;
+  uint32_t c = i0 % s.pieces, row = i0 / s.pieces % rows, head = i0 / s.pieces / rows;
+  auto at = [&](const PagePool& p) { return (head * p.head[kv] + row * p.row[kv]) * s.es + c * 16; };
+  auto step = [&]() {
+    c += step_c;
+    row += step_r;
+    if (c >= (uint32_t)s.pieces) c -= s.pieces, ++row;
+    if (row >= (uint32_t)rows) {
+      head += row / rows;
+      row %= rows;
+    }
+  };
+  if (!whole) {
+    for (uint32_t i = i0; i < total; i += NT, step()) *(f32x4*)((char*)dst + at(pb)) = *(const f32x4*)((const char*)src + at(pa));
+    return;
+  }
+  f32x4 x[U];
+  int64_t to_at[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u, step()) {
+    x[u] = *(const f32x4*)((const char*)src + at(pa));
+    to_at[u] = at(pb);
   }
 #pragma unroll
-  for (int u = 0; u < PIECES / NT; ++u) {
-    const int i = i0 + u * NT;
-    if (i < total) *piece_ptr(pb, kv, layer, to, piece_at(pb, kv, i, s.pieces, rows, s.es), s.es) = x[u];
-  }
+  for (int u = 0; u < U; ++u) *(f32x4*)((char*)dst + to_at[u]) = x[u];
 }
 
 struct CopyPlace {
-  int64_t page, layer;
-  int part, kv;
+  int page, layer, part, kv;
 };
 // the page, layer, pool and part of copying workgroup i
-__device__ __forceinline__ CopyPlace copy_place(const PageShape& s, int64_t i) {
-  const int64_t parts = (s.heads * s.page_rows * s.pieces + PIECES - 1) / PIECES;
+__device__ __forceinline__ CopyPlace copy_place(const PageShape& s, uint32_t i) {
+  const uint32_t parts = ((uint32_t)s.heads * s.page_rows * s.pieces + PIECES - 1) / PIECES, layers = (uint32_t)s.layers;
   CopyPlace c;
   c.part = (int)(i % parts);
   i /= parts;
   c.kv = (int)(i & 1);
   i >>= 1;
-  c.layer = i % s.layers;
-  c.page = i / s.layers;
+  c.layer = (int)(i % layers);
+  c.page = (int)(i / layers);
   return c;
 }
 
 __global__ __launch_bounds__(NT) void k_pages_copy(ReserveArgs a) {
   const CopyPlace c = copy_place(a.s, blockIdx.x);
   const int4 x = a.copies[c.page];
-  if (x.z) copy_page(a.pool, a.pool, a.s, c.kv, c.layer, c.part, x.x, x.y, x.z);
+  if (x.z) copy_page<false>(a.pool, a.pool, a.s, c.kv, c.layer, c.part, x.x, x.y, x.z);
 }
 
 // One token of one layer a workgroup: its keys and values to row lengths[b] + its place in the request.
 __global__ __launch_bounds__(NT) void k_pages_append(AppendArgs a) {
-  const int64_t layer = blockIdx.x % a.s.layers, i = blockIdx.x / a.s.layers;
+  const uint32_t layers = (uint32_t)a.s.layers, layer = blockIdx.x % layers, i = blockIdx.x / layers;
   int64_t b, t, from;
   if (a.offsets) {  // the last request whose first token is not behind i
     int lo = 0, hi = a.t.B;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (a.offsets[mid] <= i) lo = mid;
+      if (a.offsets[mid] <= (int64_t)i) lo = mid;
       else hi = mid;
     }
     b = lo;
-    t = i - a.offsets[b];
-    if (t < 0 || i >= a.offsets[b + 1]) return;
+    t = (int64_t)i - a.offsets[b];
+    if (t < 0 || (int64_t)i >= a.offsets[b + 1]) return;
     from = 0;
   } else {
-    b = i / a.T;
+    b = i / (uint32_t)a.T;
     t = i - b * a.T;
     from = b;
   }
-  const int64_t len = a.lengths[b], r = len + t, e = r / a.s.page_rows;
-  if (len < 0 || e >= a.t.M) return;
+  const int64_t len = a.lengths[b], r = len + t;
+  if (len < 0 || r > INT_MAX) return;
+  const int e = (int)r / a.s.page_rows;
+  if (e >= a.t.M) return;
   const int p = a.t.at[b * a.t.stride + e];
   if ((uint32_t)p >= (uint32_t)a.s.n_pages) return;
-  const int row = (int)(r - e * a.s.page_rows), each = (int)a.s.heads * a.s.pieces;
+  const int row = (int)r - e * a.s.page_rows, each = (int)a.s.heads * a.s.pieces;
   const int64_t token = a.offsets ? i : t;
   for (int x = threadIdx.x; x < 2 * each; x += NT) {
     const int kv = x >= each, y = x - kv * each, head = y / a.s.pieces, c = (y - head * a.s.pieces) * (16 / a.s.es);
@@ -278,10 +348,11 @@ __global__ __launch_bounds__(NT) void k_pages_append(AppendArgs a) {
 __global__ __launch_bounds__(NT) void k_pages_keep(KeepArgs a) {
   __shared__ int2 from[KEEP_MAX], to[KEEP_MAX];  // page (-1: none), row
   __shared__ int count;
-  int64_t i = blockIdx.x;
+  uint32_t i = blockIdx.x;
+  const uint32_t heads = (uint32_t)a.s.heads, layers = (uint32_t)a.s.layers;
   const int kv = (int)(i & 1);
   i >>= 1;
-  const int64_t head = i % a.s.heads, layer = i / a.s.heads % a.s.layers, b = i / a.s.heads / a.s.layers;
+  const uint32_t head = i % heads, rest = i / heads, layer = rest % layers, b = rest / layers;
   const int64_t len = a.lengths[b];
   if (threadIdx.x < 64) {
     const int x = threadIdx.x < a.A ? a.kept[b * a.kept_stride + threadIdx.x] : -1;
@@ -289,12 +360,12 @@ __global__ __launch_bounds__(NT) void k_pages_keep(KeepArgs a) {
     const int n = len < 0 ? 0 : over ? __builtin_ctzll(over) : 64;
     if (threadIdx.x == 0) {
       count = n;
-      if (blockIdx.x % (2 * a.s.heads * a.s.layers) == 0) a.new_lengths[b] = (int32_t)(len + n);
+      if (!kv && !head && !layer) a.new_lengths[b] = (int32_t)(len + n);
     }
     auto place = [&](int64_t r) {
-      const int64_t e = r / a.s.page_rows;
+      const int e = r > INT_MAX ? INT_MAX : (int)r / a.s.page_rows;
       const int p = e < a.t.M ? a.t.at[b * a.t.stride + e] : -1;
-      return make_int2((uint32_t)p < (uint32_t)a.s.n_pages ? p : -1, (int)(r - e * a.s.page_rows));
+      return make_int2((uint32_t)p < (uint32_t)a.s.n_pages ? p : -1, (int)r - e * a.s.page_rows);
     };
     if ((int)threadIdx.x < n) {
       int2 f = place(len + x);
@@ -310,7 +381,7 @@ __global__ __launch_bounds__(NT) void k_pages_keep(KeepArgs a) {
   if (!n) return;
   const int cols = min(a.s.pieces, U * NT / n);  // columns of a slab
   for (int c0 = 0; c0 < a.s.pieces; c0 += cols) {
-    uint4 x[U];
+    f32x4 x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = threadIdx.x + u * NT, r = k / cols, c = c0 + k % cols;
@@ -406,17 +477,18 @@ __global__ __launch_bounds__(BOOK) void k_pages_number(CompactArgs a) {
   __syncthreads();
   for (int64_t p = (fits ? have : 0) + tid; p < a.n_to; p += BOOK) a.new_refs[p] = 0;
 }
-__global__ __launch_bounds__(NT) void k_pages_move(CompactArgs a, int64_t table_wgs) {
+template <bool FLAT>
+__global__ __launch_bounds__(NT) void k_pages_move(CompactArgs a, uint32_t table_wgs) {
   const int live = a.live[a.n_to];
   if (blockIdx.x < table_wgs) {
-    const int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x;
-    if (i >= (int64_t)a.t.B * a.t.M) return;
+    const uint32_t i = blockIdx.x * NT + threadIdx.x;
+    if (i >= (uint32_t)a.t.B * (uint32_t)a.t.M) return;
     const int p = a.t.at[i / a.t.M * a.t.stride + i % a.t.M];
     a.new_table[i] = live && (uint32_t)p < (uint32_t)a.s.n_pages ? a.number[p] : -1;
     return;
   }
   const CopyPlace c = copy_place(a.s, blockIdx.x - table_wgs);
-  if (c.page < live) copy_page(a.pool, a.to, a.s, c.kv, c.layer, c.part, a.live[c.page], c.page, a.s.page_rows);
+  if (c.page < live) copy_page<FLAT>(a.pool, a.to, a.s, c.kv, c.layer, c.part, a.live[c.page], c.page, a.s.page_rows);
 }
 
 }  // namespace
@@ -467,8 +539,16 @@ hipError_t launch_compact(CompactArgs a, void* ws, hipStream_t st) {
   a.number = (int32_t*)ws;
   a.live = (int32_t*)((char*)ws + up(a.s.n_pages * 4));
   const int64_t table_wgs = cdiv((int64_t)a.t.B * a.t.M, NT);
+  const unsigned grid = (unsigned)(table_wgs + pages_workgroups(a.s, std::min(a.n_to, a.s.n_pages)));
+  bool flat = true;  // (a stride along one entry is 0)
+  for (const PagePool* p : {&a.pool, &a.to})
+    for (int i = 0; i < 2; ++i) {
+      const int64_t d = a.s.pieces * (16 / a.s.es);
+      flat &= (a.s.page_rows == 1 || p->row[i] == d) && (a.s.heads == 1 || p->head[i] == d * a.s.page_rows);
+    }
   k_pages_number<<<1, BOOK, 0, st>>>(a);
-  k_pages_move<<<(unsigned)(table_wgs + pages_workgroups(a.s, std::min(a.n_to, a.s.n_pages))), NT, 0, st>>>(a, table_wgs);
+  if (flat) k_pages_move<true><<<grid, NT, 0, st>>>(a, (uint32_t)table_wgs);
+  else k_pages_move<false><<<grid, NT, 0, st>>>(a, (uint32_t)table_wgs);
   return hipGetLastError();
 }
 

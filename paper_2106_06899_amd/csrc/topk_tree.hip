@@ -48,6 +48,7 @@ struct TreeArgs {
   TreePlan pl;
   float* po;   // [ranges][Hkv][rows][D]
   float2* ml;  // [ranges][Hkv][rows]: maximum of the scaled scores (to base 2), sum of weights
+  int2* info;  // [B]: a request's first range, how many it has
   float c;     // scale * log2(e)
   uint32_t magic;  // floor(2^16 / page_rows) + 1
 };
@@ -84,6 +85,7 @@ __device__ __forceinline__ uint32_t ranges_of(int64_t keys, uint32_t units) {
 struct TreeRange {
   int b;        // request; -1: there is none
   int of;       // ranges of the request
+  int which;    // this one's place among them
   int first;    // this one's first key
   int n;        // its keys
   int len;      // the request's
@@ -92,7 +94,7 @@ struct TreeRange {
 __device__ __forceinline__ TreeRange find_range(const TreeArgs& a, uint32_t w) {
   const int lane = threadIdx.x & 63;
   const uint32_t units = range_units(a);
-  TreeRange r = {-1, 0, 0, 0, 0};
+  TreeRange r = {-1, 0, 0, 0, 0, 0};
   uint32_t before = 0, mine = 0;
   if (!a.pl.ranges) {
     r.b = (int)w;
@@ -110,6 +112,7 @@ __device__ __forceinline__ TreeRange find_range(const TreeArgs& a, uint32_t w) {
     if (r.b < 0) return r;
   }
   const int64_t len = keys_of(a.p, r.b), first = (int64_t)mine * units * UNIT;
+  r.which = __builtin_amdgcn_readfirstlane((int)mine);
   r.len = __builtin_amdgcn_readfirstlane((int)len);
   r.of = __builtin_amdgcn_readfirstlane((int)ranges_of(len, units));
   r.first = __builtin_amdgcn_readfirstlane((int)first);
@@ -735,47 +738,66 @@ __global__ __launch_bounds__(NT, 2) void k_tree(TreeArgs a) {
   it.r = find_range(a, i);
   if (it.r.b < 0) return;
   it.slot = ((int64_t)i * a.p.Hkv + it.h) * it.R;
+  if (a.pl.ranges && !it.r.which && !it.h && !it.r0 && threadIdx.x == 0) a.info[it.r.b] = make_int2(i, it.r.of);
   TreeForm<D, F>::type::run(a, it, sh);
 }
 
-// Joins a row's partial results, where there are several. ROWS rows a workgroup: D / 4 threads take four features
-// each, by as many groups as there are left, each taking every so manieth range.
+// Joins a row's partial results, where there are several. ROWS rows a workgroup: TR threads a row, D / 4 of which take
+// four features each, by as many groups as there are left, each taking every so manieth range. The ranges' factors
+// come first, a thread a range.
 template <int D, int ROWS>
 __global__ __launch_bounds__(NT) void k_tree_join(TreeArgs a) {
-  constexpr int LR = D / 4, Q = NT / ROWS / LR;
+  constexpr int TR = NT / ROWS, LR = D / 4, Q = TR / LR, WPR = TR / 64;  // WPR: waves of a row
   static_assert(Q >= 1, "a thread has at least one column group");
-  __shared__ f32x4 part[Q][ROWS][LR];
-  const int q = threadIdx.x / (ROWS * LR), rl = threadIdx.x / LR % ROWS, c = threadIdx.x % LR;
+  __shared__ float fac[ROWS][TR], most[4], sums[4];
+  __shared__ f32x4 part[ROWS][Q][LR];
+  const int rl = threadIdx.x / TR, tr = threadIdx.x % TR, q = tr / LR, c = tr % LR;
   const int R = a.p.H / a.p.Hkv * a.p.T, per = (R + ROWS - 1) / ROWS;
   const int r = blockIdx.x % per * ROWS + rl, i = blockIdx.x / per, h = i % a.p.Hkv, b = i / a.p.Hkv;
-  // the request's ranges, and those before it
-  const uint32_t units = range_units(a);
-  const uint32_t of = ranges_of(keys_of(a.p, b), units);
+  const int2 info = a.info[b];
+  const int of = info.y;
   if (of == 1) return;
-  uint64_t before = 0;
-  for (int x = threadIdx.x & 63; x < b; x += 64) before += ranges_of(keys_of(a.p, x), units);
-  before = wave_sum64(before);
   const bool ok = r < R;
-  const int64_t at = ((int64_t)before * a.p.Hkv + h) * R + (ok ? r : 0), step = (int64_t)a.p.Hkv * R;
-  float top = -INFINITY;
-  for (uint32_t s = c; s < of; s += LR) top = larger(top, a.ml[at + s * step].x);
+  const int64_t at = ((int64_t)info.x * a.p.Hkv + h) * R + (ok ? r : 0), step = (int64_t)a.p.Hkv * R;
+  const float2 mine = tr < of ? a.ml[at + tr * step] : make_float2(-INFINITY, 0.f);
+  float top = mine.x;
+  for (int s = TR + tr; s < of; s += TR) top = larger(top, a.ml[at + s * step].x);
 #pragma unroll
-  for (int o = 1; o < LR; o <<= 1) top = larger(top, __shfl_xor(top, o, 64));
+  for (int o = 1; o < (TR < 64 ? TR : 64); o <<= 1) top = larger(top, __shfl_xor(top, o, 64));
+  if (WPR > 1) {
+    if (threadIdx.x % 64 == 0) most[threadIdx.x / 64] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WPR; ++w) top = larger(top, most[w]);
+  }
   float total = 0.f;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (uint32_t s = 0; s < of; ++s) {
-    const float2 x = a.ml[at + s * step];
+  for (int s0 = 0; s0 < of; s0 += TR) {
+    const int s = s0 + tr;
+    const float2 x = s0 == 0 ? mine : s < of ? a.ml[at + s * step] : make_float2(-INFINITY, 0.f);
     const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - top);
     total = fmaf(f, x.y, total);
-    if (s % Q == q) sum += *(const f32x4*)(a.po + (at + s * step) * D + 4 * c) * f;  // (a range without keys leaves zeros)
+    __syncthreads();
+    fac[rl][tr] = f;
+    __syncthreads();
+    const float* p = a.po + (at + s0 * step) * D + 4 * c;
+#pragma unroll 4
+    for (int k = q; k < min(TR, of - s0); k += Q) sum += *(const f32x4*)(p + k * step * D) * fac[rl][k];  // (a range without keys leaves zeros)
   }
+#pragma unroll
+  for (int o = 1; o < (TR < 64 ? TR : 64); o <<= 1) total += __shfl_xor(total, o, 64);
   if (Q > 1) {
-    part[q][rl][c] = sum;
+    part[rl][q][c] = sum;
+    if (WPR > 1 && threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = total;
     __syncthreads();
     if (q > 0) return;
 #pragma unroll
-    for (int k = 1; k < Q; ++k) sum += part[k][rl][c];
+    for (int k = 1; k < Q; ++k) sum += part[rl][k][c];
+    if (WPR > 1) {
+      total = 0.f;
+#pragma unroll
+      for (int w = 0; w < WPR; ++w) total += sums[w];
+    }
   }
   if (!ok) return;
   const int64_t to = ((int64_t)b * a.p.H + h * (a.p.H / a.p.Hkv)) * a.p.T + r;
@@ -793,6 +815,7 @@ TreeArgs args_for(const TreeProblem& p, const TreePlan& pl, const void* ws) {
   a.pl = pl;
   a.po = (float*)ws;
   a.ml = (float2*)((char*)ws + (size_t)(pl.ranges + p.B) * p.Hkv * rows_of(p) * p.d * 4);
+  a.info = (int2*)(a.ml + (size_t)(pl.ranges + p.B) * p.Hkv * rows_of(p));
   a.c = p.scale * 1.4426950408889634f;
   a.magic = (uint32_t)(65536 / std::min<int64_t>(p.page_rows, 65536) + 1);
   return a;
@@ -816,7 +839,7 @@ TreePlan tree_plan(const TreeProblem& p) {
 
 int64_t tree_workgroups(const TreeProblem& p, const TreePlan& pl) { return (pl.ranges + p.B) * p.Hkv * pl.tiles; }
 size_t tree_bytes(const TreeProblem& p, const TreePlan& pl) {
-  return pl.ranges ? (size_t)(pl.ranges + p.B) * p.Hkv * rows_of(p) * (p.d + 2) * 4 : 0;
+  return pl.ranges ? (size_t)(pl.ranges + p.B) * p.Hkv * rows_of(p) * (p.d + 2) * 4 + p.B * sizeof(int2) : 0;
 }
 
 template <int D>
