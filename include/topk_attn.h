@@ -449,14 +449,15 @@ size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64
  *   offsets    device, int32 [n + 1], not decreasing, within [0, N]; a sequence may be empty
  *   out        [H, N, d]   written, with strides of its own; tokens of no sequence are 0
  *   lse        NULL, or fp32 [H, N]: log sum_j exp(scale * s_j); -inf for tokens of no sequence
+ *   rest       NULL, or laid out as out: what rounding took from it, for the backward pass
  *
  * bf16 with d = 64 or 128 (else TOPK_E_UNSUPPORTED). Scores, softmax statistics and sums in fp32, in a
  * fixed order; weights enter the product with V rounded to bf16. A row is computed from its own
  * numbers alone: keys and values it does not see may be infinite or NaN. No workspace. Offsets that
  * decrease give no meaningful result, but no access outside the tensors.
  *
- * topk_attn_packed_backward -- its gradients, from the inputs, out and lse (required here) of the
- * forward call and d_out [H, N, d]: d_Q [H, N, d], d_K, d_V [Hkv, N, d], every element written (tokens of
+ * topk_attn_packed_backward -- its gradients, from the inputs, out, lse (required here) and rest (NULL: taken as
+ * 0, which costs d_Q and d_K a little of their precision) of the forward call and d_out [H, N, d]: d_Q [H, N, d], d_K, d_V [Hkv, N, d], every element written (tokens of
  * no sequence: 0). The weights are recomputed from lse; those below 2^-126 count as 0. Score gradients and
  * weights enter their products rounded to bf16; sums in fp32, in a fixed order, over the query
  * heads that share a key head too. d_out may be strided like the others. Workspace:
@@ -467,10 +468,10 @@ typedef struct {
   int64_t d_out_head, d_out_token, d_q_head, d_q_token, d_k_head, d_k_token, d_v_head, d_v_token;  /* backward only */
 } topk_packed_strides;
 int topk_attn_packed(const void* Q, const void* K, const void* V, const int32_t* offsets, void* out, float* lse,
-                     int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d, const topk_packed_strides* strides,
+                     void* rest, int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d, const topk_packed_strides* strides,
                      int causal, float scale, int dtype, void* hip_stream);
 int topk_attn_packed_backward(const void* Q, const void* K, const void* V, const int32_t* offsets, const void* out,
-                              const float* lse, const void* d_out, void* d_Q, void* d_K, void* d_V, int64_t n, int64_t N,
+                              const float* lse, const void* rest, const void* d_out, void* d_Q, void* d_K, void* d_V, int64_t n, int64_t N,
                               int64_t H, int64_t Hkv, int64_t d, const topk_packed_strides* strides, int causal,
                               float scale, int dtype, void* hip_stream);
 size_t topk_attn_packed_backward_workspace_bytes(int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d, int dtype);

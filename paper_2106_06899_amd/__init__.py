@@ -109,8 +109,8 @@ def lib() -> ctypes.CDLL:
         "topk_qk_norm_rope_backward_workspace_bytes": ([i64] * 6 + [i32], ctypes.c_size_t),
         "topk_attn_prefix": ([vp] * 8 + [i64] * 7 + [ctypes.POINTER(_PrefixStrides), i32, f32, i32, vp], i32),
         "topk_attn_prefix_workspace_bytes": ([i64] * 7 + [i32], ctypes.c_size_t),
-        "topk_attn_packed": ([vp] * 6 + [i64] * 5 + [ctypes.POINTER(_PackedStrides), i32, f32, i32, vp], i32),
-        "topk_attn_packed_backward": ([vp] * 10 + [i64] * 5 + [ctypes.POINTER(_PackedStrides), i32, f32, i32, vp], i32),
+        "topk_attn_packed": ([vp] * 7 + [i64] * 5 + [ctypes.POINTER(_PackedStrides), i32, f32, i32, vp], i32),
+        "topk_attn_packed_backward": ([vp] * 11 + [i64] * 5 + [ctypes.POINTER(_PackedStrides), i32, f32, i32, vp], i32),
         "topk_attn_packed_backward_workspace_bytes": ([i64] * 5 + [i32], ctypes.c_size_t),
         "topk_attn_tree": ([vp, pool, vp, i64, vp, vp, i64, vp, vp] + [i64] * 4 + [f32, i32, vp], i32),
         "topk_attn_tree_workspace_bytes": ([i64] * 7 + [i32], ctypes.c_size_t),
@@ -670,14 +670,15 @@ def _packed(q, k, v, offsets):
     return H, Hkv, N, d, _ints(offsets, "offsets", offsets.shape[0], q.device), offsets.shape[0] - 1
 
 
-def attn_packed(q, k, v, offsets, causal: bool = True, scale: float | None = None, lse: bool = False):
+def attn_packed(q, k, v, offsets, causal: bool = True, scale: float | None = None, lse: bool = False, rest: bool = False):
     """Attention over every valid key (Eq. 1) of packed sequences: q [H, N, d], k, v [Hkv, N, d], in
     which tokens offsets[s] .. offsets[s + 1] - 1 are sequence s (int32 [n + 1] on the GPU, not
     decreasing). A query sees the keys of its own sequence, ``causal``: up to itself. H / Hkv query
     heads share a key head.
 
     Returns out [H, N, d], laid out as q (0 for tokens of no sequence); with ``lse`` also the fp32
-    [H, N] logarithm of the sum of exp(scale * score). Heads may have any strides but for the last
+    [H, N] logarithm of the sum of exp(scale * score), and with ``rest`` also what rounding took from
+    out, laid out as it (both for the backward pass). Heads may have any strides but for the last
     dimension, multiples of 8 (``x.view(N, heads, d).transpose(0, 1)`` of a projection, or one
     entry of ``qk_norm_rope``'s). bf16, d = 64 or 128; differentiable as ``layers.packed_attention``."""
     import torch
@@ -687,23 +688,31 @@ def attn_packed(q, k, v, offsets, causal: bool = True, scale: float | None = Non
         scale = 1.0 / math.sqrt(d)
     out = torch.empty_like(q)
     sums = torch.empty((H, N), dtype=torch.float32, device=device) if lse else None
+    took = torch.empty_like(out) if rest else None
     st = _PackedStrides(*q.stride()[:2], *k.stride()[:2], *v.stride()[:2], *out.stride()[:2])
     if N:
         _launch(device, lib().topk_attn_packed,
-                (q.data_ptr(), k.data_ptr(), v.data_ptr(), off, out.data_ptr(), _ptr(sums), n, N, H, Hkv, d, st, int(causal), float(scale),
-                 dt, _stream_of(device)))
-    return (out, sums) if lse else out
+                (q.data_ptr(), k.data_ptr(), v.data_ptr(), off, out.data_ptr(), _ptr(sums), _ptr(took), n, N, H, Hkv, d, st, int(causal),
+                 float(scale), dt, _stream_of(device)))
+    if not (lse or rest):
+        return out
+    return (out, *(t for t in (sums, took) if t is not None))
 
 
-def attn_packed_backward(q, k, v, offsets, out, lse, d_out, causal: bool = True, scale: float | None = None):
+def attn_packed_backward(q, k, v, offsets, out, lse, d_out, causal: bool = True, scale: float | None = None, rest=None):
     """Gradients (d_q, d_k, d_v) of ``attn_packed``, laid out as q, k and v, from its inputs, what it
-    returned with ``lse`` and the gradient of out (any strides but for the last dimension,
-    multiples of 8). 0 for tokens of no sequence."""
+    returned with ``lse`` (and ``rest``, without which d_q and d_k lose a little precision) and the
+    gradient of out (any strides but for the last dimension, multiples of 8). 0 for tokens of no
+    sequence."""
     import torch
     H, Hkv, N, d, off, n = _packed(q, k, v, offsets)
     device, dt = q.device, _dtype_code(q)
     for t, name in ((out, "out"), (d_out, "d_out")):
         _rows(t, name, (H, N, d), q.dtype, device)
+    if rest is not None:
+        _rows(rest, "rest", (H, N, d), q.dtype, device)
+        if rest.stride() != out.stride():
+            raise ValueError(f"rest must be laid out as out, {out.stride()}, got {rest.stride()}")
     _check(lse, "lse", 2, torch.float32, device)
     if tuple(lse.shape) != (H, N):
         raise ValueError(f"lse must have shape {(H, N)}, got {tuple(lse.shape)}")
@@ -714,8 +723,8 @@ def attn_packed_backward(q, k, v, offsets, out, lse, d_out, causal: bool = True,
         st = _PackedStrides(*(s for t in (q, k, v, out, d_out, dq, dk, dv) for s in t.stride()[:2]))
         L = lib()
         _launch(device, L.topk_attn_packed_backward,
-                (q.data_ptr(), k.data_ptr(), v.data_ptr(), off, out.data_ptr(), lse.data_ptr(), d_out.data_ptr(), dq.data_ptr(),
-                 dk.data_ptr(), dv.data_ptr(), n, N, H, Hkv, d, st, int(causal), float(scale), dt, _stream_of(device)),
+                (q.data_ptr(), k.data_ptr(), v.data_ptr(), off, out.data_ptr(), lse.data_ptr(), _ptr(rest), d_out.data_ptr(),
+                 dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), n, N, H, Hkv, d, st, int(causal), float(scale), dt, _stream_of(device)),
                 L.topk_attn_packed_backward_workspace_bytes(n, N, H, Hkv, d, dt))
     return dq, dk, dv
 

@@ -984,7 +984,7 @@ int packed_rows(PackedRows* r, const char* name, const void* p, int64_t head, in
 }
 
 int packed_problem(PackedProblem* pp, const void* Q, const void* K, const void* V, const int32_t* offsets, const void* out, const float* lse,
-                   int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d, topk_packed_strides* st, const topk_packed_strides* strides,
+                   const void* rest, int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d, topk_packed_strides* st, const topk_packed_strides* strides,
                    int causal, float scale, int dtype) {
   int rc = packed_shape(pp, n, N, H, Hkv, d, causal, scale, dtype);
   if (rc) return rc;
@@ -995,8 +995,10 @@ int packed_problem(PackedProblem* pp, const void* Q, const void* K, const void* 
       (rc = packed_rows(&pp->out, "out", out, st->out_head, st->out_token, H, N)) || (rc = int_ptr(offsets, "offsets")))
     return rc;
   if (((uintptr_t)lse) % 4) return fail(TOPK_E_ALIGN, "lse is not 4-byte aligned");
+  if (((uintptr_t)rest) % 16) return fail(TOPK_E_ALIGN, "rest is not 16-byte aligned");
   pp->offsets = offsets;
   pp->lse = (float*)lse;
+  pp->rest = (void*)rest;
   return TOPK_OK;
 }
 
@@ -1552,12 +1554,12 @@ size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64
   return prefix_bytes(pp, prefix_plan(pp));
 }
 
-int topk_attn_packed(const void* Q, const void* K, const void* V, const int32_t* offsets, void* out, float* lse, int64_t n, int64_t N,
-                     int64_t H, int64_t Hkv, int64_t d, const topk_packed_strides* strides, int causal, float scale, int dtype, void* hip_stream) {
+int topk_attn_packed(const void* Q, const void* K, const void* V, const int32_t* offsets, void* out, float* lse, void* rest, int64_t n,
+                     int64_t N, int64_t H, int64_t Hkv, int64_t d, const topk_packed_strides* strides, int causal, float scale, int dtype, void* hip_stream) {
   g_err.clear();
   PackedProblem pp;
   topk_packed_strides t;
-  int rc = packed_problem(&pp, Q, K, V, offsets, out, lse, n, N, H, Hkv, d, &t, strides, causal, scale, dtype);
+  int rc = packed_problem(&pp, Q, K, V, offsets, out, lse, rest, n, N, H, Hkv, d, &t, strides, causal, scale, dtype);
   if (rc) return rc;
   hipStream_t st = (hipStream_t)hip_stream;
   StageTimer timer(st, ST_SCORE);
@@ -1565,12 +1567,12 @@ int topk_attn_packed(const void* Q, const void* K, const void* V, const int32_t*
 }
 
 int topk_attn_packed_backward(const void* Q, const void* K, const void* V, const int32_t* offsets, const void* out, const float* lse,
-                              const void* d_out, void* d_Q, void* d_K, void* d_V, int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d,
+                              const void* rest, const void* d_out, void* d_Q, void* d_K, void* d_V, int64_t n, int64_t N, int64_t H, int64_t Hkv, int64_t d,
                               const topk_packed_strides* strides, int causal, float scale, int dtype, void* hip_stream) {
   g_err.clear();
   PackedProblem pp;
   topk_packed_strides t;
-  int rc = packed_problem(&pp, Q, K, V, offsets, out, lse, n, N, H, Hkv, d, &t, strides, causal, scale, dtype);
+  int rc = packed_problem(&pp, Q, K, V, offsets, out, lse, rest, n, N, H, Hkv, d, &t, strides, causal, scale, dtype);
   if (rc) return rc;
   if ((rc = int_ptr(lse, "lse")) || (rc = packed_rows(&pp.d_out, "d_out", d_out, t.d_out_head, t.d_out_token, H, N)) ||
       (rc = packed_rows(&pp.dq, "d_Q", d_Q, t.d_q_head, t.d_q_token, H, N)) ||

@@ -16,6 +16,7 @@ struct PackedProblem {
   PackedRows q, k, v, out;
   PackedRows d_out, dq, dk, dv;  // (backward)
   float* lse;                    // [H, N], contiguous; NULL: not written
+  void* rest;                    // laid out as out, or NULL: what rounding took from it
   const int32_t* offsets;        // [n + 1]
   int64_t N;
   int n, H, Hkv, d, causal;

@@ -7,8 +7,8 @@
 //   * S^T = K Q^T by v_mfma_f32_32x32x16_bf16: lane l holds 16 keys' scores of row l % 32 a 32-key
 //     block, keys 8 (v / 4) + 4 (l / 32) + v % 4;
 //   * a running softmax of each row in its two lanes;
-//   * O^T += V^T P^T by the same instruction: the weights, rounded to bf16 (relative 2^-9 at most, as
-//     attn_dense does; the sum they are divided by is of the unrounded ones), are its operand in the order
+//   * O^T += V^T P^T by the same instruction: the weights, rounded to bf16 (relative 2^-9 at most) and divided by
+//     the sum of the rounded ones, in which what they have in common cancels, are its operand in the order
 //     the lane holds them, V^T comes from the row-major tile by transposing LDS reads.
 // Tiles come by direct global-to-LDS loads, one ahead. Which sequence and tile a workgroup has it finds
 // from the offsets itself, so that nothing is read back and no list is built by a launch of its own; there are at most
@@ -25,12 +25,24 @@ namespace {
 
 constexpr int NT = 256, WAVES = 4;
 
+typedef __bf16 bf16x2 __attribute__((__vector_size__(4)));
+// c and eight bf16 numbers
+__device__ __forceinline__ float sum_of(const bf16x8& x, float c) {
+  typedef bf16x2 pairs[4];
+  pairs p;
+  __builtin_memcpy(p, &x, sizeof x);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_fdot2_f32_bf16(p[e], (bf16x2){(__bf16)1.f, (__bf16)1.f}, c, false);
+  return c;
+}
+
 struct PackedArgs {
   PackedProblem p;
   float c;  // scale * log2(e)
 };
 
-template <int D, bool CAUSAL>
+// LSE: the logarithm of the sum is asked for, so that the weights are summed before rounding, too.
+template <int D, bool CAUSAL, bool LSE>
 __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   // The maximum that weights are taken against is moved, and the sums with it, only once a score leads it
   // by 2^8 in weight.
@@ -56,7 +68,9 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     const int N = (int)a.p.N, z0 = min(max(a.p.offsets[0], 0), N), z1 = max(z0, min(max(a.p.offsets[a.p.n], 0), N));
     for (int64_t i = tid; i < (int64_t)(z0 + N - z1) * CH; i += NT) {
       const int64_t r = i / CH, t = r < z0 ? r : r - z0 + z1;
-      *(uint4*)((uint16_t*)a.p.out.p + h * a.p.out.head + t * a.p.out.token + i % CH * 8) = make_uint4(0, 0, 0, 0);
+      const int64_t e = h * a.p.out.head + t * a.p.out.token + i % CH * 8;
+      *(uint4*)((uint16_t*)a.p.out.p + e) = make_uint4(0, 0, 0, 0);
+      if (a.p.rest) *(uint4*)((uint16_t*)a.p.rest + e) = make_uint4(0, 0, 0, 0);
       if (a.p.lse && i % CH == 0) a.p.lse[h * a.p.N + t] = -INFINITY;
     }
     return;
@@ -76,7 +90,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   f32x16 o[FB];
 #pragma unroll
   for (int f = 0; f < FB; ++f) o[f] = (f32x16){};
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, whole_l = 0.f;  // sums of the weights as they are multiplied; as they are
   const uint32_t kbase = Tile::straight_base(), vbase = Tile::across_base();
 
   // keys that some row of the workgroup sees; those that every row sees; those that the lane's does
@@ -146,6 +160,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
       const float alpha = mn == -INFINITY ? 1.f : exp2f(m - mn);  // (below 2^-126 too: see the weights)
       m = mn;
       l *= alpha;
+      if (LSE) whole_l *= alpha;
 #pragma unroll
       for (int f = 0; f < FB; ++f)
 #pragma unroll
@@ -165,9 +180,10 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float x = fmaf(s[st >> 1][8 * (st & 1) + e], a.c, bias), w = x < -126.f ? exp2f(x) : 0.f;
-          l += w;
+          if (LSE) whole_l += w;
           pt[e] = (__bf16)w;
         }
+        l = sum_of(pt, l);
 #pragma unroll
         for (int f = 0; f < FB; ++f) {
           o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp(st * FB + f), pt, o[f], 0, 0, 0);
@@ -181,7 +197,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     __builtin_amdgcn_s_setprio(1);  // the other wave's softmax yields to this one's products
     auto wt = [&](int v) {
       const float w = __builtin_amdgcn_exp2f(fmaf(s[v >> 4][v & 15], a.c, -off));
-      l += w;
+      if (LSE) whole_l += w;
       pb[v >> 3][v & 7] = (__bf16)w;
     };
 #pragma unroll
@@ -194,6 +210,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
       if (j + FB < VM)
 #pragma unroll
         for (int v = 0; v < 8 / FB; ++v) wt(8 + j * (8 / FB) + v);
+      if (j % FB == 0) l = sum_of(pb[j / FB], l);
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
@@ -264,6 +281,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     if (work && t * KEYS < wave_keys) tile(std::true_type{}, t, odd ? k1 : k0, odd ? v1 : v0);
   }
   l += __shfl_xor(l, 32, 64);
+  if (LSE) whole_l += __shfl_xor(whole_l, 32, 64);
   // through the wave's own part of LDS, in parts of four features permuted by the row, so that whole rows
   // are written, two (D = 128) or four a store
   __syncthreads();
@@ -285,9 +303,23 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     const int r = u * RPS + lane / PARTS, i = at.tile * PACKED_TILE + wave * 32 + r;
     const f32x4 x = mine[r * PARTS + (part ^ (r & 15))];
     const float by = __shfl(inv, r, 64);
-    if (i < at.n) *(uint2*)(to + i * a.p.out.token) = make_uint2(pack_bf16(x[0] * by, x[1] * by), pack_bf16(x[2] * by, x[3] * by));
+    if (i >= at.n) continue;
+    const uint2 y = make_uint2(pack_bf16(x[0] * by, x[1] * by), pack_bf16(x[2] * by, x[3] * by));
+    *(uint2*)(to + i * a.p.out.token) = y;
+    if (a.p.rest)
+      *(uint2*)((uint16_t*)a.p.rest + (to - (uint16_t*)a.p.out.p) + i * a.p.out.token) =
+          make_uint2(pack_bf16(x[0] * by - __uint_as_float(y.x << 16), x[1] * by - __uint_as_float(y.x & 0xFFFF0000u)),
+                     pack_bf16(x[2] * by - __uint_as_float(y.y << 16), x[3] * by - __uint_as_float(y.y & 0xFFFF0000u)));
   }
-  if (ok && !half && a.p.lse) a.p.lse[h * a.p.N + at.first + row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  if (LSE && ok && !half) a.p.lse[h * a.p.N + at.first + row] = whole_l == 0.f ? -INFINITY : (m + log2f(whole_l)) * 0.69314718055994531f;
+}
+
+template <bool LSE>
+void launch_for(const PackedArgs& a, unsigned grid, hipStream_t st) {
+  if (a.p.d == 64 && a.p.causal) k_packed<64, true, LSE><<<grid, NT, 0, st>>>(a);
+  else if (a.p.d == 64) k_packed<64, false, LSE><<<grid, NT, 0, st>>>(a);
+  else if (a.p.causal) k_packed<128, true, LSE><<<grid, NT, 0, st>>>(a);
+  else k_packed<128, false, LSE><<<grid, NT, 0, st>>>(a);
 }
 
 }  // namespace
@@ -297,10 +329,8 @@ int64_t packed_tiles(const PackedProblem& p) { return p.N / PACKED_TILE + std::m
 hipError_t launch_packed(const PackedProblem& p, hipStream_t st) {
   PackedArgs a = {p, p.scale * 1.4426950408889634f};
   const unsigned grid = (unsigned)(packed_tiles(p) * p.H);
-  if (p.d == 64 && p.causal) k_packed<64, true><<<grid, NT, 0, st>>>(a);
-  else if (p.d == 64) k_packed<64, false><<<grid, NT, 0, st>>>(a);
-  else if (p.causal) k_packed<128, true><<<grid, NT, 0, st>>>(a);
-  else k_packed<128, false><<<grid, NT, 0, st>>>(a);
+  if (p.lse) launch_for<true>(a, grid, st);
+  else launch_for<false>(a, grid, st);
   return hipGetLastError();
 }
 

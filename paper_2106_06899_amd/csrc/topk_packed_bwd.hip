@@ -1,6 +1,8 @@
 // Gradients of packed attention. With P = exp(scale S - lse), recomputed from the inputs, and
 // D_i = d_out_i . out_i (which is sum_j P_ij (d_out_i . v_j)):
 //   dV = P^T d_out,  dS = P (d_out V^T - D),  dQ = scale dS K,  dK = scale dS^T Q.
+// D is taken from out and what rounding it to bf16 took (its rounding alone would put dQ and dK off by 2.8e-3 in place
+// of 2.4e-3, of which their own rounding is 1.7e-3).
 // Three launches: the rows' lse and D; dQ, a workgroup a tile of 128 queries, over the keys; dK and dV, a
 // workgroup a tile of 128 keys and key head, over the queries of all its query heads. Each gradient is summed
 // where it ends up, in a fixed order, without atomics, which costs a second S and d_out V^T: seven products in
@@ -35,14 +37,15 @@ __global__ __launch_bounds__(NT) void k_packed_stat(BackwardArgs a) {
   const int64_t i = (int64_t)blockIdx.x * (NT / LR) + threadIdx.x / LR, h = i / a.p.N, t = i - h * a.p.N;
   if (h >= a.p.H) return;
   const int c = threadIdx.x % LR * 8;
-  const uint4 x = *(const uint4*)((const uint16_t*)a.p.out.p + h * a.p.out.head + t * a.p.out.token + c);
-  const uint4 g = *(const uint4*)((const uint16_t*)a.p.d_out.p + h * a.p.d_out.head + t * a.p.d_out.token + c);
+  const int64_t at = h * a.p.out.head + t * a.p.out.token + c;
+  const u32x4 x = *(const u32x4*)((const uint16_t*)a.p.out.p + at);
+  const u32x4 y = a.p.rest ? *(const u32x4*)((const uint16_t*)a.p.rest + at) : (u32x4){};
+  const u32x4 g = *(const u32x4*)((const uint16_t*)a.p.d_out.p + h * a.p.d_out.head + t * a.p.d_out.token + c);
   float sum = 0.f;
-  const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, gs[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    sum = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(gs[e] << 16), sum);
-    sum = fmaf(__uint_as_float(xs[e] & 0xFFFF0000u), __uint_as_float(gs[e] & 0xFFFF0000u), sum);
+    sum = fmaf(__uint_as_float(x[e] << 16) + __uint_as_float(y[e] << 16), __uint_as_float(g[e] << 16), sum);
+    sum = fmaf(__uint_as_float(x[e] & 0xFFFF0000u) + __uint_as_float(y[e] & 0xFFFF0000u), __uint_as_float(g[e] & 0xFFFF0000u), sum);
   }
 #pragma unroll
   for (int o = 1; o < LR; o <<= 1) sum += __shfl_xor(sum, o, 64);

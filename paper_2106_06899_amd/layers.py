@@ -103,18 +103,20 @@ class PackedAttentionFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, v, offsets, causal: bool, scale: float):
-        out, lse = attn_packed(q, k, v, offsets, causal, scale, lse=True)
-        ctx.save_for_backward(q, k, v, offsets, out, lse)
+        if not any(ctx.needs_input_grad):
+            return attn_packed(q, k, v, offsets, causal, scale)
+        out, lse, rest = attn_packed(q, k, v, offsets, causal, scale, lse=True, rest=True)
+        ctx.save_for_backward(q, k, v, offsets, out, lse, rest)
         ctx.how = causal, scale
         return out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, d_out):
-        q, k, v, offsets, out, lse = ctx.saved_tensors
+        q, k, v, offsets, out, lse, rest = ctx.saved_tensors
         if d_out.stride(-1) != 1 or any(s % 8 for s in d_out.stride()[:-1]) or d_out.data_ptr() % 16:
             d_out = d_out.contiguous()
-        return (*attn_packed_backward(q, k, v, offsets, out, lse, d_out, *ctx.how), None, None, None)
+        return (*attn_packed_backward(q, k, v, offsets, out, lse, d_out, *ctx.how, rest), None, None, None)
 
 
 def packed_attention(q, k, v, offsets, causal: bool = True, scale: float | None = None):

@@ -3,11 +3,13 @@
 Tolerance of an output element: half a step of bf16 relative to it, and twice the relative error
 of a weight times sum_j w_j |v_j|. A weight is off by its score's rounding (d products summed in fp32:
 at most (d + 8) 2^-24 sum |q k| scale), by the rounding of the exponent (2^-22 of the largest) and by
-its own to bf16 (2^-9 at most: the sum that it is divided by is not rounded).
+its own to bf16 (2^-9 at most; the sum that it is divided by is of the rounded ones, off by no more: that is the
+doubling).
 
 Tolerances of the gradients. With u = 2^-9 (half a step of bf16 relative to the number), w the weights,
 a = d_out v^T and D = d_out . out: a recomputed weight is off by delta' = delta and the rounding of lse
-(2^-21 (1 + |lse|), as tested), D by u |d_out| . |out| (out is stored in bf16) and sums' rounding, and
+(2^-21 (1 + |lse|), as tested), D by u |d_out| . |out| (out is stored in bf16; 2^-17 where what rounding took is
+passed on too) and sums' rounding, and
 ds = w (a - D) by its own rounding u besides; so with e = delta' and A = (d + 8) 2^-24 |d_out| |v|^T
     dv: half a step of the result, and (u + e) w^T |d_out|
     dq: half a step, and scale (u + e) |ds| |k| + scale (w (A + u |d_out| . |out| + its sums)) |k|, dk likewise with |q|.
@@ -116,6 +118,20 @@ def test_packed(name, tokens):
     _check(q, k, v, off, causal, d ** -0.5, out, lse)
     same = torch.equal(tk.attn_packed(q, k, v, off, causal), out)
     assert same
+
+
+def test_what_rounding_took():
+    """out and rest together are the result to 16 bits, 0 for tokens of no sequence."""
+    q, k, v, off = _inputs([3, 100, 300], 310, 4, 2, 128, tokens=True)
+    out, rest = tk.attn_packed(q, k, v, off, rest=True)
+    same = torch.equal(out, tk.attn_packed(q, k, v, off)) and rest.stride() == out.stride()
+    assert same and not rest[:, :3].any() and not rest[:, 300:].any()
+    assert bool((rest.float().abs() <= 2.0 ** -8 * out.float().abs()).all()) and bool(rest.any())
+    # What rounding took is at most half a step, which bf16 holds: rounded itself, it leads midway to the next number
+    # at most (the low half of the exact sum's bits is then 0x8000), where the sum may round the other way.
+    both = out.float() + rest.float()
+    other = both.bfloat16() != out
+    assert bool(((both.contiguous().view(torch.int32) & 0xFFFF)[other] == 0x8000).all())
 
 
 def test_scale_and_large_scores():
@@ -228,7 +244,7 @@ def test_refused_on_the_gpu():
     assert tk.attn_packed(q[:, :0], k[:, :0], v[:, :0], off).shape == (4, 0, 64)
 
 
-def _grad_check(q, k, v, offsets, g, causal, scale, grads, n_heads=None):
+def _grad_check(q, k, v, offsets, g, causal, scale, grads, rest=False):
     H, N, d = q.shape
     Hkv = k.shape[0]
     G = H // Hkv
@@ -255,7 +271,7 @@ def _grad_check(q, k, v, offsets, g, causal, scale, grads, n_heads=None):
                 ds = w * (x - D)
                 # (out is off by its weights too: their bound is part of D's)
                 e = 2 * ((d + 8) * 2.0 ** -24 + 2.0 ** -22) * size + 2.0 ** -21 * (1 + lse.abs())
-                out_off = 2.0 ** -9 * out.abs() + 2 * (e + u) * (w @ vv.abs())
+                out_off = 2.0 ** (-17 if rest else -9) * out.abs() + 2 * (e + u) * (w @ vv.abs())
                 D_off = (gg.abs() * out_off).sum(-1, keepdim=True) + d * 2.0 ** -24 * (gg.abs() * out.abs()).sum(-1, keepdim=True)
                 A = (d + 8) * 2.0 ** -24 * (gg.abs() @ vv.abs().t())
                 ds_off = ((u + e) * ds.abs() + w * (A + D_off)).masked_fill(hidden, 0)
@@ -282,6 +298,9 @@ def _gradient(q, k, v, off, causal=True, scale=None, seed=9, tokens=False):
     g = torch.randn(q.shape[1], q.shape[0], q.shape[2], generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").to(BF16).transpose(0, 1)
     if not tokens:
         g = g.contiguous()
+    if tokens:  # with what rounding took from out
+        out, lse, rest = tk.attn_packed(q, k, v, off, causal, scale, lse=True, rest=True)
+        return g, tk.attn_packed_backward(q, k, v, off, out, lse, g, causal, scale, rest)
     out, lse = tk.attn_packed(q, k, v, off, causal, scale, lse=True)
     return g, tk.attn_packed_backward(q, k, v, off, out, lse, g, causal, scale)
 
@@ -293,7 +312,7 @@ def test_packed_backward(name, tokens):
     q, k, v, off = _inputs(offsets, N, H, Hkv, d, tokens=tokens)
     g, grads = _gradient(q, k, v, off, causal, tokens=tokens)
     assert [t.stride() for t in grads] == [t.stride() for t in (q, k, v)]
-    _grad_check(q, k, v, off, g, causal, d ** -0.5, grads)
+    _grad_check(q, k, v, off, g, causal, d ** -0.5, grads, rest=tokens)
     same = all(torch.equal(a, b) for a, b in zip(grads, _gradient(q, k, v, off, causal, tokens=tokens)[1]))
     assert same
 
@@ -337,8 +356,8 @@ def test_autograd_on_layouts_and_broadcast_gradients():
     out = layers.packed_attention(q, k, v, off)
     out.sum().backward()
     ones = torch.ones(H, N, d, dtype=BF16, device="cuda")
-    o, lse = tk.attn_packed(q.detach(), k.detach(), v.detach(), off, lse=True)
-    want = torch.cat(tk.attn_packed_backward(q.detach(), k.detach(), v.detach(), off, o, lse, ones)).transpose(0, 1)
+    o, lse, rest = tk.attn_packed(q.detach(), k.detach(), v.detach(), off, lse=True, rest=True)
+    want = torch.cat(tk.attn_packed_backward(q.detach(), k.detach(), v.detach(), off, o, lse, ones, rest=rest)).transpose(0, 1)
     same = torch.equal(x.grad, want)
     assert same
     y = x.detach().transpose(0, 1)[:H].requires_grad_()
