@@ -737,19 +737,22 @@ def _written(t, name):
 
 def _pool(k_pages, v_pages, writes: bool = True):
     """topk_pages of a pool [pages, heads, rows, d], or of all layers' [layers, pages, heads, rows, d]."""
-    shape = k_pages.shape
+    shape, ks, vs = k_pages.shape, k_pages.stride(), v_pages.stride()
     if len(shape) not in (4, 5) or 0 in shape:
         raise ValueError(f"k_pages must be [pages, heads, rows, d] or [layers, pages, heads, rows, d], got {tuple(shape)}")
-    for t, n in ((k_pages, "k_pages"), (v_pages, "v_pages")):
-        _rows(t, n, shape, k_pages.dtype, k_pages.device)
-        if writes:
-            _written(t, n)
-    k, v, ks, vs = k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride()[:-1], v_pages.stride()[:-1]
+    if not (k_pages.is_cuda and v_pages.shape == shape and v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device
+            and ks[-1] == 1 and vs[-1] == 1):
+        for t, n in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+            _rows(t, n, shape, k_pages.dtype, k_pages.device)
+    if writes and (0 in ks or 0 in vs):
+        _written(k_pages, "k_pages")
+        _written(v_pages, "v_pages")
+    k, v = k_pages.data_ptr(), v_pages.data_ptr()
     if k == v:
         raise ValueError("k_pages and v_pages are the same memory")
     if len(shape) == 4:
-        return _Pages(k, v, 1, *shape, 0, *ks, 0, *vs)
-    return _Pages(k, v, *shape, *ks, *vs)
+        return _Pages(k, v, 1, *shape, 0, *ks[:-1], 0, *vs[:-1])
+    return _Pages(k, v, *shape, *ks[:-1], *vs[:-1])
 
 
 def _page_table(table, device, writes: bool = True):
@@ -803,7 +806,7 @@ def pages_reserve(k_pages, v_pages, table, refs, lengths, rows):
     each = None
     if isinstance(rows, torch.Tensor):
         each, rows = _ints(rows, "rows", B, device), 0
-    missing = torch.empty((), dtype=torch.int32, device=device)
+    missing = refs.new_empty(())
     L = lib()
     _launch(device, L.topk_pages_reserve,
             (pool, *at, refs_ptr, len_ptr, each, int(rows), missing.data_ptr(), _dtype_code(k_pages), _stream_of(device)),
@@ -859,7 +862,7 @@ def pages_keep(k_pages, v_pages, table, lengths, kept):
         _rows(kept, "kept", (B, 0), torch.int32, device)
         return lengths.clone()
     _rows(kept, "kept", (B, A), torch.int32, device)
-    new = torch.empty(B, dtype=torch.int32, device=device)
+    new = lengths.new_empty(B)
     _launch(device, lib().topk_pages_keep,
             (pool, *at, len_ptr, kept.data_ptr(), kept.stride(0), A, new.data_ptr(), _dtype_code(k_pages), _stream_of(device)))
     return new

@@ -15,8 +15,8 @@ import math
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import (attn, attn_backward, attn_dense, attn_packed, attn_packed_backward, attn_prefix, ffn, ffn_backward, qk_norm_rope, qk_norm_rope_append,
-               qk_norm_rope_backward, rope, rope_axes, rope_frequencies)
+from . import (attn, attn_backward, attn_dense, attn_packed, attn_packed_backward, attn_prefix, attn_tree, ffn, ffn_backward,
+               pages_append, qk_norm_rope, qk_norm_rope_append, qk_norm_rope_backward, rope, rope_axes, rope_frequencies)
 
 
 class TopkAttentionFunction(torch.autograd.Function):
@@ -126,6 +126,24 @@ def packed_attention(q, k, v, offsets, causal: bool = True, scale: float | None 
     return PackedAttentionFunction.apply(q, k, v, offsets, bool(causal), float(scale))
 
 
+def packed_positions(offsets, N: int):
+    """Each of N packed tokens' place in its own sequence, int64 [N] (for tokens of no sequence any)."""
+    t = torch.arange(N, device=offsets.device)
+    return t - offsets[torch.searchsorted(offsets[1:], t, right=True, out_int32=True).clamp(max=offsets.shape[0] - 2)]
+
+
+def tree_depths(parents):
+    """How many drafts each draft follows, int64 [T] or [B, T]: what it adds to its request's position
+    (parents as ``attn_tree`` takes them)."""
+    i = torch.arange(parents.shape[-1], device=parents.device)
+    up = torch.where((parents >= 0) & (parents < i), parents.long(), i)  # (the text: itself)
+    depth = (up != i).long()
+    for _ in range((parents.shape[-1] - 1).bit_length()):  # twice as far up each time
+        depth = depth + torch.gather(depth, -1, up)
+        up = torch.gather(up, -1, up)
+    return depth
+
+
 def rotary(x, positions, freqs, axes=None, adjacent: bool = False):
     """Differentiable rotary positions on [B, H, L, d] heads; arguments as ``rope``."""
     return RotaryFunction.apply(x, positions, freqs, None if axes is None else tuple(axes), bool(adjacent))
@@ -172,8 +190,12 @@ class TopkMultiheadAttention(torch.nn.Module):
     With ``qk_norm`` every query and key head is divided by its root mean square and scaled
     by weights of its own (q_norm, k_norm, [d_h]); with ``rope_theta`` heads are rotated by
     their positions, by one axis, or by several with ``rope_sections``, the pairs of each
-    (see ``rope_frequencies``, ``rope_axes``, and there ``rope_adjacent``). ``decode`` is the
-    serving form for a batch of requests behind a shared prefix (topk=None, causal)."""
+    (see ``rope_frequencies``, ``rope_axes``, and there ``rope_adjacent``).
+
+    With topk=None there are forms for more than a padded batch: ``packed`` for sequences that lie
+    one behind the other (with a backward pass), ``draft`` for the next tokens of requests whose
+    caches lie in pages, alone or as a tree of guesses, and ``decode`` for a batch of requests behind
+    a shared prefix (the last two causal)."""
 
     def __init__(self, d_model: int, n_heads: int, topk: int, chunk: int = 1024, causal: bool = False,
                  bias: bool = True, scale: float | None = None, device=None, dtype=torch.bfloat16, qk_norm: bool = False,
@@ -252,6 +274,48 @@ class TopkMultiheadAttention(torch.nn.Module):
         else:
             o = topk_attention(q, k, v, self.topk, self.chunk, self.causal, self.scale)
         return self.out(o.permute(0, 2, 1, 3).reshape(B, L, D))
+
+    def packed(self, x, offsets, positions=None, kv: bool = False):
+        """x [N, d_model], sequences one behind the other (``attn_packed``'s offsets); positions
+        [N] or [axes, 1, N] (default: each token's place in its own sequence, on every axis). With
+        ``kv`` also the keys and values [n_heads, N, d_h], as ``pages_append`` takes them."""
+        if self.topk is not None:
+            raise ValueError("packed attends to every key: it needs topk=None")
+        N, D = x.shape
+        if self.qk_norm or self.rope_bits is not None or positions is not None:
+            if positions is None and self.rope_bits is not None:
+                positions = packed_positions(offsets, N)
+                if self.rope_axes is not None:
+                    positions = positions.expand(self._axes(), 1, N)
+            q, k, v = (t[0] for t in self.heads(x[None], positions))
+        else:
+            q, k, v = self.qkv(x).view(N, 3, self.n_heads, self.d_head).permute(1, 2, 0, 3)
+        o = packed_attention(q, k, v, offsets, self.causal, self.scale)
+        y = self.out(o.transpose(0, 1).reshape(N, D))
+        return (y, k, v) if kv else y
+
+    @torch.no_grad()
+    def draft(self, x, k_pages, v_pages, table, lengths, parents=None, positions=None):
+        """The next T tokens x [B, T, d_model] of B requests whose caches lie in pages k_pages, v_pages
+        [pages, n_heads, page_rows, d_h], or T guesses that form a tree (``parents`` as ``attn_tree``
+        takes them): their keys and values go to the rows behind the ``lengths[b]`` that a request
+        has (``pages_reserve`` makes room for them; the caller advances lengths, with
+        ``pages_keep`` by those that are accepted), and each attends to its request's rows, itself
+        and the guesses that it follows. positions default to lengths[b] and how many guesses each
+        follows, on every axis."""
+        if self.topk is not None or not self.causal:
+            raise ValueError("draft attends to every earlier key: it needs topk=None and causal=True")
+        B, T, D = x.shape
+        if positions is None and self.rope_bits is not None:
+            steps = torch.arange(T, device=x.device) if parents is None else tree_depths(parents)
+            positions = lengths[:, None] + steps
+            if self.rope_axes is not None:
+                positions = positions.expand(self._axes(), B, T)
+        w = (self.q_norm, self.k_norm) if self.qk_norm else (None, None)
+        q, k, v = qk_norm_rope(self.qkv(x), self.n_heads, self.n_heads, *w, **self._rotation(positions, T, x.device))
+        pages_append(k, v, k_pages, v_pages, table, lengths)
+        o = attn_tree(q, k_pages, v_pages, lengths + T, table, parents, self.scale)
+        return self.out(o.permute(0, 2, 1, 3).reshape(B, T, D))
 
     @torch.no_grad()
     def decode(self, x, prefix_k, prefix_v, k_cache, v_cache, lengths, positions=None):
