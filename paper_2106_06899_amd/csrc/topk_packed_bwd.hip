@@ -510,7 +510,7 @@ void launch_d(const BackwardArgs& a, hipStream_t st) {
 // a tile is shared out until the longest has no more than three quarters of the average, or into SPLITS.
 static int packed_splits(const PackedProblem& p) {
   constexpr int SPLITS = 8;
-  const double L = (double)p.N / p.n, longest = L / ROWS * (p.H / p.Hkv), all = p.H * p.n * L * L / (ROWS * PACKED_TILE) / (p.causal ? 2 : 1) / 512;
+  const double L = (double)p.N / p.n, longest = L / ROWS * (p.H / p.Hkv), all = (double)p.H * p.n * L * L / (ROWS * PACKED_TILE) / (p.causal ? 2 : 1) / 512;
   int s = 1;
   while (s < SPLITS && longest / s > 0.75 * all && longest / s > 8) ++s;
   return s;

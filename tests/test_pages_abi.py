@@ -1,0 +1,201 @@
+"""CPU tests of packed attention, the page calls and attention over pages: every refused argument is
+refused before anything is launched, with a message, and workspace figures."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2106_06899_amd as tk
+from paper_2106_06899_amd import layers
+
+E_INVAL, E_NULL, E_ALIGN, E_UNSUPPORTED = -1, -2, -3, -4
+FAKE = 0x10000  # aligned, never dereferenced: every call below fails validation first
+BIG = 1 << 40
+
+
+def _pool(**kw):
+    a = dict(k=FAKE, v=FAKE + 64, layers=2, pages=9, heads=3, page_rows=4, d=64)
+    a.update({n: kw.pop(n) for n in list(kw) if n in a})
+    row = a["d"]
+    a.update({f"{x}_{n}": s for x in "kv" for n, s in (("layer", 9 * 12 * row), ("page", 12 * row), ("head", 4 * row), ("row", row))})
+    a.update(kw)
+    return tk._Pages(*(a[n] for n, _ in tk._Pages._fields_))
+
+
+def _call(name, a, kw):
+    pool = kw.pop("pool", {})
+    unknown = set(kw) - set(a)
+    assert not unknown, unknown
+    a.update(kw)
+    if "pool" in a:
+        a["pool"] = None if pool is None else _pool(**pool)
+    if "to" in a:
+        a["to"] = None if a["to"] is None else _pool(**{**dict(k=FAKE + 1024, v=FAKE + 2048, pages=7), **a["to"]})
+    rc = getattr(tk.lib(), name)(*a.values())
+    assert rc == 0 or tk.lib().topk_last_error()
+    return rc
+
+
+POOL = [(dict(pool=None), E_NULL), (dict(pool=dict(pages=0)), E_INVAL), (dict(pool=dict(page_rows=0)), E_INVAL), (dict(pool=dict(heads=0)), E_INVAL),
+        (dict(pool=dict(d=0)), E_INVAL), (dict(pool=dict(d=1032)), E_UNSUPPORTED), (dict(pool=dict(d=12)), E_UNSUPPORTED),
+        (dict(pool=dict(layers=0)), E_INVAL), (dict(pool=dict(pages=1 << 31)), E_UNSUPPORTED), (dict(pool=dict(page_rows=1 << 31)), E_UNSUPPORTED),
+        (dict(pool=dict(page_rows=1 << 28)), E_UNSUPPORTED), (dict(pool=dict(heads=20000)), E_UNSUPPORTED), (dict(pool=dict(layers=70000)), E_UNSUPPORTED),
+        (dict(pool=dict(k=None)), E_NULL), (dict(pool=dict(v=FAKE + 8)), E_ALIGN), (dict(pool=dict(k_row=4)), E_ALIGN), (dict(pool=dict(v_page=-8)), E_INVAL),
+        (dict(pool=dict(k_head=BIG)), E_INVAL), (dict(pool=dict(v_layer=20)), E_ALIGN), (dict(dtype=2), E_INVAL)]
+TABLE = [(dict(B=0), E_INVAL), (dict(M=0), E_INVAL), (dict(B=1 << 25), E_UNSUPPORTED), (dict(M=1 << 31), E_UNSUPPORTED), (dict(table=None), E_NULL),
+         (dict(table=FAKE + 2), E_ALIGN), (dict(stride=3), E_INVAL), (dict(stride=BIG), E_INVAL)]
+
+
+def _reserve(**kw):
+    return _call("topk_pages_reserve", dict(pool=0, table=FAKE, stride=5, B=2, M=5, refs=FAKE, lengths=FAKE, each=None, rows=3, missing=FAKE, dtype=1,
+                                            st=None), kw)
+
+
+@pytest.mark.parametrize("kw,code", POOL + TABLE + [
+    (dict(refs=None), E_NULL), (dict(refs=FAKE + 1), E_ALIGN), (dict(lengths=None), E_NULL), (dict(missing=None), E_NULL), (dict(each=FAKE + 2), E_ALIGN),
+    (dict(rows=-1), E_INVAL), (dict(rows=1 << 31), E_INVAL), (dict(B=1 << 23, M=5, stride=5), E_UNSUPPORTED)])
+def test_reserve_refusals(kw, code):
+    assert _reserve(**kw) == code
+
+
+def _append(**kw):
+    a = dict(k=FAKE, v=FAKE, kl=8, kb=1024, kh=512, kt=64, vl=8, vb=1024, vh=512, vt=64, T=8, offsets=None, pool=0, table=FAKE, stride=5, B=2, M=5,
+             lengths=FAKE, dtype=1, st=None)
+    return _call("topk_pages_append", a, kw)
+
+
+@pytest.mark.parametrize("kw,code", POOL + TABLE + [
+    (dict(k=None), E_NULL), (dict(v=FAKE + 4), E_ALIGN), (dict(kt=63), E_ALIGN), (dict(vh=-512), E_INVAL), (dict(vb=BIG), E_INVAL), (dict(T=0), E_INVAL),
+    (dict(T=1 << 24), E_UNSUPPORTED), (dict(offsets=FAKE + 1), E_ALIGN), (dict(lengths=None), E_NULL)])
+def test_append_refusals(kw, code):
+    assert _append(**kw) == code
+
+
+def _keep(**kw):
+    a = dict(pool=0, table=FAKE, stride=5, B=2, M=5, lengths=FAKE, kept=FAKE, kstride=4, A=4, new=FAKE, dtype=1, st=None)
+    return _call("topk_pages_keep", a, kw)
+
+
+@pytest.mark.parametrize("kw,code", POOL + TABLE + [
+    (dict(A=0), E_INVAL), (dict(A=65), E_UNSUPPORTED), (dict(kept=None), E_NULL), (dict(kstride=-1), E_INVAL), (dict(new=FAKE + 2), E_ALIGN),
+    (dict(lengths=FAKE + 3), E_ALIGN), (dict(B=1 << 21, stride=5), E_UNSUPPORTED)])
+def test_keep_refusals(kw, code):
+    assert _keep(**kw) == code
+
+
+def _fork(**kw):
+    return _call("topk_pages_fork", dict(table=FAKE, stride=5, B=2, M=5, refs=FAKE, pages=9, lengths=FAKE, parents=FAKE, rows=4, st=None), kw)
+
+
+def _release(**kw):
+    return _call("topk_pages_release", dict(table=FAKE, stride=5, B=2, M=5, refs=FAKE, pages=9, lengths=FAKE, rows=4, st=None), kw)
+
+
+@pytest.mark.parametrize("kw,code", TABLE + [(dict(refs=None), E_NULL), (dict(lengths=None), E_NULL), (dict(rows=0), E_INVAL), (dict(pages=0), E_INVAL),
+                                             (dict(pages=1 << 31), E_UNSUPPORTED), (dict(rows=1 << 31), E_UNSUPPORTED)])
+def test_fork_and_release_refusals(kw, code):
+    assert _fork(**dict(kw)) == code and _release(**dict(kw)) == code
+    assert _fork(parents=None) == E_NULL
+
+
+def _compact(**kw):
+    a = dict(pool=0, to={}, table=FAKE, stride=5, B=2, M=5, refs=FAKE, new_table=FAKE, new_refs=FAKE, missing=FAKE, dtype=1, st=None)
+    return _call("topk_pages_compact", a, kw)
+
+
+@pytest.mark.parametrize("kw,code", POOL[:-1] + TABLE + [
+    (dict(to=None), E_NULL), (dict(to=dict(heads=2)), E_INVAL), (dict(to=dict(page_rows=8)), E_INVAL), (dict(to=dict(layers=1)), E_INVAL),
+    (dict(to=dict(d=128)), E_INVAL), (dict(to=dict(k=FAKE)), E_INVAL), (dict(to=dict(pages=0)), E_INVAL), (dict(new_table=None), E_NULL),
+    (dict(new_refs=FAKE + 2), E_ALIGN), (dict(refs=None), E_NULL), (dict(missing=None), E_NULL),
+    (dict(pool=dict(pages=1 << 23), to=dict(pages=1 << 23)), E_UNSUPPORTED)])
+def test_compact_refusals(kw, code):
+    assert _compact(**kw) == code
+
+
+def _tree(**kw):
+    a = dict(Q=FAKE, pool=0, table=FAKE, stride=5, lengths=FAKE, parents=FAKE, pstride=3, out=FAKE, lse=None, B=2, M=5, H=6, T=3, scale=0.125, dtype=1,
+             st=None)
+    kw = dict(kw)
+    if "pool" not in kw:
+        kw["pool"] = {}
+    if kw["pool"] is not None:
+        kw["pool"] = {**dict(layers=1), **kw["pool"]}
+    return _call("topk_attn_tree", a, kw)
+
+
+@pytest.mark.parametrize("kw,code", [x for x in POOL if "v_layer" not in (x[0].get("pool") or {})] + TABLE[:4] + TABLE[5:] + [
+    (dict(H=7), E_INVAL), (dict(H=0), E_INVAL), (dict(T=0), E_INVAL), (dict(T=65), E_UNSUPPORTED), (dict(scale=0.0), E_INVAL), (dict(scale=math.nan), E_INVAL),
+    (dict(dtype=0), E_UNSUPPORTED), (dict(pool=dict(d=32)), E_UNSUPPORTED), (dict(pool=dict(layers=2)), E_INVAL), (dict(Q=None), E_NULL),
+    (dict(out=FAKE + 8), E_ALIGN), (dict(lengths=None), E_NULL), (dict(parents=FAKE + 2), E_ALIGN), (dict(pstride=-1), E_INVAL), (dict(lse=FAKE + 2), E_ALIGN),
+    (dict(B=1 << 20, stride=5, H=48), E_UNSUPPORTED)])
+def test_tree_refusals(kw, code):
+    assert _tree(**kw) == code
+
+
+def _packed(backward=False, strides=None, **kw):
+    a = dict(Q=FAKE, K=FAKE, V=FAKE, offsets=FAKE, out=FAKE, lse=FAKE, rest=None)
+    if backward:
+        a.update(d_out=FAKE, d_Q=FAKE, d_K=FAKE, d_V=FAKE)
+    a.update(n=2, N=100, H=4, Hkv=2, d=64, st=None, causal=1, scale=0.125, dtype=1, stream=None)
+    if strides is not None:
+        s = dict(zip((n for n, _ in tk._PackedStrides._fields_), [6400, 64] * 8))
+        s.update(strides)
+        a["st"] = tk._PackedStrides(*s.values())
+    return _call("topk_attn_packed_backward" if backward else "topk_attn_packed", a, dict(kw))
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=0), E_INVAL), (dict(N=0), E_INVAL), (dict(H=0), E_INVAL), (dict(H=3), E_INVAL), (dict(d=0), E_INVAL), (dict(d=96), E_UNSUPPORTED),
+    (dict(dtype=0), E_UNSUPPORTED), (dict(dtype=3), E_INVAL), (dict(causal=2), E_INVAL), (dict(scale=-1.0), E_INVAL), (dict(scale=math.inf), E_INVAL),
+    (dict(N=(1 << 30) + 1), E_UNSUPPORTED), (dict(n=1 << 31), E_UNSUPPORTED), (dict(N=1 << 30, H=4), E_UNSUPPORTED), (dict(Q=None), E_NULL),
+    (dict(K=FAKE + 8), E_ALIGN), (dict(V=None), E_NULL), (dict(out=None), E_NULL), (dict(offsets=None), E_NULL), (dict(offsets=FAKE + 2), E_ALIGN),
+    (dict(lse=FAKE + 1), E_ALIGN), (dict(rest=FAKE + 8), E_ALIGN), (dict(strides=dict(q_token=-8)), E_INVAL), (dict(strides=dict(k_token=60)), E_ALIGN),
+    (dict(strides=dict(v_head=12)), E_ALIGN), (dict(strides=dict(out_token=1 << 24)), E_UNSUPPORTED), (dict(strides=dict(q_head=BIG)), E_INVAL)])
+def test_packed_refusals(kw, code):
+    assert _packed(**kw) == code and _packed(backward=True, **kw) == code
+
+
+@pytest.mark.parametrize("kw,code", [(dict(lse=None), E_NULL), (dict(d_out=None), E_NULL), (dict(d_Q=FAKE + 2), E_ALIGN), (dict(d_K=None), E_NULL),
+                                     (dict(d_V=FAKE + 8), E_ALIGN), (dict(strides=dict(d_out_token=4)), E_ALIGN), (dict(strides=dict(d_v_head=-8)), E_INVAL)])
+def test_packed_backward_refusals(kw, code):
+    assert _packed(backward=True, **kw) == code
+
+
+def test_workspace_figures():
+    L = tk.lib()
+    assert L.topk_attn_packed_backward_workspace_bytes(1, 0, 1, 1, 64, 1) == 0 and L.topk_attn_packed_backward_workspace_bytes(1, 5, 3, 2, 64, 1) == 0
+    # two numbers a row, and where queries are shared out, so many 32-bit copies of dK and dV
+    small = L.topk_attn_packed_backward_workspace_bytes(8, 512, 4, 4, 64, 1)
+    assert small == 512 * 4 * 8
+    n = L.topk_attn_packed_backward_workspace_bytes(1, 8192, 4, 1, 128, 1) - 8192 * 4 * 8
+    assert n > 0 and n % (8192 * 128 * 8) == 0 and n // (8192 * 128 * 8) <= 8
+    assert L.topk_attn_tree_workspace_bytes(2, 5, 16, 4, 2, 1, 64, 1) == 0  # few keys: nothing is left to join
+    assert L.topk_attn_tree_workspace_bytes(2, 5000, 16, 4, 3, 1, 64, 1) == 0  # refused
+    wide = [L.topk_attn_tree_workspace_bytes(2, m, 16, 4, 2, 1, 64, 1) for m in (1000, 100000, 1 << 30)]
+    assert wide[0] > 0 and wide[0] == wide[1] == wide[2]  # whatever the table's width
+    assert L.topk_pages_reserve_workspace_bytes(0, 2, 5) == 0 and L.topk_pages_reserve_workspace_bytes(100, 2, 5) >= 2 * 16 + 10 * 8
+    assert L.topk_pages_fork_workspace_bytes(2, 5) == 0 and L.topk_pages_fork_workspace_bytes(100, 1000) == 100 * 1001 * 4
+    assert L.topk_pages_compact_workspace_bytes(100, 0) == 0 and L.topk_pages_compact_workspace_bytes(100, 50) >= 100 * 4 + 51 * 4
+
+
+def test_binding_wants_gpu_tensors():
+    i = torch.zeros(2, dtype=torch.int32)
+    k, t = torch.zeros(3, 2, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 5, dtype=torch.int32)
+    for f in (lambda: tk.pages_reserve(k, k.clone(), t, i, i, 1), lambda: tk.pages_release(t, i, i, 4), lambda: tk.pages_fork(t, i, i, i, 4),
+              lambda: tk.pages_append(k, k, k, k.clone(), t, i), lambda: tk.pages_keep(k, k.clone(), t, i, t),
+              lambda: tk.pages_compact(k, k.clone(), t, i, k.clone(), k.clone()), lambda: tk.attn_tree(k, k, k.clone(), i, t),
+              lambda: tk.attn_packed(k[0], k[0], k[0], i), lambda: layers.packed_attention(k[0], k[0], k[0], i)):
+        with pytest.raises(ValueError):
+            f()
+
+
+def test_positions_and_depths():
+    off = torch.tensor([0, 3, 3, 5], dtype=torch.int32)
+    assert layers.packed_positions(off, 5).tolist() == [0, 1, 2, 0, 1]
+    assert layers.tree_depths(torch.tensor([-1, 0, 1, 1, 7, 2], dtype=torch.int32)).tolist() == [0, 1, 2, 2, 0, 3]
+    assert layers.tree_depths(torch.tensor([[-1], [0]], dtype=torch.int32)).tolist() == [[0], [0]]
+
+
+def test_structures_are_as_the_header_has_them():
+    assert ctypes.sizeof(tk._Pages) == 15 * 8 and ctypes.sizeof(tk._PackedStrides) == 16 * 8
