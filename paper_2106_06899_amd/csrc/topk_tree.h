@@ -29,6 +29,7 @@ struct TreePlan {
                    // (weights as two bf16 numbers, as one)
   int tiles;       // row tiles of (H / Hkv) * T rows
   int64_t ranges;  // wanted, of all requests together; 0: one a request
+  int round;       // ranges whose workgroups fill the chip once
 };
 
 constexpr int TREE_MAX = 64;  // drafts of a request

@@ -70,16 +70,30 @@ __device__ __forceinline__ uint64_t wave_sum64(uint64_t x) {
 }
 __device__ __forceinline__ uint32_t units_of(int64_t keys) { return (uint32_t)((keys + UNIT - 1) / UNIT); }
 
-// Units of a range: as many as leave the wanted number of ranges of all requests' keys.
-__device__ __forceinline__ uint32_t range_units(const TreeArgs& a) {
-  if (!a.pl.ranges) return UINT32_MAX;
-  uint64_t sum = 0;
-  for (int b = threadIdx.x & 63; b < a.p.B; b += 64) sum += units_of(keys_of(a.p, b));
-  sum = wave_sum64(sum);
-  return (uint32_t)max((sum + a.pl.ranges - 1) / a.pl.ranges, (uint64_t)2);
-}
 __device__ __forceinline__ uint32_t ranges_of(int64_t keys, uint32_t units) {
   return units == UINT32_MAX ? 1u : max(1u, (units_of(keys) + units - 1) / units);
+}
+
+// Units of a range. As many as leave the wanted number of ranges of all requests' keys (two and more workgroups a
+// place on the chip, which even out: the next token of 32 requests of up to 4096 63 us, 69 in one round), or, where
+// that would be short ranges, of SINGLE units at most, the fewest that leave one round of workgroups (20 requests of
+// up to 1500: 22 us in one round of three units, 26 in two rounds of two; 30 with 8 drafts 37 and 44).
+__device__ __forceinline__ uint32_t range_units(const TreeArgs& a) {
+  constexpr uint32_t SINGLE = 8;
+  if (!a.pl.ranges) return UINT32_MAX;
+  const int lane = threadIdx.x & 63;
+  uint64_t sum = 0;
+  uint32_t mine = 0;
+  for (int b = lane; b < a.p.B; b += 64) sum += mine = units_of(keys_of(a.p, b));
+  sum = wave_sum64(sum);
+  const uint32_t least = (uint32_t)max((sum + a.pl.ranges - 1) / a.pl.ranges, (uint64_t)1);
+  if (a.pl.round > a.p.B / 2) {
+    // (requests' last ranges are half full on average; where a wave holds all lengths the ranges are counted)
+    const uint64_t full = a.p.B <= 64 ? a.pl.round : a.pl.round - a.p.B / 2;
+    for (uint32_t u = (uint32_t)max((sum + full - 1) / full, (uint64_t)least); u <= SINGLE; ++u)
+      if (a.p.B > 64 || wave_sum(lane < a.p.B ? max(1u, (mine + u - 1) / u) : 0) <= a.pl.round) return u;
+  }
+  return max(least, 2u);
 }
 
 struct TreeRange {
@@ -834,6 +848,7 @@ TreePlan tree_plan(const TreeProblem& p) {
   // Few keys: one workgroup a request, key head and row tile takes all its keys, and nothing is left to join.
   if (S <= 2 * UNIT || (pl.form < 8 && p.B * units <= 512 && S * p.d <= 1024 * 64)) return pl;
   pl.ranges = std::max(cdiv(1024, units), p.B);
+  pl.round = (int)(512 / units);
   return pl;
 }
 
