@@ -28,7 +28,10 @@ struct PackedProblem {
 };
 
 constexpr int PACKED_TILE = 128;  // rows of a workgroup
-int64_t packed_tiles(const PackedProblem& p);  // workgroups of a head at most, and one for the tokens of no sequence
+// workgroups of a head at most, of so many rows, and one for the tokens of no sequence
+int64_t packed_tiles(const PackedProblem& p, int rows = PACKED_TILE);
+// so few workgroups of PACKED_TILE rows that half as many rows are better
+bool packed_few(const PackedProblem& p, int heads);
 size_t packed_backward_bytes(const PackedProblem& p);
 hipError_t launch_packed(const PackedProblem& p, hipStream_t st);
 hipError_t launch_packed_backward(PackedProblem p, void* ws, hipStream_t st);

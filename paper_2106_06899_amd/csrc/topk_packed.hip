@@ -24,6 +24,7 @@ namespace topk {
 namespace {
 
 constexpr int NT = 256, WAVES = 4;
+#define TOPK_INLINE __attribute__((always_inline))  // (a lambda that is called captures through memory)
 
 typedef __bf16 bf16x2 __attribute__((__vector_size__(4)));
 // c and eight bf16 numbers
@@ -41,14 +42,18 @@ struct PackedArgs {
   float c;  // scale * log2(e)
 };
 
-// LSE: the logarithm of the sum is asked for, so that the weights are summed before rounding, too.
-template <int D, bool CAUSAL, bool LSE>
+// LSE: the logarithm of the sum is asked for, so that the weights are summed before rounding, too. KS = 2: half the
+// rows a workgroup, and two waves share each 32, one taking the first and one the last 32 keys of every tile: twice
+// the workgroups, each of half the length, where there are few.
+template <int D, bool CAUSAL, bool LSE, int KS>
 __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   // The maximum that weights are taken against is moved, and the sums with it, only once a score leads it
   // by 2^8 in weight.
   constexpr float LEAD = 8.f;
   typedef PackedTile<D> Tile;
+  constexpr int ROWS = PACKED_TILE / KS;  // of the workgroup
   constexpr int KEYS = 64;          // of a tile
+  constexpr int NB = 2 / KS;        // blocks of 32 of a tile that a wave takes
   constexpr int NS = D / 16;        // steps over the features of the scores
   constexpr int CH = 2 * D / 16;    // 16-byte parts of a row
   constexpr int TILEB = KEYS * 2 * D;
@@ -62,6 +67,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   __shared__ float flag[WAVES][2];
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 31, half = lane >> 5;
+  const int group = wave % (WAVES / KS), share = wave / (WAVES / KS);  // of rows; of a tile's keys
   const int2 item = packed_item(a.p.H);
   const int h = item.x;
   if (blockIdx.x >= gridDim.x - a.p.H) {  // tokens of no sequence
@@ -75,12 +81,12 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     }
     return;
   }
-  const PackedPlace at = packed_place(a.p, item.y, PACKED_TILE, CAUSAL, false);
+  const PackedPlace at = packed_place(a.p, item.y, ROWS, a.p.H, CAUSAL, false);
   if (!at.n) return;
   const int hk = h / (a.p.H / a.p.Hkv);
-  const int row = at.tile * PACKED_TILE + wave * 32 + n;  // the lane's query in its sequence
+  const int row = at.tile * ROWS + group * 32 + n;  // the lane's query in its sequence
   const bool ok = row < at.n;
-  const bool work = at.tile * PACKED_TILE + wave * 32 < at.n;  // the wave has rows
+  const bool work = at.tile * ROWS + group * 32 < at.n;  // the wave has rows
   bf16x8 bq[NS];
   {
     const uint16_t* q = (const uint16_t*)a.p.q.p + h * a.p.q.head + (at.first + (ok ? row : at.n - 1)) * a.p.q.token + (D / 2) * half;
@@ -94,9 +100,9 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   const uint32_t kbase = Tile::straight_base(), vbase = Tile::across_base();
 
   // keys that some row of the workgroup sees; those that every row sees; those that the lane's does
-  const int keys = CAUSAL ? min(at.n, at.tile * PACKED_TILE + PACKED_TILE) : at.n;
-  const int all_see = CAUSAL ? at.tile * PACKED_TILE + 1 : at.n, seen = CAUSAL ? min(at.n, row + 1) : at.n;
-  const int wave_keys = CAUSAL ? at.tile * PACKED_TILE + wave * 32 + 32 : at.n;  // beyond these the wave's rows see none
+  const int keys = CAUSAL ? min(at.n, at.tile * ROWS + ROWS) : at.n;
+  const int all_see = CAUSAL ? at.tile * ROWS + 1 : at.n, seen = CAUSAL ? min(at.n, row + 1) : at.n;
+  const int wave_keys = (CAUSAL ? at.tile * ROWS + group * 32 + 32 : at.n) - share * 32;  // its rows see none of a tile from here on
   const int tiles = (keys + KEYS - 1) / KEYS;
   const uint32_t ksl = (uint32_t)a.p.k.token * 2, vsl = (uint32_t)a.p.v.token * 2;  // bytes from one row to the next
   uint32_t koff[LPW], voff[LPW];
@@ -125,33 +131,36 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     vt += KEYS * (int64_t)vsl;
   };
 
-  auto tile = [&](auto edge, int t, const unsigned char* kb, const unsigned char* vb) {
-    f32x16 s[2] = {};
+  auto tile = [&](auto edge, int t, const unsigned char* kbuf, const unsigned char* vbuf) TOPK_INLINE {
+    const TOPK_LDS unsigned char *kb = (const TOPK_LDS unsigned char*)kbuf + (KS > 1 ? share * 32 * 2 * D : 0),
+                                 *vb = (const TOPK_LDS unsigned char*)vbuf + (KS > 1 ? share * 32 * 2 * D : 0);
+    constexpr int SV = 16 * NB;  // scores of a lane
+    f32x16 s[NB] = {};
     {
       bf16x8 kf[AHEAD_K + 1];
-      auto kp = [&](int i) { return Tile::straight((const TOPK_LDS unsigned char*)kb, kbase, i & 1, i >> 1); };
+      auto kp = [&](int i) { return Tile::straight(kb, kbase, i % NB, i / NB); };
 #pragma unroll
       for (int i = 0; i < AHEAD_K; ++i) kf[i] = kp(i);
 #pragma unroll
-      for (int i = 0; i < 2 * NS; ++i) {
-        if (i + AHEAD_K < 2 * NS) kf[(i + AHEAD_K) % (AHEAD_K + 1)] = kp(i + AHEAD_K);
-        s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % (AHEAD_K + 1)], bq[i >> 1], s[i & 1], 0, 0, 0);
+      for (int i = 0; i < NB * NS; ++i) {
+        if (i + AHEAD_K < NB * NS) kf[(i + AHEAD_K) % (AHEAD_K + 1)] = kp(i + AHEAD_K);
+        s[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % (AHEAD_K + 1)], bq[i / NB], s[i % NB], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
     float low = INFINITY;  // the tile's lowest score (masked keys' included, NaN too: they only choose the pass below)
 #pragma unroll
-    for (int v = 0; v < 32; v += 2)
+    for (int v = 0; v < SV; v += 2)
       low = __builtin_elementwise_minimum(__builtin_elementwise_minimum(low, s[v >> 4][v & 15]), s[v >> 4][(v & 15) + 1]);
     if (decltype(edge)::value) {
-      const int last = seen - t * KEYS - 4 * half;
+      const int last = seen - t * KEYS - share * 32 - 4 * half;
 #pragma unroll
-      for (int v = 0; v < 32; ++v)
+      for (int v = 0; v < SV; ++v)
         if ((v >> 4) * 32 + 8 * ((v & 15) >> 2) + (v & 3) >= last) s[v >> 4][v & 15] = -INFINITY;
     }
     float mt = -INFINITY;
 #pragma unroll
-    for (int v = 0; v < 32; v += 2)
+    for (int v = 0; v < SV; v += 2)
       mt = larger(larger(mt, s[v >> 4][v & 15]), s[v >> 4][(v & 15) + 1]);
     mt = other_half_max(mt) * a.c;
     const bool leads = !(mt <= m + LEAD);  // (NaN too)
@@ -166,16 +175,16 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[f][v] *= alpha;
     }
-    constexpr int VM = 4 * FB;
+    constexpr int VM = 2 * NB * FB;
     const float off = m == -INFINITY ? 0.f : m;
-    auto vp = [&](int j) { return Tile::across((const TOPK_LDS unsigned char*)vb, vbase, j % FB, j / FB); };  // V^T of 16 keys j / FB, features 32 (j % FB) on
+    auto vp = [&](int j) { return Tile::across(vb, vbase, j % FB, j / FB); };  // V^T of 16 keys j / FB, features 32 (j % FB) on
     // Weights below 2^-126, which the exponential instruction alone makes 0, are added by themselves where
     // the tile has any.
     if (__builtin_amdgcn_ballot_w64(!(fmaf(low, a.c, -off) >= -126.f))) {
       float bias = -off;
       asm volatile("" : "+v"(bias));  // (nothing of this pass is held for the other)
 #pragma unroll
-      for (int st = 0; st < 4; ++st) {
+      for (int st = 0; st < 2 * NB; ++st) {
         bf16x8 pt;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -191,7 +200,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
         }
       }
     }
-    bf16x8 pb[4], vf[AHEAD_V + 1];
+    bf16x8 pb[2 * NB], vf[AHEAD_V + 1];
 #pragma unroll
     for (int j = 0; j < AHEAD_V; ++j) vf[j] = vp(j);
     __builtin_amdgcn_s_setprio(1);  // the other wave's softmax yields to this one's products
@@ -282,12 +291,41 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   }
   l += __shfl_xor(l, 32, 64);
   if (LSE) whole_l += __shfl_xor(whole_l, 32, 64);
-  // through the wave's own part of LDS, in parts of four features permuted by the row, so that whole rows
-  // are written, two (D = 128) or four a store
   __syncthreads();
   TOPK_LDS unsigned char *p0 = (TOPK_LDS unsigned char*)k0, *p1 = (TOPK_LDS unsigned char*)k1, *p2 = (TOPK_LDS unsigned char*)v0,
                          *p3 = (TOPK_LDS unsigned char*)v1;
-  TOPK_LDS f32x4* mine = (TOPK_LDS f32x4*)(wave == 0 ? p0 : wave == 1 ? p1 : wave == 2 ? p2 : p3);
+  if (KS > 1) {  // the second half of the waves hand theirs over: four numbers a lane at a time, then maximum and sums
+    TOPK_LDS f32x4* to = (TOPK_LDS f32x4*)(group ? p1 : p0) + lane;
+    __shared__ float2 other[WAVES][64];
+    __shared__ float other_l[WAVES][64];
+    if (share) {
+#pragma unroll
+      for (int f = 0; f < FB; ++f)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4) to[(4 * f + v / 4) * 64] = (f32x4){o[f][v], o[f][v + 1], o[f][v + 2], o[f][v + 3]};
+      other[group][lane] = make_float2(m, l);
+      if (LSE) other_l[group][lane] = whole_l;
+    }
+    __syncthreads();
+    if (share) return;
+    const float2 x = other[group][lane];
+    const float top = larger(m, x.x), base = top == -INFINITY ? 0.f : top, f0 = exp2f(m - base), f1 = exp2f(x.x - base);  // (-inf: 0)
+    m = top;
+    l = fmaf(f0, l, f1 * x.y);
+    if (LSE) whole_l = fmaf(f0, whole_l, f1 * other_l[group][lane]);
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4) {
+        const f32x4 y = to[(4 * f + v / 4) * 64];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) o[f][v + w] = fmaf(f0, o[f][v + w], f1 * y[w]);
+      }
+    wave_sync_lds();
+  }
+  // through the wave's own part of LDS, in parts of four features permuted by the row, so that whole rows
+  // are written, two (D = 128) or four a store
+  TOPK_LDS f32x4* mine = (TOPK_LDS f32x4*)(KS > 1 ? group ? p1 : p0 : wave == 0 ? p0 : wave == 1 ? p1 : wave == 2 ? p2 : p3);
   constexpr int PARTS = D / 4, RPS = 64 / PARTS;
 #pragma unroll
   for (int f = 0; f < FB; ++f)
@@ -300,7 +338,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   uint16_t* to = (uint16_t*)a.p.out.p + h * a.p.out.head + at.first * a.p.out.token + 4 * part;
 #pragma unroll 4
   for (int u = 0; u < 32 / RPS; ++u) {
-    const int r = u * RPS + lane / PARTS, i = at.tile * PACKED_TILE + wave * 32 + r;
+    const int r = u * RPS + lane / PARTS, i = at.tile * ROWS + group * 32 + r;
     const f32x4 x = mine[r * PARTS + (part ^ (r & 15))];
     const float by = __shfl(inv, r, 64);
     if (i >= at.n) continue;
@@ -314,23 +352,30 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   if (LSE && ok && !half) a.p.lse[h * a.p.N + at.first + row] = whole_l == 0.f ? -INFINITY : (m + log2f(whole_l)) * 0.69314718055994531f;
 }
 
-template <bool LSE>
+template <bool LSE, int KS>
 void launch_for(const PackedArgs& a, unsigned grid, hipStream_t st) {
-  if (a.p.d == 64 && a.p.causal) k_packed<64, true, LSE><<<grid, NT, 0, st>>>(a);
-  else if (a.p.d == 64) k_packed<64, false, LSE><<<grid, NT, 0, st>>>(a);
-  else if (a.p.causal) k_packed<128, true, LSE><<<grid, NT, 0, st>>>(a);
-  else k_packed<128, false, LSE><<<grid, NT, 0, st>>>(a);
+  if (a.p.d == 64 && a.p.causal) k_packed<64, true, LSE, KS><<<grid, NT, 0, st>>>(a);
+  else if (a.p.d == 64) k_packed<64, false, LSE, KS><<<grid, NT, 0, st>>>(a);
+  else if (a.p.causal) k_packed<128, true, LSE, KS><<<grid, NT, 0, st>>>(a);
+  else k_packed<128, false, LSE, KS><<<grid, NT, 0, st>>>(a);
 }
 
 }  // namespace
 
-int64_t packed_tiles(const PackedProblem& p) { return p.N / PACKED_TILE + std::min<int64_t>(p.n, p.N) + 1; }
+int64_t packed_tiles(const PackedProblem& p, int rows) { return p.N / rows + std::min<int64_t>(p.n, p.N) + 1; }
+
+// (One text of 8192 tokens, heads of 128, causal: 2 heads 141 -> 98 us, 4 142 -> 105, 8 170 either way, 16 268 -> 315; all
+// keys, 8 heads 259 -> 302.)
+bool packed_few(const PackedProblem& p, int heads) { return p.N / PACKED_TILE * heads <= 256; }
 
 hipError_t launch_packed(const PackedProblem& p, hipStream_t st) {
   PackedArgs a = {p, p.scale * 1.4426950408889634f};
-  const unsigned grid = (unsigned)(packed_tiles(p) * p.H);
-  if (p.lse) launch_for<true>(a, grid, st);
-  else launch_for<false>(a, grid, st);
+  const bool few = packed_few(p, p.H);
+  const unsigned grid = (unsigned)(packed_tiles(p, few ? PACKED_TILE / 2 : PACKED_TILE) * p.H);
+  if (p.lse && few) launch_for<true, 2>(a, grid, st);
+  else if (p.lse) launch_for<true, 1>(a, grid, st);
+  else if (few) launch_for<false, 2>(a, grid, st);
+  else launch_for<false, 1>(a, grid, st);
   return hipGetLastError();
 }
 

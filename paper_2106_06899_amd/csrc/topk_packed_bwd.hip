@@ -163,9 +163,12 @@ __device__ __forceinline__ void clear_outside(const PackedProblem& p, const Pack
   }
 }
 
-template <int D, bool CAUSAL>
+// KS = 2: half the rows a workgroup, and two waves share each 32, one taking the first and one the last 32 keys of
+// every tile, as in the forward pass.
+template <int D, bool CAUSAL, int KS>
 __global__ __launch_bounds__(NT, 2) void k_packed_dq(BackwardArgs a) {
   typedef PackedTile<D> Tile;
+  constexpr int TROWS = PACKED_TILE / KS, NB = 2 / KS;  // rows of the workgroup; blocks of 32 of a tile that a wave takes
   constexpr int NS = D / 16, TILEB = ROWS * 2 * D, LPW = TILEB / 1024 / WAVES, FB = D / 32;
   __shared__ __attribute__((aligned(16))) unsigned char k0[TILEB];
   __shared__ __attribute__((aligned(16))) unsigned char k1[TILEB];
@@ -173,14 +176,15 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dq(BackwardArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char v1[TILEB];
   __shared__ int flag[WAVES][2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 31, half = lane >> 5;
+  const int group = wave % (WAVES / KS), share = wave / (WAVES / KS);  // of rows; of a tile's keys
   const int2 item = packed_item(a.p.H);
   const int h = item.x;
   if (blockIdx.x >= gridDim.x - a.p.H) return clear_outside<D>(a.p, a.p.dq, h);
-  const PackedPlace at = packed_place(a.p, item.y, PACKED_TILE, CAUSAL, false);
+  const PackedPlace at = packed_place(a.p, item.y, TROWS, a.p.H, CAUSAL, false);
   if (!at.n) return;
   const int hk = h / (a.p.H / a.p.Hkv);
-  const int row = at.tile * PACKED_TILE + wave * 32 + n;
-  const bool work = at.tile * PACKED_TILE + wave * 32 < at.n;
+  const int row = at.tile * TROWS + group * 32 + n;
+  const bool work = at.tile * TROWS + group * 32 < at.n;
   const int64_t token = at.first + min(row, at.n - 1);
   bf16x8 bq[NS], bo[NS];
   {
@@ -197,8 +201,8 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dq(BackwardArgs a) {
 #pragma unroll
   for (int f = 0; f < FB; ++f) o[f] = (f32x16){};
 
-  const int keys = CAUSAL ? min(at.n, at.tile * PACKED_TILE + PACKED_TILE) : at.n;
-  const int all_see = CAUSAL ? at.tile * PACKED_TILE + 1 : at.n, seen = CAUSAL ? min(at.n, row + 1) : at.n;
+  const int keys = CAUSAL ? min(at.n, at.tile * TROWS + TROWS) : at.n;
+  const int all_see = CAUSAL ? at.tile * TROWS + 1 : at.n, seen = CAUSAL ? min(at.n, row + 1) : at.n;
   const int tiles = (keys + ROWS - 1) / ROWS;
   const Loader<D, LPW> load_k(a.p.k.token), load_v(a.p.v.token);
   const unsigned char* kt = (const unsigned char*)((const uint16_t*)a.p.k.p + hk * a.p.k.head + at.first * a.p.k.token);
@@ -211,9 +215,10 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dq(BackwardArgs a) {
     vt += ROWS * (int64_t)load_v.sl;
   };
   auto tile = [&](bool edge, int t, const unsigned char* kbuf, const unsigned char* vbuf) TOPK_INLINE {
-    const TOPK_LDS unsigned char *kb = (const TOPK_LDS unsigned char*)kbuf, *vb = (const TOPK_LDS unsigned char*)vbuf;
+    const TOPK_LDS unsigned char *kb = (const TOPK_LDS unsigned char*)kbuf + (KS > 1 ? share * 32 * 2 * D : 0),
+                                 *vb = (const TOPK_LDS unsigned char*)vbuf + (KS > 1 ? share * 32 * 2 * D : 0);
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
+    for (int rb = 0; rb < NB; ++rb) {
       uint32_t row0 = Tile::straight_base(), col0 = Tile::across_base();
       asm volatile("" : "+v"(row0), "+v"(col0));  // (the places that follow from them are not held)
       f32x16 s = {}, g = {};
@@ -226,7 +231,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dq(BackwardArgs a) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.c, -lse)) * (g[v] - D_row);
       if (edge) {
-        const int last = seen - t * ROWS - rb * 32 - 4 * half;
+        const int last = seen - t * ROWS - (KS > 1 ? share : rb) * 32 - 4 * half;
 #pragma unroll
         for (int v = 0; v < 16; ++v)
           if (8 * (v >> 2) + (v & 3) >= last) s[v] = 0.f;
@@ -276,9 +281,29 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dq(BackwardArgs a) {
   __syncthreads();
   TOPK_LDS unsigned char *p0 = (TOPK_LDS unsigned char*)k0, *p1 = (TOPK_LDS unsigned char*)k1, *p2 = (TOPK_LDS unsigned char*)v0,
                          *p3 = (TOPK_LDS unsigned char*)v1;
-  TOPK_LDS f32x4* mine = (TOPK_LDS f32x4*)(wave == 0 ? p0 : wave == 1 ? p1 : wave == 2 ? p2 : p3);
+  if (KS > 1) {  // the second half of the waves hand their sums over, four numbers a lane at a time
+    TOPK_LDS f32x4* to = (TOPK_LDS f32x4*)(group ? p1 : p0) + lane;
+    if (share) {
+#pragma unroll
+      for (int f = 0; f < FB; ++f)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4) to[(4 * f + v / 4) * 64] = (f32x4){o[f][v], o[f][v + 1], o[f][v + 2], o[f][v + 3]};
+    }
+    __syncthreads();
+    if (share) return;
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4) {
+        const f32x4 y = to[(4 * f + v / 4) * 64];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) o[f][v + w] += y[w];
+      }
+    wave_sync_lds();
+  }
+  TOPK_LDS f32x4* mine = (TOPK_LDS f32x4*)(KS > 1 ? group ? p1 : p0 : wave == 0 ? p0 : wave == 1 ? p1 : wave == 2 ? p2 : p3);
   store_rows<D>(o, a.p.scale, mine, (uint16_t*)a.p.dq.p + h * a.p.dq.head + at.first * a.p.dq.token, a.p.dq.token,
-                at.tile * PACKED_TILE + wave * 32, at.n);
+                at.tile * TROWS + group * 32, at.n);
 }
 
 template <int D, bool CAUSAL>
@@ -301,7 +326,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dkv(BackwardArgs a) {
     clear_outside<D>(a.p, a.p.dk, hk);
     return clear_outside<D>(a.p, a.p.dv, hk);
   }
-  const PackedPlace at = packed_place(a.p, item.y, PACKED_TILE, CAUSAL, true);
+  const PackedPlace at = packed_place(a.p, item.y, PACKED_TILE, a.p.Hkv * splits, CAUSAL, true);
   if (!at.n) return;
   const int G = a.p.H / a.p.Hkv;
   const int key = at.tile * PACKED_TILE + wave * 32 + n;
@@ -498,7 +523,8 @@ template <int D, bool CAUSAL>
 void launch_d(const BackwardArgs& a, hipStream_t st) {
   const int64_t rows = a.p.H * a.p.N, per = NT / (D / 8);
   k_packed_stat<D><<<(unsigned)((rows + per - 1) / per), NT, 0, st>>>(a);
-  k_packed_dq<D, CAUSAL><<<(unsigned)(packed_tiles(a.p) * a.p.H), NT, 0, st>>>(a);
+  if (packed_few(a.p, a.p.H)) k_packed_dq<D, CAUSAL, 2><<<(unsigned)(packed_tiles(a.p, PACKED_TILE / 2) * a.p.H), NT, 0, st>>>(a);
+  else k_packed_dq<D, CAUSAL, 1><<<(unsigned)(packed_tiles(a.p) * a.p.H), NT, 0, st>>>(a);
   k_packed_dkv<D, CAUSAL><<<(unsigned)(packed_tiles(a.p) * a.p.Hkv * a.p.splits), NT, 0, st>>>(a);
   if (a.p.splits > 1) k_packed_sum<D><<<(unsigned)((2 * a.p.Hkv * a.p.N * (D / 8) + NT - 1) / NT), NT, 0, st>>>(a);
 }

@@ -37,7 +37,7 @@ __device__ __forceinline__ uint32_t wave_sum(uint32_t x) { return (uint32_t)__bu
 // Tile number t of all sequences' tiles of `rows` tokens. levels: up to 64 sequences' tiles are numbered by
 // their place in their sequence, the last places (or, from_end, the first) first: under a causal mask these
 // have the most to do. Every wave finds it by itself.
-__device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int t, int rows, bool levels, bool from_end) {
+__device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int t, int rows, int heads, bool levels, bool from_end) {
   const int lane = threadIdx.x & 63;
   PackedPlace at = {0, 0, 0};
   auto bounds = [&](int s, int* a, int* len) {
@@ -52,7 +52,11 @@ __device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int 
     if (lane < p.n) bounds(lane, &a, &len);
     const int nt = (len + rows - 1) / rows;
     auto longer = [&](int c) { return (int)wave_sum((uint32_t)max(nt - c, 0)); };  // tiles in places from c on
-    if (longer(0) <= t) return at;
+    const int all = longer(0);
+    if (all <= t) return at;
+    // Where every CU has one or two workgroups in all, those that come second are the shortest first: the longest
+    // shares its CU with the shortest.
+    if (all * heads <= 512 && t * heads >= 256) t = all - 1 - (t - (256 + heads - 1) / heads);
     int lo = 0, hi = (int)((p.N + rows - 1) / rows);  // longer(lo) > t >= longer(hi)
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
