@@ -34,9 +34,29 @@ struct PackedPlace {
 
 __device__ __forceinline__ uint32_t wave_sum(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan_full(x), 63); }
 
+// Where the interval of 256 threads' counts `mine`, laid one behind the other from `before` on, holds number t: true for
+// the thread whose it is, with the numbers before its first. *before becomes the number behind the last. By the whole
+// workgroup; `sums`: an entry a wave.
+__device__ __forceinline__ bool block_find(uint32_t mine, uint32_t t, uint32_t* before, uint32_t* first, uint32_t* sums) {
+  const int wave = threadIdx.x >> 6;
+  const uint32_t end = wave_incl_scan_full(mine);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) sums[wave] = end;
+  __syncthreads();
+  uint32_t at = *before;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) at += sums[w];
+    *before += sums[w];
+  }
+  *first = at + end - mine;
+  return t >= *first && t - *first < mine;
+}
+
 // Tile number t of all sequences' tiles of `rows` tokens. levels: up to 64 sequences' tiles are numbered by
 // their place in their sequence, the last places (or, from_end, the first) first: under a causal mask these
-// have the most to do. Every wave finds it by itself.
+// have the most to do. Every wave finds it by itself; more sequences are looked through by the whole workgroup, four a
+// thread.
 __device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int t, int rows, int heads, bool levels, bool from_end) {
   const int lane = threadIdx.x & 63;
   PackedPlace at = {0, 0, 0};
@@ -47,49 +67,73 @@ __device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int 
     if (*len < 0) *len = 0;
   };
   int s = -1;
-  if (levels && p.n <= 64) {
+  if (p.n <= 64) {
     int a, len = 0;
     if (lane < p.n) bounds(lane, &a, &len);
     const int nt = (len + rows - 1) / rows;
-    auto longer = [&](int c) { return (int)wave_sum((uint32_t)max(nt - c, 0)); };  // tiles in places from c on
-    const int all = longer(0);
-    if (all <= t) return at;
-    // Where every CU has one or two workgroups in all, those that come second are the shortest first: the longest
-    // shares its CU with the shortest.
-    if (all * heads <= 512 && t * heads >= 256) t = all - 1 - (t - (256 + heads - 1) / heads);
-    int lo = 0, hi = (int)((p.N + rows - 1) / rows);  // longer(lo) > t >= longer(hi)
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (longer(mid) > t) lo = mid;
-      else hi = mid;
-    }
-    const uint64_t those = __builtin_amdgcn_ballot_w64(nt > lo);
-    const int r = t - longer(lo + 1);
-    const uint64_t mine = __builtin_amdgcn_ballot_w64(nt > lo && (int)lanes_below(those) == r);
-    s = __builtin_ctzll(mine);
-    at.tile = lo;
-  } else {
-    uint32_t before = 0;
-    for (int s0 = 0; s0 < p.n && s < 0; s0 += 64) {
-      int a, len = 0;
-      if (s0 + lane < p.n) bounds(s0 + lane, &a, &len);
-      const uint32_t nt = (len + rows - 1) / rows, end = before + wave_incl_scan_full(nt);
-      const uint64_t those = __builtin_amdgcn_ballot_w64(end > (uint32_t)t);
-      if (those) {
-        const int l = __builtin_ctzll(those);
-        s = s0 + l;
-        at.tile = t - (__builtin_amdgcn_readlane((int)end, l) - __builtin_amdgcn_readlane((int)nt, l));
+    if (levels) {
+      auto longer = [&](int c) { return (int)wave_sum((uint32_t)max(nt - c, 0)); };  // tiles in places from c on
+      const int all = longer(0);
+      if (all <= t) return at;
+      // Where every CU has one or two workgroups in all, those that come second are the shortest first: the longest
+      // shares its CU with the shortest.
+      if (all * heads <= 512 && t * heads >= 256) t = all - 1 - (t - (256 + heads - 1) / heads);
+      int lo = 0, hi = (int)((p.N + rows - 1) / rows);  // longer(lo) > t >= longer(hi)
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (longer(mid) > t) lo = mid;
+        else hi = mid;
       }
-      before = (uint32_t)__builtin_amdgcn_readlane((int)end, 63);
+      const uint64_t those = __builtin_amdgcn_ballot_w64(nt > lo);
+      const int r = t - longer(lo + 1);
+      s = __builtin_ctzll(__builtin_amdgcn_ballot_w64(nt > lo && (int)lanes_below(those) == r));
+      at.tile = lo;
+    } else {
+      const uint32_t end = wave_incl_scan_full((uint32_t)nt);
+      const uint64_t those = __builtin_amdgcn_ballot_w64(end > (uint32_t)t);
+      if (!those) return at;
+      s = __builtin_ctzll(those);
+      at.tile = t - (__builtin_amdgcn_readlane((int)end, s) - __builtin_amdgcn_readlane(nt, s));
     }
+  } else {
+    __shared__ uint32_t sums[4];
+    __shared__ int found[2];
+    if (threadIdx.x == 0) found[0] = -1;
+    uint32_t before = 0;
+    for (int64_t s0 = 0; s0 < p.n && before <= (uint32_t)t; s0 += 1024) {
+      int nt[4], a, len;
+      uint32_t mine = 0, first;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t x = s0 + 4 * threadIdx.x + u;
+        len = 0;
+        if (x < p.n) bounds((int)x, &a, &len);
+        mine += nt[u] = (len + rows - 1) / rows;
+      }
+      if (block_find(mine, (uint32_t)t, &before, &first, sums)) {
+        uint32_t left = t - first;
+        int u = 0;
+#pragma unroll
+        for (int w = 0; w < 3; ++w)
+          if (u == w && left >= (uint32_t)nt[w]) {
+            left -= nt[w];
+            u = w + 1;
+          }
+        found[0] = (int)(s0 + 4 * threadIdx.x) + u;
+        found[1] = (int)left;
+      }
+    }
+    __syncthreads();
+    s = found[0];
     if (s < 0) return at;
+    at.tile = found[1];
   }
   int a, len;
   bounds(s, &a, &len);
   at.first = __builtin_amdgcn_readfirstlane(a);
   at.n = __builtin_amdgcn_readfirstlane(len);
   at.tile = __builtin_amdgcn_readfirstlane(at.tile);
-  if (levels && p.n <= 64 ? from_end : false) at.tile = (at.n + rows - 1) / rows - 1 - at.tile;
+  if (levels && p.n <= 64 && from_end) at.tile = (at.n + rows - 1) / rows - 1 - at.tile;
   return at;
 }
 

@@ -84,8 +84,18 @@ __device__ __forceinline__ uint32_t range_units(const TreeArgs& a) {
   const int lane = threadIdx.x & 63;
   uint64_t sum = 0;
   uint32_t mine = 0;
-  for (int b = lane; b < a.p.B; b += 64) sum += mine = units_of(keys_of(a.p, b));
-  sum = wave_sum64(sum);
+  if (a.p.B <= 64) {
+    if (lane < a.p.B) mine = units_of(keys_of(a.p, lane));
+    sum = wave_sum64(mine);
+  } else {  // (by the whole workgroup)
+    __shared__ uint64_t sums[WAVES];
+#pragma unroll 4
+    for (int b = threadIdx.x; b < a.p.B; b += NT) sum += units_of(keys_of(a.p, b));
+    sum = wave_sum64(sum);
+    if (lane == 0) sums[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = sums[0] + sums[1] + sums[2] + sums[3];
+  }
   const uint32_t least = (uint32_t)max((sum + a.pl.ranges - 1) / a.pl.ranges, (uint64_t)1);
   if (a.pl.round > a.p.B / 2) {
     // (requests' last ranges are half full on average; where a wave holds all lengths the ranges are counted)
@@ -104,26 +114,35 @@ struct TreeRange {
   int n;        // its keys
   int len;      // the request's
 };
-// Range w of all requests' (by every wave).
+// Range w of all requests', by every wave, or where there are more than 64 by the whole workgroup.
 __device__ __forceinline__ TreeRange find_range(const TreeArgs& a, uint32_t w) {
   const int lane = threadIdx.x & 63;
   const uint32_t units = range_units(a);
   TreeRange r = {-1, 0, 0, 0, 0, 0};
-  uint32_t before = 0, mine = 0;
+  uint32_t mine = 0;
   if (!a.pl.ranges) {
     r.b = (int)w;
+  } else if (a.p.B <= 64) {
+    const uint32_t n = lane < a.p.B ? ranges_of(keys_of(a.p, lane), units) : 0, end = wave_incl_scan_full(n);
+    const uint64_t those = __builtin_amdgcn_ballot_w64(end > w);
+    if (!those) return r;
+    r.b = __builtin_ctzll(those);
+    mine = w - (uint32_t)(__builtin_amdgcn_readlane((int)end, r.b) - __builtin_amdgcn_readlane((int)n, r.b));
   } else {
-    for (int64_t b0 = 0; b0 < a.p.B && r.b < 0; b0 += 64) {
-      const uint32_t n = b0 + lane < a.p.B ? ranges_of(keys_of(a.p, (int)b0 + lane), units) : 0, end = before + wave_incl_scan_full(n);
-      const uint64_t those = __builtin_amdgcn_ballot_w64(end > w);
-      if (those) {
-        const int l = __builtin_ctzll(those);
-        r.b = (int)b0 + l;
-        mine = w - (uint32_t)(__builtin_amdgcn_readlane((int)end, l) - __builtin_amdgcn_readlane((int)n, l));
+    __shared__ uint32_t sums[4], found[2];
+    if (threadIdx.x == 0) found[0] = UINT32_MAX;
+    uint32_t before = 0, first;
+    for (int64_t b0 = 0; b0 < a.p.B && before <= w; b0 += NT) {
+      const int64_t b = b0 + threadIdx.x;
+      if (block_find(b < a.p.B ? ranges_of(keys_of(a.p, (int)b), units) : 0, w, &before, &first, sums)) {
+        found[0] = (uint32_t)b;
+        found[1] = w - first;
       }
-      before = (uint32_t)__builtin_amdgcn_readlane((int)end, 63);
     }
-    if (r.b < 0) return r;
+    __syncthreads();
+    if (found[0] == UINT32_MAX) return r;
+    r.b = (int)found[0];
+    mine = found[1];
   }
   const int64_t len = keys_of(a.p, r.b), first = (int64_t)mine * units * UNIT;
   r.which = __builtin_amdgcn_readfirstlane((int)mine);

@@ -99,6 +99,14 @@ CASES = {
     "many": ([i * (i + 1) // 2 for i in range(64)], 2016, 2, 1, 64, True),
     "more_than_a_wave_of_them": ([i * 7 for i in range(150)], 1043, 2, 2, 64, True),
     "more_all_keys": ([i * 13 for i in range(70)], 897, 1, 1, 128, False),
+    "hundreds_of_them": ([(i * 5) // 2 for i in range(700)], 1748, 1, 1, 64, True),
+    "thousands": ([min(i, 2500) for i in range(2600)], 2510, 1, 1, 128, False),
+    # more than 256 workgroups of 128 rows: a workgroup's waves have rows of their own
+    "many_workgroups": ([0, 1000, 1003, 3200], 3210, 12, 3, 64, True),
+    "many_workgroups_d128": ([0, 1000, 1064, 3200], 3200, 12, 12, 128, True),
+    "many_workgroups_all_keys": ([5, 1000, 1003, 3200], 3210, 12, 3, 64, False),
+    "many_workgroups_all_keys_d128": ([0, 1000, 1003, 3200], 3210, 12, 4, 128, False),
+    "more_than_two_a_cu": ([0, 130, 3300, 3301, 5600], 5600, 14, 2, 64, True),
     "long": ([0, 2000, 5003], 5003, 2, 1, 128, True),
     "long_d64": ([0, 3001, 3002, 5000], 5000, 2, 2, 64, True),
     "shared_out": ([0, 1100, 1133, 2300], 2310, 4, 1, 128, True),
@@ -151,18 +159,19 @@ def test_cut_from_a_projection():
     assert same
 
 
+# (few heads: two waves share rows; a hundred: rows of their own)
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
-@pytest.mark.parametrize("d", [64, 128])
-def test_hidden_rows_may_hold_anything(bad, d):
+@pytest.mark.parametrize("d,H", [(64, 2), (128, 2), (64, 100), (128, 100)])
+def test_hidden_rows_may_hold_anything(bad, d, H):
     """Later tokens, other sequences and tokens of none hold numbers that are not finite: rows that
     do not see them are as if they were not there."""
     off, N = [0, 150, 200, 420], 430
-    q, k, v, o = _inputs(off, N, 2, 1, d, seed=3)
+    q, k, v, o = _inputs(off, N, H, H // 2, d, seed=3)
     want, wl = tk.attn_packed(q, k, v, o, lse=True)
     k2, v2 = k.clone(), v.clone()
     for t in (149, 100, 330, 425):
-        v2[0, t, t % d] = bad
-    k2[0, 427] = v2[0, 428] = bad
+        v2[:, t, t % d] = bad
+    k2[:, 427] = v2[:, 428] = bad
     got, gl = tk.attn_packed(q, k2, v2, o, lse=True)
     same = torch.equal(gl, wl)
     assert same
@@ -174,7 +183,7 @@ def test_hidden_rows_may_hold_anything(bad, d):
             assert all(not got[:, i, f].isfinite().any() for f in cols), i
     assert not got[:, 420:].any()
     k3 = k.clone()
-    k3[0, 300] = bad  # a key: rows before it are untouched
+    k3[:, 300] = bad  # a key: rows before it are untouched
     same = torch.equal(tk.attn_packed(q, k3, v, o)[:, :300], want[:, :300])
     assert same
 
@@ -182,20 +191,24 @@ def test_hidden_rows_may_hold_anything(bad, d):
 def test_tiny_weights_and_a_late_maximum():
     """Weights below 2^-126 still count against large values, before and behind a maximum that leads
     them by far."""
-    d, n = 64, 200
-    q = torch.zeros(1, n, d, device="cuda", dtype=BF16)
+    for H in (1, 300):
+        _tiny(64, 200, H), _tiny(128, 100, H)
+
+
+def _tiny(d, n, H):
+    q = torch.zeros(H, n, d, device="cuda", dtype=BF16)
     k, v = torch.zeros_like(q), torch.zeros_like(q)
     q[..., 0] = 1
-    for at in (10, 190):
+    for at in (10, n - 10):
         k[:] = 0
-        k[0, at, 0] = 88.5
+        k[:, at, 0] = 88.5
         v[:] = 2.0 ** 100
-        v[0, at] = 1.0
+        v[:, at] = 1.0
         off = _int([0, n])
         out = tk.attn_packed(q, k, v, off, causal=False, scale=1.0)
         s = q[0].double() @ k[0].double().t()
         ref = torch.softmax(s, -1) @ v[0].double()
-        assert bool(((out[0].double() - ref).abs() <= 2.0 ** -7 * ref.abs()).all()), at
+        assert bool(((out.double() - ref).abs() <= 2.0 ** -7 * ref.abs()).all()), at
 
 
 def test_streams_and_graphs():
@@ -317,6 +330,24 @@ def test_packed_backward(name, tokens):
     assert same
 
 
+def test_keys_shared_by_expansion():
+    """Keys and values that are one head expanded: the gradient is whole, and autograd's sum over the heads is that of
+    one shared head but for its roundings."""
+    off = _int([0, 60, 200])
+    q, k, v, _ = _inputs([0, 200], 200, 4, 1, 64)
+    g = _gradient(q, k, v, off)[0]
+    k1, v1 = k.clone().requires_grad_(), v.clone().requires_grad_()
+    out = layers.packed_attention(q, k1.expand(4, -1, -1), v1.expand(4, -1, -1), off)
+    same = torch.equal(out, tk.attn_packed(q, k, v, off))
+    assert same
+    got = torch.autograd.grad(out, (k1, v1), g)
+    k2, v2 = k.clone().requires_grad_(), v.clone().requires_grad_()
+    want = torch.autograd.grad(layers.packed_attention(q, k2, v2, off), (k2, v2), g)
+    for a, b in zip(got, want):  # four roundings of parts and their sum's
+        parts = 4 * b.float().abs().amax()
+        assert bool(((a.float() - b.float()).abs() <= 5 * 2.0 ** -9 * parts).all())
+
+
 def test_gradients_against_differences():
     """Central differences of the 64-bit definition in a few directions: what the tests above take for the
     gradient is the gradient."""
@@ -367,11 +398,11 @@ def test_autograd_on_layouts_and_broadcast_gradients():
 
 
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
-@pytest.mark.parametrize("d", [64, 128])
-def test_gradients_of_hidden_rows(bad, d):
+@pytest.mark.parametrize("d,H", [(64, 2), (128, 2), (64, 100), (128, 100)])
+def test_gradients_of_hidden_rows(bad, d, H):
     """Numbers that are not finite reach the gradients of what meets them, no other."""
     off, N = [0, 150, 290], 300
-    q, k, v, o = _inputs(off, N, 2, 1, d, seed=3)
+    q, k, v, o = _inputs(off, N, H, H // 2, d, seed=3)
     g, want = _gradient(q, k, v, o)
     out, lse = tk.attn_packed(q, k, v, o, lse=True)
     # d_out of token 100: dq of that token, dk and dv of the keys that it sees
@@ -397,7 +428,7 @@ def test_gradients_of_hidden_rows(bad, d):
     # a key and a value of token 100: rows that do not see them
     for which in (0, 1):
         kv = [k.clone(), v.clone()]
-        kv[which][0, 100, 7] = bad
+        kv[which][:, 100, 7] = bad
         out2, lse2 = tk.attn_packed(q, *kv, o, lse=True)
         got = tk.attn_packed_backward(q, *kv, o, out2, lse2, g)
         seen = list(range(100)) + list(range(150, N))
