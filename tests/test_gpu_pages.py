@@ -219,6 +219,18 @@ def test_more_requests_than_a_workgroup_takes_at_once():
     c.release()
 
 
+@pytest.mark.parametrize("B,M", [(3000, 3), (700, 40), (9000, 1), (2, 5000)])
+def test_forks_of_large_tables(B, M):
+    """More entries than one workgroup takes: cycles, chains and ends of requests at once."""
+    c = Cache(B, M, 4, 3 * B + 50, 1, 1, 8, seed=B, longest=8 if M > 1 else 4)
+    rng = c.rng
+    for _ in range(2):
+        c.fork([rng.choice([b, (b + 1) % B, rng.randrange(B), -1, b // 7 * 7]) for b in range(B)])
+    c.release()
+    c.fork([-1] * B)
+    assert not c.refs.any()
+
+
 def test_a_long_reservation():
     """More entries a request than a workgroup takes at once."""
     c = Cache(3, 4000, 2, 9000, 1, 1, 8, seed=4, longest=100)
@@ -309,6 +321,25 @@ def test_compact(shape):
         kt, vt = (torch.full((shape[4], len(live) - 1, *c.k.shape[2:]), 7.0, dtype=c.k.dtype, device="cuda") for _ in range(2))
         table, new, missing = tk.pages_compact(c.k, c.v, c.table, c.refs, kt, vt)
         assert int(missing) == 1 and not new.any() and bool((table == -1).all()) and bool((kt == 7).all())
+
+
+@pytest.mark.parametrize("page,heads,d,dtype", [(16, 8, 128, torch.bfloat16), (50, 6, 256, torch.float32), (3, 5, 24, torch.bfloat16)])
+@pytest.mark.parametrize("strided", ["from", "to", "both", "layers"])
+def test_compact_of_strided_pools(page, heads, d, dtype, strided):
+    """Pools whose rows of all heads lie together, and pools cut from larger ones; pages of few and of many pieces."""
+    c = Cache(5, 4, page, 30, 2, heads, d, dtype, seed=page)
+    live = [p for p, r in enumerate(c.refs.tolist()) if r > 0]
+    turned = lambda t: t.permute(0, 1, 3, 2, 4).contiguous().permute(0, 1, 3, 2, 4)  # noqa: E731
+    k, v = (turned(t) if strided in ("from", "both") else t for t in (c.k, c.v))
+    kt, vt = (torch.full((2, len(live) + 3, heads, page, d), 7.0, dtype=dtype, device="cuda") for _ in range(2))
+    if strided in ("to", "both"):
+        kt, vt = turned(kt), turned(vt)
+    if strided == "layers":  # every other layer of larger pools, with more pages
+        k, v, kt, vt = (torch.full((4, t.shape[1] + 2, heads, page, d), 7.0, dtype=dtype, device="cuda")[::2, :-2].copy_(t) for t in (k, v, kt, vt))
+    table, new, missing = tk.pages_compact(k, v, c.table, c.refs, kt, vt)
+    assert int(missing) == 0 and new.tolist() == [1] * len(live) + [0] * 3
+    same = torch.equal(kt[:, :len(live)], c.k[:, live]) and torch.equal(vt[:, :len(live)], c.v[:, live])
+    assert same and bool((kt[:, len(live):] == 7).all()) and bool((vt[:, len(live):] == 7).all())
 
 
 def test_strided_pools_tables_and_rows():

@@ -90,6 +90,34 @@ def test_packed_layer_learns():
         assert float((got[n].float() - p.grad.float()).norm()) <= 2.0 ** -6 * float(p.grad.float().norm()), n
 
 
+def test_captured_training_step():
+    """Forward and backward of packed sequences in a graph: every replay has the gradients of the eager step, with
+    other offsets and inputs and with eager steps in between."""
+    layer = _layer(True, qk_norm=True, rope_theta=10000.0)
+    weights = list(layer.parameters())
+    x, g = (torch.randn(180, 256, device="cuda", dtype=BF16) for _ in range(2))
+    off = _int([0, 50, 51, 180])
+    step = lambda: torch.autograd.grad(layer.packed(x, off), weights, g)  # noqa: E731
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for o in ([0, 50, 51, 180], [0, 0, 180, 180], [0, 100, 130, 180], [0, 50, 51, 180]):
+        off.copy_(_int(o))
+        x.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            same = torch.equal(a, b)
+            assert same
+
+
 def test_tree_depths():
     par = [[-1, 0, 1, 1, 3, -1, 5, 9], [3, 0, 1, 2, 3, 4, 5, 6]]
     want = [[0, 1, 2, 2, 3, 0, 1, 0], [0, 1, 2, 3, 4, 5, 6, 7]]
