@@ -28,7 +28,7 @@ struct PackedProblem {
 };
 
 constexpr int PACKED_TILE = 128;  // rows of a workgroup
-// workgroups of a head at most, of so many rows, and one for the tokens of no sequence
+// workgroups of a head at most, of so many rows, and one more, so that one is left for the tokens of no sequence
 int64_t packed_tiles(const PackedProblem& p, int rows = PACKED_TILE);
 // so few workgroups of PACKED_TILE rows that half as many rows are better
 bool packed_few(const PackedProblem& p, int heads);

@@ -70,9 +70,12 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   const int group = wave % (WAVES / KS), share = wave / (WAVES / KS);  // of rows; of a tile's keys
   const int2 item = packed_item(a.p.H);
   const int h = item.x;
-  if (blockIdx.x >= gridDim.x - a.p.H) {  // tokens of no sequence
+  int all = 0;
+  const PackedPlace at = packed_place(a.p, item.y, ROWS, a.p.H, CAUSAL, false, &all);
+  if (!at.n) {  // the workgroups of a head that have no tile share the tokens of no sequence
     const int N = (int)a.p.N, z0 = min(max(a.p.offsets[0], 0), N), z1 = max(z0, min(max(a.p.offsets[a.p.n], 0), N));
-    for (int64_t i = tid; i < (int64_t)(z0 + N - z1) * CH; i += NT) {
+    const int64_t parts = (int64_t)(z0 + N - z1) * CH, step = (int64_t)(gridDim.x / a.p.H - all) * NT;
+    for (int64_t i = (int64_t)(item.y - all) * NT + tid; i < parts; i += step) {
       const int64_t r = i / CH, t = r < z0 ? r : r - z0 + z1;
       const int64_t e = h * a.p.out.head + t * a.p.out.token + i % CH * 8;
       *(uint4*)((uint16_t*)a.p.out.p + e) = make_uint4(0, 0, 0, 0);
@@ -81,8 +84,6 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     }
     return;
   }
-  const PackedPlace at = packed_place(a.p, item.y, ROWS, a.p.H, CAUSAL, false);
-  if (!at.n) return;
   const int hk = h / (a.p.H / a.p.Hkv);
   const int row = at.tile * ROWS + group * 32 + n;  // the lane's query in its sequence
   const bool ok = row < at.n;

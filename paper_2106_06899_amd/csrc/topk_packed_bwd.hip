@@ -3,8 +3,8 @@
 //   dV = P^T d_out,  dS = P (d_out V^T - D),  dQ = scale dS K,  dK = scale dS^T Q.
 // D is taken from out and what rounding it to bf16 took (its rounding alone would put dQ and dK off by 2.8e-3 in place
 // of 2.4e-3, of which their own rounding is 1.7e-3).
-// Three launches: the rows' lse and D; dQ, a workgroup a tile of 128 queries, over the keys; dK and dV, a
-// workgroup a tile of 128 keys and key head, over the queries of all its query heads. Each gradient is summed
+// Three launches: the rows' lse and D (and zeros for the tokens of no sequence); dQ, a workgroup a tile of 128 queries,
+// over the keys; dK and dV, a workgroup a tile of 128 keys and key head, over the queries of all its query heads. Each gradient is summed
 // where it ends up, in a fixed order, without atomics, which costs a second S and d_out V^T: seven products in
 // place of five.
 //
@@ -30,13 +30,26 @@ struct BackwardArgs {
   float c;  // scale * log2(e)
 };
 
+__device__ __forceinline__ void clear_part(const PackedRows& to, int64_t h, int64_t t, int c) {
+  *(uint4*)((uint16_t*)to.p + h * to.head + t * to.token + c) = make_uint4(0, 0, 0, 0);
+}
+
 // 16 rows a workgroup (D = 128) or 32
 template <int D>
 __global__ __launch_bounds__(NT) void k_packed_stat(BackwardArgs a) {
   constexpr int LR = D / 8;  // lanes of a row
-  const int64_t i = (int64_t)blockIdx.x * (NT / LR) + threadIdx.x / LR, h = i / a.p.N, t = i - h * a.p.N;
+  const uint32_t row = blockIdx.x * (NT / LR) + threadIdx.x / LR, head = row / (uint32_t)a.p.N;  // (fewer than 2^28 rows)
+  const int64_t i = row, h = head, t = row - head * (uint32_t)a.p.N;
   if (h >= a.p.H) return;
-  const int c = threadIdx.x % LR * 8;
+  const int c = threadIdx.x % LR * 8, N = (int)a.p.N;
+  if (t < min(max(a.p.offsets[0], 0), N) || t >= min(max(a.p.offsets[a.p.n], 0), N)) {  // a token of no sequence
+    clear_part(a.p.dq, h, t, c);
+    if (h < a.p.Hkv && a.p.splits == 1) {  // (else the sums' launch does it)
+      clear_part(a.p.dk, h, t, c);
+      clear_part(a.p.dv, h, t, c);
+    }
+    return;
+  }
   const int64_t at = h * a.p.out.head + t * a.p.out.token + c;
   const u32x4 x = *(const u32x4*)((const uint16_t*)a.p.out.p + at);
   const u32x4 y = a.p.rest ? *(const u32x4*)((const uint16_t*)a.p.rest + at) : (u32x4){};
@@ -152,17 +165,6 @@ __device__ __forceinline__ void store_rows(const f32x16 (&o)[D / 32], float by, 
   wave_sync_lds();
 }
 
-// zeros for the tokens of no sequence
-template <int D>
-__device__ __forceinline__ void clear_outside(const PackedProblem& p, const PackedRows& to, int h) {
-  constexpr int CH = 2 * D / 16;
-  const int N = (int)p.N, z0 = min(max(p.offsets[0], 0), N), z1 = max(z0, min(max(p.offsets[p.n], 0), N));
-  for (int64_t i = threadIdx.x; i < (int64_t)(z0 + N - z1) * CH; i += NT) {
-    const int64_t r = i / CH, t = r < z0 ? r : r - z0 + z1;
-    *(uint4*)((uint16_t*)to.p + h * to.head + t * to.token + i % CH * 8) = make_uint4(0, 0, 0, 0);
-  }
-}
-
 // KS = 2: half the rows a workgroup, and two waves share each 32, one taking the first and one the last 32 keys of
 // every tile, as in the forward pass.
 template <int D, bool CAUSAL, int KS>
@@ -179,7 +181,6 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dq(BackwardArgs a) {
   const int group = wave % (WAVES / KS), share = wave / (WAVES / KS);  // of rows; of a tile's keys
   const int2 item = packed_item(a.p.H);
   const int h = item.x;
-  if (blockIdx.x >= gridDim.x - a.p.H) return clear_outside<D>(a.p, a.p.dq, h);
   const PackedPlace at = packed_place(a.p, item.y, TROWS, a.p.H, CAUSAL, false);
   if (!at.n) return;
   const int hk = h / (a.p.H / a.p.Hkv);
@@ -321,11 +322,6 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dkv(BackwardArgs a) {
   const int splits = a.p.splits;
   const int2 item = packed_item(a.p.Hkv * splits);
   const int hk = item.x / splits, split = item.x - hk * splits;
-  if (blockIdx.x >= gridDim.x - a.p.Hkv * splits) {
-    if (splits > 1) return;  // (the sums' launch does it)
-    clear_outside<D>(a.p, a.p.dk, hk);
-    return clear_outside<D>(a.p, a.p.dv, hk);
-  }
   const PackedPlace at = packed_place(a.p, item.y, PACKED_TILE, a.p.Hkv * splits, CAUSAL, true);
   if (!at.n) return;
   const int G = a.p.H / a.p.Hkv;

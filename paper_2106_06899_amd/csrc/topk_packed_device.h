@@ -56,8 +56,9 @@ __device__ __forceinline__ bool block_find(uint32_t mine, uint32_t t, uint32_t* 
 // Tile number t of all sequences' tiles of `rows` tokens. levels: up to 64 sequences' tiles are numbered by
 // their place in their sequence, the last places (or, from_end, the first) first: under a causal mask these
 // have the most to do. Every wave finds it by itself; more sequences are looked through by the whole workgroup, four a
-// thread.
-__device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int t, int rows, int heads, bool levels, bool from_end) {
+// thread. *tiles, for a workgroup without a tile: how many there are.
+__device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int t, int rows, int heads, bool levels, bool from_end,
+                                                    int* tiles = nullptr) {
   const int lane = threadIdx.x & 63;
   PackedPlace at = {0, 0, 0};
   auto bounds = [&](int s, int* a, int* len) {
@@ -74,6 +75,7 @@ __device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int 
     if (levels) {
       auto longer = [&](int c) { return (int)wave_sum((uint32_t)max(nt - c, 0)); };  // tiles in places from c on
       const int all = longer(0);
+      if (tiles) *tiles = all;
       if (all <= t) return at;
       // Where every CU has one or two workgroups in all, those that come second are the shortest first: the longest
       // shares its CU with the shortest.
@@ -91,6 +93,7 @@ __device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int 
     } else {
       const uint32_t end = wave_incl_scan_full((uint32_t)nt);
       const uint64_t those = __builtin_amdgcn_ballot_w64(end > (uint32_t)t);
+      if (tiles) *tiles = __builtin_amdgcn_readlane((int)end, 63);
       if (!those) return at;
       s = __builtin_ctzll(those);
       at.tile = t - (__builtin_amdgcn_readlane((int)end, s) - __builtin_amdgcn_readlane(nt, s));
@@ -125,6 +128,7 @@ __device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int 
     }
     __syncthreads();
     s = found[0];
+    if (tiles) *tiles = (int)before;
     if (s < 0) return at;
     at.tile = found[1];
   }

@@ -101,6 +101,9 @@ CASES = {
     "more_all_keys": ([i * 13 for i in range(70)], 897, 1, 1, 128, False),
     "hundreds_of_them": ([(i * 5) // 2 for i in range(700)], 1748, 1, 1, 64, True),
     "thousands": ([min(i, 2500) for i in range(2600)], 2510, 1, 1, 128, False),
+    "mostly_padding": ([100, 200, 330], 9000, 4, 2, 64, True),
+    "mostly_padding_d128": ([1000, 1200, 1201], 9001, 4, 1, 128, False),
+    "padding_behind_many": ([7 * i + 500 for i in range(100)], 7000, 2, 2, 64, True),
     # more than 256 workgroups of 128 rows: a workgroup's waves have rows of their own
     "many_workgroups": ([0, 1000, 1003, 3200], 3210, 12, 3, 64, True),
     "many_workgroups_d128": ([0, 1000, 1064, 3200], 3200, 12, 12, 128, True),
