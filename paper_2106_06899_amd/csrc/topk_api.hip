@@ -1606,7 +1606,7 @@ int topk_pages_reserve(const topk_pages* pool, int32_t* table, int64_t table_str
     return rc;
   if (rows_each && (rc = int_ptr(rows_each, "rows_each"))) return rc;
   if (rows < 0 || rows > 0x7FFFFFFFLL) return fail(TOPK_E_INVAL, "rows must be 0 to 2^31 - 1 (got %lld)", (long long)rows);
-  if (B > MAX_WGS / (pages_workgroups(a.s, 1))) return too_many_wgs(MAX_WGS + 1);
+  if (B > 0xFFFFFFFFLL / pages_parts(a.s, 1)) return fail(TOPK_E_UNSUPPORTED, "a copy of 2^32 pieces of 32 KiB or more");
   a.refs = refs;
   a.missing = missing;
   a.lengths = lengths;
@@ -1725,7 +1725,7 @@ int topk_pages_compact(const topk_pages* pool, const topk_pages* to, const int32
   if (a.s.layers != s_to.layers || a.s.heads != s_to.heads || a.s.page_rows != s_to.page_rows || a.s.pieces != s_to.pieces)
     return fail(TOPK_E_INVAL, "the pools differ in layers, heads, rows of a page or features");
   if (pool->k == to->k || pool->v == to->v) return fail(TOPK_E_INVAL, "the new pool is the old one's memory");
-  if (std::min(s_to.n_pages, a.s.n_pages) > (MAX_WGS - B * M / 256 - 1) / pages_workgroups(a.s, 1)) return too_many_wgs(MAX_WGS + 1);
+  if (std::min(s_to.n_pages, a.s.n_pages) > 0xFFFFFFFFLL / pages_parts(a.s, 1)) return fail(TOPK_E_UNSUPPORTED, "a copy of 2^32 pieces of 32 KiB or more");
   a.refs = refs;
   a.new_table = new_table;
   a.new_refs = new_refs;

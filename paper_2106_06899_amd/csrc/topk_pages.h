@@ -35,7 +35,8 @@ struct ReserveArgs {
   const int32_t *lengths, *rows_each;
   int64_t rows;
   int32_t *kind, *free_list;  // workspace: an entry of the tables each; pages found free
-  int4* copies;               // [B]: from, to, rows
+  int4* copies;               // [B + 1]: how many follow; from, to, rows of each
+  int32_t* listed;            // large pools: [cdiv(n_pages, FREE_BLOCK)] free pages of a block; and which, [n_pages]
 };
 struct AppendArgs {
   PagePool pool, from;  // from: `page` is a request's stride (or unused), `row` a token's
@@ -80,6 +81,6 @@ hipError_t launch_keep(const KeepArgs& a, hipStream_t st);
 hipError_t launch_fork(ForkArgs a, void* ws, hipStream_t st);
 hipError_t launch_release(const PageTable& t, int32_t* refs, const int32_t* lengths, int64_t n_pages, int page_rows, hipStream_t st);
 hipError_t launch_compact(CompactArgs a, void* ws, hipStream_t st);
-int64_t pages_workgroups(const PageShape& s, int64_t pages);  // of a copy of so many pages
+int64_t pages_parts(const PageShape& s, int64_t pages);  // pieces of work of a copy of so many pages
 
 }  // namespace topk

@@ -19,7 +19,9 @@ namespace {
 
 constexpr int BOOK = 1024;       // threads of a workgroup on the books
 constexpr int NT = 256;          // on rows
-constexpr int PIECES = 8 * NT;   // 16-byte pieces that a workgroup copies
+constexpr int PIECES = 8 * NT;   // 16-byte pieces that a workgroup copies at a time
+constexpr int FREE_BLOCK = 4096; // pages of a block whose free ones are listed
+constexpr int FREE_DIRECT = 4 * FREE_BLOCK;  // pages of a pool that a reservation looks through by itself
 
 int64_t cdiv(int64_t x, int64_t y) { return (x + y - 1) / y; }
 size_t up(size_t x) { return (x + 255) / 256 * 256; }
@@ -134,14 +136,30 @@ struct Entries {
   }
 };
 
+// The free pages of each block of a large pool. (A workgroup alone looks through 4096 pages in 1.6 us, a pool of a
+// million in 390 us; listed by one workgroup a block it takes 17.)
+__global__ __launch_bounds__(BOOK) void k_pages_free(ReserveArgs a) {
+  __shared__ uint32_t sums[BOOK / 64];
+  const int64_t base = (int64_t)blockIdx.x * FREE_BLOCK + 4 * threadIdx.x;
+  bool free[4];
+  uint32_t c = 0;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) c += free[u] = base + u < a.s.n_pages && a.refs[base + u] == 0;
+  uint32_t n, at = book_scan(c, sums, &n) - c;
+  int32_t* list = a.listed + gridDim.x + (int64_t)blockIdx.x * FREE_BLOCK;
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+    if (free[u]) list[at++] = (int)(base + u);
+  if (threadIdx.x == 0) a.listed[blockIdx.x] = (int)n;
+}
+
 __global__ __launch_bounds__(BOOK) void k_pages_reserve(ReserveArgs a) {
-  __shared__ uint32_t ends[BOOK], sums[BOOK / 64];
+  __shared__ uint32_t ends[BOOK], sums[BOOK / 64], blocks[BOOK];
   __shared__ int32_t firsts[BOOK], found[BOOK];
   __shared__ int any_shared;
   const int tid = threadIdx.x, n_pages = (int)a.s.n_pages;
   Entries en = {a, ends, sums, firsts};
   if (tid == 0) any_shared = 0;
-  for (int b = tid; b < a.t.B; b += BOOK) a.copies[b] = make_int4(0, 0, 0, 0);
   en.begin();
   __syncthreads();
   uint32_t need = 0;
@@ -185,7 +203,25 @@ __global__ __launch_bounds__(BOOK) void k_pages_reserve(ReserveArgs a) {
   // the free pages of the lowest numbers, as many as are needed
   const bool few = need <= BOOK;
   uint32_t have = 0;
-  for (int64_t base = 0; base < n_pages && have < need; base += 4 * BOOK) {
+  const int n_blocks = (int)(((int64_t)n_pages + FREE_BLOCK - 1) / FREE_BLOCK);
+  for (int base = 0; a.listed && base < n_blocks && have < need; base += BOOK) {
+    uint32_t n;
+    blocks[tid] = book_scan(base + tid < n_blocks ? (uint32_t)a.listed[base + tid] : 0u, sums, &n);
+    __syncthreads();
+    for (uint32_t i = tid; i < n && have + i < need; i += BOOK) {
+      int lo = 0, hi = BOOK - 1;  // the first block whose pages end behind i
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (blocks[mid] > i) hi = mid;
+        else lo = mid + 1;
+      }
+      const int p = a.listed[n_blocks + (int64_t)(base + lo) * FREE_BLOCK + (i - (lo ? blocks[lo - 1] : 0))];
+      if (few) found[have + i] = p;
+      else a.free_list[have + i] = p;
+    }
+    have += n;
+  }
+  for (int64_t base = 0; !a.listed && base < n_pages && have < need; base += 4 * BOOK) {
     bool free[4];
     uint32_t c = 0;
 #pragma unroll
@@ -205,7 +241,10 @@ __global__ __launch_bounds__(BOOK) void k_pages_reserve(ReserveArgs a) {
   }
   book_sync();
   if (have < need) {  // nothing is changed: those that left are counted again
-    if (tid == 0) *a.missing = (int)(need - have);
+    if (tid == 0) {
+      *a.missing = (int)(need - have);
+      a.copies[0].x = 0;
+    }
     if (!shared) return;
     en.each([&](bool ok, int, int, int, int p, int* k, int) {
       if (ok && *k == KEEPS) a.refs[p] = 0;
@@ -216,19 +255,28 @@ __global__ __launch_bounds__(BOOK) void k_pages_reserve(ReserveArgs a) {
     });
     return;
   }
-  if (tid == 0) *a.missing = 0;
-  uint32_t taken = 0;
+  uint32_t taken = 0, copied = 0;
   en.each([&](bool ok, int, int b, int e, int p, int* k, int left) {
     const bool takes = ok && (*k == FRESH || *k == LEAVES);
     uint32_t n;
     const uint32_t at = taken + book_scan(takes, sums, &n) - 1;
     taken += n;
+    const bool copies = takes && *k == LEAVES && left > 0;  // (`left` rows of the page are in use)
+    uint32_t copy = 0;
+    if (shared) {
+      copy = copied + book_scan(copies, sums, &n);
+      copied += n;
+    }
     if (!takes) return;
     const int to = few ? found[at] : a.free_list[at];
-    if (*k == LEAVES && left > 0) a.copies[b] = make_int4(p, to, left, 0);  // (`left` rows of the page are in use)
+    if (copies) a.copies[copy] = make_int4(p, to, left, 0);
     a.t.at[b * a.t.stride + e] = to;
     a.refs[to] = 1;
   });
+  if (tid == 0) {
+    *a.missing = 0;
+    a.copies[0].x = (int)copied;
+  }
 }
 
 __device__ __forceinline__ f32x4* piece_ptr(const PagePool& pool, int kv, int64_t layer, int64_t page, int64_t at, int es) {
@@ -289,7 +337,11 @@ __device__ __forceinline__ void copy_page(const PagePool& pa, const PagePool& pb
 struct CopyPlace {
   int page, layer, part, kv;
 };
-// the page, layer, pool and part of copying workgroup i
+// pieces of work of a page's copy in all layers
+__device__ __forceinline__ uint32_t copy_parts(const PageShape& s) {
+  return ((uint32_t)s.heads * s.page_rows * s.pieces + PIECES - 1) / PIECES * 2 * (uint32_t)s.layers;
+}
+// the page, layer, pool and part of piece i
 __device__ __forceinline__ CopyPlace copy_place(const PageShape& s, uint32_t i) {
   const uint32_t parts = ((uint32_t)s.heads * s.page_rows * s.pieces + PIECES - 1) / PIECES, layers = (uint32_t)s.layers;
   CopyPlace c;
@@ -303,9 +355,12 @@ __device__ __forceinline__ CopyPlace copy_place(const PageShape& s, uint32_t i) 
 }
 
 __global__ __launch_bounds__(NT) void k_pages_copy(ReserveArgs a) {
-  const CopyPlace c = copy_place(a.s, blockIdx.x);
-  const int4 x = a.copies[c.page];
-  if (x.z) copy_page<false>(a.pool, a.pool, a.s, c.kv, c.layer, c.part, x.x, x.y, x.z);
+  const uint32_t all = (uint32_t)a.copies[0].x * copy_parts(a.s);
+  for (uint64_t i = blockIdx.x; i < all; i += gridDim.x) {
+    const CopyPlace c = copy_place(a.s, (uint32_t)i);
+    const int4 x = a.copies[1 + c.page];
+    copy_page<false>(a.pool, a.pool, a.s, c.kv, c.layer, c.part, x.x, x.y, x.z);
+  }
 }
 
 // One token of one layer a workgroup: its keys and values to row lengths[b] + its place in the request.
@@ -409,7 +464,7 @@ __global__ __launch_bounds__(NT) void k_pages_fork(ForkArgs a) {
   int32_t* tmp = a.tmp + (int64_t)b * (a.t.M + 1);
   const int len = par < 0 ? 0 : a.lengths[par];
   const int64_t n = pages_of(len, a.page_rows);
-  for (int e = threadIdx.x; e < a.t.M; e += NT) {
+  for (int64_t e = blockIdx.y * NT + threadIdx.x; e < a.t.M; e += NT * gridDim.y) {
     const int old = a.t.at[b * a.t.stride + e];
     int p = par >= 0 && e < n ? a.t.at[par * a.t.stride + e] : -1;
     if ((uint32_t)p >= (uint32_t)a.n_pages) p = -1;
@@ -419,15 +474,15 @@ __global__ __launch_bounds__(NT) void k_pages_fork(ForkArgs a) {
     }
     tmp[e] = p;
   }
-  if (threadIdx.x == 0) tmp[a.t.M] = len;
+  if (threadIdx.x == 0 && blockIdx.y == 0) tmp[a.t.M] = len;
 }
 __global__ __launch_bounds__(NT) void k_pages_forked(ForkArgs a) {
   const int b = blockIdx.x;
   const int par = a.parents[b];
   if (par == b || par >= a.t.B) return;
   const int32_t* tmp = a.tmp + (int64_t)b * (a.t.M + 1);
-  for (int e = threadIdx.x; e < a.t.M; e += NT) a.t.at[b * a.t.stride + e] = tmp[e];
-  if (threadIdx.x == 0) a.lengths[b] = tmp[a.t.M];
+  for (int64_t e = blockIdx.y * NT + threadIdx.x; e < a.t.M; e += NT * gridDim.y) a.t.at[b * a.t.stride + e] = tmp[e];
+  if (threadIdx.x == 0 && blockIdx.y == 0) a.lengths[b] = tmp[a.t.M];
 }
 
 // The same for tables of few entries, in one launch: one workgroup reads all of the old tables before it writes.
@@ -459,7 +514,7 @@ __global__ __launch_bounds__(BOOK) void k_pages_fork_few(ForkArgs a) {
 
 __global__ __launch_bounds__(NT) void k_pages_release(PageTable t, int32_t* refs, const int32_t* lengths, int64_t n_pages, int page_rows) {
   const int b = blockIdx.x;
-  for (int64_t e = pages_of(lengths[b], page_rows) + threadIdx.x; e < t.M; e += NT) {
+  for (int64_t e = pages_of(lengths[b], page_rows) + blockIdx.y * NT + threadIdx.x; e < t.M; e += NT * gridDim.y) {
     int32_t* at = t.at + b * t.stride + e;
     const int p = *at;
     if (p == -1) continue;
@@ -516,26 +571,33 @@ __global__ __launch_bounds__(NT) void k_pages_move(CompactArgs a, uint32_t table
     a.new_table[i] = live && (uint32_t)p < (uint32_t)a.s.n_pages ? a.number[p] : -1;
     return;
   }
-  const CopyPlace c = copy_place(a.s, blockIdx.x - table_wgs);
-  if (c.page < live) copy_page<FLAT>(a.pool, a.to, a.s, c.kv, c.layer, c.part, a.live[c.page], c.page, a.s.page_rows);
+  const uint64_t all = (uint64_t)live * copy_parts(a.s);  // (below 2^32)
+  for (uint64_t i = blockIdx.x - table_wgs; i < all; i += gridDim.x - table_wgs) {
+    const CopyPlace c = copy_place(a.s, (uint32_t)i);
+    copy_page<FLAT>(a.pool, a.to, a.s, c.kv, c.layer, c.part, a.live[c.page], c.page, a.s.page_rows);
+  }
 }
 
 }  // namespace
 
-int64_t pages_workgroups(const PageShape& s, int64_t pages) {
+int64_t pages_parts(const PageShape& s, int64_t pages) {
   return pages * s.layers * 2 * cdiv(s.heads * s.page_rows * s.pieces, PIECES);
 }
 
+static size_t listed_bytes(const PageShape& s) { return s.n_pages <= FREE_DIRECT ? 0 : (cdiv(s.n_pages, FREE_BLOCK) + s.n_pages) * 4; }
 size_t reserve_bytes(const PageShape& s, const PageTable& t) {
   const int64_t entries = (int64_t)t.B * t.M;
-  return up(t.B * sizeof(int4)) + up(entries * 4) + std::min(entries, s.n_pages) * 4;
+  return up((t.B + 1) * sizeof(int4)) + up(entries * 4) + up(std::min(entries, s.n_pages) * 4) + listed_bytes(s);
 }
 hipError_t launch_reserve(ReserveArgs a, void* ws, hipStream_t st) {
+  const int64_t entries = (int64_t)a.t.B * a.t.M;
   a.copies = (int4*)ws;
-  a.kind = (int32_t*)((char*)ws + up(a.t.B * sizeof(int4)));
-  a.free_list = (int32_t*)((char*)a.kind + up((size_t)a.t.B * a.t.M * 4));
+  a.kind = (int32_t*)((char*)ws + up((a.t.B + 1) * sizeof(int4)));
+  a.free_list = (int32_t*)((char*)a.kind + up(entries * 4));
+  a.listed = listed_bytes(a.s) ? (int32_t*)((char*)a.free_list + up(std::min(entries, a.s.n_pages) * 4)) : nullptr;
+  if (a.listed) k_pages_free<<<(unsigned)cdiv(a.s.n_pages, FREE_BLOCK), BOOK, 0, st>>>(a);
   k_pages_reserve<<<1, BOOK, 0, st>>>(a);
-  k_pages_copy<<<(unsigned)pages_workgroups(a.s, a.t.B), NT, 0, st>>>(a);
+  k_pages_copy<<<(unsigned)std::min<int64_t>(pages_parts(a.s, a.t.B), 2048), NT, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -550,6 +612,9 @@ hipError_t launch_keep(const KeepArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// A workgroup a request and 1024 entries.
+static dim3 table_grid(const PageTable& t) { return dim3(t.B, (unsigned)std::min<int64_t>(cdiv(t.M, 4 * NT), 1024)); }
+
 // (64 requests with tables of 126 pages: 6.4 us in two launches or in one, which is 3.5 us less for the host)
 size_t fork_bytes(const PageTable& t) { return (int64_t)t.B * t.M <= FORK_FEW ? 0 : (size_t)t.B * (t.M + 1) * 4; }
 hipError_t launch_fork(ForkArgs a, void* ws, hipStream_t st) {
@@ -558,13 +623,13 @@ hipError_t launch_fork(ForkArgs a, void* ws, hipStream_t st) {
     return hipGetLastError();
   }
   a.tmp = (int32_t*)ws;
-  k_pages_fork<<<a.t.B, NT, 0, st>>>(a);
-  k_pages_forked<<<a.t.B, NT, 0, st>>>(a);
+  k_pages_fork<<<table_grid(a.t), NT, 0, st>>>(a);
+  k_pages_forked<<<table_grid(a.t), NT, 0, st>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_release(const PageTable& t, int32_t* refs, const int32_t* lengths, int64_t n_pages, int page_rows, hipStream_t st) {
-  k_pages_release<<<t.B, NT, 0, st>>>(t, refs, lengths, n_pages, page_rows);
+  k_pages_release<<<table_grid(t), NT, 0, st>>>(t, refs, lengths, n_pages, page_rows);
   return hipGetLastError();
 }
 
@@ -573,7 +638,7 @@ hipError_t launch_compact(CompactArgs a, void* ws, hipStream_t st) {
   a.number = (int32_t*)ws;
   a.live = (int32_t*)((char*)ws + up(a.s.n_pages * 4));
   const int64_t table_wgs = cdiv((int64_t)a.t.B * a.t.M, NT);
-  const unsigned grid = (unsigned)(table_wgs + pages_workgroups(a.s, std::min(a.n_to, a.s.n_pages)));
+  const unsigned grid = (unsigned)(table_wgs + std::min<int64_t>(pages_parts(a.s, std::min(a.n_to, a.s.n_pages)), 1 << 16));
   bool flat = true;  // (a stride along one entry is 0)
   for (const PagePool* p : {&a.pool, &a.to})
     for (int i = 0; i < 2; ++i) {

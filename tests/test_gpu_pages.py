@@ -231,6 +231,44 @@ def test_forks_of_large_tables(B, M):
     assert not c.refs.any()
 
 
+@pytest.mark.parametrize("B,M,n,held", [(40, 400, 16384, 0), (40, 400, 16385, 1), (40, 1000, 50000, 0.9), (1500, 6, 41000, 0.5),
+                                        (3, 30000, 70001, 0.3)])
+def test_large_pools(B, M, n, held):
+    """Pools whose free pages are listed by blocks: the lowest numbers all the same, most of the first ones held by
+    somebody else."""
+    c = Cache(B, M, 2, n, 1, 1, 8, seed=n, longest=20 if M > 6 else 6)
+    refs = c.refs.tolist()
+    for p in range(n // 2 if held < 1 else n - B // 2):
+        if refs[p] == 0 and c.rng.random() < held:
+            refs[p] = 1
+    c.set(c.table.tolist(), refs, c.lengths.tolist())
+    for _ in range(2):
+        c.fork([c.rng.choice([b, c.rng.randrange(B)]) for b in range(B)])
+        rows = 3 if M == 6 else 100 if held == 0 else 40 if M < 30000 else [30000, 0, 20011]
+        missing = c.reserve(rows)
+        assert (missing > 0) == (held == 1)
+        if not missing:  # (else several would write to one page)
+            c.append(2)
+    c.release()
+    live = sum(r > 0 for r in c.books.refs)
+    kt, vt = (torch.full((1, live, 1, 2, 8), 7.0, dtype=c.k.dtype, device="cuda") for _ in range(2))
+    table, new, missing = tk.pages_compact(c.k, c.v, c.table, c.refs, kt, vt)
+    at = c.refs > 0
+    same = torch.equal(kt, c.k[:, at]) and torch.equal(vt, c.v[:, at]) and torch.equal(new, c.refs[at])
+    assert int(missing) == 0 and same
+    number = torch.where(at, at.cumsum(0) - 1, -1).int()
+    assert torch.equal(table, torch.where(c.table >= 0, number[c.table.long().clamp(min=0)], -1))
+
+
+@pytest.mark.parametrize("page,heads,layers", [(64, 8, 3), (130, 5, 40)])
+def test_many_copies(page, heads, layers):
+    """Copies of more pieces than there are workgroups."""
+    c = Cache(60, 4, page, 200, layers, heads, 64, seed=page, longest=3 * page)
+    c.fork([b // 3 * 3 for b in range(60)])
+    assert c.reserve(1) == 0
+    c.append(1)
+
+
 def test_a_long_reservation():
     """More entries a request than a workgroup takes at once."""
     c = Cache(3, 4000, 2, 9000, 1, 1, 8, seed=4, longest=100)
