@@ -1606,7 +1606,7 @@ int topk_pages_reserve(const topk_pages* pool, int32_t* table, int64_t table_str
     return rc;
   if (rows_each && (rc = int_ptr(rows_each, "rows_each"))) return rc;
   if (rows < 0 || rows > 0x7FFFFFFFLL) return fail(TOPK_E_INVAL, "rows must be 0 to 2^31 - 1 (got %lld)", (long long)rows);
-  if (B > 0xFFFFFFFFLL / pages_parts(a.s, 1)) return fail(TOPK_E_UNSUPPORTED, "a copy of 2^32 pieces of 32 KiB or more");
+  if (B > MAX_WGS / pages_parts(a.s, 1)) return fail(TOPK_E_UNSUPPORTED, "too many requests and layers: their copies may come to 2^24 pieces of 32 KiB");
   a.refs = refs;
   a.missing = missing;
   a.lengths = lengths;

@@ -108,7 +108,7 @@ def _compact(**kw):
     (dict(to=None), E_NULL), (dict(to=dict(heads=2)), E_INVAL), (dict(to=dict(page_rows=8)), E_INVAL), (dict(to=dict(layers=1)), E_INVAL),
     (dict(to=dict(d=128)), E_INVAL), (dict(to=dict(k=FAKE)), E_INVAL), (dict(to=dict(pages=0)), E_INVAL), (dict(new_table=None), E_NULL),
     (dict(new_refs=FAKE + 2), E_ALIGN), (dict(refs=None), E_NULL), (dict(missing=None), E_NULL),
-    (dict(pool=dict(pages=1 << 23), to=dict(pages=1 << 23)), E_UNSUPPORTED)])
+    (dict(pool=dict(pages=1 << 30, layers=2), to=dict(pages=1 << 30, layers=2)), E_UNSUPPORTED)])
 def test_compact_refusals(kw, code):
     assert _compact(**kw) == code
 
