@@ -449,17 +449,20 @@ size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64
  *   offsets    device, int32 [n + 1], not decreasing, within [0, N]; a sequence may be empty
  *   out        [H, N, d]   written, with strides of its own; tokens of no sequence are 0
  *   lse        NULL, or fp32 [H, N]: log sum_j exp(scale * s_j); -inf for tokens of no sequence
- *   rest       NULL, or laid out as out: what rounding took from it, for the backward pass
+ *   rest       NULL, or laid out as out: what rounding took from it, for the backward pass; with lse and
+ *              d = 64, or N <= 1024, or N <= 64 n, weights are then taken to 16 significant bits
  *
  * bf16 with d = 64 or 128 (else TOPK_E_UNSUPPORTED). Scores, softmax statistics and sums in fp32, in a
- * fixed order; weights enter the product with V rounded to bf16. A row is computed from its own
+ * fixed order; weights enter the product with V rounded to bf16, and are divided by the sum of the
+ * rounded ones. A row is computed from its own
  * numbers alone: keys and values it does not see may be infinite or NaN. No workspace. Offsets that
  * decrease give no meaningful result, but no access outside the tensors.
  *
  * topk_attn_packed_backward -- its gradients, from the inputs, out, lse (required here) and rest (NULL: taken as
- * 0, which costs d_Q and d_K a little of their precision) of the forward call and d_out [H, N, d]: d_Q [H, N, d], d_K, d_V [Hkv, N, d], every element written (tokens of
- * no sequence: 0). The weights are recomputed from lse; those below 2^-126 count as 0. Score gradients and
- * weights enter their products rounded to bf16; sums in fp32, in a fixed order, over the query
+ * 0, which costs d_Q and d_K a little of their precision) of the forward call and d_out [H, N, d]:
+ * d_Q [H, N, d], d_K, d_V [Hkv, N, d], every element written (tokens of no sequence: 0). The weights are
+ * recomputed from lse; those below 2^-126 count as 0. Score gradients and weights enter their products
+ * rounded to bf16, or, with N <= 1024 or N <= 64 n, to 16 significant bits; sums in fp32, in a fixed order, over the query
  * heads that share a key head too. d_out may be strided like the others. Workspace:
  * topk_attn_packed_backward_workspace_bytes. Stage 4 of the stage timing (forward: 0).
  */

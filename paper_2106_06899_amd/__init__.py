@@ -678,7 +678,8 @@ def attn_packed(q, k, v, offsets, causal: bool = True, scale: float | None = Non
 
     Returns out [H, N, d], laid out as q (0 for tokens of no sequence); with ``lse`` also the fp32
     [H, N] logarithm of the sum of exp(scale * score), and with ``rest`` also what rounding took from
-    out, laid out as it (both for the backward pass). Heads may have any strides but for the last
+    out, laid out as it (both for the backward pass; with both, heads of 64 and short sequences have
+    their weights to 16 significant bits, otherwise 8). Heads may have any strides but for the last
     dimension, multiples of 8 (``x.view(N, heads, d).transpose(0, 1)`` of a projection, or one
     entry of ``qk_norm_rope``'s). bf16, d = 64 or 128; differentiable as ``layers.packed_attention``."""
     import torch

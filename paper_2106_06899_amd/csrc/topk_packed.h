@@ -32,6 +32,9 @@ constexpr int PACKED_TILE = 128;  // rows of a workgroup
 int64_t packed_tiles(const PackedProblem& p, int rows = PACKED_TILE);
 // so few workgroups of PACKED_TILE rows that half as many rows are better
 bool packed_few(const PackedProblem& p, int heads);
+// so few tokens, or so short sequences, that the training pass may as well have its weights and score gradients as two
+// bf16 numbers
+bool packed_short(const PackedProblem& p);
 size_t packed_backward_bytes(const PackedProblem& p);
 hipError_t launch_packed(const PackedProblem& p, hipStream_t st);
 hipError_t launch_packed_backward(PackedProblem p, void* ws, hipStream_t st);

@@ -9,7 +9,8 @@
 //   * a running softmax of each row in its two lanes;
 //   * O^T += V^T P^T by the same instruction: the weights, rounded to bf16 (relative 2^-9 at most) and divided by
 //     the sum of the rounded ones, in which what they have in common cancels, are its operand in the order
-//     the lane holds them, V^T comes from the row-major tile by transposing LDS reads.
+//     the lane holds them (TWO: as the sum of two bf16 numbers), V^T comes from the row-major tile by transposing LDS
+//     reads.
 // Tiles come by direct global-to-LDS loads, one ahead. Which sequence and tile a workgroup has it finds
 // from the offsets itself, so that nothing is read back and no list is built by a launch of its own; there are at most
 // N / 128 + n tiles a head, and those too many end at once.
@@ -45,7 +46,7 @@ struct PackedArgs {
 // LSE: the logarithm of the sum is asked for, so that the weights are summed before rounding, too. KS = 2: half the
 // rows a workgroup, and two waves share each 32, one taking the first and one the last 32 keys of every tile: twice
 // the workgroups, each of half the length, where there are few.
-template <int D, bool CAUSAL, bool LSE, int KS>
+template <int D, bool CAUSAL, bool LSE, int KS, bool TWO>
 __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   // The maximum that weights are taken against is moved, and the sums with it, only once a score leads it
   // by 2^8 in weight.
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
           if (LSE) whole_l += w;
           pt[e] = (__bf16)w;
         }
-        l = sum_of(pt, l);
+        if (!TWO) l = sum_of(pt, l);
 #pragma unroll
         for (int f = 0; f < FB; ++f) {
           o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp(st * FB + f), pt, o[f], 0, 0, 0);
@@ -201,7 +202,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
         }
       }
     }
-    bf16x8 pb[2 * NB], vf[AHEAD_V + 1];
+    bf16x8 pb[2 * NB], pl[2 * NB], vf[AHEAD_V + 1];
 #pragma unroll
     for (int j = 0; j < AHEAD_V; ++j) vf[j] = vp(j);
     __builtin_amdgcn_s_setprio(1);  // the other wave's softmax yields to this one's products
@@ -209,6 +210,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
       const float w = __builtin_amdgcn_exp2f(fmaf(s[v >> 4][v & 15], a.c, -off));
       if (LSE) whole_l += w;
       pb[v >> 3][v & 7] = (__bf16)w;
+      if (TWO) pl[v >> 3][v & 7] = (__bf16)(w - (float)pb[v >> 3][v & 7]);
     };
 #pragma unroll
     for (int v = 0; v < 8; ++v) wt(v);
@@ -217,10 +219,11 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     for (int j = 0; j < VM; ++j) {
       if (j + AHEAD_V < VM) vf[(j + AHEAD_V) % (AHEAD_V + 1)] = vp(j + AHEAD_V);
       o[j % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j % (AHEAD_V + 1)], pb[j / FB], o[j % FB], 0, 0, 0);
+      if (TWO) o[j % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j % (AHEAD_V + 1)], pl[j / FB], o[j % FB], 0, 0, 0);
       if (j + FB < VM)
 #pragma unroll
         for (int v = 0; v < 8 / FB; ++v) wt(8 + j * (8 / FB) + v);
-      if (j % FB == 0) l = sum_of(pb[j / FB], l);
+      if (!TWO && j % FB == 0) l = sum_of(pb[j / FB], l);
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
@@ -290,6 +293,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     }
     if (work && t * KEYS < wave_keys) tile(std::true_type{}, t, odd ? k1 : k0, odd ? v1 : v0);
   }
+  if (TWO) l = whole_l;
   l += __shfl_xor(l, 32, 64);
   if (LSE) whole_l += __shfl_xor(whole_l, 32, 64);
   __syncthreads();
@@ -353,12 +357,23 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   if (LSE && ok && !half) a.p.lse[h * a.p.N + at.first + row] = whole_l == 0.f ? -INFINITY : (m + log2f(whole_l)) * 0.69314718055994531f;
 }
 
-template <bool LSE, int KS>
+// In a training pass (rest is asked for) over heads of 64, or a short one, weights are two numbers: the D of the
+// backward pass is as exact as they are. (Heads of 64: dQ is off by 1.46 times its own rounding, from rounded weights
+// by 1.50; heads of 128: 1.44 and 1.47, for 7 % of a pass.)
+bool packed_two(const PackedProblem& p) { return p.rest && p.lse && (p.d == 64 || packed_short(p)); }
+
+template <bool LSE, int KS, bool TWO>
 void launch_for(const PackedArgs& a, unsigned grid, hipStream_t st) {
-  if (a.p.d == 64 && a.p.causal) k_packed<64, true, LSE, KS><<<grid, NT, 0, st>>>(a);
-  else if (a.p.d == 64) k_packed<64, false, LSE, KS><<<grid, NT, 0, st>>>(a);
-  else if (a.p.causal) k_packed<128, true, LSE, KS><<<grid, NT, 0, st>>>(a);
-  else k_packed<128, false, LSE, KS><<<grid, NT, 0, st>>>(a);
+  if (a.p.d == 64 && a.p.causal) k_packed<64, true, LSE, KS, TWO><<<grid, NT, 0, st>>>(a);
+  else if (a.p.d == 64) k_packed<64, false, LSE, KS, TWO><<<grid, NT, 0, st>>>(a);
+  else if (a.p.causal) k_packed<128, true, LSE, KS, TWO><<<grid, NT, 0, st>>>(a);
+  else k_packed<128, false, LSE, KS, TWO><<<grid, NT, 0, st>>>(a);
+}
+template <int KS>
+void launch_ks(const PackedArgs& a, unsigned grid, hipStream_t st) {
+  if (packed_two(a.p)) launch_for<true, KS, true>(a, grid, st);
+  else if (a.p.lse) launch_for<true, KS, false>(a, grid, st);
+  else launch_for<false, KS, false>(a, grid, st);
 }
 
 }  // namespace
@@ -369,14 +384,14 @@ int64_t packed_tiles(const PackedProblem& p, int rows) { return p.N / rows + std
 // keys, 8 heads 259 -> 302.)
 bool packed_few(const PackedProblem& p, int heads) { return p.N / PACKED_TILE * heads <= 256; }
 
+bool packed_short(const PackedProblem& p) { return p.N <= 1024 || p.N <= 64 * (int64_t)p.n; }
+
 hipError_t launch_packed(const PackedProblem& p, hipStream_t st) {
   PackedArgs a = {p, p.scale * 1.4426950408889634f};
   const bool few = packed_few(p, p.H);
   const unsigned grid = (unsigned)(packed_tiles(p, few ? PACKED_TILE / 2 : PACKED_TILE) * p.H);
-  if (p.lse && few) launch_for<true, 2>(a, grid, st);
-  else if (p.lse) launch_for<true, 1>(a, grid, st);
-  else if (few) launch_for<false, 2>(a, grid, st);
-  else launch_for<false, 1>(a, grid, st);
+  if (few) launch_ks<2>(a, grid, st);
+  else launch_ks<1>(a, grid, st);
   return hipGetLastError();
 }
 

@@ -2,7 +2,7 @@
 // D_i = d_out_i . out_i (which is sum_j P_ij (d_out_i . v_j)):
 //   dV = P^T d_out,  dS = P (d_out V^T - D),  dQ = scale dS K,  dK = scale dS^T Q.
 // D is taken from out and what rounding it to bf16 took (its rounding alone would put dQ and dK off by 2.8e-3 in place
-// of 2.4e-3, of which their own rounding is 1.7e-3).
+// of 2.4e-3, of which their own rounding is 1.66e-3).
 // Three launches: the rows' lse and D (and zeros for the tokens of no sequence); dQ, a workgroup a tile of 128 queries,
 // over the keys; dK and dV, a workgroup a tile of 128 keys and key head, over the queries of all its query heads. Each gradient is summed
 // where it ends up, in a fixed order, without atomics, which costs a second S and d_out V^T: seven products in
@@ -12,7 +12,10 @@
 // take the other side's rows through LDS in tiles of 64, read straight for the products over features and
 // transposed for those over rows (see PackedTile). Weights and score gradients come out of the first products
 // in the order in which the second take them; they are rounded to bf16 on the way (relative 2^-9 at most, as
-// the weights of the forward pass), sums are in fp32.
+// the weights of the forward pass), sums are in fp32. Where that costs little (packed_short) they are the sum of two
+// bf16 numbers: dQ, dK and dV are then off by what their own rounding is, in place of 1.4 times that (and, of few
+// numbers, up to 1.6). A pass over 1000 tokens takes 3 us more for it, over 2000 sequences of 30 tokens 545 -> 575; over
+// 14000 tokens, heads of 128, it would be 1670 -> 2330.
 #include "topk_packed_device.h"
 
 #include <math.h>
@@ -166,9 +169,9 @@ __device__ __forceinline__ void store_rows(const f32x16 (&o)[D / 32], float by, 
 }
 
 // KS = 2: half the rows a workgroup, and two waves share each 32, one taking the first and one the last 32 keys of
-// every tile, as in the forward pass.
-template <int D, bool CAUSAL, int KS>
-__global__ __launch_bounds__(NT, 2) void k_packed_dq(BackwardArgs a) {
+// every tile, as in the forward pass. TWO: score gradients as the sum of two bf16 numbers.
+template <int D, bool CAUSAL, int KS, bool TWO>
+__global__ __launch_bounds__(NT, TWO ? 1 : 2) void k_packed_dq(BackwardArgs a) {
   typedef PackedTile<D> Tile;
   constexpr int TROWS = PACKED_TILE / KS, NB = 2 / KS;  // rows of the workgroup; blocks of 32 of a tile that a wave takes
   constexpr int NS = D / 16, TILEB = ROWS * 2 * D, LPW = TILEB / 1024 / WAVES, FB = D / 32;
@@ -228,7 +231,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dq(BackwardArgs a) {
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::straight(kb, row0, rb, i), bq[i], s, 0, 0, 0);
         g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::straight(vb, row0, rb, i), bo[i], g, 0, 0, 0);
       }
-      bf16x8 ds[2];
+      bf16x8 ds[2], lo[2];
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.c, -lse)) * (g[v] - D_row);
       if (edge) {
@@ -238,12 +241,18 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dq(BackwardArgs a) {
           if (8 * (v >> 2) + (v & 3) >= last) s[v] = 0.f;
       }
 #pragma unroll
-      for (int v = 0; v < 16; ++v) ds[v >> 3][v & 7] = (__bf16)s[v];
+      for (int v = 0; v < 16; ++v) {
+        ds[v >> 3][v & 7] = (__bf16)s[v];
+        if (TWO) lo[v >> 3][v & 7] = (__bf16)(s[v] - (float)ds[v >> 3][v & 7]);
+      }
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
-        for (int f = 0; f < FB; ++f)
-          o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::across(kb, col0, f, rb * 2 + st), ds[st], o[f], 0, 0, 0);
+        for (int f = 0; f < FB; ++f) {
+          const bf16x8 x = Tile::across(kb, col0, f, rb * 2 + st);
+          o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, ds[st], o[f], 0, 0, 0);
+          if (TWO) o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, lo[st], o[f], 0, 0, 0);
+        }
     }
   };
   const int whole = min(keys, all_see) / ROWS;  // tiles that every row sees whole come first
@@ -307,8 +316,9 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dq(BackwardArgs a) {
                 at.tile * TROWS + group * 32, at.n);
 }
 
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(NT, 2) void k_packed_dkv(BackwardArgs a) {
+// TWO: weights and score gradients as sums of two bf16 numbers.
+template <int D, bool CAUSAL, bool TWO>
+__global__ __launch_bounds__(NT, TWO ? 1 : 2) void k_packed_dkv(BackwardArgs a) {
   typedef PackedTile<D> Tile;
   constexpr int NS = D / 16, TILEB = ROWS * 2 * D, LPW = TILEB / 1024 / WAVES, FB = D / 32;
   __shared__ __attribute__((aligned(16))) unsigned char q0[TILEB];
@@ -423,11 +433,15 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dkv(BackwardArgs a) {
           if (r >= over || (CAUSAL && r < under)) s[v] = g[v] = 0.f;
         }
       }
-      bf16x8 pb[2], ds[2];
+      bf16x8 pb[2], ds[2], pb_lo[2], ds_lo[2];
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         pb[v >> 3][v & 7] = (__bf16)s[v];
         ds[v >> 3][v & 7] = (__bf16)g[v];
+        if (TWO) {
+          pb_lo[v >> 3][v & 7] = (__bf16)(s[v] - (float)pb[v >> 3][v & 7]);
+          ds_lo[v >> 3][v & 7] = (__bf16)(g[v] - (float)ds[v >> 3][v & 7]);
+        }
       }
       bf16x8 x[AHEAD_T + 1];
       auto xp = [&](int i) TOPK_INLINE { return Tile::across(i & 1 ? qb : gb, col0, i / 2 % FB, rb * 2 + i / 2 / FB); };
@@ -438,6 +452,7 @@ __global__ __launch_bounds__(NT, 2) void k_packed_dkv(BackwardArgs a) {
         if (i + AHEAD_T < 4 * FB) x[(i + AHEAD_T) % (AHEAD_T + 1)] = xp(i + AHEAD_T);
         f32x16& to = (i & 1 ? dk : dv)[i / 2 % FB];
         to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i % (AHEAD_T + 1)], (i & 1 ? ds : pb)[i / 2 / FB], to, 0, 0, 0);
+        if (TWO) to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i % (AHEAD_T + 1)], (i & 1 ? ds_lo : pb_lo)[i / 2 / FB], to, 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -519,9 +534,16 @@ template <int D, bool CAUSAL>
 void launch_d(const BackwardArgs& a, hipStream_t st) {
   const int64_t rows = a.p.H * a.p.N, per = NT / (D / 8);
   k_packed_stat<D><<<(unsigned)((rows + per - 1) / per), NT, 0, st>>>(a);
-  if (packed_few(a.p, a.p.H)) k_packed_dq<D, CAUSAL, 2><<<(unsigned)(packed_tiles(a.p, PACKED_TILE / 2) * a.p.H), NT, 0, st>>>(a);
-  else k_packed_dq<D, CAUSAL, 1><<<(unsigned)(packed_tiles(a.p) * a.p.H), NT, 0, st>>>(a);
-  k_packed_dkv<D, CAUSAL><<<(unsigned)(packed_tiles(a.p) * a.p.Hkv * a.p.splits), NT, 0, st>>>(a);
+  const unsigned q_wgs = (unsigned)(packed_tiles(a.p) * a.p.H), half_q_wgs = (unsigned)(packed_tiles(a.p, PACKED_TILE / 2) * a.p.H),
+                 kv_wgs = (unsigned)(packed_tiles(a.p) * a.p.Hkv * a.p.splits);
+  if (packed_short(a.p)) {
+    k_packed_dq<D, CAUSAL, 2, true><<<half_q_wgs, NT, 0, st>>>(a);
+    k_packed_dkv<D, CAUSAL, true><<<kv_wgs, NT, 0, st>>>(a);
+  } else {
+    if (packed_few(a.p, a.p.H)) k_packed_dq<D, CAUSAL, 2, false><<<half_q_wgs, NT, 0, st>>>(a);
+    else k_packed_dq<D, CAUSAL, 1, false><<<q_wgs, NT, 0, st>>>(a);
+    k_packed_dkv<D, CAUSAL, false><<<kv_wgs, NT, 0, st>>>(a);
+  }
   if (a.p.splits > 1) k_packed_sum<D><<<(unsigned)((2 * a.p.Hkv * a.p.N * (D / 8) + NT - 1) / NT), NT, 0, st>>>(a);
 }
 
