@@ -17,7 +17,10 @@
  * calls (topk_attn_backward, topk_ffn_backward), which recompute from that cache
  * and the inputs only (Section 2.2, "Input checkpointing"); workspace queries and
  * registration; two process-wide settings (topk_set_memory_budget,
- * topk_set_backward_lists); and debug and test hooks.
+ * topk_set_backward_lists); debug and test hooks; and around the attention calls: heads of a
+ * projection (topk_rope, topk_qk_norm_rope*), attention behind a shared prefix (topk_attn_prefix), over
+ * packed sequences (topk_attn_packed*), over a cache in pages (topk_attn_tree), and the calls that
+ * keep such a cache (topk_pages_*).
  *
  * Conventions shared by every call:
  *  - Every tensor pointer is a caller-owned DEVICE pointer to contiguous row-major

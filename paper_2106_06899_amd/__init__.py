@@ -9,6 +9,11 @@ is no CPU or PyTorch fallback; if the library is missing the calls raise.
 * ``qk_norm_rope(qkv, ...)``, ``rope(x, ...)``    -> heads for the attention calls: head norms and
   rotary positions; ``qk_norm_rope_append`` writes keys and values to a cache
 * ``attn_prefix(q, prefix_k, prefix_v, k, v, lengths)`` -> attention of requests that share a prefix
+* ``attn_packed(q, k, v, offsets)`` -> attention over sequences that lie one behind the other (with a
+  backward pass)
+* ``attn_tree(q, k_pages, v_pages, lengths, table, parents)`` -> attention of the next tokens, or of trees of
+  drafted ones, over a cache in pages; ``pages_reserve``, ``pages_append``, ``pages_keep``,
+  ``pages_fork``, ``pages_release``, ``pages_compact`` keep such a cache
 
 Tensors live on the GPU (PyTorch provides device memory and the stream); the
 work is enqueued on ``torch.cuda.current_stream()``. The workspace is a PyTorch
@@ -25,7 +30,8 @@ __all__ = ["attn", "attn_dense", "scan_ablation", "probe_mfma", "ffn", "attn_wor
            "mfma_layout", "lib", "TopkError", "LIB_PATH", "profile_begin", "profile_end", "STAGES",
            "attn_backward", "ffn_backward", "rope", "rope_frequencies", "rope_axes", "qk_norm_rope", "qk_norm_rope_append",
            "qk_norm_rope_backward", "attn_prefix", "attn_prefix_workspace_bytes",
-           "attn_packed", "attn_packed_backward", "attn_tree", "pages_reserve", "pages_append", "pages_keep", "pages_fork", "pages_release", "pages_compact", "set_backward_lists", "set_memory_budget", "last_fallback_rows"]
+           "attn_packed", "attn_packed_backward", "attn_tree", "pages_reserve", "pages_append", "pages_keep", "pages_fork",
+           "pages_release", "pages_compact", "set_backward_lists", "set_memory_budget", "last_fallback_rows"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtopk.so")
 
@@ -721,7 +727,8 @@ def attn_packed_backward(q, k, v, offsets, out, lse, d_out, causal: bool = True,
         scale = 1.0 / math.sqrt(d)
     dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     if N:
-        st = _PackedStrides(*(s for t in (q, k, v, out, d_out, dq, dk, dv) for s in t.stride()[:2]))
+        st = _PackedStrides(*q.stride()[:2], *k.stride()[:2], *v.stride()[:2], *out.stride()[:2], *d_out.stride()[:2],
+                            *dq.stride()[:2], *dk.stride()[:2], *dv.stride()[:2])
         L = lib()
         _launch(device, L.topk_attn_packed_backward,
                 (q.data_ptr(), k.data_ptr(), v.data_ptr(), off, out.data_ptr(), lse.data_ptr(), _ptr(rest), d_out.data_ptr(),

@@ -6,7 +6,8 @@ only its inputs and the selected keys with their raw scores, the backward calls
 
 The projections around the attention are plain GEMMs left to PyTorch (rocBLAS);
 every top-k step runs in libtopk's kernels, and so do head norms and rotary positions
-(``rotary``, ``norm_rotary_heads``), which the attention layer takes as options.
+(``rotary``, ``norm_rotary_heads``), which the attention layer takes as options, and attention over packed
+sequences (``packed_attention``) and over caches in pages, which it offers beside the padded form.
 """
 from __future__ import annotations
 
@@ -114,13 +115,16 @@ class PackedAttentionFunction(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, d_out):
         q, k, v, offsets, out, lse, rest = ctx.saved_tensors
-        if d_out.stride(-1) != 1 or any(s % 8 for s in d_out.stride()[:-1]) or d_out.data_ptr() % 16:
+        head, token, one = d_out.stride()
+        if one != 1 or head % 8 or token % 8 or d_out.data_ptr() % 16:
             d_out = d_out.contiguous()
         return (*attn_packed_backward(q, k, v, offsets, out, lse, d_out, *ctx.how, rest), None, None, None)
 
 
 def packed_attention(q, k, v, offsets, causal: bool = True, scale: float | None = None):
-    """Differentiable attention over packed sequences; arguments as ``attn_packed``."""
+    """Differentiable attention over packed sequences; arguments as ``attn_packed``. (As with any function of PyTorch's:
+    a backward pass that is captured into a graph must not find an earlier eager graph of the same leaves alive, whose
+    stream the captured work would wait for.)"""
     if scale is None:
         scale = 1.0 / math.sqrt(q.shape[-1])
     return PackedAttentionFunction.apply(q, k, v, offsets, bool(causal), float(scale))
