@@ -16,11 +16,13 @@
 //
 // Few rows (up to 32): four waves take key tiles of 32 in turn, K and V in registers, each with a running softmax
 // of its own, joined through LDS; v_mfma_f32_16x16x32_bf16, S^T = K Q^T and O^T = V^T P^T, so that a lane
-// holds one row's numbers. Bound by reading the cache. Weights enter the second product as the sum of two
-// bf16 numbers (16 significant bits).
+// holds one row's numbers. Weights enter the second product as the sum of two bf16 numbers (16 significant bits).
+// Bound by reading the cache: the next token of 32 requests of 100 to 4096 keys, 32 heads of 128 on 8, 58 us (4.7 TB/s)
+// and the join's 4.8.
 // Many rows: 128, 32 a wave, every wave takes every key tile of 64 through LDS; v_mfma_f32_32x32x16_bf16, V^T by
 // transposing LDS reads. With 64 rows a request and key head and more, weights are rounded to bf16
-// (relative 2^-9 at most).
+// (relative 2^-9 at most). Bound by reading too, beside the products: 24 drafts of 48 requests of 500 to 8192 keys
+// 204 us (4.3 TB/s), 64 drafts of 2 requests of up to 100000 keys 190 (5.6), the joins 15 and 12.
 #include "topk_packed_device.h"
 #include "topk_tree.h"
 
