@@ -145,6 +145,50 @@ def test_what_rounding_took():
     assert bool(((both.contiguous().view(torch.int32) & 0xFFFF)[other] == 0x8000).all())
 
 
+@pytest.mark.parametrize("name", [n for n, (off, N, _, _, d, _) in sorted(CASES.items()) if d == 64 or N <= 1024 or N <= 64 * (len(off) - 1)])
+def test_weights_of_two_numbers(name):
+    """In a training pass over heads of 64, or a short one, out and rest together have the weights to 16 bits: off by at
+    most 2^-16 from the weights' second rounding, as much from rest's, and from sums of n terms in 32 bits."""
+    offsets, N, H, Hkv, d, causal = CASES[name]
+    q, k, v, off = _inputs(offsets, N, H, Hkv, d)
+    out, lse, rest = tk.attn_packed(q, k, v, off, causal, lse=True, rest=True)
+    _check(q, k, v, off, causal, d ** -0.5, out, lse)
+    both = out.double() + rest.double()
+    for a, z in zip(offsets, offsets[1:]):
+        for h in range(H if z > a else 0):
+            vv = v[h // (H // Hkv), a:z].double()
+            s, _, size = _sequence(q[h, a:z], k[h // (H // Hkv), a:z], causal, d ** -0.5)
+            w = torch.softmax(s, -1)
+            ref = w @ vv
+            delta = ((d + 8) * 2.0 ** -24 + 2.0 ** -22) * size
+            tol = 2.0 ** -16 * ref.abs() + 2 * (delta + 2.0 ** -17 + (z - a + 8) * 2.0 ** -24) * (w @ vv.abs()) + 1e-37
+            assert bool(((both[h, a:z] - ref).abs() <= tol).all()), (a, z, h)
+
+
+@pytest.mark.parametrize("far", ["tokens", "heads"])
+def test_tokens_and_heads_far_apart(far):
+    """Offsets past 32 bits: the same numbers as of tensors that lie in one piece."""
+    N, d = 290, 128
+    H, Hkv = (4, 2) if far == "tokens" else (2, 2)
+    q, k, v, off = _inputs([0, 130, 290], N, H, Hkv, d)
+    g, want = _gradient(q, k, v, off)
+    ref, lse = tk.attn_packed(q, k, v, off, lse=True)
+    head, token = (d, (1 << 24) - 8) if far == "tokens" else ((1 << 31) + 8, 2 * d)
+    buf = torch.zeros((N - 1) * token + (H - 1) * head + 8 * d, dtype=BF16, device="cuda")  # 5 to 10 GB
+
+    def there(x, at):
+        return buf[at:].as_strided(x.shape, (head, token, 1)).copy_(x)
+
+    second = 4 * d if far == "tokens" else d  # beside the first
+    for first, other in ((0, 1), (3, 2)):  # queries and keys; gradients and values
+        x = [q, k, v, g]
+        x[first], x[other] = there(x[first], 0), there(x[other], second)
+        out, sums = tk.attn_packed(*x[:3], off, lse=True)
+        got = tk.attn_packed_backward(*x[:3], off, out.contiguous(), sums, x[3])
+        same = torch.equal(out, ref) and torch.equal(sums, lse) and all(torch.equal(a, b) for a, b in zip(got, want))
+        assert same, first
+
+
 def test_scale_and_large_scores():
     q, k, v, off = _inputs([0, 200, 333], 333, 2, 1, 64, std=8.0)
     for scale in (1e-3, 0.7):
@@ -165,17 +209,18 @@ def test_cut_from_a_projection():
 # (few heads: two waves share rows; a hundred: rows of their own)
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
 @pytest.mark.parametrize("d,H", [(64, 2), (128, 2), (64, 100), (128, 100)])
-def test_hidden_rows_may_hold_anything(bad, d, H):
+@pytest.mark.parametrize("rest", [False, True])
+def test_hidden_rows_may_hold_anything(bad, d, H, rest):
     """Later tokens, other sequences and tokens of none hold numbers that are not finite: rows that
     do not see them are as if they were not there."""
     off, N = [0, 150, 200, 420], 430
     q, k, v, o = _inputs(off, N, H, H // 2, d, seed=3)
-    want, wl = tk.attn_packed(q, k, v, o, lse=True)
+    want, wl = tk.attn_packed(q, k, v, o, lse=True, rest=rest)[:2]
     k2, v2 = k.clone(), v.clone()
     for t in (149, 100, 330, 425):
         v2[:, t, t % d] = bad
     k2[:, 427] = v2[:, 428] = bad
-    got, gl = tk.attn_packed(q, k2, v2, o, lse=True)
+    got, gl = tk.attn_packed(q, k2, v2, o, lse=True, rest=rest)[:2]
     same = torch.equal(gl, wl)
     assert same
     for a, z, ts in ((0, 150, (100, 149)), (150, 200, ()), (200, 420, (330,))):
@@ -187,7 +232,7 @@ def test_hidden_rows_may_hold_anything(bad, d, H):
     assert not got[:, 420:].any()
     k3 = k.clone()
     k3[:, 300] = bad  # a key: rows before it are untouched
-    same = torch.equal(tk.attn_packed(q, k3, v, o)[:, :300], want[:, :300])
+    same = torch.equal(tk.attn_packed(q, k3, v, o, lse=True, rest=rest)[0][:, :300], want[:, :300])
     assert same
 
 
@@ -211,6 +256,8 @@ def _tiny(d, n, H):
         out = tk.attn_packed(q, k, v, off, causal=False, scale=1.0)
         s = q[0].double() @ k[0].double().t()
         ref = torch.softmax(s, -1) @ v[0].double()
+        assert bool(((out.double() - ref).abs() <= 2.0 ** -7 * ref.abs()).all()), at
+        out = tk.attn_packed(q, k, v, off, causal=False, scale=1.0, lse=True, rest=True)[0]
         assert bool(((out.double() - ref).abs() <= 2.0 ** -7 * ref.abs()).all()), at
 
 
@@ -402,9 +449,10 @@ def test_autograd_on_layouts_and_broadcast_gradients():
 
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
 @pytest.mark.parametrize("d,H", [(64, 2), (128, 2), (64, 100), (128, 100)])
-def test_gradients_of_hidden_rows(bad, d, H):
+@pytest.mark.parametrize("N", [300, 1300])  # (a short pass, and not)
+def test_gradients_of_hidden_rows(bad, d, H, N):
     """Numbers that are not finite reach the gradients of what meets them, no other."""
-    off, N = [0, 150, 290], 300
+    off = [0, 150, 290]
     q, k, v, o = _inputs(off, N, H, H // 2, d, seed=3)
     g, want = _gradient(q, k, v, o)
     out, lse = tk.attn_packed(q, k, v, o, lse=True)
@@ -439,8 +487,9 @@ def test_gradients_of_hidden_rows(bad, d, H):
         assert torch.equal(got[1][:, 150:], want[1][:, 150:]) and torch.equal(got[2][:, 150:], want[2][:, 150:])
 
 
-def test_backward_in_graphs_and_streams():
-    q, k, v, off = _inputs([0, 90, 400], 400, 4, 2, 128, seed=5)
+@pytest.mark.parametrize("N", [400, 1500])
+def test_backward_in_graphs_and_streams(N):
+    q, k, v, off = _inputs([0, 90, 400], N, 4, 2, 128, seed=5)
     g = _gradient(q, k, v, off)[0]
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())

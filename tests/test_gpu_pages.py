@@ -399,6 +399,33 @@ def test_strided_pools_tables_and_rows():
     assert bool((wide[:, :2] == -5).all()) and bool((wide[:, 7:] == -5).all())
 
 
+@pytest.mark.parametrize("far", ["pages", "layers", "heads"])
+def test_pools_larger_than_32_bits_reach(far):
+    """Layers, pages or heads of a pool that lie far apart."""
+    c = Cache(3, 6, 4, 20, 2, 2, 64, seed=15, longest=12)
+    st = {"pages": (512, 1 << 27, 256, 64), "layers": ((1 << 31) + 512, 512, 256, 64), "heads": (20 * 512, 256, (1 << 31) + 8, 64)}[far]
+    for name in ("k", "v"):
+        t = getattr(c, name)
+        size = sum((n - 1) * s for n, s in zip(t.shape, (*st, 1))) + 1
+        setattr(c, name, torch.zeros(size, dtype=t.dtype, device="cuda").as_strided(t.shape, (*st, 1)).copy_(t))
+    c.fork([1, 1, 2])
+    assert c.reserve(3) == 0
+    c.append(3)
+    c.keep([[2], [0], [1]])
+    c.release()
+    live = c.refs > 0
+    to = [torch.zeros(2, int(live.sum()), 2, 4, 64, dtype=c.k.dtype, device="cuda") for _ in range(2)]
+    assert int(tk.pages_compact(c.k, c.v, c.table, c.refs, *to)[2]) == 0
+    same = torch.equal(to[0], c.k[:, live]) and torch.equal(to[1], c.v[:, live])
+    assert same
+    # and back, to the first pages
+    used = to[0].shape[1]
+    pages = torch.arange(used, dtype=torch.int32, device="cuda")[None]
+    table, _, missing = tk.pages_compact(*to, pages, c.refs[live], c.k, c.v)
+    same = torch.equal(table, pages) and torch.equal(c.k[:, :used], to[0]) and torch.equal(c.v[:, :used], to[1])
+    assert same and int(missing) == 0
+
+
 def test_streams_and_graphs():
     """A decoding step's calls, captured: the books change on every replay, on the GPU alone."""
     a, b = Cache(6, 8, 4, 60, 2, 2, 64, seed=13, longest=8), Cache(6, 8, 4, 60, 2, 2, 64, seed=13, longest=8)

@@ -185,6 +185,25 @@ def test_without_a_table():
     assert bool(((out.float() - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + 2.0 ** -12).all())
 
 
+@pytest.mark.parametrize("T,H,d,page", [(1, 4, 128, 16), (5, 2, 64, 7), (20, 8, 128, 64), (64, 2, 64, 16)])
+def test_pages_far_apart(T, H, d, page):
+    """A pool whose pages, heads or rows lie further apart than 32 bits reach."""
+    q, k, v, lengths, table, parents = _inputs(H, 2, T, d, page, [3 * page, 77], spare=0)
+    want = tk.attn_tree(q, k, v, lengths, table, _int(parents))
+    P = len(k)
+    buf = torch.zeros(5 << 30, dtype=BF16, device="cuda")  # 10 GB
+    small = 2 * page * d
+    for st in (((5 << 30) // P // 8 * 8, page * d, d), (small, (1 << 32) + 8, d), (small, page * d, d)):
+        if st[0] * (P - 1) + st[1] + page * d > len(buf):
+            continue
+        far = buf.as_strided((P, 2, page, d), (*st, 1))
+        far.copy_(k)
+        same = torch.equal(tk.attn_tree(q, far, v, lengths, table, _int(parents)), want)
+        far.copy_(v)
+        same = same and torch.equal(tk.attn_tree(q, k, far, lengths, table, _int(parents)), want)
+        assert same, st
+
+
 def test_strided_pools():
     """The rows of all heads together, keys and values of a page side by side."""
     q, k, v, lengths, table, parents = _inputs(4, 2, 5, 128, 16, [200, 77])
