@@ -866,8 +866,11 @@ TreePlan tree_plan(const TreeProblem& p) {
   pl.form = R <= 16 ? (four ? 3 : 1) : R <= 32 && p.d == 64 ? (four ? 4 : 2) : R < 64 ? 8 : 9;
   pl.tiles = (int)cdiv(R, tile_rows(pl.form));
   const int64_t S = std::min(p.M * p.page_rows, KEYS_MAX), units = p.Hkv * pl.tiles;
-  // Few keys: one workgroup a request, key head and row tile takes all its keys, and nothing is left to join.
-  if (S <= 2 * UNIT || (pl.form < 8 && p.B * units <= 512 && S * p.d <= 1024 * 64)) return pl;
+  // Few keys: one workgroup a request, key head and row tile takes all its keys, and nothing is left to join. (Of many
+  // rows up to 512 keys, where that is more than a workgroup on every other CU: 188 of up to 388 keys 26 us -> 23, 480 of up to
+  // 500 38 -> 33; 128 of up to 510 22 -> 23, 40 of them 19 -> 23.)
+  const int64_t wgs = p.B * units;
+  if (S <= 2 * UNIT || (wgs <= 512 && (pl.form < 8 ? S * p.d <= 1024 * 64 : wgs > 128 && S <= 512))) return pl;
   pl.ranges = std::max(cdiv(1024, units), p.B);
   pl.round = (int)(512 / units);
   return pl;

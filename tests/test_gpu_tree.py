@@ -117,6 +117,8 @@ CASES = {
     "long_trees": (4, 2, 50, 128, 32, [5000, 60, 3333]),
     "uneven": (4, 1, 1, 128, 16, [6000] + [5] * 40),
     "more_than_a_wave": (2, 1, 2, 64, 8, [(37 * i) % 700 for i in range(150)]),
+    "many_rows_in_one_range": (8, 4, 40, 64, 16, [(97 * i) % 400 + 40 for i in range(40)]),
+    "many_rows_in_one_range_d128": (10, 5, 20, 128, 32, [(61 * i) % 450 for i in range(30)] + [0, 512]),
     "hundreds": (1, 1, 1, 64, 16, [(53 * i) % 301 for i in range(700)]),
     "hundreds_uneven": (2, 1, 3, 128, 16, [5000] + [(29 * i) % 97 + 3 for i in range(300)]),
     "out_of_range": (2, 1, 2, 64, 16, [-5, 40, 10]),
