@@ -306,7 +306,7 @@ class TopkMultiheadAttention(torch.nn.Module):
         has (``pages_reserve`` makes room for them; the caller advances lengths, with
         ``pages_keep`` by those that are accepted), and each attends to its request's rows, itself
         and the guesses that it follows. positions default to lengths[b] and how many guesses each
-        follows, on every axis."""
+        follows, on every axis. (A request of negative length writes nothing, and its output means nothing.)"""
         if self.topk is not None or not self.causal:
             raise ValueError("draft attends to every earlier key: it needs topk=None and causal=True")
         B, T, D = x.shape
