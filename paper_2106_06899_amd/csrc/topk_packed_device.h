@@ -128,7 +128,7 @@ __device__ __forceinline__ PackedPlace packed_place(const PackedProblem& p, int 
     }
     __syncthreads();
     s = found[0];
-    if (tiles) *tiles = (int)before;
+    if (tiles) *tiles = (int)min(before, (uint32_t)t);  // (t at most, whatever the offsets)
     if (s < 0) return at;
     at.tile = found[1];
   }

@@ -282,14 +282,16 @@ def test_streams_and_graphs():
         assert same
 
 
-def test_offsets_that_decrease_stay_inside():
+@pytest.mark.parametrize("more", [0, 100])  # (so many sequences more)
+def test_offsets_that_decrease_stay_inside(more):
     """No meaningful result, but nothing outside the tensors is read or written."""
-    q, k, v, off = _inputs([0, 200, 100, 300], 300, 2, 1, 64)
+    q, k, v, off = _inputs([0, 200, 100, 300] + more * [300], 300, 2, 1, 64)
     for o in ([0, 200, 100, 300], [-50, 100, 1000, 3], [2 ** 31 - 1, -2 ** 31, 300, 300]):
-        off.copy_(_int(o))
-        out = tk.attn_packed(q, k, v, off, lse=True)
+        off.copy_(_int((o * (1 + more // 4))[:4 + more]))
+        out, lse = tk.attn_packed(q, k, v, off, lse=True)
+        grads = tk.attn_packed_backward(q, k, v, off, out, lse, q)
         torch.cuda.synchronize()
-        assert out[0].shape == q.shape
+        assert [t.shape for t in (out, *grads)] == [q.shape, q.shape, k.shape, v.shape]
 
 
 def test_refused_on_the_gpu():
