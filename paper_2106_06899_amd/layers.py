@@ -20,6 +20,13 @@ from . import (attn, attn_backward, attn_dense, attn_packed, attn_packed_backwar
                pages_append, qk_norm_rope, qk_norm_rope_append, qk_norm_rope_backward, rope, rope_axes, rope_frequencies)
 
 
+def _whole(t):
+    """A gradient in one piece at an address that the kernels take. (Autograd may hand over a part of another
+    gradient, in one piece but at any address: that of ``cat``, of a view of one flat tensor.)"""
+    t = t.contiguous()
+    return t.clone() if t.data_ptr() % 16 else t
+
+
 class TopkAttentionFunction(torch.autograd.Function):
     """out = top-k attention(q, k, v) over [B, H, L, d] tensors, differentiable in
     q, k and v. The selection itself carries no gradient (the index set is piecewise
@@ -35,7 +42,7 @@ class TopkAttentionFunction(torch.autograd.Function):
     @staticmethod
     def backward(ctx, d_out):
         q, k, v, idx, dots = ctx.saved_tensors
-        dq, dk, dv = attn_backward(q, k, v, idx, dots, d_out.contiguous(), ctx.scale)
+        dq, dk, dv = attn_backward(q, k, v, idx, dots, _whole(d_out), ctx.scale)
         return dq, dk, dv, None, None, None, None
 
 
@@ -52,7 +59,7 @@ class TopkFFNFunction(torch.autograd.Function):
     @staticmethod
     def backward(ctx, d_out):
         x, w1, w2, idx, dots = ctx.saved_tensors
-        dx, dw1, dw2 = ffn_backward(x, w1, w2, idx, dots, d_out.contiguous())
+        dx, dw1, dw2 = ffn_backward(x, w1, w2, idx, dots, _whole(d_out))
         return dx, dw1, dw2, None, None
 
 
@@ -117,7 +124,7 @@ class PackedAttentionFunction(torch.autograd.Function):
         q, k, v, offsets, out, lse, rest = ctx.saved_tensors
         head, token, one = d_out.stride()
         if one != 1 or head % 8 or token % 8 or d_out.data_ptr() % 16:
-            d_out = d_out.contiguous()
+            d_out = _whole(d_out)
         return (*attn_packed_backward(q, k, v, offsets, out, lse, d_out, *ctx.how, rest), None, None, None)
 
 

@@ -170,3 +170,20 @@ def test_feed_forward_layer_parity():
     got = (X.grad.reshape(-1, dm), layer.w1.grad, layer.w2.grad)
     errs = {n: parity.check_grad_rows(n, a, b, m, wl.BF16) for n, a, b, m in zip(("dX", "dW1", "dW2"), got, ref, mag)}
     _say("ffn layer ok", errs)
+
+
+@pytest.mark.parametrize("behind", [1, 3])
+def test_gradients_at_any_address(behind):
+    """A gradient in one piece at an address that the kernels do not take, as a part of a flat one is."""
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(torch.bfloat16)  # noqa: E731
+    attention = [rand(1, 2, 200, 64).requires_grad_() for _ in range(3)], lambda x: layers.TopkAttentionFunction.apply(*x, 16, 1024, False, 0.125)
+    ffn = [rand(50, 64).requires_grad_(), rand(256, 64).requires_grad_(), rand(256, 64).requires_grad_()], lambda x: layers.TopkFFNFunction.apply(*x, 16, 1024)
+    for x, f in (attention, ffn):
+        out = f(x)
+        g = rand(*out.shape)
+        want = torch.autograd.grad(out, x, g)
+        odd = torch.cat((g.new_zeros(behind), g.flatten()))[behind:].view(g.shape)
+        assert odd.is_contiguous() and odd.data_ptr() % 16
+        got = torch.autograd.grad(f(x), x, odd)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

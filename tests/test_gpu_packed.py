@@ -508,3 +508,22 @@ def test_backward_in_graphs_and_streams(N):
         torch.cuda.synchronize()
         same = all(torch.equal(a, b) for a, b in zip(grads, _gradient(q, k, v, off)[1]))
         assert same
+
+
+@pytest.mark.parametrize("behind", [1, 3, 8])  # (8 numbers are 16 bytes: an address that is taken as it is)
+def test_gradients_at_any_address(behind):
+    """A gradient that is in one piece, but at an address that the kernels do not take: the same numbers as at one that
+    they do. Handed over, and as the backward of a flat vector of several results makes it."""
+    off = _int([0, 60, 200])
+    q, k, v, _ = _inputs([0, 200], 200, 4, 2, 64)
+    x = [t.clone().requires_grad_() for t in (q, k, v)]
+    g = _gradient(q, k, v, off)[0]
+    want = torch.autograd.grad(layers.packed_attention(*x, off), x, g)
+    odd = torch.cat((g.new_zeros(behind), g.flatten()))[behind:].view(g.shape)
+    assert odd.is_contiguous() and bool(odd.data_ptr() % 16) == (behind < 8)
+    got = torch.autograd.grad(layers.packed_attention(*x, off), x, odd)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    first = torch.ones(behind, device="cuda", dtype=BF16, requires_grad=True)
+    both = torch.cat((first, layers.packed_attention(*x, off).flatten()))
+    got = torch.autograd.grad(both, x, torch.cat((torch.ones_like(first), g.flatten())))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
