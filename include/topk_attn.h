@@ -458,7 +458,8 @@ size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64
  * bf16 with d = 64 or 128 (else TOPK_E_UNSUPPORTED). Scores, softmax statistics and sums in fp32, in a
  * fixed order; weights enter the product with V rounded to bf16, and are divided by the sum of the
  * rounded ones. A row is computed from its own
- * numbers alone: keys and values it does not see may be infinite or NaN. No workspace. Offsets that
+ * numbers alone: keys and values it does not see may be infinite or NaN. An infinite value makes the rows
+ * that see it infinite, whatever its weight is (values of both signs, or NaN: NaN). No workspace. Offsets that
  * decrease give no meaningful result, but no access outside the tensors.
  *
  * topk_attn_packed_backward -- its gradients, from the inputs, out, lse (required here) and rest (NULL: taken as
@@ -466,7 +467,8 @@ size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64
  * d_Q [H, N, d], d_K, d_V [Hkv, N, d], every element written (tokens of no sequence: 0). The weights are
  * recomputed from lse; those below 2^-126 count as 0. Score gradients and weights enter their products
  * rounded to bf16, or, with N <= 1024 or N <= 64 n, to 16 significant bits; sums in fp32, in a fixed order, over the query
- * heads that share a key head too. d_out may be strided like the others. Workspace:
+ * heads that share a key head too. What is infinite or NaN in a query, in its d_out or in a key and value reaches only
+ * the gradients that it is part of by the formulas, as an infinite number or NaN. d_out may be strided like the others. Workspace:
  * topk_attn_packed_backward_workspace_bytes. Stage 4 of the stage timing (forward: 0).
  */
 typedef struct {
@@ -570,7 +572,8 @@ size_t topk_pages_compact_workspace_bytes(int64_t pages, int64_t n_to);
  *
  * bf16 with d = 64 or 128, T <= 64, fewer than 2^24 workgroups (else TOPK_E_UNSUPPORTED). Softmax
  * statistics and sums in fp32, in a fixed order; a row is computed from its own numbers alone
- * (drafts that it does not see, and rows behind the request's, may be infinite or NaN). Weights enter
+ * (drafts that it does not see, and rows behind the request's, may be infinite or NaN; an infinite value
+ * makes the rows that see it infinite, whatever its weight is, values of both signs, or NaN, make them NaN). Weights enter
  * the product with V to 16 significant bits, or, with 64 rows a request and key head ((H / Hkv) * T)
  * and more, rounded to bf16. The work is laid out on the device by the lengths, so a table may be
  * wider than any request needs. Workspace: topk_attn_tree_workspace_bytes (M = 1 without a table).

@@ -250,8 +250,8 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
     if (work) tile(std::false_type{}, t + 1, k1, v1);
   }
   // Where rows of the workgroup do not see all its keys, values that are not finite go only to the rows that
-  // see theirs, which become NaN there; the others would meet them as 0 times NaN. Each wave looks at its part
-  // of the tile.
+  // see theirs, which become NaN there (and infinite, where they are, at the end); the others would meet them as 0
+  // times NaN. Each wave looks at its part of the tile.
   constexpr bool hides = CAUSAL;
   auto own_part = [&](unsigned char* vb, int j) { return (TOPK_LDS u32x4*)&vb[(wave * LPW + j) * 1024 + lane * 16]; };
   for (; t < tiles; ++t) {
@@ -330,6 +330,11 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
       }
     wave_sync_lds();
   }
+  float most = o[0][0];  // NaN where any of the sums is: rows that are written once more (see Infinities)
+#pragma unroll
+  for (int f = 0; f < FB; ++f)
+#pragma unroll
+    for (int v = 0; v < 16; v += 2) most = larger(larger(most, o[f][v]), o[f][v + 1]);
   // through the wave's own part of LDS, in parts of four features permuted by the row, so that whole rows
   // are written, two (D = 128) or four a store
   TOPK_LDS f32x4* mine = (TOPK_LDS f32x4*)(KS > 1 ? group ? p1 : p0 : wave == 0 ? p0 : wave == 1 ? p1 : wave == 2 ? p2 : p3);
@@ -343,19 +348,39 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int part = lane % PARTS;
   uint16_t* to = (uint16_t*)a.p.out.p + h * a.p.out.head + at.first * a.p.out.token + 4 * part;
-#pragma unroll 4
-  for (int u = 0; u < 32 / RPS; ++u) {
+  auto store = [&](int u, bool again) TOPK_INLINE {
     const int r = u * RPS + lane / PARTS, i = at.tile * ROWS + group * 32 + r;
-    const f32x4 x = mine[r * PARTS + (part ^ (r & 15))];
+    f32x4 x = mine[r * PARTS + (part ^ (r & 15))];
     const float by = __shfl(inv, r, 64);
-    if (i >= at.n) continue;
+    if (again) {
+      const bool unsure = i < at.n && by == by && Infinities::any_nan(x);
+      if (!__builtin_amdgcn_ballot_w64(unsure)) return;
+      const uint16_t* v = (const uint16_t*)a.p.v.p + hk * a.p.v.head + at.first * a.p.v.token + 4 * part;
+      Infinities is;
+      for (int j0 = 0; j0 < keys; j0 += 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int j = min(j0 + e, keys - 1);
+          is.meet(*(const uint2*)(v + j * a.p.v.token), !CAUSAL || j <= i);
+        }
+        if (!__builtin_amdgcn_ballot_w64(unsure && is.open(x))) break;
+      }
+      if (!unsure) return;
+      is.settle(x);
+    }
+    if (i >= at.n) return;
     const uint2 y = make_uint2(pack_bf16(x[0] * by, x[1] * by), pack_bf16(x[2] * by, x[3] * by));
     *(uint2*)(to + i * a.p.out.token) = y;
-    if (a.p.rest)
+    if (a.p.rest)  // (nothing was taken from what is not finite)
       *(uint2*)((uint16_t*)a.p.rest + (to - (uint16_t*)a.p.out.p) + i * a.p.out.token) =
-          make_uint2(pack_bf16(x[0] * by - __uint_as_float(y.x << 16), x[1] * by - __uint_as_float(y.x & 0xFFFF0000u)),
-                     pack_bf16(x[2] * by - __uint_as_float(y.y << 16), x[3] * by - __uint_as_float(y.y & 0xFFFF0000u)));
-  }
+          make_uint2(pack_bf16(x[0] * by - __uint_as_float(y.x << 16), x[1] * by - __uint_as_float(y.x & 0xFFFF0000u)) & ~(not_finite(y.x) * 0xFFFFu),
+                     pack_bf16(x[2] * by - __uint_as_float(y.y << 16), x[3] * by - __uint_as_float(y.y & 0xFFFF0000u)) & ~(not_finite(y.y) * 0xFFFFu));
+  };
+#pragma unroll 4
+  for (int u = 0; u < 32 / RPS; ++u) store(u, false);
+  if (__builtin_amdgcn_ballot_w64(most != most))
+#pragma unroll 1
+    for (int u = 0; u < 32 / RPS; ++u) store(u, true);
   if (LSE && ok && !half) a.p.lse[h * a.p.N + at.first + row] = whole_l == 0.f ? -INFINITY : (m + log2f(whole_l)) * 0.69314718055994531f;
 }
 

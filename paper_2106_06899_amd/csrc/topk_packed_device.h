@@ -5,6 +5,8 @@
 #include "topk_device.h"
 #include "topk_packed.h"
 
+#include <math.h>
+
 namespace topk {
 
 #define TOPK_LDS __attribute__((address_space(3)))
@@ -25,6 +27,39 @@ __device__ __forceinline__ float other_half_max(float x) {
 }
 // Of two bf16 numbers, bit 0 and bit 16: is it infinite or NaN?
 __device__ __forceinline__ uint32_t not_finite(uint32_t x) { return (((x & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u; }
+
+// A row's four sums of which some are NaN though its weights are numbers. By the definition an infinite value whose
+// weight is above 0 makes a sum infinite, values of both signs, or one that is NaN, make it NaN; the products have it as
+// NaN wherever a part of a weight is 0 (0 times infinity), so the row's values are looked at again: here four of them.
+struct Infinities {
+  uint32_t up = 0, down = 0;  // sums (bit w: the w-th) that meet +infinity or NaN; -infinity or NaN
+  static __device__ __forceinline__ bool any_nan(const f32x4& x) { return x[0] != x[0] || x[1] != x[1] || x[2] != x[2] || x[3] != x[3]; }
+  __device__ __forceinline__ void meet(uint2 x, bool sees) {
+    const uint32_t mx = not_finite(x.x), my = not_finite(x.y);
+    if (!sees || !(mx | my)) return;
+    auto nan = [](uint32_t y) { return ((y & 0x007F007Fu) + 0x007F007Fu) >> 7; };  // (bits 0 and 16, of what is not finite)
+    auto four = [](uint32_t y, uint32_t z) { return (y & 1) | y >> 15 | (z & 1) << 2 | z >> 16 << 3; };
+    up |= four(mx & (~(x.x >> 15) | nan(x.x)), my & (~(x.y >> 15) | nan(x.y)));
+    down |= four(mx & (x.x >> 15 | nan(x.x)), my & (x.y >> 15 | nan(x.y)));
+  }
+  __device__ __forceinline__ void meet(const f32x4& x) {  // (four sums of a part of the values)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      up |= (uint32_t)!(x[w] < INFINITY) << w;
+      down |= (uint32_t)!(x[w] > -INFINITY) << w;
+    }
+  }
+  // is there a sum that is NaN and may yet turn out to be infinite?
+  __device__ __forceinline__ bool open(const f32x4& x) const {
+    const uint32_t both = up & down;
+    return (x[0] != x[0] && !(both & 1)) || (x[1] != x[1] && !(both & 2)) || (x[2] != x[2] && !(both & 4)) || (x[3] != x[3] && !(both & 8));
+  }
+  __device__ __forceinline__ void settle(f32x4& x) const {
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      if (x[w] != x[w] && ((up ^ down) >> w & 1)) x[w] = up >> w & 1 ? INFINITY : -INFINITY;
+  }
+};
 
 // A workgroup's tile: tile `tile` of the sequence of n tokens from token `first` on; n = 0: none.
 struct PackedPlace {

@@ -219,6 +219,24 @@ __device__ __forceinline__ const unsigned char* pass_on(const unsigned char* p, 
   return (const unsigned char*)(uintptr_t)((uint64_t)hi << 32 | lo);
 }
 
+// The four sums x of features 4 part .. of a row (unsure: some are NaN, its weights are not) after a look at the values
+// that it sees of n keys from `first` on. By the whole wave.
+__device__ __forceinline__ void settle_row(f32x4& x, bool unsure, const Rows& rows, int first, int n, int text, uint64_t sees, int part) {
+  const int lane = threadIdx.x & 63;
+  Infinities is;
+  for (int k0 = 0; k0 < n; k0 += 64) {
+    const int2 at = rows.place(first + k0, lane, n - k0);
+    const int p = rows.lookup(at.x), d0 = first + k0 - text;  // (the draft that key 0 of these is)
+    const unsigned char* v = rows.at(1, p, at.y);
+    uint64_t seen = __builtin_amdgcn_ballot_w64(rows.valid(p));
+    if (d0 > -64) seen &= d0 >= 0 ? (d0 < 64 ? sees >> d0 : 0) : sees << -d0 | ((1ull << -d0) - 1);
+#pragma unroll 8
+    for (int j = 0; j < 64; ++j) is.meet(*(const uint2*)(pass_on(v, j) + 8 * part), seen >> j & 1);
+    if (!__builtin_amdgcn_ballot_w64(unsure && is.open(x))) break;
+  }
+  if (unsure) is.settle(x);
+}
+
 struct TreeLds {
   unsigned char *b0, *b1, *b2, *b3;
   float2 (*ml)[32], *sum;
@@ -353,8 +371,8 @@ struct TreeFew {
           for (int e = 0; e < 8; ++e)
             if (!(see[r] >> (16 * (e >> 2) + 4 * g + (e & 3)) & 1)) s[r][e >> 2][e & 3] = -INFINITY;
         }
-        // Drafts' values that are not finite go to the rows that see them, which become NaN there (at the end); the
-        // others would meet them as 0 times NaN.
+        // Drafts' values that are not finite go to the rows that see them, which become NaN there (and infinite,
+        // where they are, at the end); the others would meet them as 0 times NaN.
         uint32_t bad = 0;
         if (decltype(some_draft)::value) {
 #pragma unroll
@@ -464,14 +482,20 @@ struct TreeFew {
       if (wave == 0 && g == 0) sh.sum[16 * r + n] = make_float2(top, total);
     }
     __syncthreads();
-#pragma unroll
-    for (int u = 0; u < 16 * NR * D / 4 / NT; ++u) {
+    bool nan = false;
+    auto store = [&](int u, bool again) TOPK_INLINE {
       const int i = u * NT + tid, row = i / (D / 4), part = i % (D / 4);
       f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) sum += ((const TOPK_LDS f32x4*)sh.of(w))[row * (D / 4) + (part ^ (row & 15))];
       const float2 x = sh.sum[row];
-      if (it.r0 + row >= it.R) continue;
+      const bool unsure = it.r0 + row < it.R && x.y == x.y && Infinities::any_nan(sum);
+      if (again) {  // (rows whose sums are NaN are written once more)
+        if (!__builtin_amdgcn_ballot_w64(unsure)) return;
+        settle_row(sum, unsure, rows, it.r.first, it.r.n, text, drafts ? sh.bits[(it.r0 + row) % T] : 0, part);
+      }
+      nan |= unsure;
+      if (it.r0 + row >= it.R) return;
       if (it.r.of == 1) {
         const int64_t at = place(it.r0 + row);
         const float inv = row_factor(x.y);
@@ -482,7 +506,12 @@ struct TreeFew {
         __builtin_nontemporal_store(sum, (f32x4*)(a.po + at * D + 4 * part));
         if (part == 0) a.ml[at] = x;
       }
-    }
+    };
+#pragma unroll
+    for (int u = 0; u < 16 * NR * D / 4 / NT; ++u) store(u, false);
+    if (__builtin_amdgcn_ballot_w64(nan))
+#pragma unroll 1
+      for (int u = 0; u < 16 * NR * D / 4 / NT; ++u) store(u, true);
   }
 };
 
@@ -704,6 +733,11 @@ struct TreeWide {
           if (marks >> (16 * f + v) & 1) o[f][v] = NAN;
     }
     l += __shfl_xor(l, 32, 64);
+    float most = o[0][0];  // NaN where any of the sums is: rows that are written once more (see Infinities)
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) most = larger(larger(most, o[f][v]), o[f][v + 1]);
     // through the wave's own part of LDS, in parts of four features permuted by the row, so that whole rows
     // are written; partial results past the cache
     __syncthreads();
@@ -718,15 +752,24 @@ struct TreeWide {
     const bool last = it.r.of == 1;
     const float inv = row_factor(l);
     const int part = lane % PARTS, row0 = it.r0 + wave * 32;
-#pragma unroll 4
-    for (int u = 0; u < 32 / RPS; ++u) {
+    auto store = [&](int u, bool again) TOPK_INLINE {
       const int row = u * RPS + lane / PARTS;
-      const f32x4 x = mine[row * PARTS + (part ^ (row & 15))];
+      f32x4 x = mine[row * PARTS + (part ^ (row & 15))];
       const float by = __shfl(inv, row, 64);
-      if (row0 + row >= it.R) continue;
+      if (again) {
+        const bool unsure = row0 + row < it.R && by == by && Infinities::any_nan(x);
+        if (!__builtin_amdgcn_ballot_w64(unsure)) return;
+        settle_row(x, unsure, rows, it.r.first, it.r.n, text, drafts ? sh.bits[(row0 + row) % T] : 0, part);
+      }
+      if (row0 + row >= it.R) return;
       if (last) *(uint2*)((uint16_t*)a.p.out + (list + row0 + row) * D + 4 * part) = make_uint2(pack_bf16(x[0] * by, x[1] * by), pack_bf16(x[2] * by, x[3] * by));
       else __builtin_nontemporal_store(x, (f32x4*)(a.po + (it.slot + row0 + row) * D + 4 * part));
-    }
+    };
+#pragma unroll 4
+    for (int u = 0; u < 32 / RPS; ++u) store(u, false);
+    if (__builtin_amdgcn_ballot_w64(most != most))
+#pragma unroll 1
+      for (int u = 0; u < 32 / RPS; ++u) store(u, true);
     if (!ok || half) return;
     if (!last) a.ml[it.slot + i] = make_float2(m, l);
     else if (a.p.lse) a.p.lse[list + i] = row_log(m, l);
@@ -835,6 +878,11 @@ __global__ __launch_bounds__(NT) void k_tree_join(TreeArgs a) {
     }
   }
   if (!ok) return;
+  if (total == total && Infinities::any_nan(sum)) {  // (a range's infinity times a factor that 32 bits hold as 0)
+    Infinities is;
+    for (int s = 0; s < of; ++s) is.meet(*(const f32x4*)(a.po + (at + s * step) * D + 4 * c));
+    is.settle(sum);
+  }
   const int64_t to = ((int64_t)b * a.p.H + h * (a.p.H / a.p.Hkv)) * a.p.T + r;
   const float inv = row_factor(total);
   *(uint2*)((uint16_t*)a.p.out + to * D + 4 * c) = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));

@@ -527,3 +527,52 @@ def test_gradients_at_any_address(behind):
     both = torch.cat((first, layers.packed_attention(*x, off).flatten()))
     got = torch.autograd.grad(both, x, torch.cat((torch.ones_like(first), g.flatten())))
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,H", [(64, 2), (128, 2), (64, 100), (128, 100)])
+@pytest.mark.parametrize("rest", [False, True])
+def test_infinite_values_that_are_seen(d, H, rest, causal):
+    """By the definition a weight above 0 makes an infinite value an infinite output, of the same sign, two of different
+    signs NaN, wherever the key lies: in a tile that all rows see, on the diagonal, last of its sequence."""
+    off, N = [0, 150, 200, 420], 430
+    q, k, v, o = _inputs(off, N, H, H // 2, d, seed=3)
+    want, wl = tk.attn_packed(q, k, v, o, causal, lse=True, rest=rest)[:2]
+    inf, nan = math.inf, math.nan
+    v2 = v.clone()
+    at = [(149, 0, inf), (100, 1, -inf), (20, 2, inf), (101, 2, -inf), (199, 3, -inf), (200, 4, inf), (330, 5, nan), (300, 6, -inf), (419, 7, inf), (419, d - 1, -inf),
+          (400, d - 1, -inf), (201, 8, inf), (390, 8, -inf), (3, d - 2, nan)]
+    for t, f, x in at:
+        v2[:, t, f] = x
+    for a, z in zip(off, off[1:]):
+        here = torch.zeros(z - a, d, dtype=torch.float64)
+        for t, f, x in at:
+            if a <= t < z:
+                here[t - a if causal else 0:, f] += x
+        here = here.to(BF16).cuda()[None]
+        want[:, a:z] = torch.where(here == 0, want[:, a:z], here)
+    got = tk.attn_packed(q, k, v2, o, causal, lse=True, rest=rest)
+    assert torch.equal(got[1], wl)
+    assert bool(((got[0] == want) | (got[0].isnan() & want.isnan())).all())
+    if rest:  # nothing was taken from what is not finite
+        assert not got[2][~want.isfinite()].any()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,H", [(64, 2), (128, 2), (64, 100), (128, 100)])
+@pytest.mark.parametrize("rest", [False, True])
+def test_infinite_values_of_weights_that_32_bits_hold_as_0(d, H, rest, causal):
+    """e^-200 is above 0 all the same."""
+    n = 500
+    q, k, v = (torch.zeros(H, n, d, device="cuda", dtype=BF16) for _ in range(3))
+    q[..., 0] = 1
+    for top in (3, 250, 499):
+        k[:] = 0
+        k[:, top, 0] = 200
+        v[:] = 1
+        for t, f, x in ((0, 1, math.inf), (100, 2, -math.inf), (300, 3, math.inf), (480, 4, -math.inf), (10, 5, math.inf), (470, 5, -math.inf)):
+            v[:, t, f] = x
+        want = v.float().cumsum(1) if causal else v.float().sum(1, keepdim=True).expand(-1, n, -1)
+        want = torch.where(want.isfinite(), 1.0, want)
+        out = tk.attn_packed(q, k, v, _int([0, n]), causal, 1.0, lse=True, rest=rest)[0].float()
+        assert bool(((out == want) | (out.isnan() & want.isnan())).all()), top

@@ -305,3 +305,56 @@ def test_refused_on_the_gpu():
                  (q.repeat(1, 1, 22, 1), k, v, lengths, table)):
         with pytest.raises(tk.TopkError):
             tk.attn_tree(*args)
+
+
+@pytest.mark.parametrize("T,H,d,page", [(1, 2, 64, 8), (12, 2, 64, 8), (12, 2, 64, 7), (9, 4, 64, 16), (9, 4, 64, 5), (9, 2, 128, 16), (9, 2, 128, 7), (20, 8, 128, 16), (40, 4, 64, 64),
+                                        (5, 8, 128, 16)])
+def test_infinite_values_that_are_seen(T, H, d, page):
+    """By the definition a weight above 0 makes an infinite value an infinite output, of the same sign, two of different
+    signs NaN, whether the key is text, in a tile with drafts or not, or a draft."""
+    lens = [300, 77, 2500, T]
+    q, k, v, lengths, table, parents = _inputs(H, 1, T, d, page, lens, seed=2)
+    par = _int(parents)
+    want, wl = tk.attn_tree(q, k, v, lengths, table, par, lse=True)
+    inf, nan = math.inf, math.nan
+    v2 = v.clone()
+    for b, n in enumerate(lens):
+        text = n - T
+        at = [(n - 1, 3, inf), (text + T // 2, 4, -inf), (n - 1, 5, inf), (text, 5, -inf), (text + T // 3, 6, nan), (text, d - 1, inf), (n - 1, d - 2, -inf)]
+        if text:
+            at += [(text - 1, 7, inf), (0, 8, -inf), (0, 9, inf), (n - 1, 9, -inf), (text - 1, 10, nan)]
+        sees = _sees(parents[b])
+        here = torch.zeros(T, d, dtype=torch.float64)
+        put = {}
+        for j, f, x in at:
+            put[j, f] = x  # (with one draft some coincide: the last stands)
+        for (j, f), x in put.items():
+            v2[table[b, j // page], 0, j % page, f] = x
+            for i in range(T):
+                if j < text or j - text in sees[i]:
+                    here[i, f] += x
+        here = here.to(BF16).cuda()[None]
+        want[b] = torch.where(here == 0, want[b], here)
+    got, gl = tk.attn_tree(q, k, v2, lengths, table, par, lse=True)
+    assert torch.equal(gl, wl)
+    assert bool(((got == want) | (got.isnan() & want.isnan())).all())
+
+
+@pytest.mark.parametrize("d,T,page", [(64, 1, 16), (64, 1, 7), (128, 1, 16), (64, 5, 16), (128, 5, 7), (128, 40, 16), (64, 40, 16)])
+def test_infinite_values_of_weights_that_32_bits_hold_as_0(d, T, page):
+    """e^-200 is above 0 all the same, in the leading key's range and in others."""
+    n = 5000
+    q, k, v, lengths, table, _ = _inputs(4, 1, T, d, page, [n, T, 300])
+    q[:], k[:], v[:] = 0, 0, 1
+    q[..., 0] = 1
+    at = lambda j: (table[0, j // page], 0, j % page)  # noqa: E731
+    for j, f, x in ((0, 1, math.inf), (1000, 2, -math.inf), (4000, 3, math.inf), (n - T, 4, -math.inf), (10, 5, math.inf), (4700, 5, -math.inf)):
+        v[(*at(j), f)] = x
+    want = torch.ones(d, device="cuda")
+    want[1:6] = torch.tensor([math.inf, -math.inf, math.inf, -math.inf, math.nan])
+    for top in (3, 2500, n - T - 1):
+        k[:] = 0
+        k[(*at(top), 0)] = 200
+        out = tk.attn_tree(q, k, v, lengths, table, scale=1.0).float()
+        assert bool(((out[0] == want) | (out[0].isnan() & want.isnan())).all()), top
+        assert bool((out[1:] == 1).all())
