@@ -22,6 +22,7 @@ import os
 import re
 import subprocess
 import sys
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -92,10 +93,13 @@ def build(verbose: bool = False, variants=("main", "check", "san")) -> str:
         cmd = _command(out, extra + ([] if name == "san" else ["-Rpass-analysis=kernel-resource-usage"]))
         if verbose:
             print(" ".join(cmd), flush=True)
-        procs.append((name, out, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+        said = tempfile.TemporaryFile("w+")  # (the remarks are more than a pipe holds, and the builds are waited for in turn)
+        procs.append((name, out, said, subprocess.Popen(cmd, stdout=said, stderr=subprocess.STDOUT)))
     failed = []
-    for name, out, p in procs:
-        log, _ = p.communicate()
+    for name, out, said, p in procs:
+        p.wait()
+        said.seek(0)
+        log = said.read()
         spilled = [] if p.returncode or name == "san" else spills(log)
         if p.returncode != 0:
             sys.stderr.write(log)
