@@ -576,3 +576,106 @@ def test_infinite_values_of_weights_that_32_bits_hold_as_0(d, H, rest, causal):
         want = torch.where(want.isfinite(), 1.0, want)
         out = tk.attn_packed(q, k, v, _int([0, n]), causal, 1.0, lse=True, rest=rest)[0].float()
         assert bool(((out == want) | (out.isnan() & want.isnan())).all()), top
+
+
+TINY = 2.0 ** -127.68  # e^-88.5: as a bf16 number a multiple of 2^-133, off by 2^-134 at most, that is 2^-6.32 of it
+
+
+@pytest.mark.parametrize("lse,rest", [(False, False), (True, False), (True, True)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d,n,H", [(64, 200, 1), (64, 200, 300), (128, 100, 1), (128, 100, 300), (64, 1100, 2), (64, 1100, 40), (128, 1100, 2), (128, 1100, 40)])
+def test_tiny_weights_are_the_result(d, n, H, causal, lse, rest):
+    """Values of 2^116 whose weights are e^-88.5 beside a value of 0 that has all the rest: the output is theirs alone, before
+    and behind the key that leads them. (Rounding of the weight 2^-6.32, of the output 2^-8, of the rest less than 2^-10.)"""
+    q, k, v = (torch.zeros(H, n, d, device="cuda", dtype=BF16) for _ in range(3))
+    q[..., 0] = 1
+    for at in (0, 10, 70, n - 10, n - 1):
+        k[:], v[:] = 0, 2.0 ** 116
+        k[:, at, 0], v[:, at] = 88.5, 0
+        got = tk.attn_packed(q, k, v, _int([0, n]), causal, 1.0, lse=lse, rest=rest)
+        out = (got[0] if lse else got).double()
+        want = torch.full((n,), (n - 1) * math.exp(-88.5) * 2.0 ** 116, dtype=torch.float64, device="cuda")
+        if causal:
+            i = torch.arange(n, device="cuda").double()
+            want = torch.where(i >= at, i * math.exp(-88.5) * 2.0 ** 116, 2.0 ** 116)
+        assert bool(((out - want[None, :, None]).abs() <= (2.0 ** -6.32 + 2.0 ** -8 + 2.0 ** -10) * want[None, :, None]).all()), at
+
+
+def _gradients_in_64_bits(q, k, v, offsets, g, causal, scale, rounded=lambda x: x):
+    """dq, dk, dv; rounded: what is done to weights and score gradients on their way into the products."""
+    H, N, d = q.shape
+    G = H // k.shape[0]
+    out = [torch.zeros(t.shape, dtype=torch.float64, device="cuda") for t in (q, k, v)]
+    for a, z in zip(offsets, offsets[1:]):
+        for h in range(H if z > a else 0):
+            qq, kk, vv, gg = (t[i, a:z].double() for t, i in ((q, h), (k, h // G), (v, h // G), (g, h)))
+            w = torch.softmax(_sequence(q[h, a:z], k[h // G, a:z], causal, scale)[0], -1)
+            ds = w * (gg @ vv.t() - (gg * (w @ vv)).sum(-1, keepdim=True))
+            w, ds = rounded(w), rounded(ds)
+            out[0][h, a:z] += scale * ds @ kk
+            out[1][h // G, a:z] += scale * ds.t() @ qq
+            out[2][h // G, a:z] += w.t() @ gg
+    return out
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("offsets", [[0, 200, 201, 700], [0, 1000], [25 * i for i in range(81)]])
+def test_gradients_of_two_numbers(offsets, d, causal):
+    """A short pass has its weights and score gradients to 16 bits and D to as many: its gradients are off by what their own
+    rounding to bf16 is. In the 2-norm that is 2^-16 of the sums' terms and the scores' roundings beside it, less than a
+    tenth of it, and errors add in squares: a hundredth. With weights and score gradients of one bf16 number it would be 1.2 times
+    as much at least."""
+    N = offsets[-1] + 20
+    q, k, v, off = _inputs(offsets, N, 4, 2, d, seed=6, std=1.0)
+    g = torch.randn(q.shape, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(BF16)
+    out, lse, rest = tk.attn_packed(q, k, v, off, causal, lse=True, rest=True)
+    got = tk.attn_packed_backward(q, k, v, off, out, lse, g, causal, rest=rest)
+    want = _gradients_in_64_bits(q, k, v, offsets, g, causal, d ** -0.5)
+    one = _gradients_in_64_bits(q, k, v, offsets, g, causal, d ** -0.5, lambda x: x.to(BF16).double())
+    for name, x, y, z in zip(("dq", "dk", "dv"), got, want, one):
+        own = float((y.to(BF16).double() - y).norm())
+        assert float((z.to(BF16).double() - y).norm()) >= 1.2 * own, name  # (the test can tell them apart)
+        print(f"[case] {name}: {float((x.double() - y).norm()) / own:.3f} of its rounding", flush=True)
+        assert float((x.double() - y).norm()) <= 1.05 * own, name
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d,H,Hkv", [(64, 2, 1), (128, 6, 2)])
+@pytest.mark.parametrize("n", [3, 64, 65, 300])
+@pytest.mark.parametrize("N", [300, 1500])  # (a short pass, and not)
+def test_offsets_of_any_kind_stay_inside(N, n, d, H, Hkv, causal):
+    """Whatever the offsets are, nothing outside the tensors is written, and nothing that is read there (NaN) reaches a
+    result."""
+    pad = 1 << 16
+    rng = torch.Generator().manual_seed(n + d)
+    shapes = dict(q=(H, N, d), k=(Hkv, N, d), v=(Hkv, N, d), g=(H, N, d), out=(H, N, d), rest=(H, N, d), dq=(H, N, d), dk=(Hkv, N, d), dv=(Hkv, N, d), lse=(H, N))
+    whole, x = {}, {}
+    for name, s in shapes.items():
+        read = name in "qkvg"
+        whole[name] = torch.full((math.prod(s) + 2 * pad,), math.nan if read else 3.0, dtype=torch.float32 if name == "lse" else BF16, device="cuda")
+        x[name] = whole[name][pad:-pad].view(s)
+        if read:
+            x[name].copy_(torch.randn(s, generator=rng))
+    off = _int([0] * (n + 1))
+    st = tk._PackedStrides(*(N * d, d) * 8)
+    p = {name: t.data_ptr() for name, t in x.items()}
+    L, stream = tk.lib(), torch.cuda.current_stream().cuda_stream
+    ws = tk.lib().topk_attn_packed_backward_workspace_bytes(n, N, H, Hkv, d, 1)
+    far = torch.randint(-2 ** 31, 2 ** 31 - 1, (n + 1,), generator=rng)
+    near = torch.randint(-50, N + 50, (n + 1,), generator=rng)
+    inside = torch.randint(0, N + 1, (n + 1,), generator=rng)
+    for o in (far, near, inside, inside.sort(descending=True)[0], torch.tensor([0, N] * n)[:n + 1]):
+        off.copy_(o.int())
+        for name in shapes:
+            if name not in "qkvg":
+                x[name].fill_(3.0)
+        tk._launch(off.device, L.topk_attn_packed, (p["q"], p["k"], p["v"], off.data_ptr(), p["out"], p["lse"], p["rest"], n, N, H, Hkv, d, st, int(causal), d ** -0.5, 1, stream))
+        tk._launch(off.device, L.topk_attn_packed_backward, (p["q"], p["k"], p["v"], off.data_ptr(), p["out"], p["lse"], p["rest"], p["g"], p["dq"], p["dk"], p["dv"], n, N, H, Hkv, d, st,
+                                                             int(causal), d ** -0.5, 1, stream), ws)
+        torch.cuda.synchronize()
+        for name in shapes:
+            if name not in "qkvg":
+                assert bool((whole[name][:pad] == 3).all()) and bool((whole[name][-pad:] == 3).all()), name
+                if N == 300 or name in ("out", "rest", "lse"):  # (shares of tokens that no tile covers are added up as they are)
+                    assert not x[name].isnan().any(), name

@@ -358,3 +358,20 @@ def test_infinite_values_of_weights_that_32_bits_hold_as_0(d, T, page):
         out = tk.attn_tree(q, k, v, lengths, table, scale=1.0).float()
         assert bool(((out[0] == want) | (out[0].isnan() & want.isnan())).all()), top
         assert bool((out[1:] == 1).all())
+
+
+@pytest.mark.parametrize("d,H,T", [(64, 2, 1), (64, 4, 13), (128, 2, 1), (128, 4, 9), (128, 8, 20), (64, 2, 64), (128, 2, 64)])
+@pytest.mark.parametrize("n", [300, 1000, 16000])
+def test_tiny_weights_are_the_result(d, H, T, n):
+    """Values of 2^112 whose weights are e^-88.5 beside a value of 0 that has all the rest: the output is theirs alone, before
+    and behind the key that leads them, in its range and in others. (As a bf16 number such a weight is a multiple of
+    2^-133, off by 2^-6.32 of it at most; rounding of the output 2^-8, of the rest less than 2^-10.)"""
+    q = torch.zeros(1, H, T, d, device="cuda", dtype=BF16)
+    q[..., 0] = 1
+    k, v = (torch.zeros(1, H // 2, n, d, device="cuda", dtype=BF16) for _ in range(2))
+    for at in (0, 10, n // 2, n - T - 5):
+        k[:], v[:] = 0, 2.0 ** 112
+        k[..., at, 0], v[..., at, :] = 88.5, 0
+        out = tk.attn_tree(q, k, v, _int([n]), scale=1.0, lse=True)[0].double()
+        want = (n - T + torch.arange(T, device="cuda").double()) * math.exp(-88.5) * 2.0 ** 112  # (each follows the one before it)
+        assert bool(((out - want[None, None, :, None]).abs() <= (2.0 ** -6.32 + 2.0 ** -8 + 2.0 ** -10) * want[None, None, :, None]).all()), at
