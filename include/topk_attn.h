@@ -453,14 +453,14 @@ size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64
  *   out        [H, N, d]   written, with strides of its own; tokens of no sequence are 0
  *   lse        NULL, or fp32 [H, N]: log sum_j exp(scale * s_j); -inf for tokens of no sequence
  *   rest       NULL, or laid out as out: what rounding took from it, for the backward pass; with lse and
- *              d = 64, or N <= 1024, or N <= 64 n, weights are then taken to 16 significant bits
+ *              d = 64, or N <= 1024, or N <= 64 n, weights are then taken to 16 significant bits (n: as passed, empty sequences too)
  *
  * bf16 with d = 64 or 128 (else TOPK_E_UNSUPPORTED). Scores, softmax statistics and sums in fp32, in a
  * fixed order; weights enter the product with V rounded to bf16, and are divided by the sum of the
- * rounded ones. A row is computed from its own
- * numbers alone: keys and values it does not see may be infinite or NaN. An infinite value makes the rows
+ * rounded ones. A row is computed from its own numbers alone: keys and values it does not see may be infinite or NaN. An infinite value makes the rows
  * that see it infinite, whatever its weight is (values of both signs, or NaN: NaN). No workspace. Offsets that
- * decrease give no meaningful result, but no access outside the tensors.
+ * decrease give no meaningful result, but no access outside the tensors. The order of the sums goes by n, N, H and d,
+ * not by the offsets: what a sequence is packed with may change its last bits through these.
  *
  * topk_attn_packed_backward -- its gradients, from the inputs, out, lse (required here) and rest (NULL: taken as
  * 0, which costs d_Q and d_K a little of their precision) of the forward call and d_out [H, N, d]:
@@ -576,7 +576,7 @@ size_t topk_pages_compact_workspace_bytes(int64_t pages, int64_t n_to);
  * makes the rows that see it infinite, whatever its weight is, values of both signs, or NaN, make them NaN). Weights enter
  * the product with V to 16 significant bits, or, with 64 rows a request and key head ((H / Hkv) * T)
  * and more, rounded to bf16. The work is laid out on the device by the lengths, so a table may be
- * wider than any request needs. Workspace: topk_attn_tree_workspace_bytes (M = 1 without a table).
+ * wider than any request needs (only whether one range a request will do is decided by M * page_rows). Workspace: topk_attn_tree_workspace_bytes (M = 1 without a table).
  * Stages 0 and 3 of the stage timing.
  */
 int topk_attn_tree(const void* Q, const topk_pages* pool, const int32_t* table, int64_t table_stride, const int32_t* lengths,
