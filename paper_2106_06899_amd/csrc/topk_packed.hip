@@ -348,26 +348,14 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int part = lane % PARTS;
   uint16_t* to = (uint16_t*)a.p.out.p + h * a.p.out.head + at.first * a.p.out.token + 4 * part;
-  auto store = [&](int u, bool again) TOPK_INLINE {
+  constexpr int SU = 32 / RPS;  // stores
+  auto sums = [&](int u) TOPK_INLINE {
+    const int r = u * RPS + lane / PARTS;
+    return mine[r * PARTS + (part ^ (r & 15))];
+  };
+  auto store = [&](int u, const f32x4& x) TOPK_INLINE {
     const int r = u * RPS + lane / PARTS, i = at.tile * ROWS + group * 32 + r;
-    f32x4 x = mine[r * PARTS + (part ^ (r & 15))];
     const float by = __shfl(inv, r, 64);
-    if (again) {
-      const bool unsure = i < at.n && by == by && Infinities::any_nan(x);
-      if (!__builtin_amdgcn_ballot_w64(unsure)) return;
-      const uint16_t* v = (const uint16_t*)a.p.v.p + hk * a.p.v.head + at.first * a.p.v.token + 4 * part;
-      Infinities is;
-      for (int j0 = 0; j0 < keys; j0 += 8) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = min(j0 + e, keys - 1);
-          is.meet(*(const uint2*)(v + j * a.p.v.token), !CAUSAL || j <= i);
-        }
-        if (!__builtin_amdgcn_ballot_w64(unsure && is.open(x))) break;
-      }
-      if (!unsure) return;
-      is.settle(x);
-    }
     if (i >= at.n) return;
     const uint2 y = make_uint2(pack_bf16(x[0] * by, x[1] * by), pack_bf16(x[2] * by, x[3] * by));
     *(uint2*)(to + i * a.p.out.token) = y;
@@ -377,10 +365,35 @@ __global__ __launch_bounds__(NT, 2) void k_packed(PackedArgs a) {
                      pack_bf16(x[2] * by - __uint_as_float(y.y << 16), x[3] * by - __uint_as_float(y.y & 0xFFFF0000u)) & ~(not_finite(y.y) * 0xFFFFu));
   };
 #pragma unroll 4
-  for (int u = 0; u < 32 / RPS; ++u) store(u, false);
-  if (__builtin_amdgcn_ballot_w64(most != most))
+  for (int u = 0; u < SU; ++u) store(u, sums(u));
+  if (__builtin_amdgcn_ballot_w64(most != most)) {
+    Infinities<D, SU> is;
+    const int ln = is.own_lane(), row0 = at.tile * ROWS + group * 32 + ln / PARTS;  // the lane's row of the first store
 #pragma unroll 1
-    for (int u = 0; u < 32 / RPS; ++u) store(u, true);
+    for (int u = 0; u < SU; ++u) {
+      const float by = __shfl(inv, u * RPS + ln / PARTS, 64);
+      is.nan(u, sums(u), row0 + u * RPS < at.n && by == by);
+    }
+    constexpr int LOOKS = 4, LR = Infinities<D, SU>::ROWS;
+    const uint16_t* v = (const uint16_t*)a.p.v.p + hk * a.p.v.head + at.first * a.p.v.token + ln % CH * 8;
+    for (int j0 = 0; j0 < keys && is.unsettled(); j0 += LOOKS * LR) {
+      u32x4 x[LOOKS];
+#pragma unroll
+      for (int e = 0; e < LOOKS; ++e) x[e] = *(const u32x4*)(v + min(j0 + e * LR + ln / CH, keys - 1) * a.p.v.token);
+#pragma unroll
+      for (int e = 0; e < LOOKS; ++e)
+        is.look(ln, x[e], [&](int k, int u) TOPK_INLINE {
+          const int j = j0 + e * LR + k;
+          return j < keys && (!CAUSAL || j <= row0 + u * RPS);
+        });
+    }
+#pragma unroll 1
+    for (int u = 0; u < SU; ++u) {
+      f32x4 x = sums(u);
+      is.settle(u, x);
+      store(u, x);
+    }
+  }
   if (LSE && ok && !half) a.p.lse[h * a.p.N + at.first + row] = whole_l == 0.f ? -INFINITY : (m + log2f(whole_l)) * 0.69314718055994531f;
 }
 

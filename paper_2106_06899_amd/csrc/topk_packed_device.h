@@ -28,36 +28,59 @@ __device__ __forceinline__ float other_half_max(float x) {
 // Of two bf16 numbers, bit 0 and bit 16: is it infinite or NaN?
 __device__ __forceinline__ uint32_t not_finite(uint32_t x) { return (((x & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u; }
 
-// A row's four sums of which some are NaN though its weights are numbers. By the definition an infinite value whose
-// weight is above 0 makes a sum infinite, values of both signs, or one that is NaN, make it NaN; the products have it as
-// NaN wherever a part of a weight is 0 (0 times infinity), so the row's values are looked at again: here four of them.
+// Sums that are NaN though their rows' weights are numbers. By the definition an infinite value whose weight is above 0
+// makes a sum infinite, values of both signs, or one that is NaN, make it NaN; the products have it as NaN wherever a
+// part of a weight is 0 (0 times infinity), so the values are looked at again, by the whole wave for its rows: as they
+// lie in memory, 16 bytes a lane. (32768 causal tokens, 12 heads of 64, training: 2.69 ms, 3.58 where all see an infinite
+// value.) A lane has features 4 (lane % (D / 4)) .. of U rows; bit 4 u + w of these is of the w-th of row u.
+template <int D, int U>
 struct Infinities {
-  uint32_t up = 0, down = 0;  // sums (bit w: the w-th) that meet +infinity or NaN; -infinity or NaN
-  static __device__ __forceinline__ bool any_nan(const f32x4& x) { return x[0] != x[0] || x[1] != x[1] || x[2] != x[2] || x[3] != x[3]; }
-  __device__ __forceinline__ void meet(uint2 x, bool sees) {
-    const uint32_t mx = not_finite(x.x), my = not_finite(x.y);
-    if (!sees || !(mx | my)) return;
-    auto nan = [](uint32_t y) { return ((y & 0x007F007Fu) + 0x007F007Fu) >> 7; };  // (bits 0 and 16, of what is not finite)
-    auto four = [](uint32_t y, uint32_t z) { return (y & 1) | y >> 15 | (z & 1) << 2 | z >> 16 << 3; };
-    up |= four(mx & (~(x.x >> 15) | nan(x.x)), my & (~(x.y >> 15) | nan(x.y)));
-    down |= four(mx & (x.x >> 15 | nan(x.x)), my & (x.y >> 15 | nan(x.y)));
-  }
-  __device__ __forceinline__ void meet(const f32x4& x) {  // (four sums of a part of the values)
+  uint64_t open = 0, up = 0, down = 0;  // sums that are NaN; that meet +infinity or NaN; -infinity or NaN
+  static_assert(U <= 16, "four bits a row");
+  static constexpr int PARTS = D / 8, ROWS = 64 / PARTS;  // 16-byte parts of a row of values; rows of a look
+
+  __device__ __forceinline__ void nan(int u, const f32x4& x, bool row) {
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      up |= (uint32_t)!(x[w] < INFINITY) << w;
-      down |= (uint32_t)!(x[w] > -INFINITY) << w;
+    for (int w = 0; w < 4; ++w) open |= (uint64_t)(row && x[w] != x[w]) << (4 * u + w);
+  }
+  // is there a sum that may yet turn out to be infinite?
+  __device__ __forceinline__ bool unsettled() const { return __builtin_amdgcn_ballot_w64((open & ~(up & down)) != 0) != 0; }
+  // lane: of the wave, formed anew, so that nothing that follows from it is held from above, where registers are few
+  static __device__ __forceinline__ int own_lane() {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+  }
+  // x: the lane's part lane % PARTS of row lane / PARTS of ROWS; sees(k, u): does row u see the k-th of them?
+  template <typename F>
+  __device__ __forceinline__ void look(int lane, const u32x4& x, F sees) {
+    const int part = lane % (D / 4);
+    uint64_t hits = __builtin_amdgcn_ballot_w64((not_finite(x[0]) | not_finite(x[1]) | not_finite(x[2]) | not_finite(x[3])) != 0);
+    while (hits) {
+      const int b = __builtin_ctzll(hits);
+      hits &= hits - 1;
+      auto of = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane((int)x[i], b); };
+      const uint32_t y0 = of(0), y1 = of(1), y2 = of(2), y3 = of(3), lo = part & 1 ? y2 : y0, hi = part & 1 ? y3 : y1;
+      uint64_t rises = 0, falls = 0;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t h = (w < 2 ? lo : hi) >> 16 * (w & 1) & 0xFFFFu;
+        const bool odd = part >> 1 == b % PARTS && (h & 0x7F80u) == 0x7F80u, is_nan = h & 0x7Fu;
+        rises |= (uint64_t)(odd && (is_nan || !(h >> 15))) << w;
+        falls |= (uint64_t)(odd && (is_nan || h >> 15)) << w;
+      }
+#pragma unroll 1
+      for (int u = 0; u < U; ++u)
+        if (sees(b / PARTS, u)) {
+          up |= rises << 4 * u;
+          down |= falls << 4 * u;
+        }
     }
   }
-  // is there a sum that is NaN and may yet turn out to be infinite?
-  __device__ __forceinline__ bool open(const f32x4& x) const {
-    const uint32_t both = up & down;
-    return (x[0] != x[0] && !(both & 1)) || (x[1] != x[1] && !(both & 2)) || (x[2] != x[2] && !(both & 4)) || (x[3] != x[3] && !(both & 8));
-  }
-  __device__ __forceinline__ void settle(f32x4& x) const {
+  __device__ __forceinline__ void settle(int u, f32x4& x) const {
 #pragma unroll
     for (int w = 0; w < 4; ++w)
-      if (x[w] != x[w] && ((up ^ down) >> w & 1)) x[w] = up >> w & 1 ? INFINITY : -INFINITY;
+      if ((open & (up ^ down)) >> (4 * u + w) & 1) x[w] = up >> (4 * u + w) & 1 ? INFINITY : -INFINITY;
   }
 };
 

@@ -219,22 +219,23 @@ __device__ __forceinline__ const unsigned char* pass_on(const unsigned char* p, 
   return (const unsigned char*)(uintptr_t)((uint64_t)hi << 32 | lo);
 }
 
-// The four sums x of features 4 part .. of a row (unsure: some are NaN, its weights are not) after a look at the values
-// that it sees of n keys from `first` on. By the whole wave.
-__device__ __forceinline__ void settle_row(f32x4& x, bool unsure, const Rows& rows, int first, int n, int text, uint64_t sees, int part) {
-  const int lane = threadIdx.x & 63;
-  Infinities is;
-  for (int k0 = 0; k0 < n; k0 += 64) {
+// A look at the values of n keys from `first` on for sums that are NaN (see Infinities). sees(u): the drafts that row u sees.
+template <int D, int U, typename F>
+__device__ __forceinline__ void settle_range(Infinities<D, U>& is, const Rows& rows, int first, int n, int text, F sees) {
+  typedef Infinities<D, U> Is;
+  const int lane = is.own_lane();
+  for (int k0 = 0; k0 < n && is.unsettled(); k0 += 64) {
     const int2 at = rows.place(first + k0, lane, n - k0);
     const int p = rows.lookup(at.x), d0 = first + k0 - text;  // (the draft that key 0 of these is)
     const unsigned char* v = rows.at(1, p, at.y);
-    uint64_t seen = __builtin_amdgcn_ballot_w64(rows.valid(p));
-    if (d0 > -64) seen &= d0 >= 0 ? (d0 < 64 ? sees >> d0 : 0) : sees << -d0 | ((1ull << -d0) - 1);
-#pragma unroll 8
-    for (int j = 0; j < 64; ++j) is.meet(*(const uint2*)(pass_on(v, j) + 8 * part), seen >> j & 1);
-    if (!__builtin_amdgcn_ballot_w64(unsure && is.open(x))) break;
+    const uint64_t there = __builtin_amdgcn_ballot_w64(rows.valid(p));
+#pragma unroll 4
+    for (int j = 0; j < 64; j += Is::ROWS)
+      is.look(lane, *(const u32x4*)(pass_on(v, j + lane / Is::PARTS) + lane % Is::PARTS * 16), [&](int k, int u) TOPK_INLINE {
+        const int draft = d0 + j + k;
+        return (there >> (j + k) & 1) && (draft < 0 || (draft < 64 && (sees(u) >> draft & 1)));
+      });
   }
-  if (unsure) is.settle(x);
 }
 
 struct TreeLds {
@@ -482,19 +483,20 @@ struct TreeFew {
       if (wave == 0 && g == 0) sh.sum[16 * r + n] = make_float2(top, total);
     }
     __syncthreads();
-    bool nan = false;
-    auto store = [&](int u, bool again) TOPK_INLINE {
-      const int i = u * NT + tid, row = i / (D / 4), part = i % (D / 4);
+    constexpr int SU = 16 * NR * D / 4 / NT;  // stores
+    const int part = tid % (D / 4);
+    Infinities<D, SU> is;
+    auto row_of = [&](int u) TOPK_INLINE { return (u * NT + tid) / (D / 4); };
+    auto sums = [&](int u) TOPK_INLINE {
+      const int row = row_of(u);
       f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) sum += ((const TOPK_LDS f32x4*)sh.of(w))[row * (D / 4) + (part ^ (row & 15))];
+      return sum;
+    };
+    auto store = [&](int u, const f32x4& sum) TOPK_INLINE {
+      const int row = row_of(u);
       const float2 x = sh.sum[row];
-      const bool unsure = it.r0 + row < it.R && x.y == x.y && Infinities::any_nan(sum);
-      if (again) {  // (rows whose sums are NaN are written once more)
-        if (!__builtin_amdgcn_ballot_w64(unsure)) return;
-        settle_row(sum, unsure, rows, it.r.first, it.r.n, text, drafts ? sh.bits[(it.r0 + row) % T] : 0, part);
-      }
-      nan |= unsure;
       if (it.r0 + row >= it.R) return;
       if (it.r.of == 1) {
         const int64_t at = place(it.r0 + row);
@@ -508,10 +510,21 @@ struct TreeFew {
       }
     };
 #pragma unroll
-    for (int u = 0; u < 16 * NR * D / 4 / NT; ++u) store(u, false);
-    if (__builtin_amdgcn_ballot_w64(nan))
+    for (int u = 0; u < SU; ++u) {
+      const f32x4 x = sums(u);
+      const float l = sh.sum[row_of(u)].y;
+      is.nan(u, x, it.r0 + row_of(u) < it.R && l == l);
+      store(u, x);
+    }
+    if (__builtin_amdgcn_ballot_w64(is.open != 0)) {
+      settle_range(is, rows, it.r.first, it.r.n, text, [&](int u) TOPK_INLINE { return drafts ? sh.bits[(it.r0 + row_of(u)) % T] : 0; });
 #pragma unroll 1
-      for (int u = 0; u < 16 * NR * D / 4 / NT; ++u) store(u, true);
+      for (int u = 0; u < SU; ++u) {
+        f32x4 x = sums(u);
+        is.settle(u, x);
+        store(u, x);
+      }
+    }
   }
 };
 
@@ -752,24 +765,38 @@ struct TreeWide {
     const bool last = it.r.of == 1;
     const float inv = row_factor(l);
     const int part = lane % PARTS, row0 = it.r0 + wave * 32;
-    auto store = [&](int u, bool again) TOPK_INLINE {
+    constexpr int SU = 32 / RPS;  // stores
+    auto sums = [&](int u) TOPK_INLINE {
       const int row = u * RPS + lane / PARTS;
-      f32x4 x = mine[row * PARTS + (part ^ (row & 15))];
+      return mine[row * PARTS + (part ^ (row & 15))];
+    };
+    auto store = [&](int u, const f32x4& x) TOPK_INLINE {
+      const int row = u * RPS + lane / PARTS;
       const float by = __shfl(inv, row, 64);
-      if (again) {
-        const bool unsure = row0 + row < it.R && by == by && Infinities::any_nan(x);
-        if (!__builtin_amdgcn_ballot_w64(unsure)) return;
-        settle_row(x, unsure, rows, it.r.first, it.r.n, text, drafts ? sh.bits[(row0 + row) % T] : 0, part);
-      }
       if (row0 + row >= it.R) return;
       if (last) *(uint2*)((uint16_t*)a.p.out + (list + row0 + row) * D + 4 * part) = make_uint2(pack_bf16(x[0] * by, x[1] * by), pack_bf16(x[2] * by, x[3] * by));
       else __builtin_nontemporal_store(x, (f32x4*)(a.po + (it.slot + row0 + row) * D + 4 * part));
     };
 #pragma unroll 4
-    for (int u = 0; u < 32 / RPS; ++u) store(u, false);
-    if (__builtin_amdgcn_ballot_w64(most != most))
+    for (int u = 0; u < SU; ++u) store(u, sums(u));
+    if (__builtin_amdgcn_ballot_w64(most != most)) {
+      Infinities<D, SU> is;
+      const int ln = is.own_lane();
 #pragma unroll 1
-      for (int u = 0; u < 32 / RPS; ++u) store(u, true);
+      for (int u = 0; u < SU; ++u) {
+        const int row = u * RPS + ln / PARTS;
+        const float by = __shfl(inv, row, 64);
+        is.nan(u, sums(u), row0 + row < it.R && by == by);
+      }
+      settle_range(is, rows, it.r.first, it.r.n, text,
+                   [&](int u) TOPK_INLINE { return drafts ? sh.bits[(row0 + u * RPS + ln / PARTS) % T] : 0; });
+#pragma unroll 1
+      for (int u = 0; u < SU; ++u) {
+        f32x4 x = sums(u);
+        is.settle(u, x);
+        store(u, x);
+      }
+    }
     if (!ok || half) return;
     if (!last) a.ml[it.slot + i] = make_float2(m, l);
     else if (a.p.lse) a.p.lse[list + i] = row_log(m, l);
@@ -878,10 +905,20 @@ __global__ __launch_bounds__(NT) void k_tree_join(TreeArgs a) {
     }
   }
   if (!ok) return;
-  if (total == total && Infinities::any_nan(sum)) {  // (a range's infinity times a factor that 32 bits hold as 0)
-    Infinities is;
-    for (int s = 0; s < of; ++s) is.meet(*(const f32x4*)(a.po + (at + s * step) * D + 4 * c));
-    is.settle(sum);
+  if (total == total && (sum[0] != sum[0] || sum[1] != sum[1] || sum[2] != sum[2] || sum[3] != sum[3])) {
+    // a range's infinity times a factor that 32 bits hold as 0: what the ranges have decides
+    bool up[4] = {}, down[4] = {};
+    for (int s = 0; s < of; ++s) {
+      const f32x4 x = *(const f32x4*)(a.po + (at + s * step) * D + 4 * c);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        up[w] |= !(x[w] < INFINITY);
+        down[w] |= !(x[w] > -INFINITY);
+      }
+    }
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      if (sum[w] != sum[w] && up[w] != down[w]) sum[w] = up[w] ? INFINITY : -INFINITY;
   }
   const int64_t to = ((int64_t)b * a.p.H + h * (a.p.H / a.p.Hkv)) * a.p.T + r;
   const float inv = row_factor(total);

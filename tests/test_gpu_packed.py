@@ -679,3 +679,23 @@ def test_offsets_of_any_kind_stay_inside(N, n, d, H, Hkv, causal):
                 assert bool((whole[name][:pad] == 3).all()) and bool((whole[name][-pad:] == 3).all()), name
                 if N == 300 or name in ("out", "rest", "lse"):  # (shares of tokens that no tile covers are added up as they are)
                     assert not x[name].isnan().any(), name
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_infinite_values(d):
+    """Half of all values are infinite or NaN."""
+    q, k, v, o = _inputs([0, 333, 600], 600, 4, 2, d, seed=5)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    kind = torch.randint(0, 40, v.shape, generator=gen, device="cuda")
+    v = torch.where(kind == 0, math.inf, torch.where((kind == 1) & (torch.arange(d, device="cuda") % 2 == 0), -math.inf, v))
+    v[:, 200, 7] = math.nan
+    v[:, 300:] = torch.where(kind[:, 300:] >= 20, math.inf, v[:, 300:])
+    for causal in (True, False):
+        for rest in (True, False):
+            out = tk.attn_packed(q, k, v, o, causal, lse=True, rest=rest)[0]
+            for a, z in ((0, 333), (333, 600)):
+                here = torch.where(v[:, a:z].isfinite(), 0.0, v[:, a:z].float())
+                here = here.cumsum(1) if causal else here.sum(1, keepdim=True).expand(-1, z - a, -1)
+                here = here.repeat_interleave(2, 0)
+                got = out[:, a:z].float()
+                assert bool(((got == here) | (got.isnan() & here.isnan()) | (here == 0) & got.isfinite()).all())
