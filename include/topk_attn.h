@@ -453,12 +453,14 @@ size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64
  *   out        [H, N, d]   written, with strides of its own; tokens of no sequence are 0
  *   lse        NULL, or fp32 [H, N]: log sum_j exp(scale * s_j); -inf for tokens of no sequence
  *   rest       NULL, or laid out as out: what rounding took from it, for the backward pass; with lse and
- *              d = 64, or N <= 1024, or N <= 64 n, weights are then taken to 16 significant bits (n: as passed, empty sequences too)
+ *              d = 64, or N <= 1024, or N <= 64 n (empty sequences count), weights are then taken to 16
+ *              significant bits
  *
  * bf16 with d = 64 or 128 (else TOPK_E_UNSUPPORTED). Scores, softmax statistics and sums in fp32, in a
  * fixed order; weights enter the product with V rounded to bf16, and are divided by the sum of the
- * rounded ones. A row is computed from its own numbers alone: keys and values it does not see may be infinite or NaN. An infinite value makes the rows
- * that see it infinite, whatever its weight is (values of both signs, or NaN: NaN). No workspace. Offsets that
+ * rounded ones. A row is computed from its own numbers alone: keys and values it does not see may be
+ * infinite or NaN. An infinite value makes the rows that see it infinite, whatever its weight is (values of
+ * both signs, or NaN: NaN). No workspace. Offsets that
  * decrease give no meaningful result, but no access outside the tensors. The order of the sums goes by n, N, H and d,
  * not by the offsets: what a sequence is packed with may change its last bits through these.
  *
@@ -466,9 +468,10 @@ size_t topk_attn_prefix_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64
  * 0, which costs d_Q and d_K a little of their precision) of the forward call and d_out [H, N, d]:
  * d_Q [H, N, d], d_K, d_V [Hkv, N, d], every element written (tokens of no sequence: 0). The weights are
  * recomputed from lse; those below 2^-126 count as 0. Score gradients and weights enter their products
- * rounded to bf16, or, with N <= 1024 or N <= 64 n, to 16 significant bits; sums in fp32, in a fixed order, over the query
- * heads that share a key head too. What is infinite or NaN in a query, in its d_out or in a key and value reaches only
- * the gradients that it is part of by the formulas, as an infinite number or NaN. d_out may be strided like the others. Workspace:
+ * rounded to bf16, or, with N <= 1024 or N <= 64 n, to 16 significant bits; sums in fp32, in a fixed order,
+ * over the query heads that share a key head too. What is infinite or NaN in a query, its d_out, a key or a
+ * value reaches only the gradients that it is part of by the formulas, as an infinite number or NaN. d_out
+ * may be strided like the others. Workspace:
  * topk_attn_packed_backward_workspace_bytes. Stage 4 of the stage timing (forward: 0).
  */
 typedef struct {
@@ -573,10 +576,12 @@ size_t topk_pages_compact_workspace_bytes(int64_t pages, int64_t n_to);
  * bf16 with d = 64 or 128, T <= 64, fewer than 2^24 workgroups (else TOPK_E_UNSUPPORTED). Softmax
  * statistics and sums in fp32, in a fixed order; a row is computed from its own numbers alone
  * (drafts that it does not see, and rows behind the request's, may be infinite or NaN; an infinite value
- * makes the rows that see it infinite, whatever its weight is, values of both signs, or NaN, make them NaN). Weights enter
+ * makes the rows that see it infinite, whatever its weight is, values of both signs, or NaN, make them
+ * NaN). Weights enter
  * the product with V to 16 significant bits, or, with 64 rows a request and key head ((H / Hkv) * T)
  * and more, rounded to bf16. The work is laid out on the device by the lengths, so a table may be
- * wider than any request needs (only whether one range a request will do is decided by M * page_rows). Workspace: topk_attn_tree_workspace_bytes (M = 1 without a table).
+ * wider than any request needs (only whether one range a request will do is decided by M * page_rows).
+ * Workspace: topk_attn_tree_workspace_bytes (M = 1 without a table).
  * Stages 0 and 3 of the stage timing.
  */
 int topk_attn_tree(const void* Q, const topk_pages* pool, const int32_t* table, int64_t table_stride, const int32_t* lengths,

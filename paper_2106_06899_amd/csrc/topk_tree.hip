@@ -14,8 +14,8 @@
 // it. Keys behind the range, and keys whose entry names no page, have a row of zeros in their place and a score
 // of -inf.
 //
-// Few rows (up to 16, at d = 64 up to 32): four waves take key tiles of 32 in turn, K and V in registers, each with a running softmax
-// of its own, joined through LDS; v_mfma_f32_16x16x32_bf16, S^T = K Q^T and O^T = V^T P^T, so that a lane
+// Few rows (up to 16, at d = 64 up to 32): four waves take key tiles of 32 in turn, K and V in registers, each with
+// a running softmax of its own, joined through LDS; v_mfma_f32_16x16x32_bf16, S^T = K Q^T and O^T = V^T P^T, so that a lane
 // holds one row's numbers. Weights enter the second product as the sum of two bf16 numbers (16 significant bits).
 // Bound by reading the cache: the next token of 32 requests of 100 to 4096 keys, 32 heads of 128 on 8, 58 us (4.7 TB/s)
 // and the join's 4.8.
